@@ -66,7 +66,8 @@ typedef enum {
   A2D_OP_PARTIAL_BWD = 2,
   A2D_OP_FIX_BWD = 3,
   A2D_OP_PARTIAL_BWD_DS = 4,   /* workspace query only: a2d_partial_bwd with the dS hand-over */
-  A2D_OP_PARTIAL_BWD_SPLIT = 5 /* workspace query only: a2d_partial_bwd_gqa with A2D_TILE_SPLIT_GROUPS */
+  A2D_OP_PARTIAL_BWD_SPLIT = 5, /* workspace query only: a2d_partial_bwd_gqa with A2D_TILE_SPLIT_GROUPS */
+  A2D_OP_PARTIAL_BWD_SCORED = 6 /* workspace query only: a2d_partial_bwd_scored */
 } a2d_op;
 
 /* Most partials one a2d_fix / a2d_fix_bwd call can merge (sqrt(P) in the paper). */
@@ -338,6 +339,95 @@ a2d_status a2d_partial_bwd_gqa(const a2d_tile_desc* desc, int32_t kv_heads, int 
                                const void* V, const void* O, const void* dO, const float* lse,
                                float* dQ_part, float* dK_part, float* dV_part, void* workspace,
                                size_t workspace_bytes, void* stream);
+
+/*
+ * Tile calls whose scores follow more rules than the causal mask.  With the tokens t_i = q_off + i * token_step of query
+ * row i and u_k = kv_off + k * token_step of key k (token_step = sqrt(P) and q_off, kv_off = the block's first token in the
+ * paper's cyclic layout, 1 in a contiguous one), the score of query row i of query head h against key k is
+ *   z = scale <q_i, k_k>;   y = softcap tanh(z / softcap), or z where softcap is 0;   s = y - slopes[h] |t_i - u_k|
+ * and the key is visible iff (not desc->causal or t_i >= u_k) and first_i <= u_k < end_i, where (first_i, end_i) is the
+ * row's pair in `ranges`: documents, prefixes, windows, the lengths of a batch's sequences - whatever is one run of
+ * tokens for each row (a2d_document_ranges writes those of packed documents).  A row without a visible key has the empty partial.
+ */
+typedef struct {
+  float softcap;         /* finite, >= 0; 0: no cap                                                             */
+  int32_t token_step;    /* tokens between rows, and between keys; 1 .. 2^20                                    */
+  int32_t range_sets;    /* 1, or sets of ranges: one for each run of heads / range_sets query heads (a batch's
+                            sequences); must divide kv_heads                                                    */
+  int32_t pad;           /* must be 0                                                                           */
+  const float* slopes;   /* DEVICE [heads], or NULL: no bias                                                    */
+  const int32_t* ranges; /* DEVICE [range_sets][nq][2]: first token seen, token behind the last; NULL: no limit */
+} a2d_score_rules;
+
+/*
+ * a2d_partial_fwd_gqa and a2d_partial_bwd_gqa under score rules, of plain tiles (no sub-blocks: accumulate over them).
+ *   a2d_partial_fwd_scored: flags 0, A2D_TILE_ACCUMULATE or A2D_TILE_NORMALISED, outputs as of a2d_partial_fwd_gqa.
+ *   a2d_partial_bwd_scored: the gradients of z, so with dS = P o (dP - delta):  dZ = dS (1 - (y / softcap)^2),
+ *     dQ = scale dZ K, dK = scale dZ^T Q, dV = P^T dO.  flags: 0 (fp32 gradient partials), A2D_TILE_ACCUMULATE (dQ +=), or
+ *     A2D_TILE_NORMALISED: the tile is the whole problem, and the gradients are written in desc->dtype, rounded once.
+ *     desc->flags must be 0.  workspace: at least a2d_workspace_bytes(desc, A2D_OP_PARTIAL_BWD_SCORED, 0) bytes.
+ *     Neither the slopes nor the ranges have gradients.
+ * Partials merge as those of the plain calls do (a2d_fix, a2d_attnfix, a2d_fix_norm; lse and O of the merged rows go into the
+ * backward call).  bf16 inputs: the probabilities and dZ are rounded to bf16 in front of their contractions, all else is fp32.
+ * Rows of Q, O, dO that see no key, and keys in front of the first or behind the last one that any row sees, may hold
+ * anything (NaN, uninitialised cache): they are not read or have no effect, and their gradients are 0.
+ * With slopes no distance |t_i - u_k| of the tile may exceed 2^24 (A2D_ERR_UNSUPPORTED): they are exact in fp32 up to there.
+ * group * nq may not exceed 2^22 rows.
+ */
+a2d_status a2d_partial_fwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, const a2d_score_rules* rules, int flags,
+                                  const void* Q, const void* K, const void* V, void* out0, float* out1, float* out2,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+a2d_status a2d_partial_bwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, const a2d_score_rules* rules, int flags,
+                                  const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                                  const float* lse, void* dQ, void* dK, void* dV, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/*
+ * The ranges of packed documents.  Document d holds the tokens starts[d] .. starts[d + 1] - 1 (starts: DEVICE [documents + 1],
+ * not falling; a document may be empty).  Row i stands for token t = first + i * token_step; of its document it sees
+ *   causal: starts[d] .. max(t, starts[d] + prefix[d] - 1), but no token behind the document's last (prefix: DEVICE
+ *           [documents], tokens at its start that all of it sees, or NULL: 0; a negative one counts as 0),
+ *   not causal: all of it,
+ * and a token in no document sees nothing: (0, 0).  out: ranges [rows][2] int32.  1 <= documents, rows <= 2^22, 1 <= token_step <= 2^20.
+ */
+a2d_status a2d_document_ranges(int32_t documents, const int32_t* starts, const int32_t* prefix, int causal, int64_t first,
+                               int32_t token_step, int32_t rows, int32_t* ranges, void* stream);
+
+/*
+ * Rotary positions with several axes (time, height, width): every pair of columns follows one axis and is turned by
+ *   angle = positions[axis of the pair][row] * freqs[pair]   radians:   (x, y) -> (x cos - y sin, x sin + y cos),
+ * by -angle with inverse != 0: its inverse, and the gradient of the turned tensor on its way back.  Pair p is the columns
+ * (2 p, 2 p + 1) with interleaved != 0, else (p, p + hdim / 2); columns of no pair stay as they are.
+ * The angle is formed in 64-bit fixed point as a part of a turn, so that far positions lose nothing; values are rounded once.
+ */
+typedef struct {
+  int32_t rows;             /* 1 .. 2^22                                                                             */
+  int32_t hdim;             /* a multiple of 16, 16 .. 256                                                           */
+  int32_t pairs;            /* 1 .. hdim / 2                                                                         */
+  int32_t axes;             /* 1 .. 8                                                                                */
+  int32_t sets;             /* sets of positions: one for each run of heads / sets heads of a tensor (a batch); >= 1 */
+  int32_t in_dtype;         /* a2d_dtype of the inputs                                                               */
+  int32_t out_dtype;        /* of the outputs: in_dtype, or A2D_BF16 (fp32 gradient partials in, the model's type out) */
+  int32_t interleaved;      /* 0 or 1 */
+  int32_t inverse;          /* 0 or 1 */
+  int32_t pad;              /* must be 0 */
+  const double* freqs;      /* HOST [pairs], finite                                                                  */
+  const uint8_t* axis;      /* HOST [pairs], each < axes; NULL: all 0                                                */
+  const int32_t* positions; /* DEVICE [sets][axes][rows]; any sign                                                   */
+} a2d_rotary_desc;
+
+typedef struct {
+  const void* x;  /* [heads][rows][hdim] in in_dtype, layout lx                                          */
+  void* y;        /* the same in out_dtype, layout ly; may be x itself (in place) if type and layout are the same */
+  a2d_layout lx;  /* {0, 0}: plain; else as in the tile descriptor (rows within 4 GiB of a head's first) */
+  a2d_layout ly;
+  int32_t heads;  /* 1 .. 65535, a multiple of sets */
+  int32_t pad;    /* must be 0 */
+} a2d_rotary_tensor;
+
+#define A2D_ROTARY_MAX_TENSORS 2
+/* Turns n tensors (1 .. A2D_ROTARY_MAX_TENSORS: Q and K) in one launch.  x: HOST array. */
+a2d_status a2d_rotary(const a2d_rotary_desc* desc, int n, const a2d_rotary_tensor* x, void* stream);
 
 /*
  * Sum of k gradient partials (the reduce-scatters of Alg. 3 lines 4-5 use plain

@@ -25,6 +25,7 @@ LIB_PATH = os.path.join(_PKG, "liba2d.so")
 
 A2D_F32, A2D_BF16 = 0, 1
 OP_PARTIAL_FWD, OP_FIX, OP_PARTIAL_BWD, OP_FIX_BWD, OP_PARTIAL_BWD_DS, OP_PARTIAL_BWD_SPLIT = 0, 1, 2, 3, 4, 5
+OP_PARTIAL_BWD_SCORED = 6
 MAX_PARTS = 32
 
 EXPORTS = ("a2d_workspace_bytes", "a2d_partial_fwd", "a2d_fix", "a2d_attnfix", "a2d_partial_bwd", "a2d_fix_bwd",
@@ -32,6 +33,7 @@ EXPORTS = ("a2d_workspace_bytes", "a2d_partial_fwd", "a2d_fix", "a2d_attnfix", "
            "a2d_partial_fwd_seg", "a2d_partial_bwd_seg", "a2d_partial_fwd_acc", "a2d_partial_bwd_acc",
            "a2d_partial_fwd_norm", "a2d_fix_norm", "a2d_partial_fwd_gqa", "a2d_partial_bwd_gqa",
            "a2d_fix_strided", "a2d_fix_bwd_strided", "a2d_fix_norm_strided",
+           "a2d_partial_fwd_scored", "a2d_partial_bwd_scored", "a2d_document_ranges", "a2d_rotary",
            "a2d_mfma_ceiling_scratch_bytes", "a2d_mfma_ceiling", "a2d_forward_mix_ceiling", "a2d_backward_mix_ceiling", "a2d_lds_read_ceiling", "a2d_debug_force_generic",
            "a2d_debug_trace", "a2d_debug_trace_count", "a2d_copy_probe",
            "a2d_status_str", "a2d_last_error", "a2d_version")
@@ -52,6 +54,25 @@ class TileDesc(ctypes.Structure):
 
 class KvSegment(ctypes.Structure):
     _fields_ = [("kv_off", ctypes.c_int64), ("rows", ctypes.c_int32), ("pad", ctypes.c_int32)]
+
+
+class ScoreRules(ctypes.Structure):
+    """a2d_score_rules"""
+    _fields_ = [("softcap", ctypes.c_float), ("token_step", ctypes.c_int32), ("range_sets", ctypes.c_int32),
+                ("pad", ctypes.c_int32), ("slopes", ctypes.c_void_p), ("ranges", ctypes.c_void_p)]
+
+
+class RotaryDesc(ctypes.Structure):
+    """a2d_rotary_desc"""
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "hdim", "pairs", "axes", "sets", "in_dtype", "out_dtype",
+                                              "interleaved", "inverse", "pad")] + \
+               [("freqs", ctypes.c_void_p), ("axis", ctypes.c_void_p), ("positions", ctypes.c_void_p)]
+
+
+class RotaryTensor(ctypes.Structure):
+    """a2d_rotary_tensor"""
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("lx", Layout), ("ly", Layout),
+                ("heads", ctypes.c_int32), ("pad", ctypes.c_int32)]
 
 
 MAX_SEGMENTS = 32
@@ -134,6 +155,17 @@ def lib():
         L.a2d_fix_bwd_strided.restype = ctypes.c_int
         L.a2d_fix_bwd_strided.argtypes = [ctypes.c_int, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                           ctypes.POINTER(vp), vp, ctypes.POINTER(Layout), vp]
+        L.a2d_partial_fwd_scored.restype = ctypes.c_int
+        L.a2d_partial_fwd_scored.argtypes = [ctypes.POINTER(TileDesc), ctypes.c_int32, ctypes.POINTER(ScoreRules),
+                                             ctypes.c_int, vp, vp, vp, vp, fp, fp, vp, ctypes.c_size_t, vp]
+        L.a2d_partial_bwd_scored.restype = ctypes.c_int
+        L.a2d_partial_bwd_scored.argtypes = [ctypes.POINTER(TileDesc), ctypes.c_int32, ctypes.POINTER(ScoreRules),
+                                             ctypes.c_int, vp, vp, vp, vp, vp, fp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.a2d_document_ranges.restype = ctypes.c_int
+        L.a2d_document_ranges.argtypes = [ctypes.c_int32, vp, vp, ctypes.c_int, ctypes.c_int64, ctypes.c_int32,
+                                          ctypes.c_int32, vp, vp]
+        L.a2d_rotary.restype = ctypes.c_int
+        L.a2d_rotary.argtypes = [ctypes.POINTER(RotaryDesc), ctypes.c_int, ctypes.POINTER(RotaryTensor), vp]
         L.a2d_mfma_ceiling_scratch_bytes.restype = ctypes.c_size_t
         L.a2d_mfma_ceiling_scratch_bytes.argtypes = []
         L.a2d_mfma_ceiling.restype = ctypes.c_int
@@ -288,6 +320,59 @@ def partial_bwd_static(Q, K, V, O, dO, lse, q_off=0, kv_off=0, causal=False, sca
 def fix_bwd(parts, out_dtype=torch.bfloat16, out=None):
     """a2d_fix_bwd: sum of k fp32 partials, rounded once to out_dtype."""
     return (_native or _ext()).fix_bwd(parts, out_dtype, out)
+
+
+def partial_fwd_scored(Q, K, V, q_off=0, kv_off=0, causal=False, scale=None, softcap=0.0, slopes=None, ranges=None,
+                       token_step=1, out=None, accumulate=False, normalised=False):
+    """a2d_partial_fwd_scored: partial_fwd (grouped heads too) with rules on the scores.  softcap: s = softcap tanh(s / softcap)
+    of the scaled scores, 0: none; slopes: fp32 [heads], s -= slope |distance in tokens|; ranges: int32 [nq][2] (or
+    [sets][nq][2], a set for each run of heads / sets query heads), the tokens that each row may see, first and behind the last
+    (see document_ranges); token_step: tokens between rows and between keys (the grid side in the cyclic layout, with
+    q_off, kv_off the blocks' first tokens).  Returns (O_part, m, l) fp32, or with normalised=True (O in Q's dtype, lse)."""
+    return (_native or _ext()).partial_fwd_scored(Q, K, V, q_off, kv_off, causal, scale, softcap, slopes, ranges, token_step,
+                                                  out, accumulate, normalised)
+
+
+def partial_bwd_scored(Q, K, V, O, dO, lse, q_off=0, kv_off=0, causal=False, scale=None, softcap=0.0, slopes=None,
+                       ranges=None, token_step=1, out=None, workspace=None, accumulate=False, rounded=False):
+    """a2d_partial_bwd_scored: the gradients under the rules of partial_fwd_scored, from the merged O and lse.  Returns
+    (dQ_part, dK_part, dV_part) fp32, or with rounded=True (the tile is the whole problem) dQ, dK, dV in Q's dtype.
+    accumulate: onto the dQ_part of `out`.  workspace: bytes of workspace_bytes(desc, OP_PARTIAL_BWD_SCORED)."""
+    return (_native or _ext()).partial_bwd_scored(Q, K, V, O, dO, lse, q_off, kv_off, causal, scale, softcap, slopes, ranges,
+                                                  token_step, out, workspace, accumulate, rounded)
+
+
+def document_ranges(starts, rows, prefix=None, first=0, step=1, causal=True, out=None):
+    """a2d_document_ranges: the ranges [rows][2] (int32) of rows that stand for the tokens first + i * step of a sequence of
+    packed documents.  starts: int32 [documents + 1] on the device; causal: a row sees its document up to itself, and
+    the document's first prefix[d] tokens (int32 [documents]); not causal: all of its document; a token of no
+    document (padding) sees nothing."""
+    return (_native or _ext()).document_ranges(starts, rows, prefix, first, step, causal, out)
+
+
+def rotary_frequencies(hdim, sections, base=10000.0, restart=False):
+    """(freqs, axis) for rotary(), on the host: sections[a] pairs of columns follow axis a, one after another.  Pair p turns by
+    base ** (-2 p / hdim) radians a position; restart=True: each axis has its own falling sequence, base ** (-2 j / (2 n)) for
+    pair j of its n."""
+    sections = [int(n) for n in sections]
+    if not sections or min(sections) < 0 or not 0 < sum(sections) <= hdim // 2:
+        raise A2DError(-1, "sections %s: 1 to %d pairs" % (sections, hdim // 2))
+    if restart:
+        freqs = [base ** (-float(j) / n) for n in sections for j in range(n)]
+    else:
+        freqs = [base ** (-2.0 * p / hdim) for p in range(sum(sections))]
+    return (torch.tensor(freqs, dtype=torch.float64),
+            torch.tensor([a for a, n in enumerate(sections) for _ in range(n)], dtype=torch.uint8))
+
+
+def rotary(X, positions, freqs, axis=None, interleaved=False, inverse=False, out=None, out_dtype=None):
+    """a2d_rotary: turns the pairs of columns of X - a [heads][rows][H] tensor or view, or a pair of them (Q and K, of any numbers
+    of heads) in one launch - by positions[axis of the pair][row] * freqs[pair] radians.  positions: int32 [axes][rows], or
+    [sets][axes][rows], a set for each run of heads / sets heads; freqs (fp64), axis (uint8): host tensors [pairs], see
+    rotary_frequencies; interleaved: pair p is the columns (2 p, 2 p + 1), not (p, p + H / 2).  inverse=True turns back: the
+    gradient with respect to X of the gradient with respect to the turned X.  out: as X, may be X itself; else new tensors in
+    out_dtype (X's, or bf16 for fp32 gradient partials)."""
+    return (_native or _ext()).rotary(X, positions, freqs, axis, interleaved, inverse, out, out_dtype)
 
 
 def mfma_ceiling(iters=20000, random_data=True):

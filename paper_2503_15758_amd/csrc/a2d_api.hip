@@ -6,7 +6,7 @@
 #include <cstdlib>
 #include <cstring>
 
-#include "a2d_common.hpp"
+#include "a2d_scored.hpp"
 
 namespace {
 
@@ -361,9 +361,11 @@ a2d_status a2d_partial_bwd_static(const a2d_tile_desc* desc, const void* Q, cons
 
 size_t a2d_workspace_bytes(const a2d_tile_desc* desc, int op, int k) {
   if (!desc || desc->heads < 1 || desc->nq < 1) return 0;
-  if (op != A2D_OP_PARTIAL_BWD && op != A2D_OP_PARTIAL_BWD_DS && op != A2D_OP_PARTIAL_BWD_SPLIT) return 0;
+  if (op != A2D_OP_PARTIAL_BWD && op != A2D_OP_PARTIAL_BWD_DS && op != A2D_OP_PARTIAL_BWD_SPLIT && op != A2D_OP_PARTIAL_BWD_SCORED)
+    return 0;
   const size_t rows = (size_t)desc->heads * (size_t)desc->nq;
   const size_t delta_bytes = ((rows * sizeof(float) + 255) / 256) * 256;
+  if (op == A2D_OP_PARTIAL_BWD_SCORED) return 3 * delta_bytes;          // delta, and each row's run of keys
   if (op == A2D_OP_PARTIAL_BWD || desc->nkv < 1) return delta_bytes;
   // (the dS area is sized for the plain tile whether or not a call ends up using it, so that the
   // areas behind it have a fixed place)
@@ -688,6 +690,173 @@ a2d_status a2d_partial_bwd(const a2d_tile_desc* desc, const void* Q, const void*
 a2d_status a2d_fix_bwd(int k, int64_t n, int32_t out_dtype, const float* const* parts, void* out,
                        void* stream) {
   return fix_bwd_impl(k, n, 4, out_dtype, parts, out, a2d::plain_out(), stream, "a2d_fix_bwd");
+}
+
+// ---- attention under score rules, and what goes with it
+
+namespace {
+
+int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0); }
+
+a2d_status make_rules(const a2d_tile_desc* d, int32_t kv_heads, const a2d_score_rules* in, const char* who, a2d::ScoreRules* r) {
+  memset(r, 0, sizeof(*r));
+  if (!in) return fail(A2D_ERR_INVALID_ARG, "%s: rules is NULL", who);
+  if (!(in->softcap >= 0.f) || !std::isfinite(in->softcap))
+    return fail(A2D_ERR_INVALID_ARG, "%s: softcap must be finite and >= 0", who);
+  // (below, scale / softcap or its square is no normal number any more)
+  if (in->softcap != 0.f && (in->softcap < 1e-6f || in->softcap > 1e6f || d->scale > 1e20f || d->scale < 1e-20f))
+    return fail(A2D_ERR_UNSUPPORTED, "%s: softcap=%g outside 1e-6 .. 1e6, or scale=%g outside 1e-20 .. 1e20 with it", who, in->softcap, d->scale);
+  if (in->token_step < 1 || in->token_step > (1 << 20))
+    return fail(A2D_ERR_INVALID_ARG, "%s: token_step=%d outside 1..2^20", who, in->token_step);
+  if (in->pad != 0) return fail(A2D_ERR_INVALID_ARG, "%s: rules->pad must be 0", who);
+  a2d::SegList g;
+  A2D_TRY(group_of(d, kv_heads, who, &g));
+  if (in->range_sets < 1 || kv_heads % in->range_sets != 0)
+    return fail(A2D_ERR_INVALID_ARG, "%s: range_sets=%d must be >= 1 and divide kv_heads=%d", who, in->range_sets, kv_heads);
+  if (in->slopes) A2D_TRY(check_ptr(in->slopes, who, "slopes"));
+  if (in->ranges) A2D_TRY(check_ptr(in->ranges, who, "ranges"));
+  r->cap = in->softcap;
+  r->step = in->token_step;
+  r->heads_per_set = d->heads / in->range_sets;
+  r->group = g.group;
+  r->rel = d->q_off - d->kv_off;
+  r->kv_off = d->kv_off;
+  r->slopes = in->slopes;
+  r->ranges = reinterpret_cast<const int2*>(in->ranges);
+  const int64_t shift = floor_div(r->rel, r->step), lim = (int64_t)1 << 30;      // (beyond, every row sees all keys, or none)
+  r->row_shift = (int)(shift < -lim ? -lim : shift > lim ? lim : shift);
+  if (r->slopes) {
+    const int64_t a = r->rel + (int64_t)(d->nq - 1) * r->step, b = r->rel - (int64_t)(d->nkv - 1) * r->step, most = (int64_t)1 << 24;
+    if (a > most || b < -most)
+      return fail(A2D_ERR_UNSUPPORTED, "%s: slopes with tokens %lld .. %lld apart (2^24 at the most)", who, (long long)b, (long long)a);
+  }
+  return A2D_OK;
+}
+
+}  // namespace
+
+a2d_status a2d_partial_fwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, const a2d_score_rules* rules, int flags,
+                                  const void* Q, const void* K, const void* V, void* out0, float* out1, float* out2,
+                                  void* /*workspace*/, size_t /*workspace_bytes*/, void* stream) {
+  const char* who = "a2d_partial_fwd_scored";
+  A2D_TRY(check_desc(desc, who));
+  if (flags != 0 && flags != A2D_TILE_ACCUMULATE && flags != A2D_TILE_NORMALISED)
+    return fail(A2D_ERR_INVALID_ARG, "%s: flags=%d must be 0, A2D_TILE_ACCUMULATE or A2D_TILE_NORMALISED", who, flags);
+  a2d::ScoreRules r;
+  A2D_TRY(make_rules(desc, kv_heads, rules, who, &r));
+  r.acc = flags == A2D_TILE_ACCUMULATE;
+  r.norm = flags == A2D_TILE_NORMALISED;
+  if (r.norm) out2 = out1;
+  A2D_TRY(check_ptr(Q, who, "Q"));
+  A2D_TRY(check_ptr(K, who, "K"));
+  A2D_TRY(check_ptr(V, who, "V"));
+  A2D_TRY(check_ptr(out0, who, "out0"));
+  A2D_TRY(check_ptr(out1, who, "out1"));
+  A2D_TRY(check_ptr(out2, who, "out2"));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  a2d_tile_desc dd;
+  A2D_TRY(resolve_layouts(desc, r.group, false, who, &dd));
+  a2d::trace_mark(s);
+  return hip_result(a2d::launch_scored_fwd_generic(dd, r, Q, K, V, out0, out1, out2, s), who);
+}
+
+a2d_status a2d_partial_bwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, const a2d_score_rules* rules, int flags,
+                                  const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                                  const float* lse, void* dQ, void* dK, void* dV, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  const char* who = "a2d_partial_bwd_scored";
+  A2D_TRY(check_desc(desc, who));
+  if (desc->flags != 0) return fail(A2D_ERR_UNSUPPORTED, "%s: desc->flags must be 0 (dS is not kept under score rules)", who);
+  if (flags != 0 && flags != A2D_TILE_ACCUMULATE && flags != A2D_TILE_NORMALISED)
+    return fail(A2D_ERR_INVALID_ARG, "%s: flags=%d must be 0, A2D_TILE_ACCUMULATE or A2D_TILE_NORMALISED", who, flags);
+  a2d::ScoreRules r;
+  A2D_TRY(make_rules(desc, kv_heads, rules, who, &r));
+  r.acc = flags == A2D_TILE_ACCUMULATE;
+  r.norm = flags == A2D_TILE_NORMALISED;
+  A2D_TRY(check_ptr(Q, who, "Q"));
+  A2D_TRY(check_ptr(K, who, "K"));
+  A2D_TRY(check_ptr(V, who, "V"));
+  A2D_TRY(check_ptr(O, who, "O"));
+  A2D_TRY(check_ptr(dO, who, "dO"));
+  A2D_TRY(check_ptr(lse, who, "lse"));
+  A2D_TRY(check_ptr(dQ, who, "dQ"));
+  A2D_TRY(check_ptr(dK, who, "dK"));
+  A2D_TRY(check_ptr(dV, who, "dV"));
+  const size_t need = a2d_workspace_bytes(desc, A2D_OP_PARTIAL_BWD_SCORED, 0);
+  if (workspace_bytes > ((size_t)1 << 46))
+    return fail(A2D_ERR_INVALID_ARG, "%s: workspace_bytes = %zu is not a plausible size (size_t expected)", who, workspace_bytes);
+  if (!workspace || workspace_bytes < need)
+    return fail(A2D_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace ? workspace_bytes : (size_t)0);
+  if (!aligned16(workspace)) return fail(A2D_ERR_MISALIGNED, "%s: workspace is not 16-byte aligned", who);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  a2d_tile_desc dd;
+  A2D_TRY(resolve_layouts(desc, r.group, true, who, &dd));
+  a2d::trace_mark(s);
+  return hip_result(a2d::launch_scored_bwd_generic(dd, r, Q, K, V, O, dO, lse, static_cast<float*>(workspace), dQ, dK, dV, s), who);
+}
+
+a2d_status a2d_document_ranges(int32_t documents, const int32_t* starts, const int32_t* prefix, int causal, int64_t first,
+                               int32_t token_step, int32_t rows, int32_t* ranges, void* stream) {
+  const char* who = "a2d_document_ranges";
+  if (documents < 1 || documents > (1 << 22) || rows < 1 || rows > (1 << 22))
+    return fail(A2D_ERR_INVALID_ARG, "%s: documents=%d, rows=%d must be 1..2^22", who, documents, rows);
+  if (token_step < 1 || token_step > (1 << 20))
+    return fail(A2D_ERR_INVALID_ARG, "%s: token_step=%d outside 1..2^20", who, token_step);
+  if (causal != 0 && causal != 1) return fail(A2D_ERR_INVALID_ARG, "%s: causal must be 0 or 1", who);
+  if (first < -((int64_t)1 << 40) || first > ((int64_t)1 << 40)) return fail(A2D_ERR_INVALID_ARG, "%s: first out of range", who);
+  A2D_TRY(check_ptr(starts, who, "starts"));
+  if (prefix) A2D_TRY(check_ptr(prefix, who, "prefix"));
+  A2D_TRY(check_ptr(ranges, who, "ranges"));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  a2d::trace_mark(s);
+  return hip_result(a2d::launch_document_ranges(documents, starts, prefix, causal, first, token_step, rows, ranges, s), who);
+}
+
+a2d_status a2d_rotary(const a2d_rotary_desc* desc, int n, const a2d_rotary_tensor* x, void* stream) {
+  const char* who = "a2d_rotary";
+  if (!desc) return fail(A2D_ERR_INVALID_ARG, "%s: descriptor is NULL", who);
+  if (n < 1 || n > A2D_ROTARY_MAX_TENSORS) return fail(A2D_ERR_INVALID_ARG, "%s: n=%d outside 1..%d", who, n, A2D_ROTARY_MAX_TENSORS);
+  if (!x || !desc->freqs) return fail(A2D_ERR_INVALID_ARG, "%s: pointer array is NULL", who);
+  const a2d_rotary_desc& d = *desc;
+  if (d.rows < 1 || d.rows > (1 << 22)) return fail(A2D_ERR_INVALID_ARG, "%s: rows=%d outside 1..2^22", who, d.rows);
+  if (d.hdim < 16 || d.hdim > 256 || d.hdim % 16 != 0)
+    return fail(A2D_ERR_UNSUPPORTED, "%s: hdim=%d must be a multiple of 16 in 16..256", who, d.hdim);
+  if (d.pairs < 1 || d.pairs > d.hdim / 2) return fail(A2D_ERR_INVALID_ARG, "%s: pairs=%d outside 1..hdim / 2", who, d.pairs);
+  if (d.axes < 1 || d.axes > 8) return fail(A2D_ERR_INVALID_ARG, "%s: axes=%d outside 1..8", who, d.axes);
+  if (d.sets < 1) return fail(A2D_ERR_INVALID_ARG, "%s: sets=%d must be >= 1", who, d.sets);
+  const bool f32 = d.in_dtype == A2D_F32;
+  if ((!f32 && d.in_dtype != A2D_BF16) || (d.out_dtype != A2D_BF16 && !(f32 && d.out_dtype == A2D_F32)))
+    return fail(A2D_ERR_UNSUPPORTED, "%s: dtype %d / %d not supported", who, d.in_dtype, d.out_dtype);
+  if ((d.interleaved & ~1) || (d.inverse & ~1) || d.pad != 0)
+    return fail(A2D_ERR_INVALID_ARG, "%s: interleaved and inverse must be 0 or 1, pad 0", who);
+  A2D_TRY(check_ptr(d.positions, who, "positions"));
+  for (int p = 0; p < d.pairs; ++p) {
+    if (!std::isfinite(d.freqs[p])) return fail(A2D_ERR_INVALID_ARG, "%s: freqs[%d] is not finite", who, p);
+    if (d.axis && d.axis[p] >= d.axes) return fail(A2D_ERR_INVALID_ARG, "%s: axis[%d]=%d, axes=%d", who, p, d.axis[p], d.axes);
+  }
+  a2d_rotary_tensor t[A2D_ROTARY_MAX_TENSORS];
+  for (int i = 0; i < n; ++i) {
+    t[i] = x[i];
+    if (t[i].heads < 1 || t[i].heads > 65535 || t[i].heads % d.sets != 0 || t[i].pad != 0)
+      return fail(A2D_ERR_INVALID_ARG, "%s: heads=%d must be 1..65535 and a multiple of sets=%d, pad 0", who, t[i].heads, d.sets);
+    A2D_TRY(check_ptr(t[i].x, who, "x"));
+    A2D_TRY(check_ptr(t[i].y, who, "y"));
+    a2d_tile_desc as{};                            // (what the layouts are checked against)
+    as.hdim = d.hdim;
+    as.dtype = d.in_dtype;
+    A2D_TRY(resolve_layout(&t[i].lx, "x", 1, d.rows, &as, who));
+    as.dtype = d.out_dtype;
+    A2D_TRY(resolve_layout(&t[i].ly, "y", 1, d.rows, &as, who));
+    if (t[i].x == t[i].y && (d.in_dtype != d.out_dtype || t[i].lx.head != t[i].ly.head || t[i].lx.row != t[i].ly.row))
+      return fail(A2D_ERR_INVALID_ARG, "%s: in place needs one type and one layout", who);
+  }
+  if (n == 2 && (t[0].y == t[1].y || t[0].y == t[1].x || t[0].x == t[1].y))
+    return fail(A2D_ERR_INVALID_ARG, "%s: an output is the other tensor too", who);
+  int cus = 0;
+  A2D_TRY(hip_result(a2d::device_cus(&cus), who));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  a2d::trace_mark(s);
+  return hip_result(a2d::launch_rotary(d, n, t, cus, s), who);
 }
 
 const char* a2d_status_str(a2d_status status) {

@@ -1,0 +1,155 @@
+// Rotary positions with several axes: (x, y) -> (x cos - y sin, x sin + y cos) of the pairs of columns of Q and K.
+//
+// The angle of a pair is a position times a frequency.  Taken as a part of a turn it needs only what is left of the product
+// behind its whole turns, so the frequency comes as a 64-bit fixed-point part of a turn (2^-64 units, made on the host)
+// and the product is formed modulo 2^64: one wrapping multiplication, no reduction, and a position of 2^31 is off by
+// 2^-33 turns at most.  The top 32 bits, read as a signed number, are the angle in -1/2 .. 1/2 turns.  Results of 16
+// bits take the hardware's sine and cosine, whose argument is in turns (their error, some 2^-20, is far below half a step of
+// the result); fp32 results take sincospif.
+//
+// Bound: HBM, each value read and written once.  A thread owns eight pairs of a row (two 16-byte pieces a head in bf16):
+// it makes their sines and cosines once and walks over heads, as many as still leave the chip full of wavefronts.
+#include "a2d_scored.hpp"
+
+namespace a2d {
+namespace {
+
+constexpr int MAX_PAIRS = 128;
+struct Turns {
+  uint64_t step[MAX_PAIRS];      // part of a turn for a position, 2^-64 units
+  uint8_t axis[MAX_PAIRS];
+};
+struct RotaryArgs {
+  int rows, chunks;              // chunks of eight pairs of a row (hdim / 16)
+  int half;                      // hdim / 2
+  int pairs, axes, inverse;
+  int runs, per;                 // runs of heads of a set, `per` heads each
+  int heads[2];                  // of a set
+  const int32_t* positions;
+  const void* x[2];
+  void* y[2];
+  a2d_layout lx[2], ly[2];
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8]);
+template <>
+__device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float (&v)[8]) {
+  const bf16x8 b = *reinterpret_cast<const bf16x8*>(p);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)b[i];
+}
+template <>
+__device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+}
+__device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
+  bf16x8 b;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b[i] = (bf16_t)v[i];
+  *reinterpret_cast<bf16x8*>(p) = b;
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+  *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+
+// (x and y may be the same memory: a thread reads its pieces of a head before it writes them, and no other thread touches them)
+template <typename TI, typename TO, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Turns turns) {
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int row = (int)(t / a.chunks), chunk = (int)(t - (int64_t)row * a.chunks);
+  if (row >= a.rows) return;
+  const int set = blockIdx.y / a.runs, run = blockIdx.y - set * a.runs;
+  const int32_t* pos = a.positions + (int64_t)set * a.axes * a.rows + row;
+  float cs[8], sn[8];
+  const int p0 = 8 * chunk, live = min(max(a.pairs - p0, 0), 8);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int p = min(p0 + i, a.pairs - 1);
+    const int64_t at = pos[(int64_t)turns.axis[p] * a.rows];
+    const int part = (int)(uint32_t)(((uint64_t)at * turns.step[p]) >> 32);
+    const float turn = (float)part * 0x1p-32f;
+    if constexpr (sizeof(TO) == 2) {
+      sn[i] = __builtin_amdgcn_sinf(turn);
+      cs[i] = __builtin_amdgcn_cosf(turn);
+    } else {
+      sincospif(2.f * turn, &sn[i], &cs[i]);
+    }
+    if (a.inverse) sn[i] = -sn[i];
+  }
+  const int at0 = INTERLEAVED ? 2 * p0 : p0, at1 = INTERLEAVED ? 2 * p0 + 8 : p0 + a.half;
+  const int end = min((run + 1) * a.per, a.heads[0] + a.heads[1]);
+  for (int h = run * a.per; h < end; ++h) {
+    const int which = h >= a.heads[0], head = set * a.heads[which] + h - (which ? a.heads[0] : 0);
+    const TI* x = static_cast<const TI*>(a.x[which]) + head * a.lx[which].head + row * a.lx[which].row;
+    TO* y = static_cast<TO*>(a.y[which]) + head * a.ly[which].head + row * a.ly[which].row;
+    float u[8], v[8], ou[8], ov[8];
+    load8<TI>(x + at0, u);
+    load8<TI>(x + at1, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      // pair i: columns (u[i], v[i]), or (w[2 i], w[2 i + 1]) of the sixteen w = u, v
+      float& px = INTERLEAVED ? (i < 4 ? u[2 * i] : v[2 * i - 8]) : u[i];
+      float& py = INTERLEAVED ? (i < 4 ? u[2 * i + 1] : v[2 * i - 7]) : v[i];
+      float& qx = INTERLEAVED ? (i < 4 ? ou[2 * i] : ov[2 * i - 8]) : ou[i];
+      float& qy = INTERLEAVED ? (i < 4 ? ou[2 * i + 1] : ov[2 * i - 7]) : ov[i];
+      qx = i < live ? px * cs[i] - py * sn[i] : px;      // (columns of no pair: not even times 1, plus 0 times the other)
+      qy = i < live ? px * sn[i] + py * cs[i] : py;
+    }
+    store8(y + at0, ou);
+    store8(y + at1, ov);
+  }
+}
+
+template <typename TI, typename TO>
+hipError_t go(const RotaryArgs& a, const Turns& t, dim3 grid, bool interleaved, hipStream_t s) {
+  if (interleaved) A2D_LAUNCH((rotary_kernel<TI, TO, true>), grid, dim3(256), 0, s, a, t);
+  else A2D_LAUNCH((rotary_kernel<TI, TO, false>), grid, dim3(256), 0, s, a, t);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const a2d_rotary_desc& d, int n, const a2d_rotary_tensor* x, int cus, hipStream_t s) {
+  RotaryArgs a{};
+  Turns t{};
+  a.rows = d.rows;
+  a.chunks = d.hdim / 16;
+  a.half = d.hdim / 2;
+  a.pairs = d.pairs;
+  a.axes = d.axes;
+  a.inverse = d.inverse;
+  a.positions = d.positions;
+  for (int i = 0; i < n; ++i) {
+    a.heads[i] = x[i].heads / d.sets;
+    a.x[i] = x[i].x;
+    a.y[i] = x[i].y;
+    a.lx[i] = x[i].lx;
+    a.ly[i] = x[i].ly;
+  }
+  for (int p = 0; p < d.pairs; ++p) {
+    const long double turns = (long double)d.freqs[p] / (2 * 3.14159265358979323846264338327950288L);
+    const long double part = turns - __builtin_floorl(turns);            // 0 <= part < 1, or 1 by rounding
+    t.step[p] = part >= 1 ? 0 : (uint64_t)(part * 0x1p64L);
+    t.axis[p] = d.axis ? d.axis[p] : 0;
+  }
+  const int heads = a.heads[0] + a.heads[1];
+  const int64_t blocks = ((int64_t)d.rows * a.chunks + 255) / 256;
+  // heads of a thread: as many as leave eight workgroups for each compute unit, at least one
+  int64_t runs = (8 * cus + blocks * d.sets - 1) / (blocks * d.sets);
+  if (runs > heads) runs = heads;
+  if (runs > 65535 / d.sets) runs = 65535 / d.sets;                     // (a launch's second dimension)
+  if (runs < 1) runs = 1;
+  a.per = (heads + (int)runs - 1) / (int)runs;
+  a.runs = (heads + a.per - 1) / a.per;
+  const dim3 grid((unsigned)blocks, (unsigned)(a.runs * d.sets));
+  const bool f = d.in_dtype == A2D_F32;
+  return f && d.out_dtype == A2D_F32 ? go<float, float>(a, t, grid, d.interleaved != 0, s)
+         : f                         ? go<float, bf16_t>(a, t, grid, d.interleaved != 0, s)
+                                     : go<bf16_t, bf16_t>(a, t, grid, d.interleaved != 0, s);
+}
+
+}  // namespace a2d

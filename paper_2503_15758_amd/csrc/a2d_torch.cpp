@@ -9,11 +9,13 @@
 
 #include <ATen/ATen.h>
 #include <ATen/hip/HIPGeneratorImpl.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 #include <string>
@@ -625,6 +627,238 @@ PyObject* fix_bwd(Args a) {
   return o.one(0);
 }
 
+// ---- attention under score rules, and what goes with it
+
+// on the current device, whose current stream the call goes to
+void here(const at::Tensor& t, const char* name) {
+  if (!t.is_cuda() || t.device().index() != c10::hip::current_device())
+    fail(A2D_ERR_INVALID_ARG, std::string(name) + " must be on the current device");
+}
+// an output or plain input of known shape and type
+void exactly(const at::Tensor& t, at::IntArrayRef shape, at::ScalarType dt, const char* name) {
+  if (t.sizes() != shape || t.scalar_type() != dt || !t.is_contiguous())
+    fail(A2D_ERR_INVALID_ARG, std::string(name) + " must be a contiguous tensor of the documented shape and type");
+  here(t, name);
+}
+double number(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw PythonError();
+  return v;
+}
+int32_t int32_of(PyObject* o, const char* name) {
+  const int64_t v = integer(o);
+  if (v < INT32_MIN || v > INT32_MAX) fail(A2D_ERR_INVALID_ARG, std::string(name) + " does not fit 32 bits");
+  return (int32_t)v;
+}
+
+// softcap, slopes, ranges, token_step
+a2d_score_rules score_rules(const at::Tensor& Q, const at::Tensor& K, Args a) {
+  a2d_score_rules r;
+  r.softcap = (float)number(a[0]);
+  r.token_step = int32_of(a[3], "token_step");
+  r.range_sets = 1;
+  r.pad = 0;
+  r.slopes = nullptr;
+  r.ranges = nullptr;
+  if (a[1] != Py_None) {
+    const at::Tensor& t = tensor(a[1], "slopes");
+    exactly(t, {Q.size(0)}, at::kFloat, "slopes (fp32 [heads])");
+    r.slopes = data<float>(t);
+  }
+  if (a[2] != Py_None) {
+    const at::Tensor& t = tensor(a[2], "ranges");
+    const char* what = "ranges (int32 [nq][2] or [sets][nq][2])";
+    if (t.dim() == 3) r.range_sets = (int32_t)t.size(0);
+    if (t.dim() == 3) exactly(t, {t.size(0), Q.size(1), 2}, at::kInt, what);
+    else exactly(t, {Q.size(1), 2}, at::kInt, what);
+    r.ranges = data<int32_t>(t);
+  }
+  here(Q, "Q");
+  here(K, "K");
+  return r;
+}
+
+// Q, K, V, q_off, kv_off, causal, scale, softcap, slopes, ranges, token_step, out, accumulate, normalised
+PyObject* partial_fwd_scored(Args a) {
+  const at::Tensor &Q = tensor(a[0], "Q"), &K = tensor(a[1], "K"), &V = tensor(a[2], "V");
+  qkv(Q, K, V);
+  here(V, "V");
+  const a2d_tile_desc d = descriptor(Q, K, V, a + 3, 0);
+  const a2d_score_rules r = score_rules(Q, K, a + 7);
+  const bool acc = truth(a[12]), norm = truth(a[13]);
+  if (acc && norm) fail(A2D_ERR_INVALID_ARG, "a normalised partial is not accumulated into");
+  if (acc && a[11] == Py_None) fail(A2D_ERR_INVALID_ARG, "accumulate needs out=(O_part, m, l)");
+  Outputs o;
+  const at::ScalarType ot = norm ? Q.scalar_type() : at::kFloat;
+  if (a[11] == Py_None) {
+    o.add(empty_like_shape(Q, Q.sizes(), ot));
+    for (int i = norm ? 1 : 0; i < 2; ++i) o.add(empty_like_shape(Q, rows_shape(Q), at::kFloat));
+  } else {
+    const char* what = norm ? "out=(O_norm, lse)" : "out=(O_part, m, l)";
+    o.take(a[11], norm ? 2 : 3, what);
+    exactly(o.t[0], Q.sizes(), ot, what);
+    for (int i = 1; i < o.n; ++i) exactly(o.t[i], rows_shape(Q), at::kFloat, what);
+  }
+  void* s = stream();
+  const void *q = Q.data_ptr(), *k = K.data_ptr(), *v = V.data_ptr();
+  void* N = o.t[0].data_ptr();
+  float *m = data<float>(o.t[1]), *l = norm ? nullptr : data<float>(o.t[2]);
+  const int kvh = (int)K.size(0);
+  const Scratch scratch(Q, s);
+  check(unlocked([&] {
+    return a2d_partial_fwd_scored(&d, kvh, &r, acc ? A2D_TILE_ACCUMULATE : norm ? A2D_TILE_NORMALISED : 0, q, k, v, N, m, l,
+                                  nullptr, 0, s);
+  }));
+  scratch.tell();
+  return o.give();
+}
+
+// Q, K, V, O, dO, lse, q_off, kv_off, causal, scale, softcap, slopes, ranges, token_step, out, workspace, accumulate, rounded
+PyObject* partial_bwd_scored(Args a) {
+  const Saved x(a);
+  if (!x.match() || x.K.size(2) != x.Q.size(2) || x.K.scalar_type() != x.Q.scalar_type() || x.V.scalar_type() != x.Q.scalar_type())
+    fail(A2D_ERR_INVALID_ARG, "K, V, O, dO, lse do not match Q (lse: plain fp32 [heads][nq])");
+  for (const at::Tensor* t : {&x.V, &x.O, &x.dO, &x.lse}) here(*t, "V, O, dO, lse");
+  a2d_tile_desc d = descriptor(x.Q, x.K, x.V, a + 6, 0);
+  d.lo = layout(x.O);
+  d.ldo = layout(x.dO);
+  const a2d_score_rules r = score_rules(x.Q, x.K, a + 10);
+  const bool acc = truth(a[16]), rounded = truth(a[17]);
+  if (acc && rounded) fail(A2D_ERR_INVALID_ARG, "rounded gradients are not accumulated into");
+  if (acc && a[14] == Py_None) fail(A2D_ERR_INVALID_ARG, "accumulate needs out=(dQ_part, dK_part, dV_part)");
+  Outputs o;
+  const at::ScalarType ot = rounded ? x.Q.scalar_type() : at::kFloat;
+  if (a[14] == Py_None) {
+    o.add(empty_like_shape(x.Q, x.Q.sizes(), ot));
+    for (int i = 0; i < 2; ++i) o.add(empty_like_shape(x.Q, x.K.sizes(), ot));
+  } else {
+    const char* what = rounded ? "out=(dQ, dK, dV)" : "out=(dQ_part, dK_part, dV_part)";
+    o.take(a[14], 3, what);
+    for (int i = 0; i < 3; ++i) exactly(o.t[i], i ? x.K.sizes() : x.Q.sizes(), ot, what);
+  }
+  at::Tensor ws;
+  if (a[15] == Py_None) {
+    ws = empty_like_shape(x.Q, {(int64_t)a2d_workspace_bytes(&d, A2D_OP_PARTIAL_BWD_SCORED, 0)}, at::kByte);
+  } else {
+    ws = tensor(a[15], "workspace");
+    plain(ws, "workspace");
+    here(ws, "workspace");
+  }
+  void *s = stream(), *w = ws.data_ptr();
+  const size_t wb = (size_t)ws.numel() * ws.element_size();
+  const void *q = x.Q.data_ptr(), *k = x.K.data_ptr(), *v = x.V.data_ptr(), *O = x.O.data_ptr(), *g = x.dO.data_ptr();
+  const float* lse = data<float>(x.lse);
+  void *dq = o.t[0].data_ptr(), *dk = o.t[1].data_ptr(), *dv = o.t[2].data_ptr();
+  const int kvh = (int)x.K.size(0);
+  const Scratch scratch(x.Q, s);
+  check(unlocked([&] {
+    return a2d_partial_bwd_scored(&d, kvh, &r, acc ? A2D_TILE_ACCUMULATE : rounded ? A2D_TILE_NORMALISED : 0, q, k, v, O, g, lse,
+                                  dq, dk, dv, w, wb, s);
+  }));
+  scratch.tell();
+  return o.give();
+}
+
+// starts, rows, prefix, first, step, causal, out
+PyObject* document_ranges(Args a) {
+  const at::Tensor& starts = tensor(a[0], "starts");
+  const char* what = "starts (int32 [documents + 1])";
+  if (starts.dim() != 1 || starts.size(0) < 2) fail(A2D_ERR_INVALID_ARG, std::string(what) + ": one document at least");
+  exactly(starts, starts.sizes(), at::kInt, what);
+  const int32_t documents = (int32_t)(starts.size(0) - 1), rows = int32_of(a[1], "rows");
+  const int32_t* prefix = nullptr;
+  if (a[2] != Py_None) {
+    const at::Tensor& t = tensor(a[2], "prefix");
+    exactly(t, {documents}, at::kInt, "prefix (int32 [documents])");
+    prefix = data<int32_t>(t);
+  }
+  const int64_t first = integer(a[3]);
+  const int32_t step = int32_of(a[4], "step");
+  const bool causal = truth(a[5]);
+  if (rows < 1) fail(A2D_ERR_INVALID_ARG, "rows must be >= 1");
+  Outputs o;
+  if (a[6] == Py_None) {
+    o.add(empty_like_shape(starts, {rows, 2}, at::kInt));
+  } else {
+    o.n = 1;
+    o.given[0] = a[6];
+    Py_INCREF(a[6]);
+    o.t[0] = tensor(a[6], "out");
+    exactly(o.t[0], {rows, 2}, at::kInt, "out (int32 [rows][2])");
+  }
+  void* s = stream();
+  check(unlocked([&] {
+    return a2d_document_ranges(documents, data<int32_t>(starts), prefix, causal, first, step, rows, data<int32_t>(o.t[0]), s);
+  }));
+  return o.one(0);
+}
+
+// X (a tensor, or a sequence of up to two), positions, freqs, axis, interleaved, inverse, out (as X), out_dtype
+PyObject* rotary(Args a) {
+  const bool one = THPVariable_Check(a[0]);
+  std::vector<at::Tensor> xs;
+  if (one) {
+    xs.push_back(THPVariable_Unpack(a[0]));
+  } else {
+    const Parts p(a[0], "X");
+    for (auto* t : p.t) xs.push_back(*t);
+  }
+  const int n = (int)xs.size();
+  if (n < 1 || n > A2D_ROTARY_MAX_TENSORS) fail(A2D_ERR_INVALID_ARG, "X must be one or two tensors");
+  const at::Tensor &positions = tensor(a[1], "positions"), &freqs = tensor(a[2], "freqs");
+  if (!freqs.device().is_cpu() || freqs.scalar_type() != at::kDouble || freqs.dim() != 1 || !freqs.is_contiguous())
+    fail(A2D_ERR_INVALID_ARG, "freqs must be a contiguous fp64 tensor [pairs] on the host");
+  a2d_rotary_desc d{};
+  d.rows = (int32_t)xs[0].size(xs[0].dim() > 1 ? 1 : 0);
+  d.hdim = (int32_t)xs[0].size(-1);
+  if (freqs.size(0) > 128) fail(A2D_ERR_INVALID_ARG, "freqs: more pairs than a head has");
+  d.pairs = (int32_t)freqs.size(0);
+  d.freqs = data<double>(freqs);
+  if (a[3] != Py_None) {
+    const at::Tensor& t = tensor(a[3], "axis");
+    if (!t.device().is_cpu() || t.scalar_type() != at::kByte || t.sizes() != freqs.sizes() || !t.is_contiguous())
+      fail(A2D_ERR_INVALID_ARG, "axis must be a contiguous uint8 tensor [pairs] on the host");
+    d.axis = data<uint8_t>(t);
+  }
+  const char* what = "positions (int32 [axes][rows] or [sets][axes][rows])";
+  if (positions.dim() != 2 && positions.dim() != 3) fail(A2D_ERR_INVALID_ARG, std::string(what) + " expected");
+  exactly(positions, positions.sizes(), at::kInt, what);
+  if (positions.size(-1) != d.rows) fail(A2D_ERR_INVALID_ARG, std::string(what) + ": as many rows as X expected");
+  d.axes = (int32_t)std::min<int64_t>(positions.size(-2), 1 << 20);
+  d.sets = positions.dim() == 3 ? (int32_t)std::min<int64_t>(positions.size(0), 1 << 20) : 1;
+  d.positions = data<int32_t>(positions);
+  d.interleaved = truth(a[4]);
+  d.inverse = truth(a[5]);
+  const at::ScalarType it = xs[0].scalar_type(), ot = a[7] == Py_None ? it : dtype_arg(a[7]);
+  d.in_dtype = dtype_code(it);
+  d.out_dtype = dtype_code(ot);
+  Outputs o;
+  if (a[6] == Py_None) {
+    for (int i = 0; i < n; ++i) o.add(at::empty_like(xs[i], xs[i].options().dtype(ot).requires_grad(false)));
+  } else if (one) {
+    o.n = 1;
+    o.given[0] = a[6];
+    Py_INCREF(a[6]);
+    o.t[0] = tensor(a[6], "out");
+  } else {
+    o.take(a[6], n, "out", false);
+  }
+  a2d_rotary_tensor t[A2D_ROTARY_MAX_TENSORS];
+  for (int i = 0; i < n; ++i) {
+    dev3(xs[i], "X");
+    dev3(o.t[i], "out");
+    here(xs[i], "X");
+    here(o.t[i], "out");
+    if (xs[i].size(1) != d.rows || xs[i].size(2) != d.hdim || xs[i].scalar_type() != it || o.t[i].sizes() != xs[i].sizes() ||
+        o.t[i].scalar_type() != ot)
+      fail(A2D_ERR_INVALID_ARG, "the tensors of a call have one number of rows, one head size and one type; out as X, in out_dtype");
+    t[i] = a2d_rotary_tensor{xs[i].data_ptr(), o.t[i].data_ptr(), layout(xs[i]), layout(o.t[i]), (int32_t)xs[i].size(0), 0};
+  }
+  void* s = stream();
+  check(unlocked([&] { return a2d_rotary(&d, n, t, s); }));
+  return one ? o.one(0) : o.give();
+}
+
 // the layout with its strides written out
 a2d_layout full(const at::Tensor& t) {
   const a2d_layout l = layout(t);
@@ -782,6 +1016,8 @@ PyMethodDef g_methods[] = {
     A2D_ENTRY(partial_bwd_static, 11), A2D_ENTRY(fix, 5),          A2D_ENTRY(fix_norm, 4),
     A2D_ENTRY(attnfix, 4),         A2D_ENTRY(fix_bwd, 3),          A2D_ENTRY(grid_forward, 7),
     A2D_ENTRY(grid_backward, 10),  A2D_ENTRY(tile_route, 12),      A2D_ENTRY(grid_route, 9),
+    A2D_ENTRY(partial_fwd_scored, 14), A2D_ENTRY(partial_bwd_scored, 18), A2D_ENTRY(document_ranges, 7),
+    A2D_ENTRY(rotary, 8),
     {"set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
