@@ -704,8 +704,8 @@ a2d_status make_rules(const a2d_tile_desc* d, int32_t kv_heads, const a2d_score_
   if (!(in->softcap >= 0.f) || !std::isfinite(in->softcap))
     return fail(A2D_ERR_INVALID_ARG, "%s: softcap must be finite and >= 0", who);
   // (below, scale / softcap or its square is no normal number any more)
-  if (in->softcap != 0.f && (in->softcap < 1e-6f || in->softcap > 1e6f || d->scale > 1e20f || d->scale < 1e-20f))
-    return fail(A2D_ERR_UNSUPPORTED, "%s: softcap=%g outside 1e-6 .. 1e6, or scale=%g outside 1e-20 .. 1e20 with it", who, in->softcap, d->scale);
+  if (in->softcap != 0.f && (in->softcap < 1e-6f || in->softcap > 1e6f || d->scale / in->softcap > 1e4f || d->scale < 1e-20f))
+    return fail(A2D_ERR_UNSUPPORTED, "%s: softcap=%g outside 1e-6 .. 1e6 or below scale / 1e4, or scale=%g below 1e-20 with it", who, in->softcap, d->scale);
   if (in->token_step < 1 || in->token_step > (1 << 20))
     return fail(A2D_ERR_INVALID_ARG, "%s: token_step=%d outside 1..2^20", who, in->token_step);
   if (in->pad != 0) return fail(A2D_ERR_INVALID_ARG, "%s: rules->pad must be 0", who);
@@ -716,6 +716,17 @@ a2d_status make_rules(const a2d_tile_desc* d, int32_t kv_heads, const a2d_score_
   if (in->slopes) A2D_TRY(check_ptr(in->slopes, who, "slopes"));
   if (in->ranges) A2D_TRY(check_ptr(in->ranges, who, "ranges"));
   r->cap = in->softcap;
+  if (r->cap != 0.f) {
+    // tanh(x) / x = sum c_i x^(2 i) for |x| <= 0.7, the largest relative error (3e-7) the least possible: a weighted least-squares fit on
+    // Chebyshev points, weights moved to where the error is largest until it is even.  Taken at x = scale z / cap, times cap log2(e).
+    const double tanh_of[5] = {0.999999697, -0.333302129, 0.132811123, -0.0508362276, 0.0137737021};
+    const double a = (double)d->scale / r->cap, top = (double)r->cap * 1.4426950408889634;
+    double power = a * top;
+    for (int i = 0; i < 5; ++i, power *= a * a) r->capped.c[i] = (float)(tanh_of[i] * power);
+    r->capped.small = (float)(0.7 / a);
+    r->capped.rate = (float)(2 * 1.4426950408889634 * a);
+    r->capped.top = (float)top;
+  }
   r->step = in->token_step;
   r->heads_per_set = d->heads / in->range_sets;
   r->group = g.group;
@@ -756,8 +767,36 @@ a2d_status a2d_partial_fwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, c
   hipStream_t s = static_cast<hipStream_t>(stream);
   a2d_tile_desc dd;
   A2D_TRY(resolve_layouts(desc, r.group, false, who, &dd));
+  if (a2d::force_generic() || dd.dtype == A2D_F32) {
+    a2d::trace_mark(s);
+    return hip_result(a2d::launch_scored_fwd_generic(dd, r, Q, K, V, out0, out1, out2, s), who);
+  }
+  // N, m, l: where the tile kernel leaves its result - the outputs, or the partials of a split walk
+  const int64_t rows = (int64_t)dd.heads * dd.nq, H = dd.hdim;
+  float *N = static_cast<float*>(out0), *tm = out1, *tl = out2;
+  int cus = 0;
+  A2D_TRY(hip_result(a2d::device_cus(&cus), who));
+  a2d::ScoredPlan plan = a2d::plan_scored_fwd(dd, r, cus, a2d::scratch_offered() ? cap_of(rows * (H + 2)) : 1);
+  if (plan.parts > 1) {
+    N = static_cast<float*>(a2d::scratch_get((size_t)plan.parts * rows * (H + 2) * sizeof(float)));
+    if (N) {
+      tm = N + plan.parts * rows * H;
+      tl = tm + plan.parts * rows;
+    } else {
+      N = static_cast<float*>(out0);
+      plan = a2d::plan_scored_fwd(dd, r, cus, 1);
+    }
+  }
+  const a2d::FwdInput in{static_cast<const float*>(out0), out1, out2};
+  A2D_TRY(hip_result(a2d::launch_scored_fwd(a2d::PREPARE, dd, r, plan, Q, K, V, N, tm, tl, in, s), who));
   a2d::trace_mark(s);
-  return hip_result(a2d::launch_scored_fwd_generic(dd, r, Q, K, V, out0, out1, out2, s), who);
+  A2D_TRY(hip_result(a2d::launch_scored_fwd(a2d::LAUNCH, dd, r, plan, Q, K, V, N, tm, tl, in, s), who));
+  if (plan.parts == 1) return A2D_OK;
+  a2d::FixPtrs p;
+  memset(&p, 0, sizeof(p));
+  for (int z = 0; z < plan.parts; ++z) { p.o[z] = N + z * rows * H; p.m[z] = tm + z * rows; p.l[z] = tl + z * rows; }
+  if (r.norm) return hip_result(a2d::launch_fix(plan.parts, rows, dd.hdim, dd.dtype, p, a2d::plain_out(), out0, out1, s), who);
+  return hip_result(a2d::launch_attnfix(plan.parts, rows, dd.hdim, p, static_cast<float*>(out0), out1, out2, s), who);
 }
 
 a2d_status a2d_partial_bwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, const a2d_score_rules* rules, int flags,

@@ -41,21 +41,13 @@
 // other.  Each lane tracks the true maximum of its own scores; at the end they
 // are combined and N, l are brought to the true row maximum, so (N, m, l) leave the
 // kernel exactly as Eq. (3) defines them.
-#include "a2d_mfma.hpp"
+#include "a2d_fwd.hpp"
 
 namespace a2d {
 namespace {
 
 using namespace mfma;
 
-constexpr int BN = 64;             // keys per step
-__host__ __device__ constexpr int buf_bytes(int hd) { return 2 * BN * 2 * hd; }   // { K tile, V tile }, in blocks
-__host__ __device__ constexpr int lds_bytes(int hd) { return 2 * buf_bytes(hd); }          // of a key lane
-// of a launch: 16 rows of every wavefront come in (accumulating calls) and go out at a time
-__host__ __device__ constexpr int fwd_lds(int waves, int hd, int kl) {
-  const int tiles = kl * lds_bytes(hd), rows = waves / kl * acc_area(hd / 16);
-  return tiles > rows ? tiles : rows;
-}
 // log2 units.  (Peaky rows move their references often: at 32, 8 x 16384 x 16384, sigma 4 917 -> 874 us.  But a probability of 1, which the
 // maximum has where its row's reference has just moved, is rounded to itself, and such rows consist of little else: their results
 // were ten times as far off, 5e-4 of O instead of 3e-5.)
@@ -82,57 +74,6 @@ constexpr FwdCosts kFwdCosts[2] = {
      {0.907, 1.211, 1.609}, {3.5, 3.39, 2.95}, {0.891, 1.288, 1.398}, {3.85, 3.78, 4.22}, 4.42, 4.65, 0.46},
     {{1.314, 1.34, 1.62}, 1.138, 0.707, {1.033, 1.033, 1.033}, 4.06, 1.15, 0.19, 1.77, 0, 0, 0, 0,
      {1.015, 1.119, 1.405}, {3.13, 3.84, 3.97}, {0.888, 1.125, 1.315}, {4.48, 4.18, 4.66}, 3.55, 4.66, 0.141}};
-
-template <int HR>
-struct FwdState {
-  f32x4 o[HR / 16][2];   // column tiles x the wavefront's two tiles of 16 query rows
-  // of the lane's row in each tile:
-  float m_lane[2];       // true running max of this lane's raw dot products
-  float m_ref[2];        // reference the exponentials are taken against (raw units, same in the four lanes of a row)
-  float l_run[2];        // this lane's share of the row sum, relative to m_ref
-};
-
-// A 64-key block for one wavefront, in three pieces; at: its buffer's offset from the addresses in rd.  S^T in tiles of 16 keys (k) x 16
-// queries (q): lane = query, registers = keys 16 k + 4 grp + 0..3; the registers of two key tiles are the eight contraction indices of a
-// lane in O^T += V^T P^T.
-// Fragments of K and V go through rings four deep: each is requested four slots of two MFMAs before its use (the scheduling fences
-// keep the compiler from sinking the requests back to their uses), the first ones before the piece that uses them.
-using Scores = f32x4[4][2];
-using Ring = bf16x8[4];
-template <int HR, int I>                           // slot I of the scores: key tile I & 3, slice I >> 2 of H, both query tiles
-__device__ __forceinline__ void fwd_key(Ring& kr, const Blocks16& rd, unsigned at) {
-  kr[I & 3] = lds_load_b128(rd.nat + at + ((I & 3) * (padded_head(HR) / 32) + (I >> 2)) * BLOCK);
-}
-template <int HR, int I>                           // step I of the products: 32-key group I / HT, column tile I % HT
-__device__ __forceinline__ void fwd_value(Ring& vr, const Blocks16& rd, unsigned at) {
-  constexpr int KS = padded_head(HR) / 32, HT = HR / 16, K_BYTES = buf_bytes(padded_head(HR)) / 2;
-  const unsigned a = (I % HT & 1 ? rd.tr_o : rd.tr_e) + at + K_BYTES + ((I / HT) * 2 * KS + (I % HT >> 1)) * BLOCK;
-  vr[I & 3] = lds_load_tr(a, a + KS * BLOCK);
-}
-template <int HR>
-__device__ __forceinline__ void fwd_first_keys(Ring& kr, const Blocks16& rd, unsigned at) {
-  static_for<0, 4>([&](auto I) { fwd_key<HR, decltype(I)::value>(kr, rd, at); });
-  __builtin_amdgcn_sched_barrier(0);
-}
-template <int HR>
-__device__ __forceinline__ void fwd_first_values(Ring& vr, const Blocks16& rd, unsigned at) {
-  static_for<0, 4>([&](auto I) { fwd_value<HR, decltype(I)::value>(vr, rd, at); });
-  __builtin_amdgcn_sched_barrier(0);
-}
-
-template <int HR>
-__device__ __forceinline__ void fwd_scores(Scores& s, Ring& kr, const bf16x8 (&qf)[padded_head(HR) / 32][2], const Blocks16& rd, unsigned at) {
-  constexpr int KS = padded_head(HR) / 32;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) s[k][0] = s[k][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-  static_for<0, 4 * KS>([&](auto I) {
-    constexpr int i = decltype(I)::value;
-#pragma unroll
-    for (int q = 0; q < 2; ++q) s[i & 3][q] = mma16(kr[i & 3], qf[i >> 2][q], s[i & 3][q]);
-    if constexpr (i + 4 < 4 * KS) fwd_key<HR, i + 4>(kr, rd, at);
-    __builtin_amdgcn_sched_barrier(0);
-  });
-}
 
 // masked: some of the wavefront's rows do not see all of the block's keys
 // (values: called in front of the exponentials)
@@ -191,19 +132,6 @@ __device__ __forceinline__ void fwd_softmax(FwdState<HR>& st, Scores& s, bf16x8 
     st.l_run[q] += psum;
   }
   __builtin_amdgcn_sched_barrier(0);
-}
-
-// O^T += V^T P^T
-template <int HR>
-__device__ __forceinline__ void fwd_products(FwdState<HR>& st, const bf16x8 (&pb)[2][2], Ring& vr, const Blocks16& rd, unsigned at) {
-  constexpr int HT = HR / 16;
-  static_for<0, 2 * HT>([&](auto I) {
-    constexpr int i = decltype(I)::value;
-#pragma unroll
-    for (int q = 0; q < 2; ++q) st.o[i % HT][q] = mma16(vr[i & 3], pb[i / HT][q], st.o[i % HT][q]);
-    if constexpr (i + 4 < 2 * HT) fwd_value<HR, i + 4>(vr, rd, at);
-    __builtin_amdgcn_sched_barrier(0);
-  });
 }
 
 // the three in order

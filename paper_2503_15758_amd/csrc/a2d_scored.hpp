@@ -5,8 +5,15 @@
 
 namespace a2d {
 
+// The cap in log2 units, y = cap log2(e) tanh(scale z / cap) of a raw dot product z: up to |z| = small (0.7 cap / scale) an odd polynomial
+// z (c0 + .. + c4 z^8), fitted to tanh with 3e-7 of it; beyond, top - 2 top / (1 + 2^(rate z)), whose error, some 2^-22 of top, is relative to
+// a y of 0.6 top and more.  (That form alone would be off by 2^-22 of the cap everywhere: as much as y itself for a wide cap.)
+struct CapArgs {
+  float small, rate, top, c[5];
+};
 struct ScoreRules {
   float cap;            // 0: none
+  CapArgs capped;
   int step;
   int heads_per_set;    // query heads of a set of ranges
   int group;            // query heads per key/value head
@@ -46,6 +53,25 @@ __device__ __forceinline__ Run visible_run(const a2d_tile_desc& d, const ScoreRu
   }
   return Run{lo, hi > lo ? hi - lo : 0};
 }
+
+template <bool SMALL_ONLY>
+__device__ __forceinline__ float cap_log2(const CapArgs& a, float z) {
+  const float u = z * z;
+  const float y = z * fmaf(u, fmaf(u, fmaf(u, fmaf(u, a.c[4], a.c[3]), a.c[2]), a.c[1]), a.c[0]);
+  if constexpr (SMALL_ONLY) return y;
+  const float beyond = fmaf(-2.f * a.top, __builtin_amdgcn_rcpf(1.f + fast_exp2(z * a.rate)), a.top);
+  return fabsf(z) <= a.small ? y : beyond;           // (NaN: beyond, which is NaN too)
+}
+
+// bf16 forward on the matrix units (a2d_scored_fwd.hip).  How a call goes out: the form of its workgroups, and how many
+// share a walk of the keys (their partials [parts][heads][nq] in place of the outputs, to be merged).
+struct ScoredPlan {
+  int form, parts;
+};
+enum { SCORED_256, SCORED_LANES, SCORED_32 };        // 256 rows; 128 rows in two key lanes; 32 rows in eight
+ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap);
+hipError_t launch_scored_fwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, const void* Q, const void* K,
+                             const void* V, float* out0, float* out1, float* out2, const FwdInput& in, hipStream_t s);
 
 // one row or key in a workgroup, vector ALU (a2d_scored_generic.hip): both types, every shape
 hipError_t launch_scored_fwd_generic(const a2d_tile_desc& d, const ScoreRules& r, const void* Q, const void* K, const void* V,

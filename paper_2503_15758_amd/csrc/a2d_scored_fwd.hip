@@ -1,0 +1,664 @@
+// bf16 forward tile under score rules (a2d_score_rules in a2d.h) on the matrix units, H = 128, 96, 80 and 64.
+//
+// The contractions are those of fwd_mfma_kernel and fwd_small_kernel: S^T = K Q^T with a lane holding four keys of one query
+// row in each tile of 16 x 16, and P^T as it stands as an operand of O^T += V^T P^T.  Between them the scores are brought into log2
+// units (z -> cap -> minus the bias), so that 2^x follows directly; without cap and bias they stay raw and the exponent
+// takes them in with its multiply-add.  The rules cost vector instructions a score: the cap 6 (a polynomial, see CapArgs; where some
+// score of a wavefront's block is beyond its range 12, two of them of a quarter of the rate), the bias 2.
+//
+// Masks: whatever they are made of, a query row sees one run of keys (visible_run).  A workgroup walks the hull of
+// its rows' runs; a wavefront leaves out the blocks that none of its rows sees, and compares keys only in blocks that some row does not see
+// whole.  Keys outside the hull are not read (rows of a block beyond it re-read the hull's first or last key), so
+// that a cache's unused slots may hold anything.
+//
+// Rows: the query rows of the heads that share a key/value head follow one another (packed) where a head has fewer rows
+// than a workgroup: a token of each of the group's heads reads the keys once.
+#include "a2d_fwd.hpp"
+#include "a2d_scored.hpp"
+
+namespace a2d {
+namespace {
+
+using namespace mfma;
+
+constexpr float kRescaleThreshold = 8.0f;            // log2 units (as in a2d_fwd_mfma.hip)
+
+// Where the rows of a launch lie: `sub` runs of `rows` query rows for a key/value head, cut into blocks
+struct RowMap {
+  int sub, rows;         // packed: 1, group * nq; else group, nq
+  int by_size;           // blocks in order of size (see xcd_map): the causal mask crosses the tile
+  int parts;
+};
+
+// what a wavefront knows of its two tiles of 16 rows; of the lane's row in each
+struct RowState {
+  int64_t q_at[2];       // its place in Q, from the key/value head's first
+  Run run[2];
+  float at[2], slope[2]; // tokens behind key 0; slope in log2 units
+  int lo, hi;            // hull of the wavefront's runs; lo > hi: nothing seen
+  int all_lo, all_hi;    // keys that all of its rows see
+};
+
+// min or max over the 16 lanes of a lane's tile (every 16 lanes hold the same rows)
+template <class F>
+__device__ __forceinline__ int over16(int x, F&& f) {
+#pragma unroll
+  for (int o = 8; o; o >>= 1) x = f(x, __shfl_xor(x, o, 64));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+// rows w0 .. w0 + 31 of the run of map.rows rows that starts at row 0 of query head `head`
+template <bool BIAS>
+__device__ __forceinline__ void look_up_rows(RowState& rs, const a2d_tile_desc& d, const ScoreRules& r, const RowMap& map, int head, int w0,
+                                             int lane) {
+  const auto least = [](int a, int b) { return min(a, b); };
+  const auto most = [](int a, int b) { return max(a, b); };
+  int lo = INT_MAX, hi = 0, all_lo = 0, all_hi = INT_MAX;
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int row = w0 + 16 * q + (lane & 15), in = min(row, map.rows - 1);
+    const Split hd = map.sub == 1 ? Split{in / d.nq, in - in / d.nq * d.nq} : Split{0, in};
+    rs.q_at[q] = hd.q * d.lq.head + hd.r * d.lq.row;
+    rs.run[q] = visible_run(d, r, head + hd.q, hd.r);
+    if constexpr (BIAS) {
+      rs.at[q] = (float)(int)(r.rel + (int64_t)hd.r * r.step);
+      rs.slope[q] = r.slopes[head + hd.q] * kLog2e;
+    }
+    if (row >= map.rows) rs.run[q] = Run{0, 0};                // (never stored; asks for nothing)
+    if (rs.run[q].n > 0) {
+      lo = min(lo, rs.run[q].lo);
+      hi = max(hi, rs.run[q].lo + rs.run[q].n);
+    }
+    if (row < map.rows) {
+      all_lo = max(all_lo, rs.run[q].lo);
+      all_hi = min(all_hi, rs.run[q].lo + rs.run[q].n);
+    }
+  }
+  rs.lo = over16(lo, least);
+  rs.hi = over16(hi, most);
+  rs.all_lo = over16(all_lo, most);
+  rs.all_hi = over16(all_hi, least);
+}
+
+// Raw dot products -> scores in the units of the exponent: log2 with a cap or a bias, else raw.  raw: log2 units of a raw one.  NT tiles of 16 keys from k0 on.
+template <int NT, bool CAP, bool BIAS>
+__device__ __forceinline__ void to_scores(f32x4 (&s)[NT][2], const ScoreRules& r, const RowState& rs, bool masked, int k0, int grp, float raw) {
+  if constexpr (CAP) {
+    float big = 0.f;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int e = 0; e < 4 * NT; ++e) big = fmaxf(big, fabsf(s[e >> 2][q][e & 3]));
+    // (a NaN is left out of the maximum, and comes through the polynomial as NaN)
+    if (A2D_SELDOM(__builtin_amdgcn_ballot_w64(big > r.capped.small) != 0)) {
+      asm volatile("" ::: "memory");                 // keep this a branch
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int e = 0; e < 4 * NT; ++e) s[e >> 2][q][e & 3] = cap_log2<false>(r.capped, s[e >> 2][q][e & 3]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int e = 0; e < 4 * NT; ++e) s[e >> 2][q][e & 3] = cap_log2<true>(r.capped, s[e >> 2][q][e & 3]);
+    }
+  }
+  if constexpr (BIAS) {
+    const float step = (float)r.step;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const float from = fmaf((float)-(k0 + 4 * grp), step, rs.at[q]);       // (whole numbers below 2^24: exact)
+#pragma unroll
+      for (int e = 0; e < 4 * NT; ++e) {
+        const float far = fmaf((float)-(16 * (e >> 2) + (e & 3)), step, from);
+        const float x = s[e >> 2][q][e & 3];
+        s[e >> 2][q][e & 3] = fmaf(-rs.slope[q], fabsf(far), CAP ? x : x * raw);
+      }
+    }
+  }
+  if (A2D_SELDOM(masked)) {
+    asm volatile("" ::: "memory");                   // keep this a branch
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int e = 0; e < 4 * NT; ++e) {
+        const int key = k0 + 16 * (e >> 2) + 4 * grp + (e & 3) - rs.run[q].lo;
+        s[e >> 2][q][e & 3] = (unsigned)key < (unsigned)rs.run[q].n ? s[e >> 2][q][e & 3] : -INFINITY;
+      }
+  }
+}
+
+// One softmax step over NT tiles of 16 keys: the running maximum and its lazy reference (as in fwd_softmax), P^T in bf16.
+// m_lane, m_ref, l_run, o: as in FwdState.  (values: called in front of the exponentials)
+template <int NT, int HT, class F>
+__device__ __forceinline__ void softmax_step(f32x4 (&s)[NT][2], float (&m_lane)[2], float (&m_ref)[2], float (&l_run)[2], f32x4 (&o)[HT][2],
+                                             bf16x8 (&pb)[NT / 2][2], float c, F&& values) {
+  bool grow = false;
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    float mx = m_lane[q];
+#pragma unroll
+    for (int e = 0; e < 4 * NT; ++e) mx = fmaxf(mx, s[e >> 2][q][e & 3]);
+    m_lane[q] = mx;
+    // (m_lane - m_ref is +inf on the first visible block, NaN (-> false) while nothing is visible)
+    grow |= (mx - m_ref[q]) * c > kRescaleThreshold;
+  }
+  if (A2D_SELDOM(__builtin_amdgcn_ballot_w64(grow) != 0)) {
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const float m_row = row_max(m_lane[q]);
+      const float m_use = (m_row == -INFINITY) ? 0.f : m_row;
+      const float alpha = fast_exp2((m_ref[q] - m_use) * c);   // m_ref = -inf gives 0
+      m_ref[q] = m_row;
+      l_run[q] *= alpha;
+#pragma unroll
+      for (int t = 0; t < HT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[t][q][e] *= alpha;
+    }
+  }
+  values();
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const float mc = (m_ref[q] == -INFINITY) ? 0.f : m_ref[q] * c;
+    float psum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4 * NT; ++e) {
+      const float p = fast_exp2(fmaf(s[e >> 2][q][e & 3], c, -mc));
+      psum += p;
+      pb[e >> 3][q][e & 7] = (bf16_t)p;              // (the sum takes the probability before its rounding)
+    }
+    l_run[q] += psum;
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// units of the exponent -> 1: m in natural units, and what the exponentials are multiplied with
+template <bool CAP, bool BIAS>
+struct Units {
+  float raw, c, to_m;                                // exponent of 2 for a raw product, for a unit; m for a unit
+  __device__ __forceinline__ Units(const a2d_tile_desc& d)
+      : raw(uniform(d.scale * kLog2e)), c(CAP || BIAS ? 1.f : raw), to_m(CAP || BIAS ? 1.f / kLog2e : d.scale) {}
+};
+
+// KL = 1: 256 rows, eight wavefronts of 32.  KL = 2: 128 rows in two key lanes of four wavefronts, which take alternate key blocks and
+// are merged through LDS at the end.  (Staging, fragments and epilogue as in fwd_mfma_kernel.)
+// (out0, out1, out2 are not __restrict__: an accumulating call's `in` is the same memory)
+template <int HR, int KL, bool CAP, bool BIAS>
+__global__ __launch_bounds__(512, 1) void scored_fwd_kernel(
+    a2d_tile_desc d, ScoreRules r, RowMap map, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
+    const bf16_t* __restrict__ V, float* out0, float* out1, float* out2, FwdInput in) {
+  constexpr int WAVES = 8, RW = WAVES / KL, BM = 32 * RW, kThreads = 64 * RW;
+  constexpr int HD = padded_head(HR), H = HR, KS = HD / 32, HT = HR / 16, BUF_BYTES = buf_bytes(HD);
+  extern __shared__ __attribute__((aligned(1024))) char lds_all[];
+  __shared__ int hull[2 * RW];
+  const int kl = KL == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads);
+  char* const lds = lds_all + kl * lds_bytes(HD);
+  const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+
+  const int nqb = (map.rows + BM - 1) / BM;
+  int unit, blk;
+  if (!xcd_map(blockIdx.x, d.heads / r.group * map.parts, map.sub * nqb, map.by_size != 0, unit, blk, kXcdCus)) return;
+  const Split up = split_by(unit, map.parts);
+  const int kvh = up.q, part = up.r;
+  const Split in_group = query_head(blk, map.sub, nqb, map.by_size != 0);
+  const int head = kvh * r.group + in_group.r;
+  const int q0 = (nqb - 1 - in_group.q) * BM;         // heavy (late) query blocks first: under a causal mask they walk more keys
+  const int tid = (int)threadIdx.x - kl * kThreads;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, grp = lane >> 4;
+  Q += (int64_t)head * d.lq.head;
+  K += (int64_t)kvh * d.lk.head;
+  V += (int64_t)kvh * d.lv.head;
+  if (map.parts > 1) {
+    const int64_t slot = (int64_t)part * d.heads * d.nq;
+    out0 += slot * H;
+    out1 += slot;
+    out2 += slot;
+  }
+  const int64_t row0 = (int64_t)head * d.nq;          // of the run of rows, in the outputs
+  const Units<CAP, BIAS> units(d);
+
+  RowState rs;
+  look_up_rows<BIAS>(rs, d, r, map, head, q0 + wave * 32, lane);
+  bf16x8 qf[KS][2];
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      const int at = 32 * x + 8 * grp;
+      qf[x][q] = *reinterpret_cast<const bf16x8*>(Q + rs.q_at[q] + min(at, H - 8));
+      if (32 * x + 32 > H && at >= H) qf[x][q] = bf16x8{};
+    }
+  if ((KL == 1 || kl == 0) && lane == 0) {
+    hull[2 * wave] = rs.lo;
+    hull[2 * wave + 1] = rs.hi;
+  }
+  if constexpr (H != HD) {
+    // the K tiles' columns past the head size are zero for good (those of V are not read)
+    for (int i = tid; i < 2 * BN * (HD - H) / 8; i += kThreads) {
+      const int row = i % BN, x = i / BN, buf = x / ((HD - H) / 8), ch = H % 32 / 8 + x % ((HD - H) / 8);
+      *reinterpret_cast<u32x4*>(lds + buf * BUF_BYTES + ((row >> 4) * KS + H / 32) * BLOCK + (row & 15) * 64 +
+                                16 * (ch ^ block_swap((row & 15) >> 2))) = u32x4{0, 0, 0, 0};
+    }
+  }
+  FwdState<HR> st;
+#pragma unroll
+  for (int t = 0; t < HT; ++t) st.o[t][0] = st.o[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_in[2] = {-INFINITY, -INFINITY};
+  st.l_run[0] = st.l_run[1] = 0.f;
+  if (r.acc && part == 0 && kl == 0) {
+    // continues the stored partial: N into the accumulators, m as the exponent's reference, l into one of the four lanes of a row
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int row = q0 + wave * 32 + 16 * q + (lane & 15);
+      if (row >= map.rows) continue;
+      m_in[q] = in.m[row0 + row];
+      st.l_run[q] = grp == 0 ? in.l[row0 + row] : 0.f;
+#pragma unroll
+      for (int t = 0; t < HT; ++t) st.o[t][q] = *reinterpret_cast<const f32x4*>(in.N + (row0 + row) * H + 16 * t + 4 * grp);
+    }
+  }
+  __syncthreads();
+  int lo = INT_MAX, hi = 0;
+#pragma unroll
+  for (int w = 0; w < RW; ++w) {
+    lo = min(lo, hull[2 * w]);
+    hi = max(hi, hull[2 * w + 1]);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  const int first = hi > lo ? lo / BN : 0, end = hi > lo ? (hi + BN - 1) / BN : 0;     // key blocks of the walk
+
+  // ---- staging, straight into LDS: of eight wavefronts 0 .. 3 load a row tile of K each and 4 .. 7 one of V, each of four
+  // one of both.  Rows outside the hull re-read its first or last key.
+  constexpr int LD_N = RW == 8 ? 1 : 2;
+  const int ld_first = RW == 8 ? wave >> 2 : 0, ld_tile = wave & 3, ld_row = 16 * ld_tile + (lane >> 2);
+  const int ld_chunk = (lane & 3) ^ block_swap(lane >> 4);
+  const char* ld_base[LD_N];
+  unsigned ld_row_bytes[LD_N];
+#pragma unroll
+  for (int x = 0; x < LD_N; ++x) {
+    const bool v = ld_first + x != 0;
+    ld_base[x] = reinterpret_cast<const char*>(v ? V : K);
+    ld_row_bytes[x] = __builtin_amdgcn_readfirstlane((unsigned)(v ? d.lv.row : d.lk.row) * 2);
+  }
+  auto load_tile = [&](int j, int boff) {
+    const int from = max(j * BN, lo), row = min(max(j * BN + ld_row, lo), hi - 1) - from;
+#pragma unroll
+    for (int x = 0; x < LD_N; ++x)
+      dma_blocks<KS, H>(lds_base + boff + (4 * (ld_first + x) + ld_tile) * KS * BLOCK,
+                        uniform_gptr(ld_base[x] + (unsigned)from * ld_row_bytes[x]), __umul24(row, ld_row_bytes[x]) + 16 * ld_chunk, ld_chunk);
+  };
+  Blocks16 rd;
+  rd.init(lane, lds_base);
+  const int stride = KL * map.parts;
+  int lead = first + part * KL, j = lead + kl;        // key lane 0's block; this lane's
+  if (j < end) load_tile(j, 0);
+  wait_vmem_all();                                    // (the Q rows and the first tiles together)
+#pragma unroll
+  for (int q = 0; q < 2; ++q) st.m_lane[q] = st.m_ref[q] = m_in[q] / units.to_m;       // -inf stays -inf
+  __syncthreads();
+
+  int boff = 0;
+  for (; lead < end; lead += stride) {
+    if (A2D_OFTEN(j + stride < end)) load_tile(j + stride, BUF_BYTES - boff);
+    const int k0 = j * BN;
+    if (j < end && k0 + BN > rs.lo && k0 < rs.hi) {
+      const bool masked = k0 < rs.all_lo || k0 + BN > rs.all_hi;
+      Scores s;
+      Ring kr, vr;
+      bf16x8 pb[2][2];
+      fwd_first_keys<HR>(kr, rd, boff);
+      fwd_scores<HR>(s, kr, qf, rd, boff);
+      to_scores<4, CAP, BIAS>(s, r, rs, masked, k0, grp, units.raw);
+      softmax_step<4, HT>(s, st.m_lane, st.m_ref, st.l_run, st.o, pb, units.c, [&]() { fwd_first_values<HR>(vr, rd, boff); });
+      fwd_products<HR>(st, pb, vr, rd, boff);
+    }
+    wait_vmem_all();
+    __syncthreads();
+    j += stride;
+    boff = BUF_BYTES - boff;
+  }
+
+  // ---- epilogue: N and l to the true row maximum
+  const float c = units.c;
+  float m_row[2], f[2], l_tot[2];
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    m_row[q] = row_max(st.m_lane[q]);
+    f[q] = (m_row[q] == -INFINITY) ? 0.f : fast_exp2((st.m_ref[q] - m_row[q]) * c);
+    l_tot[q] = row_sum(st.l_run[q]) * f[q];
+  }
+  if constexpr (KL == 2) {
+    // key lane 1 hands its (N, m, l) to lane 0 through LDS, which merges them as two partials (Alg. 2)
+    constexpr int NV = HT * 8 + 4;
+    static_assert(RW * NV * 256 <= KL * lds_bytes(HD), "the exchange area must fit the tile buffers");
+    float* xch = reinterpret_cast<float*>(lds_all) + wave * NV * 64 + lane;
+    if (kl == 1) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+#pragma unroll
+        for (int t = 0; t < HT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) xch[(8 * t + 4 * q + e) * 64] = st.o[t][q][e] * f[q];
+        xch[(HT * 8 + 2 * q) * 64] = m_row[q];
+        xch[(HT * 8 + 2 * q + 1) * 64] = l_tot[q];
+      }
+    }
+    __syncthreads();
+    if (kl == 1) return;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const float m1 = xch[(HT * 8 + 2 * q) * 64], l1 = xch[(HT * 8 + 2 * q + 1) * 64];
+      const float m_new = fmaxf(m_row[q], m1);
+      const float a0 = (m_row[q] == -INFINITY) ? 0.f : f[q] * fast_exp2((m_row[q] - m_new) * c);
+      const float a1 = (m1 == -INFINITY) ? 0.f : fast_exp2((m1 - m_new) * c);
+#pragma unroll
+      for (int t = 0; t < HT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st.o[t][q][e] = st.o[t][q][e] * a0 + xch[(8 * t + 4 * q + e) * 64] * a1;
+      l_tot[q] = (m_row[q] == -INFINITY ? 0.f : l_tot[q] * fast_exp2((m_row[q] - m_new) * c)) + l1 * a1;
+      m_row[q] = m_new;
+      f[q] = 1.f;
+    }
+  }
+  // (KL = 2: inside what this wavefront has read of the exchange)
+  char* const area = lds_all + wave * (KL == 2 ? (HT * 8 + 4) * 256 : acc_area(HT));
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int row = q0 + wave * 32 + 16 * q, n = map.rows - row;
+    const bool stat = grp == 0 && (lane & 15) < n;
+    const int64_t at = row0 + row;
+    if (r.norm && map.parts == 1) {
+      store_acc16(reinterpret_cast<bf16_t*>(out0) + at * H, H, n, area, st.o, q, lane, l_tot[q] > 0.f ? f[q] / l_tot[q] : 0.f);
+      if (stat) out1[at + (lane & 15)] = l_tot[q] > 0.f ? m_row[q] * units.to_m + logf(l_tot[q]) : -INFINITY;
+    } else {
+      store_acc16(out0 + at * H, H, n, area, st.o, q, lane, f[q]);
+      if (stat) {
+        out1[at + (lane & 15)] = m_row[q] * units.to_m;         // -inf stays -inf
+        out2[at + (lane & 15)] = l_tot[q];
+      }
+    }
+  }
+}
+
+// ---- 32 rows and eight key lanes: for few rows.  Every wavefront holds the same rows and takes every eighth slab of 32 keys,
+// which it stages in LDS of its own, without a barrier in the walk (as fwd_small_kernel); the eight (N, m, l) are merged at the end.  Single
+// tokens against a long cache are bound by reading it: a compute unit keeps up to 96 KiB (H = 128) of requests in flight.
+constexpr int SB = 32;
+constexpr int STAT = 8 * 16 * 1024;                  // (slabs, at the end every wavefront's results) | m, l of every wavefront's rows
+constexpr int SMALL_LDS = STAT + 2 * 8 * SB * 4;
+
+template <int HR, bool CAP, bool BIAS>
+__global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
+    a2d_tile_desc d, ScoreRules r, RowMap map, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
+    const bf16_t* __restrict__ V, float* out0, float* out1, float* out2, FwdInput in) {
+  constexpr int HD = padded_head(HR), H = HR, KS = HD / 32, HT = HR / 16, WAVES = 8, BM = 32;
+  constexpr int V_AT = 2 * KS * BLOCK, SLAB_BYTES = 2 * V_AT;
+  static_assert(WAVES * SLAB_BYTES <= STAT && HT * 2 <= 16, "slabs and results must fit");
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int grp = lane >> 4;
+
+  const int nqb = (map.rows + BM - 1) / BM;
+  int unit, blk;
+  if (!xcd_map(blockIdx.x, d.heads / r.group * map.parts, map.sub * nqb, map.by_size != 0, unit, blk, kXcdCus)) return;
+  const Split up = split_by(unit, map.parts);
+  const int kvh = up.q, part = up.r;
+  const Split in_group = query_head(blk, map.sub, nqb, map.by_size != 0);
+  const int head = kvh * r.group + in_group.r;
+  const int q0 = (nqb - 1 - in_group.q) * BM;
+  Q += (int64_t)head * d.lq.head;
+  K += (int64_t)kvh * d.lk.head;
+  V += (int64_t)kvh * d.lv.head;
+  if (map.parts > 1) {
+    const int64_t slot = (int64_t)part * d.heads * d.nq;
+    out0 += slot * H;
+    out1 += slot;
+    out2 += slot;
+  }
+  const int64_t row0 = (int64_t)head * d.nq;
+  const Units<CAP, BIAS> units(d);
+  const float c = units.c;
+
+  RowState rs;
+  look_up_rows<BIAS>(rs, d, r, map, head, q0, lane);
+  bf16x8 qf[KS][2];
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      const int at = 32 * x + 8 * grp;
+      qf[x][q] = *reinterpret_cast<const bf16x8*>(Q + rs.q_at[q] + min(at, H - 8));
+      if (32 * x + 32 > H && at >= H) qf[x][q] = bf16x8{};
+    }
+  const int lo = rs.lo, hi = rs.hi;
+  const int first = hi > lo ? lo / SB : 0, end = hi > lo ? (hi + SB - 1) / SB : 0;
+
+  const unsigned k_row_bytes = __builtin_amdgcn_readfirstlane((unsigned)d.lk.row * 2);
+  const unsigned v_row_bytes = __builtin_amdgcn_readfirstlane((unsigned)d.lv.row * 2);
+  const unsigned slab = lds_base + wave * SLAB_BYTES;
+  const int ld_chunk = (lane & 3) ^ block_swap(lane >> 4);
+  constexpr int LOADS = 2 * KS;                      // of a K or V slab
+  auto load = [&](bool v, int j) {
+    const unsigned row_bytes = v ? v_row_bytes : k_row_bytes;
+    const int from = max(j * SB, lo);
+    const gptr_t base = uniform_gptr(reinterpret_cast<const char*>(v ? V : K) + (unsigned)from * row_bytes);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int row = min(max(j * SB + 16 * t + (lane >> 2), lo), hi - 1) - from;
+      dma_blocks<KS, H>(slab + (v ? V_AT : 0) + t * KS * BLOCK, base, __umul24(row, row_bytes) + 16 * ld_chunk, ld_chunk);
+    }
+  };
+  if constexpr (H != HD) {
+    // the columns of the K slabs past the head size are zero for good (those of V are not read)
+    for (int i = lane; i < SB * (HD - H) / 8; i += 64) {
+      const int row = i % SB, ch = H % 32 / 8 + i / SB;
+      *reinterpret_cast<u32x4*>(lds + wave * SLAB_BYTES + ((row >> 4) * KS + H / 32) * BLOCK + (row & 15) * 64 +
+                                16 * (ch ^ block_swap((row & 15) >> 2))) = u32x4{0, 0, 0, 0};
+    }
+  }
+  Blocks16 rd;
+  rd.init(lane, slab);
+
+  f32x4 o[HT][2];
+#pragma unroll
+  for (int t = 0; t < HT; ++t) o[t][0] = o[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_lane[2] = {-INFINITY, -INFINITY}, m_ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+  if (r.acc && part == 0 && wave == 0) {
+    // the first wavefront continues the stored partial
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int row = q0 + 16 * q + (lane & 15);
+      if (row >= map.rows) continue;
+      m_lane[q] = m_ref[q] = in.m[row0 + row] / units.to_m;
+      l_run[q] = grp == 0 ? in.l[row0 + row] : 0.f;
+#pragma unroll
+      for (int t = 0; t < HT; ++t) o[t][q] = *reinterpret_cast<const f32x4*>(in.N + (row0 + row) * H + 16 * t + 4 * grp);
+    }
+  }
+  wait_vmem_all();                                   // (Q, and what an accumulating call starts from: the waits below count slabs alone)
+  const int stride = WAVES * map.parts;
+  int j = first + part * WAVES + wave;
+  if (j < end) {
+    load(false, j);
+    load(true, j);
+    wait_dma<LOADS>();                               // (K)
+  }
+  // the next K goes where the last one was read from while the exponentials and V P^T are under way, the next V behind those
+  for (; j < end; j += stride) {
+    const bool more = j + stride < end;
+    const int k0 = j * SB;
+    f32x4 s[2][2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) s[k][0] = s[k][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < KS; ++x)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const bf16x8 a = lds_load_b128(rd.nat + (k * KS + x) * BLOCK);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) s[k][q] = mma16(a, qf[x][q], s[k][q]);
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) load(false, j + stride);
+    to_scores<2, CAP, BIAS>(s, r, rs, k0 < rs.all_lo || k0 + SB > rs.all_hi, k0, grp, units.raw);
+    bf16x8 pb[1][2];
+    softmax_step<2, HT>(s, m_lane, m_ref, l_run, o, pb, c, [] {});
+    if (more) wait_dma<LOADS>(); else wait_dma();    // V has arrived
+#pragma unroll
+    for (int t = 0; t < HT; ++t) {
+      const unsigned at = (t & 1 ? rd.tr_o : rd.tr_e) + V_AT + (t >> 1) * BLOCK;
+      const bf16x8 a = lds_load_tr(at, at + KS * BLOCK);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) o[t][q] = mma16(a, pb[0][q], o[t][q]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) {
+      load(true, j + stride);
+      wait_dma<LOADS>();
+    }
+  }
+
+  // ---- the wavefronts' (N, m, l) become one (Alg. 2)
+  float* const xm = reinterpret_cast<float*>(lds + STAT) + (lane & 31);
+  float* const xl = xm + WAVES * 32;
+  float m_row[2], l_row[2], f[2];
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    m_row[q] = row_max(m_lane[q]);
+    f[q] = (m_row[q] == -INFINITY) ? 0.f : fast_exp2((m_ref[q] - m_row[q]) * c);
+    l_row[q] = row_sum(l_run[q]) * f[q];
+  }
+  if (lane < 32) {                                   // (lanes 0 .. 15 hold tile 0's rows, 16 .. 31 tile 1's)
+    xm[wave * 32] = m_row[grp & 1];
+    xl[wave * 32] = l_row[grp & 1];
+  }
+  __syncthreads();
+  f32x4* const x = reinterpret_cast<f32x4*>(lds);
+  const bool norm = r.norm && map.parts == 1;
+  float m_new = -INFINITY, l_tot = 0.f, use[2], fn[2] = {0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < WAVES; ++k) m_new = fmaxf(m_new, xm[k * 32]);
+  const float m_use = m_new == -INFINITY ? 0.f : m_new;
+  row_pair(m_use, use);
+  if (norm || wave == 0) {
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) l_tot += xl[k * 32] * fast_exp2((xm[k * 32] - m_use) * c);
+    row_pair(l_tot > 0.f ? 1.0f / l_tot : 0.f, fn);
+  }
+  if (wave == 0 && lane < 32 && q0 + lane < map.rows) {
+    const int64_t row = row0 + q0 + lane;
+    if (norm) out1[row] = l_tot > 0.f ? m_new * units.to_m + logf(l_tot) : -INFINITY;
+    else {
+      out1[row] = m_new * units.to_m;
+      out2[row] = l_tot;
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const float a = f[q] * fast_exp2((m_row[q] - use[q]) * c);
+    // every wavefront leaves its pieces of four columns, [wavefront][piece][lane], and adds up and stores two of them
+#pragma unroll
+    for (int t = 0; t < HT; ++t)
+      x[(wave * 16 + 2 * t + q) * 64 + lane] = f32x4{o[t][q][0] * a, o[t][q][1] * a, o[t][q][2] * a, o[t][q][3] * a};
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int piece = wave + WAVES * i, q = piece & 1, col = 16 * (piece >> 1) + 4 * grp, row = q0 + 16 * q + (lane & 15);
+    if (piece >= 2 * HT || row >= map.rows) continue;
+    f32x4 v = x[piece * 64 + lane];
+#pragma unroll
+    for (int k = 1; k < WAVES; ++k) {
+      const f32x4 w = x[(k * 16 + piece) * 64 + lane];
+      v[0] += w[0]; v[1] += w[1]; v[2] += w[2]; v[3] += w[3];
+    }
+    const int64_t at = (row0 + row) * H + col;
+    if (norm) {
+      const float by = q ? fn[1] : fn[0];
+      bf16x4 b;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) b[e] = (bf16_t)(v[e] * by);
+      *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16_t*>(out0) + at) = b;
+    } else {
+      *reinterpret_cast<f32x4*>(out0 + at) = v;
+    }
+  }
+}
+
+constexpr int kRows[3] = {256, 128, 32};
+
+RowMap row_map(const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan) {
+  const bool packed = r.group > 1 && d.nq < kRows[plan.form];
+  // (a mask by ranges is not known here)
+  const bool by_size = !packed && d.causal && !r.ranges && r.row_shift < d.nkv && (int64_t)d.nq + r.row_shift > 0 && d.nq > 1;
+  return RowMap{packed ? 1 : r.group, packed ? r.group * d.nq : d.nq, by_size, plan.parts};
+}
+
+template <int HR, bool CAP, bool BIAS>
+hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, const void* Q, const void* K, const void* V,
+              float* out0, float* out1, float* out2, const FwdInput& in, hipStream_t s) {
+  const RowMap map = row_map(d, r, plan);
+  const int bm = kRows[plan.form];
+  const int bytes = plan.form == SCORED_32 ? SMALL_LDS : fwd_lds(8, padded_head(HR), plan.form == SCORED_LANES ? 2 : 1);
+  const auto run = [&](auto* kernel) {
+    if (ph == PREPARE) return ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes);
+    const dim3 grid(xcd_grid(d.heads / r.group * map.parts, map.sub * ((map.rows + bm - 1) / bm)));
+    A2D_LAUNCH(kernel, grid, dim3(512), bytes, s, d, r, map, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, out0, out1, out2, in);
+    return hipGetLastError();
+  };
+  return plan.form == SCORED_256     ? run(scored_fwd_kernel<HR, 1, CAP, BIAS>)
+         : plan.form == SCORED_LANES ? run(scored_fwd_kernel<HR, 2, CAP, BIAS>)
+                                     : run(scored_fwd_small_kernel<HR, CAP, BIAS>);
+}
+
+}  // namespace
+
+ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap) {
+  const int kv_heads = d.heads / r.group;
+  double least = 0;
+  ScoredPlan best{SCORED_256, 1};
+  for (int f = 0; f < 3; ++f) {
+    const int bm = kRows[f];
+    const bool packed = r.group > 1 && d.nq < bm;
+    const int64_t blocks = packed ? (int64_t)kv_heads * (((int64_t)r.group * d.nq + bm - 1) / bm)
+                                  : (int64_t)d.heads * ((d.nq + bm - 1) / bm);
+    const double keys = f == SCORED_32 ? 256 : f == SCORED_LANES ? 128 : 64;
+    double most = d.nkv / keys + 0.2, mean = most;
+    if (d.causal && !packed) {
+      const double last = (double)d.nq + r.row_shift, first = 1.0 + r.row_shift;
+      const auto seen = [&](double x) { return x < 0 ? 0.0 : x > d.nkv ? (double)d.nkv : x; };
+      most = seen(last) / keys + 0.2;
+      mean = 0.5 * (seen(first) + seen(last)) / keys + 0.2;
+    }
+    const double step = f == SCORED_32 ? 1.6 : f == SCORED_LANES ? 2.0 : 1.8, fixed = f == SCORED_32 ? 4.0 : 5.0;
+    const WalkModel m{blocks, cus, mean, most, step, fixed, 0, 0, nullptr, 0, 0.5};
+    const double part_us = (double)d.heads * d.nq * (d.hdim + 2) * 8 / 4.5e6;
+    double t;
+    const int parts = best_parts(m, cap, 4.5, part_us, &t);
+    if (f == 0 || t < 0.98 * least) {
+      least = t;
+      best = ScoredPlan{f, parts};
+    }
+  }
+  return best;
+}
+
+hipError_t launch_scored_fwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, const void* Q, const void* K,
+                             const void* V, float* out0, float* out1, float* out2, const FwdInput& in, hipStream_t s) {
+#define A2D_RULES(HR)                                                                                  \
+  return r.cap != 0.f ? (r.slopes ? go<HR, true, true>(ph, d, r, plan, Q, K, V, out0, out1, out2, in, s)   \
+                                  : go<HR, true, false>(ph, d, r, plan, Q, K, V, out0, out1, out2, in, s)) \
+                      : (r.slopes ? go<HR, false, true>(ph, d, r, plan, Q, K, V, out0, out1, out2, in, s)  \
+                                  : go<HR, false, false>(ph, d, r, plan, Q, K, V, out0, out1, out2, in, s))
+  if (d.hdim == 128) { A2D_RULES(128); }
+  if (d.hdim == 96) { A2D_RULES(96); }
+  if (d.hdim == 80) { A2D_RULES(80); }
+  A2D_RULES(64);
+#undef A2D_RULES
+}
+
+}  // namespace a2d
