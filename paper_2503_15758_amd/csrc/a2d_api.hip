@@ -363,9 +363,9 @@ size_t a2d_workspace_bytes(const a2d_tile_desc* desc, int op, int k) {
   if (!desc || desc->heads < 1 || desc->nq < 1) return 0;
   if (op != A2D_OP_PARTIAL_BWD && op != A2D_OP_PARTIAL_BWD_DS && op != A2D_OP_PARTIAL_BWD_SPLIT && op != A2D_OP_PARTIAL_BWD_SCORED)
     return 0;
+  if (op == A2D_OP_PARTIAL_BWD_SCORED) return a2d::scored_bwd_bytes(*desc);
   const size_t rows = (size_t)desc->heads * (size_t)desc->nq;
   const size_t delta_bytes = ((rows * sizeof(float) + 255) / 256) * 256;
-  if (op == A2D_OP_PARTIAL_BWD_SCORED) return 3 * delta_bytes;          // delta, and each row's run of keys
   if (op == A2D_OP_PARTIAL_BWD || desc->nkv < 1) return delta_bytes;
   // (the dS area is sized for the plain tile whether or not a call ends up using it, so that the
   // areas behind it have a fixed place)
@@ -698,6 +698,13 @@ namespace {
 
 int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0); }
 
+// as cap_of, of dQ, dK or dV of a backward call under score rules: grouped heads over long rows leave half of the chip without dK / dV
+// workgroups, and a partial of theirs is already tens of MiB
+int scored_cap(int64_t floats) {
+  const int64_t n = ((int64_t)128 << 20) / (int64_t)sizeof(float) / floats;
+  return n < 1 ? 1 : n > A2D_MAX_PARTS ? A2D_MAX_PARTS : (int)n;
+}
+
 a2d_status make_rules(const a2d_tile_desc* d, int32_t kv_heads, const a2d_score_rules* in, const char* who, a2d::ScoreRules* r) {
   memset(r, 0, sizeof(*r));
   if (!in) return fail(A2D_ERR_INVALID_ARG, "%s: rules is NULL", who);
@@ -730,6 +737,7 @@ a2d_status make_rules(const a2d_tile_desc* d, int32_t kv_heads, const a2d_score_
   r->step = in->token_step;
   r->heads_per_set = d->heads / in->range_sets;
   r->group = g.group;
+  for (int i = 0; i < 6; ++i) r->steps[i] = (float)(in->token_step * (i < 3 ? i + 1 : 16 * (i - 2)));
   r->rel = d->q_off - d->kv_off;
   r->kv_off = d->kv_off;
   r->slopes = in->slopes;
@@ -830,8 +838,40 @@ a2d_status a2d_partial_bwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, c
   hipStream_t s = static_cast<hipStream_t>(stream);
   a2d_tile_desc dd;
   A2D_TRY(resolve_layouts(desc, r.group, true, who, &dd));
+  if (a2d::force_generic() || dd.dtype == A2D_F32) {
+    a2d::trace_mark(s);
+    return hip_result(a2d::launch_scored_bwd_generic(dd, r, Q, K, V, O, dO, lse, static_cast<float*>(workspace), dQ, dK, dV, s), who);
+  }
+  const int64_t nq = (int64_t)dd.heads * dd.nq * dd.hdim, nk = (int64_t)kv_heads * dd.nkv * dd.hdim;
+  int cus = 0;
+  A2D_TRY(hip_result(a2d::device_cus(&cus), who));
+  const bool offered = a2d::scratch_offered();
+  a2d::ScoredBwdPlan plan = a2d::plan_scored_bwd(dd, r, cus, offered ? scored_cap(nq) : 1, offered ? scored_cap(nk) : 1);
+  const int64_t dq_floats = plan.parts_q > 1 ? plan.parts_q * nq : 0, kv_floats = plan.parts_kv > 1 ? plan.parts_kv * nk : 0;
+  float* more = nullptr;
+  if (dq_floats + kv_floats > 0 && !(more = static_cast<float*>(a2d::scratch_get((size_t)(dq_floats + 2 * kv_floats) * sizeof(float)))))
+    plan = a2d::plan_scored_bwd(dd, r, cus, 1, 1);
+  float* const dq = plan.parts_q > 1 ? more : static_cast<float*>(dQ);
+  float* const dk = plan.parts_kv > 1 ? more + dq_floats : static_cast<float*>(dK);
+  float* const dv = plan.parts_kv > 1 ? dk + kv_floats : static_cast<float*>(dV);
+  A2D_TRY(hip_result(a2d::launch_scored_bwd(a2d::PREPARE, dd, r, plan, Q, K, V, O, dO, lse, workspace, dq, dk, dv, s), who));
   a2d::trace_mark(s);
-  return hip_result(a2d::launch_scored_bwd_generic(dd, r, Q, K, V, O, dO, lse, static_cast<float*>(workspace), dQ, dK, dV, s), who);
+  A2D_TRY(hip_result(a2d::launch_scored_bwd(a2d::LAUNCH, dd, r, plan, Q, K, V, O, dO, lse, workspace, dq, dk, dv, s), who));
+  const a2d::PartSet sets[3] = {{dk, static_cast<float*>(dK), nk, plan.parts_kv, 0},
+                                {dv, static_cast<float*>(dV), nk, plan.parts_kv, 0},
+                                {dq, static_cast<float*>(dQ), nq, plan.parts_q, r.acc}};
+  if (r.norm) {
+    for (const a2d::PartSet& x : sets) {
+      if (x.k == 1) continue;
+      a2d::SumPtrs p;
+      memset(&p, 0, sizeof(p));
+      for (int z = 0; z < x.k; ++z) p.p[z] = x.p + z * x.n;
+      A2D_TRY(hip_result(a2d::launch_fix_bwd(x.k, x.n, 1, A2D_BF16, p, a2d::plain_out(), x.out, s), who));
+    }
+    return A2D_OK;
+  }
+  const int at = plan.parts_kv > 1 ? 0 : 2, n = (plan.parts_kv > 1 ? 2 : 0) + (plan.parts_q > 1 ? 1 : 0);
+  return n ? hip_result(a2d::launch_sum_parts(n, sets + at, s), who) : A2D_OK;
 }
 
 a2d_status a2d_document_ranges(int32_t documents, const int32_t* starts, const int32_t* prefix, int causal, int64_t first,

@@ -6,7 +6,7 @@
 namespace a2d {
 
 // The cap in log2 units, y = cap log2(e) tanh(scale z / cap) of a raw dot product z: up to |z| = small (0.7 cap / scale) an odd polynomial
-// z (c0 + .. + c4 z^8), fitted to tanh with 3e-7 of it; beyond, top - 2 top / (1 + 2^(rate z)), whose error, some 2^-22 of top, is relative to
+// z (c0 + .. + c4 z^8), fitted to tanh with 3e-7 of it; beyond, top (1 - 2 / (1 + 2^(rate z))), whose error, some 2^-22 of top, is relative to
 // a y of 0.6 top and more.  (That form alone would be off by 2^-22 of the cap everywhere: as much as y itself for a wide cap.)
 struct CapArgs {
   float small, rate, top, c[5];
@@ -20,6 +20,7 @@ struct ScoreRules {
   int row_shift;        // causal: row i sees the keys k <= i + row_shift = floor((q_off - kv_off) / step) + i
   int acc, norm;        // as in SegList
   int64_t rel, kv_off;  // tokens: of row 0 behind key 0; of key 0
+  float steps[6];       // step times 1, 2, 3, 16, 32, 48: between the scores that a lane holds
   const float* slopes;
   const int2* ranges;
 };
@@ -54,12 +55,20 @@ __device__ __forceinline__ Run visible_run(const a2d_tile_desc& d, const ScoreRu
   return Run{lo, hi > lo ? hi - lo : 0};
 }
 
+// Distance of score i of tile t (16 rows or keys each) of a lane whose first one is `first` tokens off: each of its additions takes
+// its step from a scalar register (as a multiply-add by a constant it needs a vector register for each constant).
+template <int SIGN>
+__device__ __forceinline__ float distance(const ScoreRules& r, float first, int t, int i) {
+  const float f = t == 0 ? first : SIGN > 0 ? first + r.steps[2 + t] : first - r.steps[2 + t];
+  return i == 0 ? f : SIGN > 0 ? f + r.steps[i - 1] : f - r.steps[i - 1];
+}
+
 template <bool SMALL_ONLY>
 __device__ __forceinline__ float cap_log2(const CapArgs& a, float z) {
   const float u = z * z;
   const float y = z * fmaf(u, fmaf(u, fmaf(u, fmaf(u, a.c[4], a.c[3]), a.c[2]), a.c[1]), a.c[0]);
   if constexpr (SMALL_ONLY) return y;
-  const float beyond = fmaf(-2.f * a.top, __builtin_amdgcn_rcpf(1.f + fast_exp2(z * a.rate)), a.top);
+  const float beyond = a.top * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + fast_exp2(z * a.rate)), 1.f);
   return fabsf(z) <= a.small ? y : beyond;           // (NaN: beyond, which is NaN too)
 }
 
@@ -72,6 +81,18 @@ enum { SCORED_256, SCORED_LANES, SCORED_32 };        // 256 rows; 128 rows in tw
 ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap);
 hipError_t launch_scored_fwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, const void* Q, const void* K,
                              const void* V, float* out0, float* out1, float* out2, const FwdInput& in, hipStream_t s);
+
+// bf16 backward (a2d_scored_bwd.hip).  ws: scored_bwd_bytes(d); parts > 1: dQ, or dK and dV, are partials [parts][heads][rows][H] in fp32,
+// to be summed; else r.norm writes bf16 and r.acc adds to dQ.
+struct ScoredBwdPlan {
+  int lanes, parts_q, parts_kv;                      // key lanes of a dQ workgroup (1: 256 rows, 2: 128); workgroups that share a walk
+};
+constexpr int SCORED_MOST_BITS = 16384;              // bytes: a bit a step of 64 rows of each query head of a group, group * nq <= 2^22
+size_t scored_bwd_bytes(const a2d_tile_desc& d);
+ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap_q, int cap_kv);
+hipError_t launch_scored_bwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K,
+                             const void* V, const void* O, const void* dO, const float* lse, void* ws, float* dQ, float* dK, float* dV,
+                             hipStream_t s);
 
 // one row or key in a workgroup, vector ALU (a2d_scored_generic.hip): both types, every shape
 hipError_t launch_scored_fwd_generic(const a2d_tile_desc& d, const ScoreRules& r, const void* Q, const void* K, const void* V,

@@ -1,0 +1,777 @@
+// bf16 backward tile under score rules (a2d_score_rules in a2d.h) on the matrix units, H = 128, 96, 80 and 64.
+//
+// P = 2^(y - bias - lse) and dP as ever; with t = tanh(z / cap), the gradient of a raw product is dZ = P (1 - t^2) (dP - delta), so a
+// cap costs the polynomial again (see CapArgs) and three vector instructions.  Two kernels, both recomputing S and dP (7 contractions for
+// the 5 of the definition): scored_dq_kernel, whose wavefronts own 32 query rows and walk the keys of their hull, and
+// scored_dkdv_kernel, whose wavefronts own 32 keys and walk the query rows.  (Structure, fragments and staging: dq_rows and dkdv_wide.)
+//
+// Masks.  The dQ kernel looks up what each row sees and leaves it for the other one: per row its run of keys, lse and delta in the
+// units that are used (a row that sees nothing: lse = +inf, so that its P is 0), per 32 rows the hull of their runs and the keys that
+// all of them see.  From the hulls a dK / dV workgroup makes a bit for every step of 64 query rows, and walks the set ones: documents cost
+// nothing but their own scores, wherever they lie.  Rows that see nothing are not loaded (zeros in their place), nor are keys
+// outside a hull: they may hold anything.
+#include "a2d_bwd.hpp"
+#include "a2d_scored.hpp"
+
+namespace a2d {
+namespace {
+
+using namespace mfma;
+
+// what the dQ kernel leaves of the rows, [heads][padded]: padded = nq up to the next multiple of 64
+struct RowTile {
+  int lo, hi;            // hull of the runs (none: lo > hi)
+  int all_lo, all_hi;    // keys that all rows see that see any
+  unsigned live;         // bit i: row i sees something
+  int pad[3];
+};
+struct RowTable {
+  int padded;
+  float *from, *delta;   // lse in log2 units, with a cap; without one -lse in units of raw products: what the scores start from.  -(dO . O)
+  int *lo, *n;           // run of keys
+  RowTile* tiles;        // [heads][padded / 32]
+};
+
+template <class F>
+__device__ __forceinline__ int over16(int x, F&& f) {
+#pragma unroll
+  for (int o = 8; o; o >>= 1) x = f(x, __shfl_xor(x, o, 64));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+// z -> y in log2 units, of 2 x 2 tiles
+__device__ __forceinline__ void cap_in_place(f32x4 (&s)[2][2], const CapArgs& a) {
+  float big = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) big = fmaxf(big, fabsf(s[e >> 3][(e >> 2) & 1][e & 3]));
+  if (A2D_SELDOM(__builtin_amdgcn_ballot_w64(big > a.small) != 0)) {
+    asm volatile("" ::: "memory");                   // keep this a branch
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e >> 3][(e >> 2) & 1][e & 3] = cap_log2<false>(a, s[e >> 3][(e >> 2) & 1][e & 3]);
+      if (e & 1) __builtin_amdgcn_sched_barrier(0);  // (more at a time takes registers that dK and dV need)
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e >> 3][(e >> 2) & 1][e & 3] = cap_log2<true>(a, s[e >> 3][(e >> 2) & 1][e & 3]);
+      if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ dQ
+
+constexpr int BKS = 64;                              // keys per step
+__host__ __device__ constexpr int dq_buf(int hd) { return 2 * BKS * 2 * hd; }      // { K tile, V tile }, in blocks
+__host__ __device__ constexpr int dq_launch_lds(int hd, int kl) {
+  return kl * 2 * dq_buf(hd) > 8 * acc_area(hd / 16) ? kl * 2 * dq_buf(hd) : 8 * acc_area(hd / 16);
+}
+__host__ __device__ constexpr int dq_ring(int hd) { return hd == 64 ? 4 : 2; }
+
+// KL = 1: 256 rows, KL = 2: 128 rows in two key lanes (see scored_fwd_kernel)
+template <int HR, int KL, bool CAP, bool BIAS>
+__global__ __launch_bounds__(512, 1) void scored_dq_kernel(
+    a2d_tile_desc d, ScoreRules r, int by_size, int parts, RowTable tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
+    const bf16_t* __restrict__ V, const bf16_t* __restrict__ O, const bf16_t* __restrict__ dO, const float* __restrict__ lse,
+    float* dQ, int rounded) {
+  constexpr int WAVES = 8, RW = WAVES / KL, BM = 32 * RW, kThreads = 64 * RW;
+  constexpr int HD = padded_head(HR), H = HR, KS = HD / 32, HT = HR / 16, DQ_BUF = dq_buf(HD), RING = dq_ring(HD);
+  extern __shared__ __attribute__((aligned(1024))) char lds_all[];
+  __shared__ int hull[2 * RW];
+  const int kl = KL == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads);
+  char* const lds = lds_all + kl * (2 * DQ_BUF);
+  const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const int nqb = (d.nq + BM - 1) / BM;
+  int unit, blk;
+  if (!xcd_map(blockIdx.x, d.heads / r.group * parts, r.group * nqb, by_size != 0, unit, blk, kXcdCus)) return;
+  const Split up = split_by(unit, parts);
+  const int kvh = up.q, part = up.r;
+  const Split in_group = query_head(blk, r.group, nqb, by_size != 0);
+  const int head = kvh * r.group + in_group.r;
+  const int q0 = (nqb - 1 - in_group.q) * BM;          // heavy blocks first under a causal mask
+  const int tid = (int)threadIdx.x - kl * kThreads;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, grp = lane >> 4;
+  Q += (int64_t)head * d.lq.head;
+  O += (int64_t)head * d.lo.head;
+  dO += (int64_t)head * d.ldo.head;
+  K += (int64_t)kvh * d.lk.head;
+  V += (int64_t)kvh * d.lv.head;
+  const float raw = uniform(d.scale * kLog2e), inv_top = CAP ? 1.f / r.capped.top : 0.f;
+  const float slope = BIAS ? uniform(r.slopes[head] * kLog2e) : 0.f;
+
+  // ---- the rows: fragments, delta, what they see
+  const int w0 = q0 + wave * 32;
+  bf16x8 qf[KS][2], gf[KS][2];
+  f32x4 start[2];                                      // -delta: what dP starts from
+  float lse2[2], from[2];
+  Run run[2];
+  int lo = INT_MAX, hi = 0, all_lo = 0, all_hi = INT_MAX;
+  unsigned live_rows = 0;
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int row = w0 + 16 * q + (lane & 15), in = min(row, d.nq - 1);
+    bf16x8 of[KS];
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      const int at = 32 * x + 8 * grp, ld = min(at, H - 8);
+      qf[x][q] = *reinterpret_cast<const bf16x8*>(Q + (int64_t)in * d.lq.row + ld);
+      gf[x][q] = *reinterpret_cast<const bf16x8*>(dO + (int64_t)in * d.ldo.row + ld);
+      of[x] = *reinterpret_cast<const bf16x8*>(O + (int64_t)in * d.lo.row + ld);
+      if (32 * x + 32 > H && at >= H) qf[x][q] = gf[x][q] = of[x] = bf16x8{};
+    }
+    const float L = lse[(int64_t)head * d.nq + in];
+    run[q] = visible_run(d, r, head, in);
+    if (row >= d.nq || L == -INFINITY) run[q].n = 0;
+    const bool live = run[q].n > 0;
+    live_rows |= ((unsigned)__builtin_amdgcn_ballot_w64(live) & 0xFFFFu) << (16 * q);
+    float del = 0.f;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) del = dot8(__builtin_bit_cast(u32x4, of[x]), __builtin_bit_cast(u32x4, gf[x][q]), del);
+    del = row_sum(del);
+    if (!live) del = 0.f;
+    lse2[q] = live ? L * kLog2e : INFINITY;            // +inf: P = 0
+    if (!live) {
+#pragma unroll
+      for (int x = 0; x < KS; ++x) qf[x][q] = gf[x][q] = bf16x8{};
+    }
+    start[q] = f32x4{-del, -del, -del, -del};
+    if (BIAS) from[q] = (float)(int)(r.rel + (int64_t)in * r.step);
+    if (live) {
+      lo = min(lo, run[q].lo);
+      hi = max(hi, run[q].lo + run[q].n);
+      all_lo = max(all_lo, run[q].lo);
+      all_hi = min(all_hi, run[q].lo + run[q].n);
+    }
+    if (part == 0 && kl == 0 && grp == 0 && row < tab.padded) {
+      const int64_t at = (int64_t)head * tab.padded + row;
+      tab.from[at] = CAP ? lse2[q] : live ? -L / d.scale : -INFINITY;
+      tab.delta[at] = -del;
+      tab.lo[at] = run[q].lo;
+      tab.n[at] = run[q].n;
+    }
+  }
+  const auto least = [](int a, int b) { return min(a, b); };
+  const auto most = [](int a, int b) { return max(a, b); };
+  lo = over16(lo, least);
+  hi = over16(hi, most);
+  all_lo = over16(all_lo, most);
+  all_hi = over16(all_hi, least);
+  if (kl == 0 && lane == 0) {
+    if (part == 0 && w0 < tab.padded) tab.tiles[((int64_t)head * tab.padded + w0) / 32] = RowTile{lo, hi, all_lo, all_hi, live_rows, {0, 0, 0}};
+    hull[2 * wave] = lo;
+    hull[2 * wave + 1] = hi;
+  }
+  if constexpr (H != HD) {                             // columns past the head size are zero for good
+    for (int i = tid; i < 4 * BKS * (HD - H) / 8; i += kThreads) {
+      const int row = i % BKS, x = i / BKS, tile = x / ((HD - H) / 8), ch = H % 32 / 8 + x % ((HD - H) / 8);
+      *reinterpret_cast<u32x4*>(lds + tile * (DQ_BUF / 2) + ((row >> 4) * KS + H / 32) * BLOCK + (row & 15) * 64 +
+                                16 * (ch ^ block_swap((row & 15) >> 2))) = u32x4{0, 0, 0, 0};
+    }
+  }
+  __syncthreads();
+  int wg_lo = INT_MAX, wg_hi = 0;
+#pragma unroll
+  for (int w = 0; w < RW; ++w) {
+    wg_lo = min(wg_lo, hull[2 * w]);
+    wg_hi = max(wg_hi, hull[2 * w + 1]);
+  }
+  wg_lo = __builtin_amdgcn_readfirstlane(wg_lo);
+  wg_hi = __builtin_amdgcn_readfirstlane(wg_hi);
+  const bool some = wg_hi > wg_lo;
+  const int first = some ? wg_lo / BKS : 0, end = some ? (wg_hi + BKS - 1) / BKS : 0;
+
+  f32x4 dq[HT][2];
+#pragma unroll
+  for (int t = 0; t < HT; ++t) dq[t][0] = dq[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  Blocks16 ka;                                         // K tile of the current buffer (V's stands DQ_BUF / 2 behind it)
+  ka.init(lane, lds_base);
+
+  // ---- staging (as in scored_fwd_kernel)
+  constexpr int LD_N = RW == 8 ? 1 : 2;
+  const int ld_first = RW == 8 ? wave >> 2 : 0, ld_tile = wave & 3, ld_row = 16 * ld_tile + (lane >> 2);
+  const int ld_chunk = (lane & 3) ^ block_swap(lane >> 4);
+  const char* ld_base[LD_N];
+  unsigned ld_row_bytes[LD_N];
+#pragma unroll
+  for (int x = 0; x < LD_N; ++x) {
+    const bool v = ld_first + x != 0;
+    ld_base[x] = reinterpret_cast<const char*>(v ? V : K);
+    ld_row_bytes[x] = __builtin_amdgcn_readfirstlane((unsigned)(v ? d.lv.row : d.lk.row) * 2);
+  }
+  auto load_tile = [&](int j, int boff) {
+    const int at = max(j * BKS, wg_lo), row = min(max(j * BKS + ld_row, wg_lo), wg_hi - 1) - at;
+#pragma unroll
+    for (int x = 0; x < LD_N; ++x)
+      dma_blocks<KS, H>(lds_base + boff + (4 * (ld_first + x) + ld_tile) * KS * BLOCK,
+                        uniform_gptr(ld_base[x] + (unsigned)at * ld_row_bytes[x]), __umul24(row, ld_row_bytes[x]) + 16 * ld_chunk, ld_chunk);
+  };
+
+  // one 32-key x 32-query piece, half T of the step at key0 - 32 T (as dq_piece): S^T and dP^T in tiles of 16 keys (k) x 16 queries (q)
+  auto piece = [&](auto TT, int key0) {
+    constexpr int T = decltype(TT)::value, N = 2 * KS, RB = T * 2 * KS * BLOCK, VT = DQ_BUF / 2;
+    bf16x8 kr[RING], vr[RING], kt[RING];
+    auto ld1 = [&](auto X) {
+      constexpr int x = decltype(X)::value;
+      const unsigned at = ka.nat + RB + ((x & 1) * KS + (x >> 1)) * BLOCK;
+      kr[x % RING] = lds_load_b128(at);
+      vr[x % RING] = lds_load_b128(at + VT);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto ld2 = [&](auto I) {
+      constexpr int i = decltype(I)::value;
+      const unsigned at = (i & 1 ? ka.tr_o : ka.tr_e) + RB + (i >> 1) * BLOCK;
+      kt[i % RING] = lds_load_tr(at, at + KS * BLOCK);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    static_for<0, RING>(ld1);
+    f32x4 s[2][2], dp[2][2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) { s[k][q] = f32x4{0.f, 0.f, 0.f, 0.f}; dp[k][q] = start[q]; }
+    static_for<0, N>([&](auto X) {
+      constexpr int x = decltype(X)::value, k = x & 1;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        s[k][q] = mma16(kr[x % RING], qf[x >> 1][q], s[k][q]);
+        dp[k][q] = mma16(vr[x % RING], gf[x >> 1][q], dp[k][q]);
+      }
+      if constexpr (x + RING < N) ld1(std::integral_constant<int, x + RING>{});
+      else ld2(std::integral_constant<int, x + RING - N>{});
+    });
+    if constexpr (CAP) cap_in_place(s, r.capped);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const float base = BIAS ? fmaf((float)-(key0 + 4 * grp), r.steps[0], from[q]) : 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float y = s[e >> 2][q][e & 3];
+        float x = CAP ? y - lse2[q] : fmaf(y, raw, -lse2[q]);
+        if constexpr (BIAS) x = fmaf(-slope, fabsf(distance<-1>(r, base, e >> 2, e & 3)), x);
+        float p = fast_exp2(x);
+        if constexpr (CAP) {
+          const float t = y * inv_top;
+          p = fmaf(-p * t, t, p);
+        }
+        s[e >> 2][q][e & 3] = p * dp[e >> 2][q][e & 3];
+      }
+    }
+    if (A2D_SELDOM(key0 < all_lo || key0 + 32 > all_hi)) {
+      asm volatile("" ::: "memory");                   // keep this a branch
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int key = key0 + 16 * (e >> 2) + 4 * grp + (e & 3) - run[q].lo;
+          s[e >> 2][q][e & 3] = (unsigned)key < (unsigned)run[q].n ? s[e >> 2][q][e & 3] : 0.f;
+        }
+    }
+    bf16x8 dsb[2];                                     // dZ is rounded to the inputs' type, as P is
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dsb[q][e] = (bf16_t)s[e >> 2][q][e & 3];
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<0, HT>([&](auto I) {
+      constexpr int i = decltype(I)::value;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) dq[i][q] = mma16(kt[i % RING], dsb[q], dq[i][q]);
+      if constexpr (i + RING < HT) ld2(std::integral_constant<int, i + RING>{});
+    });
+  };
+
+  const int stride = KL * parts;
+  int lead = first + part * KL, j = lead + kl;
+  if (j < end) load_tile(j, 0);
+  wait_vmem_all();
+  __syncthreads();
+  int boff = 0;
+  for (; lead < end; lead += stride) {
+    if (A2D_OFTEN(j + stride < end)) load_tile(j + stride, DQ_BUF - boff);
+    const int k0 = j * BKS;
+    if (j < end && k0 + 32 > lo && k0 < hi) piece(std::integral_constant<int, 0>{}, k0);
+    if (j < end && k0 + 64 > lo && k0 + 32 < hi) piece(std::integral_constant<int, 1>{}, k0 + 32);
+    const int tog = boff ? -DQ_BUF : DQ_BUF;
+    ka.nat += tog; ka.tr_e += tog; ka.tr_o += tog;
+    boff = DQ_BUF - boff;
+    wait_vmem_all();
+    __syncthreads();
+    j += stride;
+  }
+  if constexpr (KL == 2) {
+    // lane 1 hands its sums to lane 0 through LDS
+    static_assert(RW * HT * 8 * 256 <= KL * 2 * DQ_BUF, "the exchange area must fit the tile buffers");
+    float* xch = reinterpret_cast<float*>(lds_all) + wave * (HT * 8 * 64) + lane;
+    if (kl == 1) {
+#pragma unroll
+      for (int t = 0; t < HT; ++t)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) xch[(8 * t + e) * 64] = dq[t][e >> 2][e & 3];
+    }
+    __syncthreads();
+    if (kl == 1) return;
+#pragma unroll
+    for (int t = 0; t < HT; ++t)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dq[t][e >> 2][e & 3] += xch[(8 * t + e) * 64];
+  }
+  char* const area = lds_all + wave * (KL == 2 ? HT * 8 * 256 : acc_area(HT));
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int row = w0 + 16 * q;
+    const int64_t at = (((int64_t)part * d.heads + head) * d.nq + row) * H;
+    if (rounded) store_acc16(reinterpret_cast<bf16_t*>(dQ) + at, H, d.nq - row, area, dq, q, lane, d.scale);
+    else store_acc16(dQ + at, H, d.nq - row, area, dq, q, lane, d.scale, parts == 1 && r.acc != 0);
+  }
+}
+
+// --------------------------------------------------------------------------------------------- dK, dV
+
+constexpr int WK_KEYS = 256, WK_THREADS = 512, WK_ROWS = 64;
+__host__ __device__ constexpr int wk_tile(int hd) { return WK_ROWS * 2 * hd; }
+// LDS: two buffers { Q tile, dO tile } in blocks | two of { from [64], -delta [64], lo [64], n [64] } | two of two RowTiles | bits
+// (64-bit words) of the steps.  (At the end 16 keys of every wavefront go out at a time.)
+constexpr int WK_STAT = 4 * WK_ROWS * 4, WK_TILES = 2 * sizeof(RowTile);
+__host__ __device__ constexpr int wk_stat(int hd) { return 4 * wk_tile(hd); }
+__host__ __device__ constexpr int wk_bits(int hd) {
+  const int walk = wk_stat(hd) + 2 * WK_STAT + 2 * WK_TILES, rows = 8 * acc_area(hd / 16);
+  return walk > rows ? walk : rows;
+}
+
+// slices of H whose K^T and V^T fragments wait in LDS, behind the bits
+__host__ __device__ constexpr int wk_park(int hd) { return hd == 128 ? 1 : 0; }
+__host__ __device__ constexpr int wk_lds(int hd) { return wk_bits(hd) + SCORED_MOST_BITS + wk_park(hd) * 8 * 4 * BLOCK; }
+
+template <int HR, bool CAP, bool BIAS>
+__global__ __launch_bounds__(WK_THREADS) void scored_dkdv_kernel(
+    a2d_tile_desc d, ScoreRules r, int by_size, int parts, RowTable tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
+    const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO, float* __restrict__ dK, float* __restrict__ dV, int rounded) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  constexpr int HD = padded_head(HR), H = HR, TILE = wk_tile(HD), BUF = 2 * TILE;
+  constexpr int KS = HD / 32, HT = HR / 16;
+  constexpr bool TIGHT = HD == 128;                  // registers (see dkdv_wide)
+  const int kv_heads = d.heads / r.group, nkb = (d.nkv + WK_KEYS - 1) / WK_KEYS;
+  int unit, blk;
+  if (!xcd_map(blockIdx.x, kv_heads * parts, nkb, by_size != 0, unit, blk)) return;
+  const Split up = split_by(unit, parts);
+  const int head = up.q, part = up.r, qh0 = head * r.group;
+  const int k0 = blk * WK_KEYS;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int l16 = lane & 15, grp = lane >> 4;
+  Q += (int64_t)qh0 * d.lq.head;
+  dO += (int64_t)qh0 * d.ldo.head;
+  K += (int64_t)head * d.lk.head;
+  V += (int64_t)head * d.lv.head;
+  const float raw = uniform(d.scale * kLog2e), inv_top = CAP ? uniform(1.f / r.capped.top) : 0.f;
+
+  // ---- the steps of 64 query rows, of all query heads one after another, that see a key of the workgroup: a bit each
+  const int nsteps = tab.padded / WK_ROWS, all_steps = nsteps * r.group, words = (all_steps + 63) / 64;
+  uint64_t* const bits = reinterpret_cast<uint64_t*>(lds + wk_bits(HD));
+  const RowTile* const tiles = tab.tiles + (int64_t)qh0 * (tab.padded / 32);
+  for (int w = wave; w < words; w += 8) {
+    const int s = 64 * w + lane;
+    bool seen = false;
+    if (s < all_steps) {
+      const RowTile &a = tiles[2 * s], &b = tiles[2 * s + 1];    // (a head's tiles follow the one before's: 2 a step)
+      const int al = a.lo, ah = a.hi, bl = b.lo, bh = b.hi;
+      seen = (al < ah && al < k0 + WK_KEYS && ah > k0) || (bl < bh && bl < k0 + WK_KEYS && bh > k0);
+    }
+    const uint64_t m = __builtin_amdgcn_ballot_w64(seen);
+    if (lane == 0) bits[w] = m;
+  }
+
+  // ---- K^T and V^T fragments of the wavefront's 32 keys, two tiles of 16: lane = key.  Keys beyond nkv re-read the last one; no
+  // row's run holds them.  (Columns past the head size are zero.)
+  const int wk = k0 + wave * 32, key = wk + l16;     // (of tile 0)
+  // Where registers are tight the first slice of both stays in LDS instead (PARK): it is read where a contraction begins, when
+  // its results' registers are still free.
+  constexpr int PARK = wk_park(HD);
+  const unsigned park = lds_base + wk_bits(HD) + SCORED_MOST_BITS + wave * 4 * BLOCK;
+  bf16x8 kf[KS - PARK][2], vf[KS - PARK][2];
+#pragma unroll
+  for (int kt = 0; kt < 2; ++kt) {
+    const int64_t at_row = min(key + 16 * kt, d.nkv - 1);
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      const int at = 32 * x + 8 * grp, ld = min(at, H - 8);
+      bf16x8 kx = *reinterpret_cast<const bf16x8*>(K + at_row * d.lk.row + ld);
+      bf16x8 vx = *reinterpret_cast<const bf16x8*>(V + at_row * d.lv.row + ld);
+      if (32 * x + 32 > H && at >= H) kx = vx = bf16x8{};
+      if (x < PARK) {
+        auto* const p = reinterpret_cast<__attribute__((address_space(3))) bf16x8*>((uintptr_t)(park + 16 * lane));
+        p[64 * kt] = kx;
+        p[64 * (2 + kt)] = vx;
+      } else {
+        kf[x - PARK][kt] = kx;
+        vf[x - PARK][kt] = vx;
+      }
+    }
+  }
+  f32x4 dk[HT][2], dv[HT][2];
+#pragma unroll
+  for (int x = 0; x < HT; ++x)
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) dk[x][kt] = dv[x][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if constexpr (H != HD) {                           // columns past the head size are zero for good
+    for (int i = tid; i < 4 * WK_ROWS * (HD - H) / 8; i += WK_THREADS) {
+      const int row = i % WK_ROWS, x = i / WK_ROWS, tile = x / ((HD - H) / 8), ch = H % 32 / 8 + x % ((HD - H) / 8);
+      *reinterpret_cast<u32x4*>(lds + tile * TILE + ((row >> 4) * KS + H / 32) * BLOCK + (row & 15) * 64 +
+                                16 * (ch ^ block_swap((row & 15) >> 2))) = u32x4{0, 0, 0, 0};
+    }
+  }
+  __syncthreads();
+  const auto word = [&](int w) -> uint64_t {
+    const uint64_t b = bits[w];
+    return (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
+  };
+  // this part's share of the set bits: from number `skip` on, `total` of them
+  int total = 0, skip = 0, at_word = 0;
+  for (int w = 0; w < words; ++w) total += __builtin_popcountll(word(w));
+  if (parts > 1) {
+    skip = (int)((int64_t)part * total / parts);
+    total = (int)((int64_t)(part + 1) * total / parts) - skip;
+  }
+  uint64_t left = words ? word(0) : 0;
+  while (skip > 0) {
+    const int n = __builtin_popcountll(left);
+    if (n <= skip) {
+      skip -= n;
+      if (++at_word == words) break;
+      left = word(at_word);
+    } else {
+      for (; skip > 0; --skip) left &= left - 1;
+    }
+  }
+  const auto next_step = [&]() -> int {              // (called `total` times)
+    while (left == 0 && at_word + 1 < words) left = word(++at_word);
+    const int s = 64 * at_word + __builtin_ctzll(left);
+    left &= left - 1;
+    return s;
+  };
+
+  // ---- staging, straight into LDS: wavefronts 0 .. 3 load a row tile of Q each, 4 .. 7 of dO; 0 .. 3 also bring one of the row
+  // tables each, 4 the tiles' records.  The next step is requested while one is computed.  Rows that see nothing are
+  // zeros (what they see has been asked for a step earlier: live).
+  const bool is_g = wave >= 4;
+  const int ld_tile = 16 * (wave & 3);
+  const bf16_t* const ld_base = is_g ? dO : Q;
+  const int64_t ld_head = is_g ? d.ldo.head : d.lq.head;
+  const unsigned ld_row_bytes = __builtin_amdgcn_readfirstlane((unsigned)(is_g ? d.ldo.row : d.lq.row) * 2);
+  const int* const ld_table = wave == 0   ? reinterpret_cast<const int*>(tab.from)
+                              : wave == 1 ? reinterpret_cast<const int*>(tab.delta)
+                              : wave == 2 ? tab.lo
+                                          : tab.n;
+  struct Step {
+    int head, i0;                                    // of the group; first row
+  };
+  const auto place = [&](int s) {
+    const int h = s / nsteps;
+    return Step{h, (s - h * nsteps) * WK_ROWS};
+  };
+  // which of the 16 rows that this wavefront loads see anything (a scalar load: the table is an earlier kernel's)
+  const auto ask_live = [&](Step st) -> unsigned {
+    const int64_t at = (((int64_t)qh0 + st.head) * tab.padded + st.i0 + ld_tile) / 32;
+    const auto* p = reinterpret_cast<const __attribute__((address_space(4))) RowTile*>(reinterpret_cast<uint64_t>(tab.tiles + at));
+    return p->live >> (ld_tile & 16) & 0xFFFFu;
+  };
+  const auto load_step = [&](Step st, unsigned live, int buf) {
+    const int ln = TIGHT ? lane_again() : lane, ch = (ln & 3) ^ block_swap(ln >> 4);
+    const unsigned at = lds_base + buf * BUF + wave * KS * BLOCK;
+    const gptr_t base = uniform_gptr(reinterpret_cast<const char*>(ld_base + st.head * ld_head) + (int64_t)(st.i0 + ld_tile) * ld_row_bytes);
+    const unsigned off = __umul24(ln >> 2, ld_row_bytes) + 16 * ch;
+    if (A2D_OFTEN(live == 0xFFFFu)) {
+      dma_blocks<KS, H>(at, base, off, ch);
+    } else if (live >> (ln >> 2) & 1) {
+      dma_blocks<KS, H>(at, base, off, ch);
+    } else {
+#pragma unroll
+      for (int x = 0; x < KS; ++x)
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4*>((uintptr_t)(at + x * BLOCK + 16 * ln)) = u32x4{0, 0, 0, 0};
+    }
+    const int64_t row = ((int64_t)qh0 + st.head) * tab.padded + st.i0;
+    const unsigned stat = lds_base + wk_stat(HD);
+    if (wave < 4) {
+      dma_b32<0>(stat + buf * WK_STAT + wave * (4 * WK_ROWS), uniform_gptr(ld_table + row), 4 * ln);
+    } else if (wave == 4) {
+      if (ln < WK_TILES / 4) dma_b32<0>(stat + 2 * WK_STAT + buf * WK_TILES, uniform_gptr(tab.tiles + row / 32), 4 * ln);
+    }
+  };
+  Step now{0, 0}, then{0, 0};
+  unsigned live = 0;
+  if (total > 0) {
+    now = place(next_step());
+    load_step(now, ask_live(now), 0);
+    if (total > 1) {
+      then = place(next_step());
+      live = ask_live(then);
+    }
+  }
+  wait_dma();
+  __syncthreads();
+
+  Blocks16 da;
+  da.init(lane, lds_base);
+  unsigned st_addr = lds_base + wk_stat(HD) + 16 * grp;
+
+  // Half a step: S and dP of 32 rows in tiles of 16 rows (t) x 16 keys (kt), lane = key, registers = rows 16 t + 4 grp + 0..3 (see
+  // dkdv_wide).  i0: its first row
+  constexpr int N1 = 2 * KS, N2 = 4 * KS, N3 = N2 + HT, N4 = N3 + HT, RING = TIGHT || N4 % 4 != 0 ? 2 : 4;
+  auto compute = [&](int i0, float slope, bool masked) {
+    bf16x8 a[RING];
+    auto ld = [&](auto I) {
+      constexpr int i = decltype(I)::value;
+      if constexpr (i < N2) a[i % RING] = lds_load_b128(da.nat + (i < N1 ? 0 : TILE) + ((i & 1) * KS + (i % N1 >> 1)) * BLOCK);
+      else if constexpr (i < N4) {
+        constexpr int y = i < N3 ? i - N2 : i - N3;
+        const unsigned at = (y & 1 ? da.tr_e ^ 32 : da.tr_e) + (i < N3 ? TILE : 0) + (y >> 1) * BLOCK;
+        a[i % RING] = lds_load_tr(at, at + KS * BLOCK);
+      }
+    };
+    bf16x8 first[2];                                   // (parked)
+    const auto fetch = [&](int v) {
+      const unsigned at = park + 16 * (TIGHT ? lane_again() : lane) + 2 * BLOCK * v;
+      first[0] = lds_load_b128(at);
+      first[1] = lds_load_b128(at + BLOCK);
+    };
+    if constexpr (PARK) fetch(0);
+    static_for<0, RING>(ld);
+    f32x4 s[2][2], dp[2][2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) s[t][0] = s[t][1] = CAP ? f32x4{0.f, 0.f, 0.f, 0.f} : lds_load_f32x4(st_addr + 64 * t);
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<0, N1>([&](auto I) {
+      constexpr int i = decltype(I)::value, x = i >> 1, t = i & 1;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) s[t][kt] = mma16(a[i % RING], x < PARK ? first[kt] : kf[x < PARK ? 0 : x - PARK][kt], s[t][kt]);
+      ld(std::integral_constant<int, i + RING>{});
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (CAP) cap_in_place(s, r.capped);
+    if constexpr (PARK) fetch(1);
+    f32x4 l2[2];                                       // (with a cap)
+    if constexpr (CAP) l2[0] = lds_load_f32x4(st_addr);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) dp[t][0] = dp[t][1] = lds_load_f32x4(st_addr + WK_ROWS * 4 + 64 * t);
+    float base[2] = {0.f, 0.f};
+    if constexpr (BIAS) {
+      const int ln = TIGHT ? lane_again() : lane;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+        base[kt] = (float)(int)(r.rel + (int64_t)(i0 + 4 * (ln >> 4) - (wk + (ln & 15) + 16 * kt)) * r.step);
+    }
+    bf16x8 pb[2], sb[2];
+    // score e of the lane's 16: row tile e >> 3, key tile (e >> 2) & 1, row e & 3 of the lane's four.  P to pb, P (1 - t^2) stays in s
+    auto prob = [&](int e) {
+      const int t = e >> 3, kt = (e >> 2) & 1, i = e & 3;
+      const float y = s[t][kt][i];
+      float x = CAP ? y - l2[t][i] : y * raw;
+      if constexpr (BIAS) x = fmaf(-slope, fabsf(distance<1>(r, base[kt], t, i)), x);
+      const float p = fast_exp2(x);
+      pb[kt][4 * t + i] = (bf16_t)p;
+      if constexpr (CAP) {
+        const float u = y * inv_top;
+        s[t][kt][i] = fmaf(-p * u, u, p);
+      } else {
+        s[t][kt][i] = p;
+      }
+    };
+    // (hidden pairs: their products may have overflowed, so they are taken out of the scores themselves.  HIDDEN: 2^x of it is 0; with
+    // a cap its square, times 0, must be 0 too)
+    auto mask = [&]() {
+      if (A2D_SELDOM(masked)) {
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const u32x4 lo = __builtin_bit_cast(u32x4, lds_load_f32x4(st_addr + 2 * WK_ROWS * 4 + 64 * t));
+          const u32x4 n = __builtin_bit_cast(u32x4, lds_load_f32x4(st_addr + 3 * WK_ROWS * 4 + 64 * t));
+          const int ln = TIGHT ? lane_again() : lane;
+          float HIDDEN = CAP ? -1e30f : -INFINITY;
+          asm volatile("" : "+v"(HIDDEN));             // (it would be kept in a register for all steps)
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              s[t][kt][i] = (unsigned)(wk + (ln & 15) + 16 * kt) - lo[i] < n[i] ? s[t][kt][i] : HIDDEN;
+        }
+      }
+    };
+    auto dscore = [&](int e) {
+      const int t = e >> 3, kt = (e >> 2) & 1, i = e & 3;
+      sb[kt][4 * t + i] = (bf16_t)(s[t][kt][i] * dp[t][kt][i]);
+    };
+    mask();
+    static_for<0, N1>([&](auto I) {
+      constexpr int i = decltype(I)::value, x = i >> 1, t = i & 1;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) dp[t][kt] = mma16(a[(N1 + i) % RING], x < PARK ? first[kt] : vf[x < PARK ? 0 : x - PARK][kt], dp[t][kt]);
+      if constexpr (CAP && i == N1 / 2 - 1) l2[1] = lds_load_f32x4(st_addr + 64);
+#pragma unroll
+      for (int e = 16 * i / N1; e < 16 * (i + 1) / N1; ++e) prob(e);
+      ld(std::integral_constant<int, N1 + i + RING>{});
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (A2D_SELDOM(masked)) {
+      // (0 times the product of a dO with what an unseen key's V holds)
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int t = (e >> 2) & 1, kt = e >> 3, i = e & 3;
+        dp[t][kt][i] = s[t][kt][i] == 0.f ? 0.f : dp[t][kt][i];
+      }
+    }
+    static_for<0, HT>([&](auto Y) {
+      constexpr int y = decltype(Y)::value;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) dv[y][kt] = mma16(a[(N2 + y) % RING], pb[kt], dv[y][kt]);
+#pragma unroll
+      for (int e = 16 * y / HT; e < 16 * (y + 1) / HT; ++e) dscore(e);
+      ld(std::integral_constant<int, N2 + y + RING>{});
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    static_for<0, HT>([&](auto Y) {
+      constexpr int y = decltype(Y)::value;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) dk[y][kt] = mma16(a[(N3 + y) % RING], sb[kt], dk[y][kt]);
+      ld(std::integral_constant<int, N3 + y + RING>{});
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+
+  constexpr int HALF = 2 * KS * BLOCK;               // of a tile
+  int buf = 0;
+#pragma nounroll
+  for (int n = 0; n < total; ++n) {
+    const Step cur = now;
+    if (n + 1 < total) {
+      load_step(then, live, buf ^ 1);
+      now = then;
+      if (n + 2 < total) {
+        then = place(next_step());
+        live = ask_live(then);
+      }
+    }
+    const float slope = BIAS ? uniform(r.slopes[qh0 + cur.head] * kLog2e) : 0.f;
+#pragma nounroll
+    for (int h = 0; h < 2; ++h) {
+      const u32x4 rec = __builtin_bit_cast(u32x4, lds_load_f32x4(lds_base + wk_stat(HD) + 2 * WK_STAT + buf * WK_TILES + (int)sizeof(RowTile) * h));
+      const int lo = __builtin_amdgcn_readfirstlane(rec[0]), hi = __builtin_amdgcn_readfirstlane(rec[1]);
+      const int all_lo = __builtin_amdgcn_readfirstlane(rec[2]), all_hi = __builtin_amdgcn_readfirstlane(rec[3]);
+      if (lo < wk + 32 && hi > wk) compute(cur.i0 + 32 * h, slope, all_lo > wk || all_hi < wk + 32);
+      const int go = h == 0 ? HALF : buf ? -BUF - HALF : BUF - HALF;
+      da.nat += go; da.tr_e += go;
+      st_addr += h == 0 ? 32 * 4 : buf ? -WK_STAT - 32 * 4 : WK_STAT - 32 * 4;
+    }
+    buf ^= 1;
+    wait_dma();
+    __syncthreads();
+  }
+
+  char* const area = lds + wave * acc_area(HT);
+  const int ln = TIGHT ? lane_again() : lane;
+#pragma unroll
+  for (int kt = 0; kt < 2; ++kt) {
+    const int first = wk + 16 * kt, n = d.nkv - first;
+    const int64_t at = (((int64_t)part * kv_heads + head) * d.nkv + first) * H;
+    if (rounded) {
+      store_acc16(reinterpret_cast<bf16_t*>(dV) + at, H, n, area, dv, kt, ln, 1.0f);
+      store_acc16(reinterpret_cast<bf16_t*>(dK) + at, H, n, area, dk, kt, ln, d.scale);
+    } else {
+      store_acc16(dV + at, H, n, area, dv, kt, ln, 1.0f);
+      store_acc16(dK + at, H, n, area, dk, kt, ln, d.scale);
+    }
+  }
+}
+
+// (of one tile's rows and keys: the table in `ws`, see scored_bwd_bytes)
+RowTable row_table(const a2d_tile_desc& d, void* ws) {
+  RowTable t;
+  t.padded = (d.nq + 63) / 64 * 64;
+  const int64_t n = (int64_t)d.heads * t.padded;
+  t.from = static_cast<float*>(ws);
+  t.delta = t.from + n;
+  t.lo = reinterpret_cast<int*>(t.delta + n);
+  t.n = t.lo + n;
+  t.tiles = reinterpret_cast<RowTile*>(t.n + n);
+  return t;
+}
+
+template <int HR, bool CAP, bool BIAS>
+hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K, const void* V,
+              const void* O, const void* dO, const float* lse, void* ws, float* dQ, float* dK, float* dV, hipStream_t s) {
+  constexpr int HD = padded_head(HR);
+  const RowTable tab = row_table(d, ws);
+  const int by_size = d.causal && !r.ranges && r.row_shift < d.nkv && (int64_t)d.nq + r.row_shift > 0 && d.nq > 1;
+  const int kvh = d.heads / r.group, dq_bytes = dq_launch_lds(HD, plan.lanes);
+  const int words = (tab.padded / WK_ROWS * r.group + 63) / 64, wk_bytes = wk_park(HD) ? wk_lds(HD) : wk_bits(HD) + 8 * words;
+  const auto dq = [&](auto* kernel) {
+    if (ph == PREPARE) return ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), dq_bytes);
+    const int bm = plan.lanes == 2 ? 128 : 256;
+    A2D_LAUNCH(kernel, dim3(xcd_grid(kvh * plan.parts_q, r.group * ((d.nq + bm - 1) / bm))), dim3(512), dq_bytes, s, d, r, by_size,
+               plan.parts_q, tab, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, (const bf16_t*)O, (const bf16_t*)dO, lse, dQ,
+               (int)(r.norm && plan.parts_q == 1));
+    return hipGetLastError();
+  };
+  hipError_t e = plan.lanes == 2 ? dq(scored_dq_kernel<HR, 2, CAP, BIAS>) : dq(scored_dq_kernel<HR, 1, CAP, BIAS>);
+  if (e != hipSuccess) return e;
+  // (the most a call can ask for: ensure_dynamic_lds is asked once for a kernel)
+  if (ph == PREPARE) return ensure_dynamic_lds(reinterpret_cast<const void*>(scored_dkdv_kernel<HR, CAP, BIAS>), wk_lds(HD));
+  A2D_LAUNCH((scored_dkdv_kernel<HR, CAP, BIAS>), dim3(xcd_grid(kvh * plan.parts_kv, (d.nkv + WK_KEYS - 1) / WK_KEYS)), dim3(WK_THREADS),
+             wk_bytes, s, d, r, by_size, plan.parts_kv, tab, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, (const bf16_t*)dO, dK, dV,
+             (int)(r.norm && plan.parts_kv == 1));
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t scored_bwd_bytes(const a2d_tile_desc& d) {
+  const size_t n = (size_t)d.heads * ((d.nq + 63) / 64 * 64);
+  return 16 * n + n / 32 * sizeof(RowTile);
+}
+
+ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap_q, int cap_kv) {
+  const auto seen = [&](double x) { return x < 0 ? 0.0 : x > d.nkv ? (double)d.nkv : x; };
+  double most = d.nkv, mean = most, rows_mean = (double)d.nq * r.group;
+  if (d.causal) {
+    most = seen((double)d.nq + r.row_shift);
+    mean = 0.5 * (seen(1.0 + r.row_shift) + most);
+    rows_mean *= mean / d.nkv;
+  }
+  ScoredBwdPlan best{1, 1, 1};
+  double least = 0;
+  const double part_q = (double)d.heads * d.nq * d.hdim * 8 / 4.5e6, part_kv = (double)(d.heads / r.group) * d.nkv * d.hdim * 16 / 4.5e6;
+  for (int lanes = 1; lanes <= 2; ++lanes) {
+    const int bm = 256 / lanes;
+    const WalkModel m{(int64_t)d.heads * ((d.nq + bm - 1) / bm), cus, mean / (64 * lanes) + 0.2, most / (64 * lanes) + 0.2,
+                      lanes == 1 ? 2.6 : 2.9, 5.0, 0, 0, nullptr, 0, 0.5};
+    double t;
+    const int parts = best_parts(m, cap_q, 4.5, part_q, &t);
+    if (lanes == 1 || t < 0.98 * least) {
+      least = t;
+      best.lanes = lanes;
+      best.parts_q = parts;
+    }
+  }
+  const WalkModel m{(int64_t)(d.heads / r.group) * ((d.nkv + WK_KEYS - 1) / WK_KEYS), cus, rows_mean / WK_ROWS + 0.2,
+                    (double)d.nq * r.group / WK_ROWS + 0.2, 3.4, 5.0, 0, 0, nullptr, 0, 0.5};
+  best.parts_kv = best_parts(m, cap_kv, 4.5, part_kv, nullptr);
+  return best;
+}
+
+hipError_t launch_scored_bwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K,
+                             const void* V, const void* O, const void* dO, const float* lse, void* ws, float* dQ, float* dK, float* dV,
+                             hipStream_t s) {
+#define A2D_RULES(HR)                                                                                                \
+  return r.cap != 0.f ? (r.slopes ? go<HR, true, true>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, dQ, dK, dV, s)       \
+                                  : go<HR, true, false>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, dQ, dK, dV, s))     \
+                      : (r.slopes ? go<HR, false, true>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, dQ, dK, dV, s)      \
+                                  : go<HR, false, false>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, dQ, dK, dV, s))
+  if (d.hdim == 128) { A2D_RULES(128); }
+  if (d.hdim == 96) { A2D_RULES(96); }
+  if (d.hdim == 80) { A2D_RULES(80); }
+  A2D_RULES(64);
+#undef A2D_RULES
+}
+
+}  // namespace a2d

@@ -104,13 +104,12 @@ __device__ __forceinline__ void to_scores(f32x4 (&s)[NT][2], const ScoreRules& r
     }
   }
   if constexpr (BIAS) {
-    const float step = (float)r.step;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const float from = fmaf((float)-(k0 + 4 * grp), step, rs.at[q]);       // (whole numbers below 2^24: exact)
+      const float from = fmaf((float)-(k0 + 4 * grp), r.steps[0], rs.at[q]);       // (whole numbers below 2^24: exact)
 #pragma unroll
       for (int e = 0; e < 4 * NT; ++e) {
-        const float far = fmaf((float)-(16 * (e >> 2) + (e & 3)), step, from);
+        const float far = distance<-1>(r, from, e >> 2, e & 3);
         const float x = s[e >> 2][q][e & 3];
         s[e >> 2][q][e & 3] = fmaf(-rs.slope[q], fabsf(far), CAP ? x : x * raw);
       }

@@ -81,7 +81,8 @@ def test_distances_of_a_bias(b):
 def test_workspace(b):
     d = desc(b)
     need = b.workspace_bytes(d, b.OP_PARTIAL_BWD_SCORED)
-    assert need == 3 * 4 * 128 * 4
+    assert need == 4 * 128 * 16 + 4 * 4 * 32       # 16 bytes a row, 32 for each 32 rows; rows up to a multiple of 64
+    assert b.workspace_bytes(desc(b, heads=3, nq=65), b.OP_PARTIAL_BWD_SCORED) == b.workspace_bytes(desc(b, heads=3), b.OP_PARTIAL_BWD_SCORED)
     assert bwd(b, d, rules(b), wb=need - 1) == WORKSPACE and bwd(b, d, rules(b), ws=NULL) == WORKSPACE
     assert bwd(b, d, rules(b), ws=ODD) == MISALIGNED and bwd(b, d, rules(b), wb=1 << 60) == INVALID
 
