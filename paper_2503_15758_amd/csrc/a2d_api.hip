@@ -724,12 +724,16 @@ a2d_status make_rules(const a2d_tile_desc* d, int32_t kv_heads, const a2d_score_
   if (in->ranges) A2D_TRY(check_ptr(in->ranges, who, "ranges"));
   r->cap = in->softcap;
   if (r->cap != 0.f) {
-    // tanh(x) / x = sum c_i x^(2 i) for |x| <= 0.7, the largest relative error (3e-7) the least possible: a weighted least-squares fit on
-    // Chebyshev points, weights moved to where the error is largest until it is even.  Taken at x = scale z / cap, times cap log2(e).
+    // tanh(x) / x = sum c_i x^(2 i) for |x| <= 0.7, the largest relative error (3e-7; 1.4e-8) the least possible: a weighted least-squares
+    // fit on Chebyshev points, weights moved to where the error is largest until it is even.  Taken at x = scale z / cap, times cap log2(e).
     const double tanh_of[5] = {0.999999697, -0.333302129, 0.132811123, -0.0508362276, 0.0137737021};
+    const double finer[6] = {0.999999986, -0.333331304, 0.133284147, -0.0535260078, 0.0200244543, -0.00508833311};
     const double a = (double)d->scale / r->cap, top = (double)r->cap * 1.4426950408889634;
     double power = a * top;
-    for (int i = 0; i < 5; ++i, power *= a * a) r->capped.c[i] = (float)(tanh_of[i] * power);
+    for (int i = 0; i < 6; ++i, power *= a * a) {
+      if (i < 5) r->capped.c[i] = (float)(tanh_of[i] * power);
+      r->capped.fine[i] = (float)(finer[i] * power);
+    }
     r->capped.small = (float)(0.7 / a);
     r->capped.rate = (float)(2 * 1.4426950408889634 * a);
     r->capped.top = (float)top;
@@ -775,7 +779,7 @@ a2d_status a2d_partial_fwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, c
   hipStream_t s = static_cast<hipStream_t>(stream);
   a2d_tile_desc dd;
   A2D_TRY(resolve_layouts(desc, r.group, false, who, &dd));
-  if (a2d::force_generic() || dd.dtype == A2D_F32) {
+  if (a2d::force_generic()) {
     a2d::trace_mark(s);
     return hip_result(a2d::launch_scored_fwd_generic(dd, r, Q, K, V, out0, out1, out2, s), who);
   }
@@ -784,7 +788,10 @@ a2d_status a2d_partial_fwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, c
   float *N = static_cast<float*>(out0), *tm = out1, *tl = out2;
   int cus = 0;
   A2D_TRY(hip_result(a2d::device_cus(&cus), who));
-  a2d::ScoredPlan plan = a2d::plan_scored_fwd(dd, r, cus, a2d::scratch_offered() ? cap_of(rows * (H + 2)) : 1);
+  const bool f32 = dd.dtype == A2D_F32;
+  const auto plan_of = f32 ? a2d::plan_scored_fwd_f32 : a2d::plan_scored_fwd;
+  const auto launch = f32 ? a2d::launch_scored_fwd_f32 : a2d::launch_scored_fwd;
+  a2d::ScoredPlan plan = plan_of(dd, r, cus, a2d::scratch_offered() ? cap_of(rows * (H + 2)) : 1);
   if (plan.parts > 1) {
     N = static_cast<float*>(a2d::scratch_get((size_t)plan.parts * rows * (H + 2) * sizeof(float)));
     if (N) {
@@ -792,13 +799,13 @@ a2d_status a2d_partial_fwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, c
       tl = tm + plan.parts * rows;
     } else {
       N = static_cast<float*>(out0);
-      plan = a2d::plan_scored_fwd(dd, r, cus, 1);
+      plan = plan_of(dd, r, cus, 1);
     }
   }
   const a2d::FwdInput in{static_cast<const float*>(out0), out1, out2};
-  A2D_TRY(hip_result(a2d::launch_scored_fwd(a2d::PREPARE, dd, r, plan, Q, K, V, N, tm, tl, in, s), who));
+  A2D_TRY(hip_result(launch(a2d::PREPARE, dd, r, plan, Q, K, V, N, tm, tl, in, s), who));
   a2d::trace_mark(s);
-  A2D_TRY(hip_result(a2d::launch_scored_fwd(a2d::LAUNCH, dd, r, plan, Q, K, V, N, tm, tl, in, s), who));
+  A2D_TRY(hip_result(launch(a2d::LAUNCH, dd, r, plan, Q, K, V, N, tm, tl, in, s), who));
   if (plan.parts == 1) return A2D_OK;
   a2d::FixPtrs p;
   memset(&p, 0, sizeof(p));
@@ -838,29 +845,31 @@ a2d_status a2d_partial_bwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, c
   hipStream_t s = static_cast<hipStream_t>(stream);
   a2d_tile_desc dd;
   A2D_TRY(resolve_layouts(desc, r.group, true, who, &dd));
-  if (a2d::force_generic() || dd.dtype == A2D_F32) {
+  if (a2d::force_generic()) {
     a2d::trace_mark(s);
     return hip_result(a2d::launch_scored_bwd_generic(dd, r, Q, K, V, O, dO, lse, static_cast<float*>(workspace), dQ, dK, dV, s), who);
   }
   const int64_t nq = (int64_t)dd.heads * dd.nq * dd.hdim, nk = (int64_t)kv_heads * dd.nkv * dd.hdim;
   int cus = 0;
   A2D_TRY(hip_result(a2d::device_cus(&cus), who));
-  const bool offered = a2d::scratch_offered();
-  a2d::ScoredBwdPlan plan = a2d::plan_scored_bwd(dd, r, cus, offered ? scored_cap(nq) : 1, offered ? scored_cap(nk) : 1);
+  const bool offered = a2d::scratch_offered(), f32 = dd.dtype == A2D_F32;
+  const auto plan_of = f32 ? a2d::plan_scored_bwd_f32 : a2d::plan_scored_bwd;
+  const auto launch = f32 ? a2d::launch_scored_bwd_f32 : a2d::launch_scored_bwd;
+  a2d::ScoredBwdPlan plan = plan_of(dd, r, cus, offered ? scored_cap(nq) : 1, offered ? scored_cap(nk) : 1);
   const int64_t dq_floats = plan.parts_q > 1 ? plan.parts_q * nq : 0, kv_floats = plan.parts_kv > 1 ? plan.parts_kv * nk : 0;
   float* more = nullptr;
   if (dq_floats + kv_floats > 0 && !(more = static_cast<float*>(a2d::scratch_get((size_t)(dq_floats + 2 * kv_floats) * sizeof(float)))))
-    plan = a2d::plan_scored_bwd(dd, r, cus, 1, 1);
+    plan = plan_of(dd, r, cus, 1, 1);
   float* const dq = plan.parts_q > 1 ? more : static_cast<float*>(dQ);
   float* const dk = plan.parts_kv > 1 ? more + dq_floats : static_cast<float*>(dK);
   float* const dv = plan.parts_kv > 1 ? dk + kv_floats : static_cast<float*>(dV);
-  A2D_TRY(hip_result(a2d::launch_scored_bwd(a2d::PREPARE, dd, r, plan, Q, K, V, O, dO, lse, workspace, dq, dk, dv, s), who));
+  A2D_TRY(hip_result(launch(a2d::PREPARE, dd, r, plan, Q, K, V, O, dO, lse, workspace, dq, dk, dv, s), who));
   a2d::trace_mark(s);
-  A2D_TRY(hip_result(a2d::launch_scored_bwd(a2d::LAUNCH, dd, r, plan, Q, K, V, O, dO, lse, workspace, dq, dk, dv, s), who));
+  A2D_TRY(hip_result(launch(a2d::LAUNCH, dd, r, plan, Q, K, V, O, dO, lse, workspace, dq, dk, dv, s), who));
   const a2d::PartSet sets[3] = {{dk, static_cast<float*>(dK), nk, plan.parts_kv, 0},
                                 {dv, static_cast<float*>(dV), nk, plan.parts_kv, 0},
                                 {dq, static_cast<float*>(dQ), nq, plan.parts_q, r.acc}};
-  if (r.norm) {
+  if (r.norm && !f32) {
     for (const a2d::PartSet& x : sets) {
       if (x.k == 1) continue;
       a2d::SumPtrs p;

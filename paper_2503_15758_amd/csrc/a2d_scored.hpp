@@ -8,8 +8,9 @@ namespace a2d {
 // The cap in log2 units, y = cap log2(e) tanh(scale z / cap) of a raw dot product z: up to |z| = small (0.7 cap / scale) an odd polynomial
 // z (c0 + .. + c4 z^8), fitted to tanh with 3e-7 of it; beyond, top (1 - 2 / (1 + 2^(rate z))), whose error, some 2^-22 of top, is relative to
 // a y of 0.6 top and more.  (That form alone would be off by 2^-22 of the cap everywhere: as much as y itself for a wide cap.)
+// fine: one coefficient more (1e-7), for fp32 inputs.
 struct CapArgs {
-  float small, rate, top, c[5];
+  float small, rate, top, c[5], fine[6];
 };
 struct ScoreRules {
   float cap;            // 0: none
@@ -72,6 +73,24 @@ __device__ __forceinline__ float cap_log2(const CapArgs& a, float z) {
   return fabsf(z) <= a.small ? y : beyond;           // (NaN: beyond, which is NaN too)
 }
 
+__device__ __forceinline__ float cap_log2_f32(const CapArgs& a, float z) {
+  const float u = z * z;
+  const float y = z * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, a.fine[5], a.fine[4]), a.fine[3]), a.fine[2]), a.fine[1]), a.fine[0]);
+  const float beyond = a.top * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + fast_exp2(z * a.rate)), 1.f);
+  return fabsf(z) <= a.small ? y : beyond;
+}
+
+// keys of a row's walk, on average and at most, as far as sizes and the causal mask tell
+struct WalkKeys {
+  double mean, most;
+};
+inline WalkKeys walk_keys(const a2d_tile_desc& d, const ScoreRules& r) {
+  if (!d.causal) return WalkKeys{(double)d.nkv, (double)d.nkv};
+  const auto seen = [&](double x) { return x < 0 ? 0.0 : x > d.nkv ? (double)d.nkv : x; };
+  const double most = seen((double)d.nq + r.row_shift);
+  return WalkKeys{0.5 * (seen(1.0 + r.row_shift) + most), most};
+}
+
 // bf16 forward on the matrix units (a2d_scored_fwd.hip).  How a call goes out: the form of its workgroups, and how many
 // share a walk of the keys (their partials [parts][heads][nq] in place of the outputs, to be merged).
 struct ScoredPlan {
@@ -93,6 +112,15 @@ ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int c
 hipError_t launch_scored_bwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K,
                              const void* V, const void* O, const void* dO, const float* lse, void* ws, float* dQ, float* dK, float* dV,
                              hipStream_t s);
+
+// the same for fp32 (a2d_scored_f32.hip; plan.form: 1 or 2 tiles of 16 rows a workgroup)
+ScoredPlan plan_scored_fwd_f32(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap);
+hipError_t launch_scored_fwd_f32(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, const void* Q, const void* K,
+                                 const void* V, float* out0, float* out1, float* out2, const FwdInput& in, hipStream_t s);
+ScoredBwdPlan plan_scored_bwd_f32(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap_q, int cap_kv);
+hipError_t launch_scored_bwd_f32(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q,
+                                 const void* K, const void* V, const void* O, const void* dO, const float* lse, void* ws, float* dQ,
+                                 float* dK, float* dV, hipStream_t s);
 
 // one row or key in a workgroup, vector ALU (a2d_scored_generic.hip): both types, every shape
 hipError_t launch_scored_fwd_generic(const a2d_tile_desc& d, const ScoreRules& r, const void* Q, const void* K, const void* V,

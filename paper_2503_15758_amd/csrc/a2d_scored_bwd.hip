@@ -11,33 +11,12 @@
 // nothing but their own scores, wherever they lie.  Rows that see nothing are not loaded (zeros in their place), nor are keys
 // outside a hull: they may hold anything.
 #include "a2d_bwd.hpp"
-#include "a2d_scored.hpp"
+#include "a2d_scored_rows.hpp"
 
 namespace a2d {
 namespace {
 
 using namespace mfma;
-
-// what the dQ kernel leaves of the rows, [heads][padded]: padded = nq up to the next multiple of 64
-struct RowTile {
-  int lo, hi;            // hull of the runs (none: lo > hi)
-  int all_lo, all_hi;    // keys that all rows see that see any
-  unsigned live;         // bit i: row i sees something
-  int pad[3];
-};
-struct RowTable {
-  int padded;
-  float *from, *delta;   // lse in log2 units, with a cap; without one -lse in units of raw products: what the scores start from.  -(dO . O)
-  int *lo, *n;           // run of keys
-  RowTile* tiles;        // [heads][padded / 32]
-};
-
-template <class F>
-__device__ __forceinline__ int over16(int x, F&& f) {
-#pragma unroll
-  for (int o = 8; o; o >>= 1) x = f(x, __shfl_xor(x, o, 64));
-  return __builtin_amdgcn_readfirstlane(x);
-}
 
 // z -> y in log2 units, of 2 x 2 tiles
 __device__ __forceinline__ void cap_in_place(f32x4 (&s)[2][2], const CapArgs& a) {
@@ -422,35 +401,14 @@ __global__ __launch_bounds__(WK_THREADS) void scored_dkdv_kernel(
     }
   }
   __syncthreads();
-  const auto word = [&](int w) -> uint64_t {
-    const uint64_t b = bits[w];
-    return (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
-  };
-  // this part's share of the set bits: from number `skip` on, `total` of them
-  int total = 0, skip = 0, at_word = 0;
-  for (int w = 0; w < words; ++w) total += __builtin_popcountll(word(w));
+  // this part's share of the set bits: `total` of them
+  StepWalk walk;
+  int total = walk.open(bits, words);
   if (parts > 1) {
-    skip = (int)((int64_t)part * total / parts);
+    const int skip = (int)((int64_t)part * total / parts);
     total = (int)((int64_t)(part + 1) * total / parts) - skip;
+    walk.skip(skip);
   }
-  uint64_t left = words ? word(0) : 0;
-  while (skip > 0) {
-    const int n = __builtin_popcountll(left);
-    if (n <= skip) {
-      skip -= n;
-      if (++at_word == words) break;
-      left = word(at_word);
-    } else {
-      for (; skip > 0; --skip) left &= left - 1;
-    }
-  }
-  const auto next_step = [&]() -> int {              // (called `total` times)
-    while (left == 0 && at_word + 1 < words) left = word(++at_word);
-    const int s = 64 * at_word + __builtin_ctzll(left);
-    left &= left - 1;
-    return s;
-  };
-
   // ---- staging, straight into LDS: wavefronts 0 .. 3 load a row tile of Q each, 4 .. 7 of dO; 0 .. 3 also bring one of the row
   // tables each, 4 the tiles' records.  The next step is requested while one is computed.  Rows that see nothing are
   // zeros (what they see has been asked for a step earlier: live).
@@ -501,10 +459,10 @@ __global__ __launch_bounds__(WK_THREADS) void scored_dkdv_kernel(
   Step now{0, 0}, then{0, 0};
   unsigned live = 0;
   if (total > 0) {
-    now = place(next_step());
+    now = place(walk.next());
     load_step(now, ask_live(now), 0);
     if (total > 1) {
-      then = place(next_step());
+      then = place(walk.next());
       live = ask_live(then);
     }
   }
@@ -648,7 +606,7 @@ __global__ __launch_bounds__(WK_THREADS) void scored_dkdv_kernel(
       load_step(then, live, buf ^ 1);
       now = then;
       if (n + 2 < total) {
-        then = place(next_step());
+        then = place(walk.next());
         live = ask_live(then);
       }
     }
@@ -684,25 +642,12 @@ __global__ __launch_bounds__(WK_THREADS) void scored_dkdv_kernel(
   }
 }
 
-// (of one tile's rows and keys: the table in `ws`, see scored_bwd_bytes)
-RowTable row_table(const a2d_tile_desc& d, void* ws) {
-  RowTable t;
-  t.padded = (d.nq + 63) / 64 * 64;
-  const int64_t n = (int64_t)d.heads * t.padded;
-  t.from = static_cast<float*>(ws);
-  t.delta = t.from + n;
-  t.lo = reinterpret_cast<int*>(t.delta + n);
-  t.n = t.lo + n;
-  t.tiles = reinterpret_cast<RowTile*>(t.n + n);
-  return t;
-}
-
 template <int HR, bool CAP, bool BIAS>
 hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K, const void* V,
               const void* O, const void* dO, const float* lse, void* ws, float* dQ, float* dK, float* dV, hipStream_t s) {
   constexpr int HD = padded_head(HR);
   const RowTable tab = row_table(d, ws);
-  const int by_size = d.causal && !r.ranges && r.row_shift < d.nkv && (int64_t)d.nq + r.row_shift > 0 && d.nq > 1;
+  const int by_size = blocks_by_size(d, r);
   const int kvh = d.heads / r.group, dq_bytes = dq_launch_lds(HD, plan.lanes);
   const int words = (tab.padded / WK_ROWS * r.group + 63) / 64, wk_bytes = wk_park(HD) ? wk_lds(HD) : wk_bits(HD) + 8 * words;
   const auto dq = [&](auto* kernel) {
@@ -731,13 +676,8 @@ size_t scored_bwd_bytes(const a2d_tile_desc& d) {
 }
 
 ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap_q, int cap_kv) {
-  const auto seen = [&](double x) { return x < 0 ? 0.0 : x > d.nkv ? (double)d.nkv : x; };
-  double most = d.nkv, mean = most, rows_mean = (double)d.nq * r.group;
-  if (d.causal) {
-    most = seen((double)d.nq + r.row_shift);
-    mean = 0.5 * (seen(1.0 + r.row_shift) + most);
-    rows_mean *= mean / d.nkv;
-  }
+  const WalkKeys w = walk_keys(d, r);
+  const double most = w.most, mean = w.mean, rows_mean = (double)d.nq * r.group * (mean / d.nkv);
   ScoredBwdPlan best{1, 1, 1};
   double least = 0;
   const double part_q = (double)d.heads * d.nq * d.hdim * 8 / 4.5e6, part_kv = (double)(d.heads / r.group) * d.nkv * d.hdim * 16 / 4.5e6;

@@ -14,7 +14,7 @@
 // Rows: the query rows of the heads that share a key/value head follow one another (packed) where a head has fewer rows
 // than a workgroup: a token of each of the group's heads reads the keys once.
 #include "a2d_fwd.hpp"
-#include "a2d_scored.hpp"
+#include "a2d_scored_rows.hpp"
 
 namespace a2d {
 namespace {
@@ -23,66 +23,9 @@ using namespace mfma;
 
 constexpr float kRescaleThreshold = 8.0f;            // log2 units (as in a2d_fwd_mfma.hip)
 
-// Where the rows of a launch lie: `sub` runs of `rows` query rows for a key/value head, cut into blocks
-struct RowMap {
-  int sub, rows;         // packed: 1, group * nq; else group, nq
-  int by_size;           // blocks in order of size (see xcd_map): the causal mask crosses the tile
-  int parts;
-};
-
-// what a wavefront knows of its two tiles of 16 rows; of the lane's row in each
-struct RowState {
-  int64_t q_at[2];       // its place in Q, from the key/value head's first
-  Run run[2];
-  float at[2], slope[2]; // tokens behind key 0; slope in log2 units
-  int lo, hi;            // hull of the wavefront's runs; lo > hi: nothing seen
-  int all_lo, all_hi;    // keys that all of its rows see
-};
-
-// min or max over the 16 lanes of a lane's tile (every 16 lanes hold the same rows)
-template <class F>
-__device__ __forceinline__ int over16(int x, F&& f) {
-#pragma unroll
-  for (int o = 8; o; o >>= 1) x = f(x, __shfl_xor(x, o, 64));
-  return __builtin_amdgcn_readfirstlane(x);
-}
-
-// rows w0 .. w0 + 31 of the run of map.rows rows that starts at row 0 of query head `head`
-template <bool BIAS>
-__device__ __forceinline__ void look_up_rows(RowState& rs, const a2d_tile_desc& d, const ScoreRules& r, const RowMap& map, int head, int w0,
-                                             int lane) {
-  const auto least = [](int a, int b) { return min(a, b); };
-  const auto most = [](int a, int b) { return max(a, b); };
-  int lo = INT_MAX, hi = 0, all_lo = 0, all_hi = INT_MAX;
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int row = w0 + 16 * q + (lane & 15), in = min(row, map.rows - 1);
-    const Split hd = map.sub == 1 ? Split{in / d.nq, in - in / d.nq * d.nq} : Split{0, in};
-    rs.q_at[q] = hd.q * d.lq.head + hd.r * d.lq.row;
-    rs.run[q] = visible_run(d, r, head + hd.q, hd.r);
-    if constexpr (BIAS) {
-      rs.at[q] = (float)(int)(r.rel + (int64_t)hd.r * r.step);
-      rs.slope[q] = r.slopes[head + hd.q] * kLog2e;
-    }
-    if (row >= map.rows) rs.run[q] = Run{0, 0};                // (never stored; asks for nothing)
-    if (rs.run[q].n > 0) {
-      lo = min(lo, rs.run[q].lo);
-      hi = max(hi, rs.run[q].lo + rs.run[q].n);
-    }
-    if (row < map.rows) {
-      all_lo = max(all_lo, rs.run[q].lo);
-      all_hi = min(all_hi, rs.run[q].lo + rs.run[q].n);
-    }
-  }
-  rs.lo = over16(lo, least);
-  rs.hi = over16(hi, most);
-  rs.all_lo = over16(all_lo, most);
-  rs.all_hi = over16(all_hi, least);
-}
-
 // Raw dot products -> scores in the units of the exponent: log2 with a cap or a bias, else raw.  raw: log2 units of a raw one.  NT tiles of 16 keys from k0 on.
 template <int NT, bool CAP, bool BIAS>
-__device__ __forceinline__ void to_scores(f32x4 (&s)[NT][2], const ScoreRules& r, const RowState& rs, bool masked, int k0, int grp, float raw) {
+__device__ __forceinline__ void to_scores(f32x4 (&s)[NT][2], const ScoreRules& r, const RowState<2>& rs, bool masked, int k0, int grp, float raw) {
   if constexpr (CAP) {
     float big = 0.f;
 #pragma unroll
@@ -218,8 +161,8 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_kernel(
   const int64_t row0 = (int64_t)head * d.nq;          // of the run of rows, in the outputs
   const Units<CAP, BIAS> units(d);
 
-  RowState rs;
-  look_up_rows<BIAS>(rs, d, r, map, head, q0 + wave * 32, lane);
+  RowState<2> rs;
+  look_up_rows<2, BIAS>(rs, d, r, map, head, q0 + wave * 32, lane);
   bf16x8 qf[KS][2];
 #pragma unroll
   for (int q = 0; q < 2; ++q)
@@ -422,8 +365,8 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
   const Units<CAP, BIAS> units(d);
   const float c = units.c;
 
-  RowState rs;
-  look_up_rows<BIAS>(rs, d, r, map, head, q0, lane);
+  RowState<2> rs;
+  look_up_rows<2, BIAS>(rs, d, r, map, head, q0, lane);
   bf16x8 qf[KS][2];
 #pragma unroll
   for (int q = 0; q < 2; ++q)
@@ -590,18 +533,11 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
 
 constexpr int kRows[3] = {256, 128, 32};
 
-RowMap row_map(const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan) {
-  const bool packed = r.group > 1 && d.nq < kRows[plan.form];
-  // (a mask by ranges is not known here)
-  const bool by_size = !packed && d.causal && !r.ranges && r.row_shift < d.nkv && (int64_t)d.nq + r.row_shift > 0 && d.nq > 1;
-  return RowMap{packed ? 1 : r.group, packed ? r.group * d.nq : d.nq, by_size, plan.parts};
-}
-
 template <int HR, bool CAP, bool BIAS>
 hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, const void* Q, const void* K, const void* V,
               float* out0, float* out1, float* out2, const FwdInput& in, hipStream_t s) {
-  const RowMap map = row_map(d, r, plan);
   const int bm = kRows[plan.form];
+  const RowMap map = row_map(d, r, bm, plan.parts);
   const int bytes = plan.form == SCORED_32 ? SMALL_LDS : fwd_lds(8, padded_head(HR), plan.form == SCORED_LANES ? 2 : 1);
   const auto run = [&](auto* kernel) {
     if (ph == PREPARE) return ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes);
@@ -626,13 +562,8 @@ ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus,
     const int64_t blocks = packed ? (int64_t)kv_heads * (((int64_t)r.group * d.nq + bm - 1) / bm)
                                   : (int64_t)d.heads * ((d.nq + bm - 1) / bm);
     const double keys = f == SCORED_32 ? 256 : f == SCORED_LANES ? 128 : 64;
-    double most = d.nkv / keys + 0.2, mean = most;
-    if (d.causal && !packed) {
-      const double last = (double)d.nq + r.row_shift, first = 1.0 + r.row_shift;
-      const auto seen = [&](double x) { return x < 0 ? 0.0 : x > d.nkv ? (double)d.nkv : x; };
-      most = seen(last) / keys + 0.2;
-      mean = 0.5 * (seen(first) + seen(last)) / keys + 0.2;
-    }
+    const WalkKeys w = walk_keys(d, r);
+    const double most = w.most / keys + 0.2, mean = packed ? most : w.mean / keys + 0.2;
     const double step = f == SCORED_32 ? 1.6 : f == SCORED_LANES ? 2.0 : 1.8, fixed = f == SCORED_32 ? 4.0 : 5.0;
     const WalkModel m{blocks, cus, mean, most, step, fixed, 0, 0, nullptr, 0, 0.5};
     const double part_us = (double)d.heads * d.nq * (d.hdim + 2) * 8 / 4.5e6;

@@ -1,0 +1,144 @@
+// Query rows and steps as the matrix-unit kernels under score rules take them (a2d_scored_fwd.hip, a2d_scored_bwd.hip, a2d_scored_f32.hip).
+#pragma once
+#include <limits.h>
+
+#include "a2d_mfma.hpp"
+#include "a2d_scored.hpp"
+
+namespace a2d {
+
+// Where the rows of a launch lie: `sub` runs of `rows` query rows for a key/value head, cut into blocks
+struct RowMap {
+  int sub, rows;         // packed: 1, group * nq; else group, nq
+  int by_size;           // blocks in order of size (see xcd_map): the causal mask crosses the tile
+  int parts;
+};
+
+// what a wavefront knows of its NT tiles of 16 rows; of the lane's row in each
+template <int NT>
+struct RowState {
+  int64_t q_at[NT];       // its place in Q, from the key/value head's first
+  Run run[NT];
+  float at[NT], slope[NT]; // tokens behind key 0; slope in log2 units
+  int lo, hi;            // hull of the wavefront's runs; lo > hi: nothing seen
+  int all_lo, all_hi;    // keys that all of its rows see
+};
+
+// min or max over the 16 lanes of a lane's tile (every 16 lanes hold the same rows)
+template <class F>
+__device__ __forceinline__ int over16(int x, F&& f) {
+#pragma unroll
+  for (int o = 8; o; o >>= 1) x = f(x, __shfl_xor(x, o, 64));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+// rows w0 .. w0 + 16 NT - 1 of the run of map.rows rows that starts at row 0 of query head `head`
+template <int NT, bool BIAS>
+__device__ __forceinline__ void look_up_rows(RowState<NT>& rs, const a2d_tile_desc& d, const ScoreRules& r, const RowMap& map, int head, int w0,
+                                             int lane) {
+  const auto least = [](int a, int b) { return min(a, b); };
+  const auto most = [](int a, int b) { return max(a, b); };
+  int lo = INT_MAX, hi = 0, all_lo = 0, all_hi = INT_MAX;
+#pragma unroll
+  for (int q = 0; q < NT; ++q) {
+    const int row = w0 + 16 * q + (lane & 15), in = min(row, map.rows - 1);
+    const mfma::Split hd = map.sub == 1 ? mfma::Split{in / d.nq, in - in / d.nq * d.nq} : mfma::Split{0, in};
+    rs.q_at[q] = hd.q * d.lq.head + hd.r * d.lq.row;
+    rs.run[q] = visible_run(d, r, head + hd.q, hd.r);
+    if constexpr (BIAS) {
+      rs.at[q] = (float)(int)(r.rel + (int64_t)hd.r * r.step);
+      rs.slope[q] = r.slopes[head + hd.q] * kLog2e;
+    }
+    if (row >= map.rows) rs.run[q] = Run{0, 0};                // (never stored; asks for nothing)
+    if (rs.run[q].n > 0) {
+      lo = min(lo, rs.run[q].lo);
+      hi = max(hi, rs.run[q].lo + rs.run[q].n);
+    }
+    if (row < map.rows) {
+      all_lo = max(all_lo, rs.run[q].lo);
+      all_hi = min(all_hi, rs.run[q].lo + rs.run[q].n);
+    }
+  }
+  rs.lo = over16(lo, least);
+  rs.hi = over16(hi, most);
+  rs.all_lo = over16(all_lo, most);
+  rs.all_hi = over16(all_hi, least);
+}
+
+// A tile that the causal mask crosses (by ranges: not known here)
+inline bool blocks_by_size(const a2d_tile_desc& d, const ScoreRules& r) {
+  return d.causal && !r.ranges && r.row_shift < d.nkv && (int64_t)d.nq + r.row_shift > 0 && d.nq > 1;
+}
+// for workgroups of bm rows
+inline RowMap row_map(const a2d_tile_desc& d, const ScoreRules& r, int bm, int parts) {
+  const bool packed = r.group > 1 && d.nq < bm;
+  return RowMap{packed ? 1 : r.group, packed ? r.group * d.nq : d.nq, !packed && blocks_by_size(d, r), parts};
+}
+
+// what the dQ kernel leaves of the rows, [heads][padded]: padded = nq up to the next multiple of 64
+struct RowTile {
+  int lo, hi;            // hull of the runs (none: lo > hi)
+  int all_lo, all_hi;    // keys that all rows see that see any
+  unsigned live;         // bit i: row i sees something
+  int pad[3];
+};
+struct RowTable {
+  int padded;
+  float *from, *delta;   // lse in log2 units, with a cap; without one -lse in units of raw products: what the scores start from.  -(dO . O)
+  int *lo, *n;           // run of keys
+  RowTile* tiles;        // [heads][padded / 32]
+};
+
+// (of one tile's rows and keys: the table in `ws`, see scored_bwd_bytes)
+inline RowTable row_table(const a2d_tile_desc& d, void* ws) {
+  RowTable t;
+  t.padded = (d.nq + 63) / 64 * 64;
+  const int64_t n = (int64_t)d.heads * t.padded;
+  t.from = static_cast<float*>(ws);
+  t.delta = t.from + n;
+  t.lo = reinterpret_cast<int*>(t.delta + n);
+  t.n = t.lo + n;
+  t.tiles = reinterpret_cast<RowTile*>(t.n + n);
+  return t;
+}
+
+// The set bits of a map in LDS, one after another, by all lanes of a wavefront alike
+struct StepWalk {
+  const uint64_t* bits;
+  int words, at;
+  uint64_t left;
+  __device__ __forceinline__ uint64_t word(int w) const {
+    const uint64_t b = bits[w];
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
+  }
+  __device__ __forceinline__ int open(const uint64_t* map, int n) {     // returns how many there are; n >= 1
+    bits = map;
+    words = n;
+    at = 0;
+    int total = 0;
+    for (int w = 0; w < n; ++w) total += __builtin_popcountll(word(w));
+    left = word(0);
+    return total;
+  }
+  __device__ __forceinline__ void skip(int n) {                         // fewer than are left, or all
+    while (n > 0) {
+      const int here = __builtin_popcountll(left);
+      if (here <= n) {
+        n -= here;
+        left = 0;
+        if (++at >= words) { at = words - 1; return; }
+        left = word(at);
+      } else {
+        for (; n > 0; --n) left &= left - 1;
+      }
+    }
+  }
+  __device__ __forceinline__ int next() {                               // there is one left
+    while (left == 0 && at + 1 < words) left = word(++at);
+    const int s = 64 * at + __builtin_ctzll(left);
+    left &= left - 1;
+    return s;
+  }
+};
+
+}  // namespace a2d
