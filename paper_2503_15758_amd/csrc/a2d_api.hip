@@ -724,17 +724,17 @@ a2d_status make_rules(const a2d_tile_desc* d, int32_t kv_heads, const a2d_score_
   if (in->ranges) A2D_TRY(check_ptr(in->ranges, who, "ranges"));
   r->cap = in->softcap;
   if (r->cap != 0.f) {
-    // tanh(x) / x = sum c_i x^(2 i) for |x| <= 0.7, the largest relative error (3e-7; 1.4e-8) the least possible: a weighted least-squares
+    // tanh(x) / x = sum c_i x^(2 i) for |x| <= 0.5, the largest relative error (5.4e-7; 1.3e-8) the least possible: a weighted least-squares
     // fit on Chebyshev points, weights moved to where the error is largest until it is even.  Taken at x = scale z / cap, times cap log2(e).
-    const double tanh_of[5] = {0.999999697, -0.333302129, 0.132811123, -0.0508362276, 0.0137737021};
-    const double finer[6] = {0.999999986, -0.333331304, 0.133284147, -0.0535260078, 0.0200244543, -0.00508833311};
+    const double tanh_of[4] = {0.999999456, -0.333263179, 0.131902963, -0.0444022184};
+    const double finer[5] = {0.999999987, -0.333330694, 0.133247793, -0.0529860738, 0.0171350036};
     const double a = (double)d->scale / r->cap, top = (double)r->cap * 1.4426950408889634;
     double power = a * top;
-    for (int i = 0; i < 6; ++i, power *= a * a) {
-      if (i < 5) r->capped.c[i] = (float)(tanh_of[i] * power);
+    for (int i = 0; i < 5; ++i, power *= a * a) {
+      if (i < 4) r->capped.c[i] = (float)(tanh_of[i] * power);
       r->capped.fine[i] = (float)(finer[i] * power);
     }
-    r->capped.small = (float)(0.7 / a);
+    r->capped.small = (float)(0.5 / a);
     r->capped.rate = (float)(2 * 1.4426950408889634 * a);
     r->capped.top = (float)top;
   }

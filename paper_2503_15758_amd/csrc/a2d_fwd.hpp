@@ -68,12 +68,12 @@ __device__ __forceinline__ void fwd_scores(Scores& s, Ring& kr, const bf16x8 (&q
 
 // O^T += V^T P^T
 template <int HR>
-__device__ __forceinline__ void fwd_products(FwdState<HR>& st, const bf16x8 (&pb)[2][2], Ring& vr, const Blocks16& rd, unsigned at) {
+__device__ __forceinline__ void fwd_products(f32x4 (&o)[HR / 16][2], const bf16x8 (&pb)[2][2], Ring& vr, const Blocks16& rd, unsigned at) {
   constexpr int HT = HR / 16;
   static_for<0, 2 * HT>([&](auto I) {
     constexpr int i = decltype(I)::value;
 #pragma unroll
-    for (int q = 0; q < 2; ++q) st.o[i % HT][q] = mma16(vr[i & 3], pb[i / HT][q], st.o[i % HT][q]);
+    for (int q = 0; q < 2; ++q) o[i % HT][q] = mma16(vr[i & 3], pb[i / HT][q], o[i % HT][q]);
     if constexpr (i + 4 < 2 * HT) fwd_value<HR, i + 4>(vr, rd, at);
     __builtin_amdgcn_sched_barrier(0);
   });

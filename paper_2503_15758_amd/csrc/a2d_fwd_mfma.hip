@@ -144,7 +144,7 @@ __device__ __forceinline__ void fwd_block(FwdState<HR>& st, const bf16x8 (&qf)[p
   fwd_first_keys<HR>(kr, rd, at);
   fwd_scores<HR>(s, kr, qf, rd, at);
   fwd_softmax<HR>(st, s, pb, masked, k0, my_vis, grp, c, [&]() { fwd_first_values<HR>(vr, rd, at); });
-  fwd_products<HR>(st, pb, vr, rd, at);
+  fwd_products<HR>(st.o, pb, vr, rd, at);
 }
 
 // WAVES wavefronts per workgroup, in KL key lanes of WAVES / KL wavefronts (32 query rows each):
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void fwd_mfma_kernel(
       }
       if (mine) {
         fwd_first_values<HR>(vr, rd, boff);
-        fwd_products<HR>(st, pb, vr, rd, boff);
+        fwd_products<HR>(st.o, pb, vr, rd, boff);
       }
       __builtin_amdgcn_s_setprio(1);
       if (behind) {

@@ -5,12 +5,12 @@
 
 namespace a2d {
 
-// The cap in log2 units, y = cap log2(e) tanh(scale z / cap) of a raw dot product z: up to |z| = small (0.7 cap / scale) an odd polynomial
-// z (c0 + .. + c4 z^8), fitted to tanh with 3e-7 of it; beyond, top (1 - 2 / (1 + 2^(rate z))), whose error, some 2^-22 of top, is relative to
-// a y of 0.6 top and more.  (That form alone would be off by 2^-22 of the cap everywhere: as much as y itself for a wide cap.)
-// fine: one coefficient more (1e-7), for fp32 inputs.
+// The cap in log2 units, y = cap log2(e) tanh(scale z / cap) of a raw dot product z: up to |z| = small (half of cap / scale) an odd polynomial
+// z (c0 + .. + c3 z^6), fitted to tanh with 5e-7 of it; beyond, top (1 - 2 / (1 + 2^(rate z))), whose error, some 2^-22 of top, is relative to
+// a y of 0.46 top and more.  (That form alone would be off by 2^-22 of the cap everywhere: as much as y itself for a wide cap.)
+// fine: one coefficient more (1e-8 and the roundings), for fp32 inputs.
 struct CapArgs {
-  float small, rate, top, c[5], fine[6];
+  float small, rate, top, c[4], fine[5];
 };
 struct ScoreRules {
   float cap;            // 0: none
@@ -64,20 +64,22 @@ __device__ __forceinline__ float distance(const ScoreRules& r, float first, int 
   return i == 0 ? f : SIGN > 0 ? f + r.steps[i - 1] : f - r.steps[i - 1];
 }
 
-template <bool SMALL_ONLY>
-__device__ __forceinline__ float cap_log2(const CapArgs& a, float z) {
+// z -> (factor of z: y = z * factor), for |z| <= small
+__device__ __forceinline__ float cap_factor(const CapArgs& a, float z) {
   const float u = z * z;
-  const float y = z * fmaf(u, fmaf(u, fmaf(u, fmaf(u, a.c[4], a.c[3]), a.c[2]), a.c[1]), a.c[0]);
-  if constexpr (SMALL_ONLY) return y;
-  const float beyond = a.top * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + fast_exp2(z * a.rate)), 1.f);
-  return fabsf(z) <= a.small ? y : beyond;           // (NaN: beyond, which is NaN too)
+  return fmaf(u, fmaf(u, fmaf(u, a.c[3], a.c[2]), a.c[1]), a.c[0]);
 }
-
+__device__ __forceinline__ float cap_beyond(const CapArgs& a, float z) {
+  return a.top * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + fast_exp2(z * a.rate)), 1.f);
+}
+// any z (NaN: beyond, which is NaN too)
+__device__ __forceinline__ float cap_log2(const CapArgs& a, float z) {
+  return fabsf(z) <= a.small ? z * cap_factor(a, z) : cap_beyond(a, z);
+}
 __device__ __forceinline__ float cap_log2_f32(const CapArgs& a, float z) {
   const float u = z * z;
-  const float y = z * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, a.fine[5], a.fine[4]), a.fine[3]), a.fine[2]), a.fine[1]), a.fine[0]);
-  const float beyond = a.top * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + fast_exp2(z * a.rate)), 1.f);
-  return fabsf(z) <= a.small ? y : beyond;
+  const float y = z * fmaf(u, fmaf(u, fmaf(u, fmaf(u, a.fine[4], a.fine[3]), a.fine[2]), a.fine[1]), a.fine[0]);
+  return fabsf(z) <= a.small ? y : cap_beyond(a, z);
 }
 
 // keys of a row's walk, on average and at most, as far as sizes and the causal mask tell
@@ -96,7 +98,8 @@ inline WalkKeys walk_keys(const a2d_tile_desc& d, const ScoreRules& r) {
 struct ScoredPlan {
   int form, parts;
 };
-enum { SCORED_256, SCORED_LANES, SCORED_32 };        // 256 rows; 128 rows in two key lanes; 32 rows in eight
+enum { SCORED_256, SCORED_LANES, SCORED_PAIRS, SCORED_32 };   // 256 rows; 128 rows in two key lanes; 128 rows in four wavefronts, two
+                                                              // workgroups a compute unit; 32 rows in eight key lanes
 ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap);
 hipError_t launch_scored_fwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, const void* Q, const void* K,
                              const void* V, float* out0, float* out1, float* out2, const FwdInput& in, hipStream_t s);

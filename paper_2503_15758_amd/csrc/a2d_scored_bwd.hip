@@ -27,13 +27,13 @@ __device__ __forceinline__ void cap_in_place(f32x4 (&s)[2][2], const CapArgs& a)
     asm volatile("" ::: "memory");                   // keep this a branch
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      s[e >> 3][(e >> 2) & 1][e & 3] = cap_log2<false>(a, s[e >> 3][(e >> 2) & 1][e & 3]);
+      s[e >> 3][(e >> 2) & 1][e & 3] = cap_log2(a, s[e >> 3][(e >> 2) & 1][e & 3]);
       if (e & 1) __builtin_amdgcn_sched_barrier(0);  // (more at a time takes registers that dK and dV need)
     }
   } else {
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      s[e >> 3][(e >> 2) & 1][e & 3] = cap_log2<true>(a, s[e >> 3][(e >> 2) & 1][e & 3]);
+      s[e >> 3][(e >> 2) & 1][e & 3] *= cap_factor(a, s[e >> 3][(e >> 2) & 1][e & 3]);
       if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -50,25 +50,24 @@ __host__ __device__ constexpr int dq_ring(int hd) { return hd == 64 ? 4 : 2; }
 
 // KL = 1: 256 rows, KL = 2: 128 rows in two key lanes (see scored_fwd_kernel)
 template <int HR, int KL, bool CAP, bool BIAS>
-__global__ __launch_bounds__(512, 1) void scored_dq_kernel(
-    a2d_tile_desc d, ScoreRules r, int by_size, int parts, RowTable tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
-    const bf16_t* __restrict__ V, const bf16_t* __restrict__ O, const bf16_t* __restrict__ dO, const float* __restrict__ lse,
-    float* dQ, int rounded) {
+__device__ __forceinline__ void scored_dq_rows(
+    int id, char* const lds_all, int* const hull, const Ranks& ranks, const a2d_tile_desc& d, const ScoreRules& r, int by_size, int parts,
+    const RowTable& tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V,
+    const bf16_t* __restrict__ O, const bf16_t* __restrict__ dO, const float* __restrict__ lse, float* dQ, int rounded) {
   constexpr int WAVES = 8, RW = WAVES / KL, BM = 32 * RW, kThreads = 64 * RW;
   constexpr int HD = padded_head(HR), H = HR, KS = HD / 32, HT = HR / 16, DQ_BUF = dq_buf(HD), RING = dq_ring(HD);
-  extern __shared__ __attribute__((aligned(1024))) char lds_all[];
-  __shared__ int hull[2 * RW];
   const int kl = KL == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads);
   char* const lds = lds_all + kl * (2 * DQ_BUF);
   const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const int nqb = (d.nq + BM - 1) / BM;
   int unit, blk;
-  if (!xcd_map(blockIdx.x, d.heads / r.group * parts, r.group * nqb, by_size != 0, unit, blk, kXcdCus)) return;
+  if (!xcd_map(id, d.heads / r.group * parts, r.group * nqb, by_size != 0, unit, blk, kXcdCus)) return;
   const Split up = split_by(unit, parts);
   const int kvh = up.q, part = up.r;
   const Split in_group = query_head(blk, r.group, nqb, by_size != 0);
   const int head = kvh * r.group + in_group.r;
-  const int q0 = (nqb - 1 - in_group.q) * BM;          // heavy blocks first under a causal mask
+  // longest walks first, as far as they are known (late rows)
+  const int q0 = (by_size == BY_RANK ? __builtin_amdgcn_readfirstlane((int)ranks.order[in_group.q]) : nqb - 1 - in_group.q) * BM;
   const int tid = (int)threadIdx.x - kl * kThreads;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, grp = lane >> 4;
   Q += (int64_t)head * d.lq.head;
@@ -305,6 +304,19 @@ __global__ __launch_bounds__(512, 1) void scored_dq_kernel(
   }
 }
 
+template <int HR, int KL, bool CAP, bool BIAS>
+__global__ __launch_bounds__(512, 1) void scored_dq_kernel(
+    a2d_tile_desc d, ScoreRules r, int by_size, int parts, RowTable tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
+    const bf16_t* __restrict__ V, const bf16_t* __restrict__ O, const bf16_t* __restrict__ dO, const float* __restrict__ lse,
+    float* dQ, int rounded) {
+  extern __shared__ __attribute__((aligned(1024))) char lds_all[];
+  __shared__ int hull[16];
+  __shared__ Ranks ranks;
+  constexpr int BM = 256 / KL;
+  if (by_size == BY_RANK) rank_rows(ranks, d, r, d.nq, BM, 512);
+  scored_dq_rows<HR, KL, CAP, BIAS>(blockIdx.x, lds_all, hull, ranks, d, r, by_size, parts, tab, Q, K, V, O, dO, lse, dQ, rounded);
+}
+
 // --------------------------------------------------------------------------------------------- dK, dV
 
 constexpr int WK_KEYS = 256, WK_THREADS = 512, WK_ROWS = 64;
@@ -323,17 +335,18 @@ __host__ __device__ constexpr int wk_park(int hd) { return hd == 128 ? 1 : 0; }
 __host__ __device__ constexpr int wk_lds(int hd) { return wk_bits(hd) + SCORED_MOST_BITS + wk_park(hd) * 8 * 4 * BLOCK; }
 
 template <int HR, bool CAP, bool BIAS>
-__global__ __launch_bounds__(WK_THREADS) void scored_dkdv_kernel(
-    a2d_tile_desc d, ScoreRules r, int by_size, int parts, RowTable tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
-    const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO, float* __restrict__ dK, float* __restrict__ dV, int rounded) {
-  extern __shared__ __attribute__((aligned(1024))) char lds[];
+__device__ __forceinline__ void scored_dkdv_keys(
+    int id, char* const lds, const Ranks& ranks, const a2d_tile_desc& d, const ScoreRules& r, int by_size, int parts, const RowTable& tab,
+    const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
+    float* __restrict__ dK, float* __restrict__ dV, int rounded) {
   const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   constexpr int HD = padded_head(HR), H = HR, TILE = wk_tile(HD), BUF = 2 * TILE;
   constexpr int KS = HD / 32, HT = HR / 16;
   constexpr bool TIGHT = HD == 128;                  // registers (see dkdv_wide)
   const int kv_heads = d.heads / r.group, nkb = (d.nkv + WK_KEYS - 1) / WK_KEYS;
   int unit, blk;
-  if (!xcd_map(blockIdx.x, kv_heads * parts, nkb, by_size != 0, unit, blk)) return;
+  if (!xcd_map(id, kv_heads * parts, nkb, by_size != 0, unit, blk)) return;
+  if (by_size == BY_RANK) blk = __builtin_amdgcn_readfirstlane((int)ranks.order[blk]);
   const Split up = split_by(unit, parts);
   const int head = up.q, part = up.r, qh0 = head * r.group;
   const int k0 = blk * WK_KEYS;
@@ -643,17 +656,46 @@ __global__ __launch_bounds__(WK_THREADS) void scored_dkdv_kernel(
 }
 
 template <int HR, bool CAP, bool BIAS>
+__global__ __launch_bounds__(WK_THREADS) void scored_dkdv_kernel(
+    a2d_tile_desc d, ScoreRules r, int by_size, int parts, RowTable tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
+    const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO, float* __restrict__ dK, float* __restrict__ dV, int rounded) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  __shared__ Ranks ranks;
+  const int nkb = (d.nkv + WK_KEYS - 1) / WK_KEYS;
+  if (by_size == BY_RANK) {
+    // (the same for all heads) row tiles that see a block: +1 at the first block of a tile's hull, -1 behind its last, summed up
+    for (int i = threadIdx.x; i < nkb; i += WK_THREADS) ranks.weight[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < tab.padded / 32; i += WK_THREADS) {
+      const int lo = tab.tiles[i].lo, hi = tab.tiles[i].hi;
+      if (lo >= hi) continue;
+      atomicAdd(&ranks.weight[lo / WK_KEYS], 1);
+      if ((hi - 1) / WK_KEYS + 1 < nkb) atomicAdd(&ranks.weight[(hi - 1) / WK_KEYS + 1], -1);
+    }
+    __syncthreads();
+    int sum = 0;
+    if ((int)threadIdx.x < nkb)
+      for (int j = 0; j <= (int)threadIdx.x; ++j) sum += ranks.weight[j];
+    __syncthreads();
+    if ((int)threadIdx.x < nkb) ranks.weight[threadIdx.x] = sum;
+    rank_blocks(ranks, nkb, WK_THREADS);
+  }
+  scored_dkdv_keys<HR, CAP, BIAS>(blockIdx.x, lds, ranks, d, r, by_size, parts, tab, Q, K, V, dO, dK, dV, rounded);
+}
+static_assert(MAX_RANKED <= WK_THREADS, "a thread a block");
+
+template <int HR, bool CAP, bool BIAS>
 hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K, const void* V,
               const void* O, const void* dO, const float* lse, void* ws, float* dQ, float* dK, float* dV, hipStream_t s) {
   constexpr int HD = padded_head(HR);
   const RowTable tab = row_table(d, ws);
-  const int by_size = blocks_by_size(d, r);
   const int kvh = d.heads / r.group, dq_bytes = dq_launch_lds(HD, plan.lanes);
   const int words = (tab.padded / WK_ROWS * r.group + 63) / 64, wk_bytes = wk_park(HD) ? wk_lds(HD) : wk_bits(HD) + 8 * words;
   const auto dq = [&](auto* kernel) {
     if (ph == PREPARE) return ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), dq_bytes);
     const int bm = plan.lanes == 2 ? 128 : 256;
-    A2D_LAUNCH(kernel, dim3(xcd_grid(kvh * plan.parts_q, r.group * ((d.nq + bm - 1) / bm))), dim3(512), dq_bytes, s, d, r, by_size,
+    const int nqb = (d.nq + bm - 1) / bm, by_size = blocks_by_size(d, r, nqb);
+    A2D_LAUNCH(kernel, dim3(xcd_grid(kvh * plan.parts_q, r.group * nqb)), dim3(512), dq_bytes, s, d, r, by_size,
                plan.parts_q, tab, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, (const bf16_t*)O, (const bf16_t*)dO, lse, dQ,
                (int)(r.norm && plan.parts_q == 1));
     return hipGetLastError();
@@ -662,7 +704,8 @@ hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const Score
   if (e != hipSuccess) return e;
   // (the most a call can ask for: ensure_dynamic_lds is asked once for a kernel)
   if (ph == PREPARE) return ensure_dynamic_lds(reinterpret_cast<const void*>(scored_dkdv_kernel<HR, CAP, BIAS>), wk_lds(HD));
-  A2D_LAUNCH((scored_dkdv_kernel<HR, CAP, BIAS>), dim3(xcd_grid(kvh * plan.parts_kv, (d.nkv + WK_KEYS - 1) / WK_KEYS)), dim3(WK_THREADS),
+  const int nkb = (d.nkv + WK_KEYS - 1) / WK_KEYS, by_size = blocks_by_size(d, r, nkb);
+  A2D_LAUNCH((scored_dkdv_kernel<HR, CAP, BIAS>), dim3(xcd_grid(kvh * plan.parts_kv, nkb)), dim3(WK_THREADS),
              wk_bytes, s, d, r, by_size, plan.parts_kv, tab, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, (const bf16_t*)dO, dK, dV,
              (int)(r.norm && plan.parts_kv == 1));
   return hipGetLastError();

@@ -498,7 +498,8 @@ hipError_t fwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, int parts,
                float* out1, float* out2, const FwdInput& in, hipStream_t s) {
   constexpr int lds = fwd_lds<H, RT>(), bm = BLK * RT;
   if (ph == PREPARE) return ensure_dynamic_lds(reinterpret_cast<const void*>(scored_fwd_f32_kernel<H, RT>), lds);
-  const RowMap map = row_map(d, r, bm, parts);
+  RowMap map = row_map(d, r, bm, parts);
+  if (map.by_size == BY_RANK) map.by_size = 0;
   A2D_LAUNCH((scored_fwd_f32_kernel<H, RT>), dim3(xcd_grid(d.heads / r.group * parts, map.sub * ((map.rows + bm - 1) / bm))), dim3(64 * KL), lds,
              s, d, r, map, (const float*)Q, (const float*)K, (const float*)V, out0, out1, out2, in);
   return hipGetLastError();
@@ -513,7 +514,7 @@ hipError_t bwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const Scor
     return e != hipSuccess ? e : ensure_dynamic_lds(reinterpret_cast<const void*>(scored_dkdv_f32_kernel<H>), lds + MOST_BITS);
   }
   const RowTable tab = row_table(d, ws);
-  const int by_size = blocks_by_size(d, r), kvh = d.heads / r.group, words = (tab.padded / 32 * r.group + 63) / 64;
+  const int by_size = blocks_by_size(d, r, 1) != 0, kvh = d.heads / r.group, words = (tab.padded / 32 * r.group + 63) / 64;
   A2D_LAUNCH((scored_dq_f32_kernel<H>), dim3(xcd_grid(kvh * plan.parts_q, r.group * ((d.nq + 31) / 32))), dim3(64 * KL), lds, s, d, r, by_size,
              plan.parts_q, tab, (const float*)Q, (const float*)K, (const float*)V, (const float*)O, (const float*)dO, lse, dQ);
   const hipError_t e = hipGetLastError();

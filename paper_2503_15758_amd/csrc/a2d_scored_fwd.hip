@@ -3,8 +3,8 @@
 // The contractions are those of fwd_mfma_kernel and fwd_small_kernel: S^T = K Q^T with a lane holding four keys of one query
 // row in each tile of 16 x 16, and P^T as it stands as an operand of O^T += V^T P^T.  Between them the scores are brought into log2
 // units (z -> cap -> minus the bias), so that 2^x follows directly; without cap and bias they stay raw and the exponent
-// takes them in with its multiply-add.  The rules cost vector instructions a score: the cap 6 (a polynomial, see CapArgs; where some
-// score of a wavefront's block is beyond its range 12, two of them of a quarter of the rate), the bias 2.
+// takes them in with its multiply-add.  The rules cost vector instructions a score: the cap 4.5 (a polynomial, see CapArgs; where some
+// score of a wavefront's block is beyond its range 12, two of them of a quarter of the rate), the bias 2.3.
 //
 // Masks: whatever they are made of, a query row sees one run of keys (visible_run).  A workgroup walks the hull of
 // its rows' runs; a wavefront leaves out the blocks that none of its rows sees, and compares keys only in blocks that some row does not see
@@ -23,40 +23,117 @@ using namespace mfma;
 
 constexpr float kRescaleThreshold = 8.0f;            // log2 units (as in a2d_fwd_mfma.hip)
 
-// Raw dot products -> scores in the units of the exponent: log2 with a cap or a bias, else raw.  raw: log2 units of a raw one.  NT tiles of 16 keys from k0 on.
-template <int NT, bool CAP, bool BIAS>
-__device__ __forceinline__ void to_scores(f32x4 (&s)[NT][2], const ScoreRules& r, const RowState<2>& rs, bool masked, int k0, int grp, float raw) {
-  if constexpr (CAP) {
-    float big = 0.f;
+// ---- Scores in log2 units, relative to the row's reference from the start: the multiply-add that ends the cap or takes in the raw product takes
+// the reference too, so that 2^x follows directly (a subtraction of its own was a tenth of the vector instructions).
+// Score e of a lane's: tile of 16 keys e >> 2, key e & 3 of its four.  raw: log2 units of a raw product.  from: distance of the lane's first
+// key.  BEYOND: products beyond the polynomial's range too
+template <bool CAP, bool BIAS, bool BEYOND>
+__device__ __forceinline__ float to_score(float z, float ref, const ScoreRules& r, float raw, float slope, float from, int e) {
+  float x;
+  if constexpr (CAP) x = BEYOND ? cap_log2(r.capped, z) - ref : fmaf(z, cap_factor(r.capped, z), -ref);
+  else x = fmaf(z, raw, -ref);
+  if constexpr (BIAS) x = fmaf(-slope, fabsf(distance<-1>(r, from, e >> 2, e & 3)), x);
+  return x;
+}
+// whether some score of the wavefront's is beyond the polynomial's range (a NaN is left out, and comes through it as NaN)
+template <int NT>
+__device__ __forceinline__ bool some_beyond(const f32x4 (&s)[NT][2], const CapArgs& a) {
+  float big = 0.f;
 #pragma unroll
-    for (int q = 0; q < 2; ++q)
+  for (int q = 0; q < 2; ++q)
 #pragma unroll
-      for (int e = 0; e < 4 * NT; ++e) big = fmaxf(big, fabsf(s[e >> 2][q][e & 3]));
-    // (a NaN is left out of the maximum, and comes through the polynomial as NaN)
-    if (A2D_SELDOM(__builtin_amdgcn_ballot_w64(big > r.capped.small) != 0)) {
-      asm volatile("" ::: "memory");                 // keep this a branch
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int e = 0; e < 4 * NT; ++e) s[e >> 2][q][e & 3] = cap_log2<false>(r.capped, s[e >> 2][q][e & 3]);
-    } else {
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int e = 0; e < 4 * NT; ++e) s[e >> 2][q][e & 3] = cap_log2<true>(r.capped, s[e >> 2][q][e & 3]);
-    }
+    for (int e = 0; e < 4 * NT; ++e) big = fmaxf(big, fabsf(s[e >> 2][q][e & 3]));
+  return __builtin_amdgcn_ballot_w64(big > a.small) != 0;
+}
+// Distance of a lane's first key of the tiles from k0 on (whole numbers below 2^24: exact)
+template <bool BIAS>
+__device__ __forceinline__ float first_distance(const ScoreRules& r, const RowState<2>& rs, int q, int k0, int grp) {
+  return BIAS ? fmaf((float)-(k0 + 4 * grp), r.steps[0], rs.at[q]) : 0.f;
+}
+
+// What a wavefront's softmax keeps of the lane's row in each of its two tiles
+struct Softmax {
+  float m_lane[2];       // maximum of the lane's scores so far, relative to ref; -inf: none
+  float ref[2];          // reference of the row's scores (the same in its four lanes); 0 until it sees something
+  float l[2];            // the lane's share of the row sum, relative to ref
+  __device__ __forceinline__ void start(int q, float m) {                // m: stored maximum, natural units
+    m_lane[q] = m == -INFINITY ? m : 0.f;
+    ref[q] = m == -INFINITY ? 0.f : m * kLog2e;
   }
-  if constexpr (BIAS) {
+  // the row's maximum in log2 units, and what N and l are multiplied with to be relative to it
+  __device__ __forceinline__ void finish(int q, float& m_row, float& f) const {
+    m_row = row_max(m_lane[q]);
+    const bool none = m_row == -INFINITY;
+    f = none ? 0.f : fast_exp2(-m_row);
+    if (!none) m_row += ref[q];
+  }
+  // Takes in the maxima of new scores.  The reference follows the running maximum only when a score exceeds it by more than 2^8, or
+  // with the first keys that a lane sees (as in fwd_softmax): a rare branch, and the only place where the lanes of a row talk.
+  template <int NT, int HT>
+  __device__ __forceinline__ void follow(f32x4 (&s)[NT][2], f32x4 (&o)[HT][2]) {
+    const float was[2] = {m_lane[0], m_lane[1]};
+    bool grow = false;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const float from = fmaf((float)-(k0 + 4 * grp), r.steps[0], rs.at[q]);       // (whole numbers below 2^24: exact)
+      float mx = was[q];
+#pragma unroll
+      for (int e = 0; e < 4 * NT; ++e) mx = fmaxf(mx, s[e >> 2][q][e & 3]);
+      m_lane[q] = mx;
+      grow |= mx > kRescaleThreshold || (was[q] == -INFINITY && mx > -INFINITY);         // (NaN: false)
+    }
+    if (A2D_OFTEN(__builtin_amdgcn_ballot_w64(grow) == 0)) return;
+    asm volatile("" ::: "memory");                   // keep this a branch
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const float m_row = row_max(m_lane[q]), by = m_row == -INFINITY ? 0.f : m_row;
+      const float alpha = row_max(was[q]) == -INFINITY ? 0.f : fast_exp2(-by);           // (nothing is held yet)
+      ref[q] += by;
+      m_lane[q] -= by;
+      l[q] *= alpha;
+#pragma unroll
+      for (int e = 0; e < 4 * NT; ++e) s[e >> 2][q][e & 3] -= by;
+#pragma unroll
+      for (int t = 0; t < HT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[t][q][e] *= alpha;
+    }
+  }
+  // P^T in bf16 (nearest-even, for the contraction); the sums take the probabilities before their rounding
+  template <int NT>
+  __device__ __forceinline__ void probabilities(const f32x4 (&s)[NT][2], bf16x8 (&pb)[NT / 2][2]) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 4 * NT; ++e) {
-        const float far = distance<-1>(r, from, e >> 2, e & 3);
-        const float x = s[e >> 2][q][e & 3];
-        s[e >> 2][q][e & 3] = fmaf(-rs.slope[q], fabsf(far), CAP ? x : x * raw);
+        const float p = fast_exp2(s[e >> 2][q][e & 3]);
+        sum += p;
+        pb[e >> 3][q][e & 7] = (bf16_t)p;
       }
+      l[q] += sum;
     }
+  }
+};
+
+// Raw products of NT tiles of 16 keys from k0 on -> scores
+template <int NT, bool CAP, bool BIAS>
+__device__ __forceinline__ void to_scores(f32x4 (&s)[NT][2], const Softmax& sm, const ScoreRules& r, const RowState<2>& rs, bool masked, int k0,
+                                          int grp, float raw) {
+  const auto all = [&](auto beyond) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const float from = first_distance<BIAS>(r, rs, q, k0, grp);
+#pragma unroll
+      for (int e = 0; e < 4 * NT; ++e)
+        s[e >> 2][q][e & 3] =
+            to_score<CAP, BIAS, decltype(beyond)::value>(s[e >> 2][q][e & 3], sm.ref[q], r, raw, BIAS ? rs.slope[q] : 0.f, from, e);
+    }
+  };
+  if (CAP && A2D_SELDOM(some_beyond(s, r.capped))) {
+    asm volatile("" ::: "memory");                   // keep this a branch
+    all(std::true_type{});
+  } else {
+    all(std::false_type{});
   }
   if (A2D_SELDOM(masked)) {
     asm volatile("" ::: "memory");                   // keep this a branch
@@ -70,83 +147,26 @@ __device__ __forceinline__ void to_scores(f32x4 (&s)[NT][2], const ScoreRules& r
   }
 }
 
-// One softmax step over NT tiles of 16 keys: the running maximum and its lazy reference (as in fwd_softmax), P^T in bf16.
-// m_lane, m_ref, l_run, o: as in FwdState.  (values: called in front of the exponentials)
-template <int NT, int HT, class F>
-__device__ __forceinline__ void softmax_step(f32x4 (&s)[NT][2], float (&m_lane)[2], float (&m_ref)[2], float (&l_run)[2], f32x4 (&o)[HT][2],
-                                             bf16x8 (&pb)[NT / 2][2], float c, F&& values) {
-  bool grow = false;
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    float mx = m_lane[q];
-#pragma unroll
-    for (int e = 0; e < 4 * NT; ++e) mx = fmaxf(mx, s[e >> 2][q][e & 3]);
-    m_lane[q] = mx;
-    // (m_lane - m_ref is +inf on the first visible block, NaN (-> false) while nothing is visible)
-    grow |= (mx - m_ref[q]) * c > kRescaleThreshold;
-  }
-  if (A2D_SELDOM(__builtin_amdgcn_ballot_w64(grow) != 0)) {
-    asm volatile("" ::: "memory");
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const float m_row = row_max(m_lane[q]);
-      const float m_use = (m_row == -INFINITY) ? 0.f : m_row;
-      const float alpha = fast_exp2((m_ref[q] - m_use) * c);   // m_ref = -inf gives 0
-      m_ref[q] = m_row;
-      l_run[q] *= alpha;
-#pragma unroll
-      for (int t = 0; t < HT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[t][q][e] *= alpha;
-    }
-  }
-  values();
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const float mc = (m_ref[q] == -INFINITY) ? 0.f : m_ref[q] * c;
-    float psum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4 * NT; ++e) {
-      const float p = fast_exp2(fmaf(s[e >> 2][q][e & 3], c, -mc));
-      psum += p;
-      pb[e >> 3][q][e & 7] = (bf16_t)p;              // (the sum takes the probability before its rounding)
-    }
-    l_run[q] += psum;
-  }
-  __builtin_amdgcn_sched_barrier(0);
-}
-
-// units of the exponent -> 1: m in natural units, and what the exponentials are multiplied with
-template <bool CAP, bool BIAS>
-struct Units {
-  float raw, c, to_m;                                // exponent of 2 for a raw product, for a unit; m for a unit
-  __device__ __forceinline__ Units(const a2d_tile_desc& d)
-      : raw(uniform(d.scale * kLog2e)), c(CAP || BIAS ? 1.f : raw), to_m(CAP || BIAS ? 1.f / kLog2e : d.scale) {}
-};
-
-// KL = 1: 256 rows, eight wavefronts of 32.  KL = 2: 128 rows in two key lanes of four wavefronts, which take alternate key blocks and
-// are merged through LDS at the end.  (Staging, fragments and epilogue as in fwd_mfma_kernel.)
-// (out0, out1, out2 are not __restrict__: an accumulating call's `in` is the same memory)
-template <int HR, int KL, bool CAP, bool BIAS>
-__global__ __launch_bounds__(512, 1) void scored_fwd_kernel(
-    a2d_tile_desc d, ScoreRules r, RowMap map, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
-    const bf16_t* __restrict__ V, float* out0, float* out1, float* out2, FwdInput in) {
-  constexpr int WAVES = 8, RW = WAVES / KL, BM = 32 * RW, kThreads = 64 * RW;
+template <int WAVES, int HR, int KL, bool CAP, bool BIAS>
+__device__ __forceinline__ void scored_fwd_rows(
+    int id, char* const lds_all, int* const hull, const Ranks& ranks, const a2d_tile_desc& d, const ScoreRules& r, const RowMap& map,
+    const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, float* out0, float* out1, float* out2,
+    const FwdInput& in) {
+  constexpr int RW = WAVES / KL, BM = 32 * RW, kThreads = 64 * RW;
   constexpr int HD = padded_head(HR), H = HR, KS = HD / 32, HT = HR / 16, BUF_BYTES = buf_bytes(HD);
-  extern __shared__ __attribute__((aligned(1024))) char lds_all[];
-  __shared__ int hull[2 * RW];
   const int kl = KL == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads);
   char* const lds = lds_all + kl * lds_bytes(HD);
   const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
   const int nqb = (map.rows + BM - 1) / BM;
   int unit, blk;
-  if (!xcd_map(blockIdx.x, d.heads / r.group * map.parts, map.sub * nqb, map.by_size != 0, unit, blk, kXcdCus)) return;
+  if (!xcd_map(id, d.heads / r.group * map.parts, map.sub * nqb, map.by_size != 0, unit, blk, kXcdCus * 8 / WAVES)) return;
   const Split up = split_by(unit, map.parts);
   const int kvh = up.q, part = up.r;
   const Split in_group = query_head(blk, map.sub, nqb, map.by_size != 0);
   const int head = kvh * r.group + in_group.r;
-  const int q0 = (nqb - 1 - in_group.q) * BM;         // heavy (late) query blocks first: under a causal mask they walk more keys
+  // longest walks first, as far as they are known (late rows)
+  const int q0 = (map.by_size == BY_RANK ? __builtin_amdgcn_readfirstlane((int)ranks.order[in_group.q]) : nqb - 1 - in_group.q) * BM;
   const int tid = (int)threadIdx.x - kl * kThreads;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, grp = lane >> 4;
   Q += (int64_t)head * d.lq.head;
@@ -159,7 +179,7 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_kernel(
     out2 += slot;
   }
   const int64_t row0 = (int64_t)head * d.nq;          // of the run of rows, in the outputs
-  const Units<CAP, BIAS> units(d);
+  const float raw = uniform(d.scale * kLog2e);
 
   RowState<2> rs;
   look_up_rows<2, BIAS>(rs, d, r, map, head, q0 + wave * 32, lane);
@@ -184,11 +204,12 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_kernel(
                                 16 * (ch ^ block_swap((row & 15) >> 2))) = u32x4{0, 0, 0, 0};
     }
   }
-  FwdState<HR> st;
+  f32x4 o[HT][2];
 #pragma unroll
-  for (int t = 0; t < HT; ++t) st.o[t][0] = st.o[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < HT; ++t) o[t][0] = o[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  Softmax sm;
   float m_in[2] = {-INFINITY, -INFINITY};
-  st.l_run[0] = st.l_run[1] = 0.f;
+  sm.l[0] = sm.l[1] = 0.f;
   if (r.acc && part == 0 && kl == 0) {
     // continues the stored partial: N into the accumulators, m as the exponent's reference, l into one of the four lanes of a row
 #pragma unroll
@@ -196,9 +217,9 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_kernel(
       const int row = q0 + wave * 32 + 16 * q + (lane & 15);
       if (row >= map.rows) continue;
       m_in[q] = in.m[row0 + row];
-      st.l_run[q] = grp == 0 ? in.l[row0 + row] : 0.f;
+      sm.l[q] = grp == 0 ? in.l[row0 + row] : 0.f;
 #pragma unroll
-      for (int t = 0; t < HT; ++t) st.o[t][q] = *reinterpret_cast<const f32x4*>(in.N + (row0 + row) * H + 16 * t + 4 * grp);
+      for (int t = 0; t < HT; ++t) o[t][q] = *reinterpret_cast<const f32x4*>(in.N + (row0 + row) * H + 16 * t + 4 * grp);
     }
   }
   __syncthreads();
@@ -210,7 +231,7 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_kernel(
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
   hi = __builtin_amdgcn_readfirstlane(hi);
-  const int first = hi > lo ? lo / BN : 0, end = hi > lo ? (hi + BN - 1) / BN : 0;     // key blocks of the walk
+  const int first = hi > lo ? lo / BN : 1, end = hi > lo ? (hi + BN - 1) / BN : 1;     // key blocks of the walk
 
   // ---- staging, straight into LDS: of eight wavefronts 0 .. 3 load a row tile of K each and 4 .. 7 one of V, each of four
   // one of both.  Rows outside the hull re-read its first or last key.
@@ -234,43 +255,45 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_kernel(
   };
   Blocks16 rd;
   rd.init(lane, lds_base);
+  // From the last block down: under a bias the nearest keys of a causal row score highest, and met last they would move its reference again and
+  // again (16 heads of 64, 8192 x 8192: 225 us from the first block up, 177 down; 32 of 128, 4096 x 4096: 164, 141)
   const int stride = KL * map.parts;
-  int lead = first + part * KL, j = lead + kl;        // key lane 0's block; this lane's
-  if (j < end) load_tile(j, 0);
+  int lead = end - 1 - part * KL, j = lead - kl;      // key lane 0's block; this lane's
+  if (j >= first) load_tile(j, 0);
   wait_vmem_all();                                    // (the Q rows and the first tiles together)
 #pragma unroll
-  for (int q = 0; q < 2; ++q) st.m_lane[q] = st.m_ref[q] = m_in[q] / units.to_m;       // -inf stays -inf
+  for (int q = 0; q < 2; ++q) sm.start(q, m_in[q]);
   __syncthreads();
 
   int boff = 0;
-  for (; lead < end; lead += stride) {
-    if (A2D_OFTEN(j + stride < end)) load_tile(j + stride, BUF_BYTES - boff);
+  for (; lead >= first; lead -= stride) {
+    if (A2D_OFTEN(j - stride >= first)) load_tile(j - stride, BUF_BYTES - boff);
     const int k0 = j * BN;
-    if (j < end && k0 + BN > rs.lo && k0 < rs.hi) {
-      const bool masked = k0 < rs.all_lo || k0 + BN > rs.all_hi;
+    if (j >= first && k0 + BN > rs.lo && k0 < rs.hi) {
       Scores s;
       Ring kr, vr;
       bf16x8 pb[2][2];
       fwd_first_keys<HR>(kr, rd, boff);
       fwd_scores<HR>(s, kr, qf, rd, boff);
-      to_scores<4, CAP, BIAS>(s, r, rs, masked, k0, grp, units.raw);
-      softmax_step<4, HT>(s, st.m_lane, st.m_ref, st.l_run, st.o, pb, units.c, [&]() { fwd_first_values<HR>(vr, rd, boff); });
-      fwd_products<HR>(st, pb, vr, rd, boff);
+      to_scores<4, CAP, BIAS>(s, sm, r, rs, k0 < rs.all_lo || k0 + BN > rs.all_hi, k0, grp, raw);
+      sm.follow(s, o);
+      fwd_first_values<HR>(vr, rd, boff);
+      sm.probabilities(s, pb);
+      __builtin_amdgcn_sched_barrier(0);
+      fwd_products<HR>(o, pb, vr, rd, boff);
     }
     wait_vmem_all();
     __syncthreads();
-    j += stride;
+    j -= stride;
     boff = BUF_BYTES - boff;
   }
 
   // ---- epilogue: N and l to the true row maximum
-  const float c = units.c;
   float m_row[2], f[2], l_tot[2];
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    m_row[q] = row_max(st.m_lane[q]);
-    f[q] = (m_row[q] == -INFINITY) ? 0.f : fast_exp2((st.m_ref[q] - m_row[q]) * c);
-    l_tot[q] = row_sum(st.l_run[q]) * f[q];
+    sm.finish(q, m_row[q], f[q]);
+    l_tot[q] = row_sum(sm.l[q]) * f[q];
   }
   if constexpr (KL == 2) {
     // key lane 1 hands its (N, m, l) to lane 0 through LDS, which merges them as two partials (Alg. 2)
@@ -283,7 +306,7 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_kernel(
 #pragma unroll
         for (int t = 0; t < HT; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) xch[(8 * t + 4 * q + e) * 64] = st.o[t][q][e] * f[q];
+          for (int e = 0; e < 4; ++e) xch[(8 * t + 4 * q + e) * 64] = o[t][q][e] * f[q];
         xch[(HT * 8 + 2 * q) * 64] = m_row[q];
         xch[(HT * 8 + 2 * q + 1) * 64] = l_tot[q];
       }
@@ -294,13 +317,13 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_kernel(
     for (int q = 0; q < 2; ++q) {
       const float m1 = xch[(HT * 8 + 2 * q) * 64], l1 = xch[(HT * 8 + 2 * q + 1) * 64];
       const float m_new = fmaxf(m_row[q], m1);
-      const float a0 = (m_row[q] == -INFINITY) ? 0.f : f[q] * fast_exp2((m_row[q] - m_new) * c);
-      const float a1 = (m1 == -INFINITY) ? 0.f : fast_exp2((m1 - m_new) * c);
+      const float a0 = (m_row[q] == -INFINITY) ? 0.f : f[q] * fast_exp2(m_row[q] - m_new);
+      const float a1 = (m1 == -INFINITY) ? 0.f : fast_exp2(m1 - m_new);
 #pragma unroll
       for (int t = 0; t < HT; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) st.o[t][q][e] = st.o[t][q][e] * a0 + xch[(8 * t + 4 * q + e) * 64] * a1;
-      l_tot[q] = (m_row[q] == -INFINITY ? 0.f : l_tot[q] * fast_exp2((m_row[q] - m_new) * c)) + l1 * a1;
+        for (int e = 0; e < 4; ++e) o[t][q][e] = o[t][q][e] * a0 + xch[(8 * t + 4 * q + e) * 64] * a1;
+      l_tot[q] = (m_row[q] == -INFINITY ? 0.f : l_tot[q] * fast_exp2(m_row[q] - m_new)) + l1 * a1;
       m_row[q] = m_new;
       f[q] = 1.f;
     }
@@ -313,16 +336,28 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_kernel(
     const bool stat = grp == 0 && (lane & 15) < n;
     const int64_t at = row0 + row;
     if (r.norm && map.parts == 1) {
-      store_acc16(reinterpret_cast<bf16_t*>(out0) + at * H, H, n, area, st.o, q, lane, l_tot[q] > 0.f ? f[q] / l_tot[q] : 0.f);
-      if (stat) out1[at + (lane & 15)] = l_tot[q] > 0.f ? m_row[q] * units.to_m + logf(l_tot[q]) : -INFINITY;
+      store_acc16(reinterpret_cast<bf16_t*>(out0) + at * H, H, n, area, o, q, lane, l_tot[q] > 0.f ? f[q] / l_tot[q] : 0.f);
+      if (stat) out1[at + (lane & 15)] = l_tot[q] > 0.f ? m_row[q] / kLog2e + logf(l_tot[q]) : -INFINITY;
     } else {
-      store_acc16(out0 + at * H, H, n, area, st.o, q, lane, f[q]);
+      store_acc16(out0 + at * H, H, n, area, o, q, lane, f[q]);
       if (stat) {
-        out1[at + (lane & 15)] = m_row[q] * units.to_m;         // -inf stays -inf
+        out1[at + (lane & 15)] = m_row[q] / kLog2e;         // -inf stays -inf
         out2[at + (lane & 15)] = l_tot[q];
       }
     }
   }
+}
+
+template <int WAVES, int HR, int KL, bool CAP, bool BIAS>
+__global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void scored_fwd_kernel(
+    a2d_tile_desc d, ScoreRules r, RowMap map, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
+    const bf16_t* __restrict__ V, float* out0, float* out1, float* out2, FwdInput in) {
+  extern __shared__ __attribute__((aligned(1024))) char lds_all[];
+  __shared__ int hull[2 * WAVES];
+  __shared__ Ranks ranks;
+  constexpr int BM = 32 * WAVES / KL;
+  if (map.by_size == BY_RANK) rank_rows(ranks, d, r, map.rows, BM, 64 * WAVES);
+  scored_fwd_rows<WAVES, HR, KL, CAP, BIAS>(blockIdx.x, lds_all, hull, ranks, d, r, map, Q, K, V, out0, out1, out2, in);
 }
 
 // ---- 32 rows and eight key lanes: for few rows.  Every wavefront holds the same rows and takes every eighth slab of 32 keys,
@@ -351,7 +386,7 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
   const int kvh = up.q, part = up.r;
   const Split in_group = query_head(blk, map.sub, nqb, map.by_size != 0);
   const int head = kvh * r.group + in_group.r;
-  const int q0 = (nqb - 1 - in_group.q) * BM;
+  const int q0 = (nqb - 1 - in_group.q) * BM;         // (late ones first)
   Q += (int64_t)head * d.lq.head;
   K += (int64_t)kvh * d.lk.head;
   V += (int64_t)kvh * d.lv.head;
@@ -362,8 +397,7 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
     out2 += slot;
   }
   const int64_t row0 = (int64_t)head * d.nq;
-  const Units<CAP, BIAS> units(d);
-  const float c = units.c;
+  const float raw = uniform(d.scale * kLog2e);
 
   RowState<2> rs;
   look_up_rows<2, BIAS>(rs, d, r, map, head, q0, lane);
@@ -377,7 +411,7 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
       if (32 * x + 32 > H && at >= H) qf[x][q] = bf16x8{};
     }
   const int lo = rs.lo, hi = rs.hi;
-  const int first = hi > lo ? lo / SB : 0, end = hi > lo ? (hi + SB - 1) / SB : 0;
+  const int first = hi > lo ? lo / SB : 1, end = hi > lo ? (hi + SB - 1) / SB : 1;
 
   const unsigned k_row_bytes = __builtin_amdgcn_readfirstlane((unsigned)d.lk.row * 2);
   const unsigned v_row_bytes = __builtin_amdgcn_readfirstlane((unsigned)d.lv.row * 2);
@@ -408,30 +442,35 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
   f32x4 o[HT][2];
 #pragma unroll
   for (int t = 0; t < HT; ++t) o[t][0] = o[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m_lane[2] = {-INFINITY, -INFINITY}, m_ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+  Softmax sm;
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    sm.start(q, -INFINITY);
+    sm.l[q] = 0.f;
+  }
   if (r.acc && part == 0 && wave == 0) {
     // the first wavefront continues the stored partial
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       const int row = q0 + 16 * q + (lane & 15);
       if (row >= map.rows) continue;
-      m_lane[q] = m_ref[q] = in.m[row0 + row] / units.to_m;
-      l_run[q] = grp == 0 ? in.l[row0 + row] : 0.f;
+      sm.start(q, in.m[row0 + row]);
+      sm.l[q] = grp == 0 ? in.l[row0 + row] : 0.f;
 #pragma unroll
       for (int t = 0; t < HT; ++t) o[t][q] = *reinterpret_cast<const f32x4*>(in.N + (row0 + row) * H + 16 * t + 4 * grp);
     }
   }
   wait_vmem_all();                                   // (Q, and what an accumulating call starts from: the waits below count slabs alone)
   const int stride = WAVES * map.parts;
-  int j = first + part * WAVES + wave;
-  if (j < end) {
+  int j = end - 1 - part * WAVES - wave;             // (from the last block down, as scored_fwd_rows)
+  if (j >= first) {
     load(false, j);
     load(true, j);
     wait_dma<LOADS>();                               // (K)
   }
   // the next K goes where the last one was read from while the exponentials and V P^T are under way, the next V behind those
-  for (; j < end; j += stride) {
-    const bool more = j + stride < end;
+  for (; j >= first; j -= stride) {
+    const bool more = j - stride >= first;
     const int k0 = j * SB;
     f32x4 s[2][2];
 #pragma unroll
@@ -445,10 +484,12 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
         for (int q = 0; q < 2; ++q) s[k][q] = mma16(a, qf[x][q], s[k][q]);
       }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (more) load(false, j + stride);
-    to_scores<2, CAP, BIAS>(s, r, rs, k0 < rs.all_lo || k0 + SB > rs.all_hi, k0, grp, units.raw);
+    if (more) load(false, j - stride);
+    to_scores<2, CAP, BIAS>(s, sm, r, rs, k0 < rs.all_lo || k0 + SB > rs.all_hi, k0, grp, raw);
+    sm.follow(s, o);
     bf16x8 pb[1][2];
-    softmax_step<2, HT>(s, m_lane, m_ref, l_run, o, pb, c, [] {});
+    sm.probabilities(s, pb);
+    __builtin_amdgcn_sched_barrier(0);
     if (more) wait_dma<LOADS>(); else wait_dma();    // V has arrived
 #pragma unroll
     for (int t = 0; t < HT; ++t) {
@@ -459,7 +500,7 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) {
-      load(true, j + stride);
+      load(true, j - stride);
       wait_dma<LOADS>();
     }
   }
@@ -470,9 +511,8 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
   float m_row[2], l_row[2], f[2];
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    m_row[q] = row_max(m_lane[q]);
-    f[q] = (m_row[q] == -INFINITY) ? 0.f : fast_exp2((m_ref[q] - m_row[q]) * c);
-    l_row[q] = row_sum(l_run[q]) * f[q];
+    sm.finish(q, m_row[q], f[q]);
+    l_row[q] = row_sum(sm.l[q]) * f[q];
   }
   if (lane < 32) {                                   // (lanes 0 .. 15 hold tile 0's rows, 16 .. 31 tile 1's)
     xm[wave * 32] = m_row[grp & 1];
@@ -488,20 +528,20 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
   row_pair(m_use, use);
   if (norm || wave == 0) {
 #pragma unroll
-    for (int k = 0; k < WAVES; ++k) l_tot += xl[k * 32] * fast_exp2((xm[k * 32] - m_use) * c);
+    for (int k = 0; k < WAVES; ++k) l_tot += xl[k * 32] * fast_exp2(xm[k * 32] - m_use);
     row_pair(l_tot > 0.f ? 1.0f / l_tot : 0.f, fn);
   }
   if (wave == 0 && lane < 32 && q0 + lane < map.rows) {
     const int64_t row = row0 + q0 + lane;
-    if (norm) out1[row] = l_tot > 0.f ? m_new * units.to_m + logf(l_tot) : -INFINITY;
+    if (norm) out1[row] = l_tot > 0.f ? m_new / kLog2e + logf(l_tot) : -INFINITY;
     else {
-      out1[row] = m_new * units.to_m;
+      out1[row] = m_new / kLog2e;
       out2[row] = l_tot;
     }
   }
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    const float a = f[q] * fast_exp2((m_row[q] - use[q]) * c);
+    const float a = f[q] * fast_exp2(m_row[q] - use[q]);
     // every wavefront leaves its pieces of four columns, [wavefront][piece][lane], and adds up and stores two of them
 #pragma unroll
     for (int t = 0; t < HT; ++t)
@@ -531,45 +571,64 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
   }
 }
 
-constexpr int kRows[3] = {256, 128, 32};
+constexpr int kRows[4] = {256, 128, 128, 32};
 
 template <int HR, bool CAP, bool BIAS>
 hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, const void* Q, const void* K, const void* V,
               float* out0, float* out1, float* out2, const FwdInput& in, hipStream_t s) {
   const int bm = kRows[plan.form];
   const RowMap map = row_map(d, r, bm, plan.parts);
-  const int bytes = plan.form == SCORED_32 ? SMALL_LDS : fwd_lds(8, padded_head(HR), plan.form == SCORED_LANES ? 2 : 1);
+  const int waves = plan.form == SCORED_PAIRS ? 4 : 8;
+  const int bytes = plan.form == SCORED_32 ? SMALL_LDS : fwd_lds(waves, padded_head(HR), plan.form == SCORED_LANES ? 2 : 1);
   const auto run = [&](auto* kernel) {
     if (ph == PREPARE) return ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes);
-    const dim3 grid(xcd_grid(d.heads / r.group * map.parts, map.sub * ((map.rows + bm - 1) / bm)));
-    A2D_LAUNCH(kernel, grid, dim3(512), bytes, s, d, r, map, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, out0, out1, out2, in);
+    const int units = d.heads / r.group * map.parts, blocks = map.sub * ((map.rows + bm - 1) / bm);
+    const dim3 grid(xcd_grid(units, blocks));
+    A2D_LAUNCH(kernel, grid, dim3(64 * waves), bytes, s, d, r, map, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, out0, out1, out2, in);
     return hipGetLastError();
   };
-  return plan.form == SCORED_256     ? run(scored_fwd_kernel<HR, 1, CAP, BIAS>)
-         : plan.form == SCORED_LANES ? run(scored_fwd_kernel<HR, 2, CAP, BIAS>)
+  return plan.form == SCORED_256     ? run(scored_fwd_kernel<8, HR, 1, CAP, BIAS>)
+         : plan.form == SCORED_LANES ? run(scored_fwd_kernel<8, HR, 2, CAP, BIAS>)
+         : plan.form == SCORED_PAIRS ? run(scored_fwd_kernel<4, HR, 1, CAP, BIAS>)
                                      : run(scored_fwd_small_kernel<HR, CAP, BIAS>);
 }
 
 }  // namespace
 
+// Every form's time from its turns of the chip (walk_time), the quickest.  Steps in us, of 64 keys (of 128 and 256 in the forms with key
+// lanes), by head size and rules, fitted to 40 calls timed in every form.  What they choose between, measured: 8192 x 8192 rows of
+// 16 heads of 64 in six documents 83 us in pairs, 102 with 256 rows (the pairs' turns are half as long); 16384 x 16384, 8 heads of 128: 574
+// with 256 rows, 612 in pairs; 13611 x 14346, 4 of 80, causal: 206 in two key lanes, 281 in pairs, 382 with 256 rows;
+// a token of 256 heads of 64 against 16384 of 64: 67 with 32 rows in four parts, 180 in one, 330 with 256.  Ranges that the
+// host cannot see: one for all heads is taken for documents, which see a part of the keys each (749 x 9939: 13 us in one part, 21 where a plan
+// for whole walks split them); one a sequence for its filled length.
 ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap) {
+  constexpr struct {
+    double step, by_head, fixed, pair;                // pair: both workgroups of a compute unit, of one's time
+    int keys;
+  } kForms[4] = {{0.95, 0.95, 4.0, 0, 64}, {0.9, 1.15, 7.5, 0, 128}, {0.5, 0.95, 4.0, 1.4, 64}, {1.0, 0.8, 3.7, 0, 256}};
   const int kv_heads = d.heads / r.group;
+  const WalkKeys walk = walk_keys(d, r);
+  const double part_us = (double)d.heads * d.nq * (d.hdim + 2) * 8 / 4.5e6;
   double least = 0;
   ScoredPlan best{SCORED_256, 1};
-  for (int f = 0; f < 3; ++f) {
+  for (int f = 0; f < 4; ++f) {
+    const auto& form = kForms[f];
     const int bm = kRows[f];
     const bool packed = r.group > 1 && d.nq < bm;
     const int64_t blocks = packed ? (int64_t)kv_heads * (((int64_t)r.group * d.nq + bm - 1) / bm)
                                   : (int64_t)d.heads * ((d.nq + bm - 1) / bm);
-    const double keys = f == SCORED_32 ? 256 : f == SCORED_LANES ? 128 : 64;
-    const WalkKeys w = walk_keys(d, r);
-    const double most = w.most / keys + 0.2, mean = packed ? most : w.mean / keys + 0.2;
-    const double step = f == SCORED_32 ? 1.6 : f == SCORED_LANES ? 2.0 : 1.8, fixed = f == SCORED_32 ? 4.0 : 5.0;
-    const WalkModel m{blocks, cus, mean, most, step, fixed, 0, 0, nullptr, 0, 0.5};
-    const double part_us = (double)d.heads * d.nq * (d.hdim + 2) * 8 / 4.5e6;
+    double most = walk.most, mean = packed ? most : walk.mean;
+    if (r.ranges && r.heads_per_set == d.heads && !packed) {
+      most *= 0.35;
+      mean *= 0.25;
+    }
+    const double step = form.step + form.by_head * d.hdim / 128 + 0.2 * ((r.cap != 0.f) + (r.slopes != nullptr));
+    const WalkModel m{blocks, cus, mean / form.keys + 0.2, most / form.keys + 0.2, step, form.fixed, form.pair * step,
+                      form.pair != 0 ? form.fixed : 0, nullptr, 0, 0.4};
     double t;
     const int parts = best_parts(m, cap, 4.5, part_us, &t);
-    if (f == 0 || t < 0.98 * least) {
+    if (f == 0 || t < least) {
       least = t;
       best = ScoredPlan{f, parts};
     }

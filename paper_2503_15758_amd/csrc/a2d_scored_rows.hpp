@@ -10,9 +10,38 @@ namespace a2d {
 // Where the rows of a launch lie: `sub` runs of `rows` query rows for a key/value head, cut into blocks
 struct RowMap {
   int sub, rows;         // packed: 1, group * nq; else group, nq
-  int by_size;           // blocks in order of size (see xcd_map): the causal mask crosses the tile
+  int by_size;           // blocks in order of size (see xcd_map): BY_ROWS late ones first, the causal mask crosses the tile; BY_RANK
   int parts;
 };
+enum { BY_ROWS = 1, BY_RANK = 2 };
+
+// Blocks by the length of their walks, longest first, where ranges of tokens say it (of one set, for all heads alike): what the host
+// cannot know, every workgroup finds out for itself.  weight[i] of block i (n <= MAX_RANKED) -> order[rank].
+constexpr int MAX_RANKED = 512;
+struct Ranks {
+  int weight[MAX_RANKED];
+  unsigned short order[MAX_RANKED];
+};
+__device__ __forceinline__ void rank_blocks(Ranks& r, int n, int threads) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += threads) {
+    const int w = r.weight[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += r.weight[j] > w || (r.weight[j] == w && j > i);
+    r.order[rank] = (unsigned short)i;
+  }
+  __syncthreads();
+}
+// of bm query rows each: by the hull of a block's first and last row
+__device__ __forceinline__ void rank_rows(Ranks& ranks, const a2d_tile_desc& d, const ScoreRules& r, int rows, int bm, int threads) {
+  const int n = (rows + bm - 1) / bm;
+  for (int i = threadIdx.x; i < n; i += threads) {
+    const Run a = visible_run(d, r, 0, i * bm), b = visible_run(d, r, 0, min((i + 1) * bm, rows) - 1);
+    const int lo = min(a.n ? a.lo : INT_MAX, b.n ? b.lo : INT_MAX), hi = max(a.lo + a.n, b.lo + b.n);
+    ranks.weight[i] = lo < hi ? hi - lo : 0;
+  }
+  rank_blocks(ranks, n, threads);
+}
 
 // what a wavefront knows of its NT tiles of 16 rows; of the lane's row in each
 template <int NT>
@@ -65,14 +94,15 @@ __device__ __forceinline__ void look_up_rows(RowState<NT>& rs, const a2d_tile_de
   rs.all_hi = over16(all_hi, least);
 }
 
-// A tile that the causal mask crosses (by ranges: not known here)
-inline bool blocks_by_size(const a2d_tile_desc& d, const ScoreRules& r) {
-  return d.causal && !r.ranges && r.row_shift < d.nkv && (int64_t)d.nq + r.row_shift > 0 && d.nq > 1;
+// how the blocks of a tile are ordered, of which there are n a head
+inline int blocks_by_size(const a2d_tile_desc& d, const ScoreRules& r, int n) {
+  if (r.ranges) return r.heads_per_set == d.heads && n > 1 && n <= MAX_RANKED ? BY_RANK : 0;
+  return d.causal && r.row_shift < d.nkv && (int64_t)d.nq + r.row_shift > 0 && d.nq > 1 ? BY_ROWS : 0;
 }
 // for workgroups of bm rows
 inline RowMap row_map(const a2d_tile_desc& d, const ScoreRules& r, int bm, int parts) {
   const bool packed = r.group > 1 && d.nq < bm;
-  return RowMap{packed ? 1 : r.group, packed ? r.group * d.nq : d.nq, !packed && blocks_by_size(d, r), parts};
+  return RowMap{packed ? 1 : r.group, packed ? r.group * d.nq : d.nq, packed ? 0 : blocks_by_size(d, r, (d.nq + bm - 1) / bm), parts};
 }
 
 // what the dQ kernel leaves of the rows, [heads][padded]: padded = nq up to the next multiple of 64
