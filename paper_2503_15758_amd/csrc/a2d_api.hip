@@ -866,21 +866,9 @@ a2d_status a2d_partial_bwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, c
   A2D_TRY(hip_result(launch(a2d::PREPARE, dd, r, plan, Q, K, V, O, dO, lse, workspace, dq, dk, dv, s), who));
   a2d::trace_mark(s);
   A2D_TRY(hip_result(launch(a2d::LAUNCH, dd, r, plan, Q, K, V, O, dO, lse, workspace, dq, dk, dv, s), who));
-  const a2d::PartSet sets[3] = {{dk, static_cast<float*>(dK), nk, plan.parts_kv, 0},
-                                {dv, static_cast<float*>(dV), nk, plan.parts_kv, 0},
-                                {dq, static_cast<float*>(dQ), nq, plan.parts_q, r.acc}};
-  if (r.norm && !f32) {
-    for (const a2d::PartSet& x : sets) {
-      if (x.k == 1) continue;
-      a2d::SumPtrs p;
-      memset(&p, 0, sizeof(p));
-      for (int z = 0; z < x.k; ++z) p.p[z] = x.p + z * x.n;
-      A2D_TRY(hip_result(a2d::launch_fix_bwd(x.k, x.n, 1, A2D_BF16, p, a2d::plain_out(), x.out, s), who));
-    }
-    return A2D_OK;
-  }
+  const a2d::PartSet sets[3] = {{dk, dK, nk, plan.parts_kv, 0}, {dv, dV, nk, plan.parts_kv, 0}, {dq, dQ, nq, plan.parts_q, r.acc}};
   const int at = plan.parts_kv > 1 ? 0 : 2, n = (plan.parts_kv > 1 ? 2 : 0) + (plan.parts_q > 1 ? 1 : 0);
-  return n ? hip_result(a2d::launch_sum_parts(n, sets + at, s), who) : A2D_OK;
+  return n ? hip_result(a2d::launch_sum_parts(n, sets + at, s, r.norm && !f32), who) : A2D_OK;
 }
 
 a2d_status a2d_document_ranges(int32_t documents, const int32_t* starts, const int32_t* prefix, int causal, int64_t first,

@@ -718,28 +718,41 @@ size_t scored_bwd_bytes(const a2d_tile_desc& d) {
   return 16 * n + n / 32 * sizeof(RowTile);
 }
 
+// As plan_scored_fwd: steps in us, fitted to 40 calls timed with each number of key lanes and parts; one launch sums up every result that is
+// split.  What they choose between, measured: 4096 x 4096, 32 / 8 heads of 128, causal under a cap: dK / dV in four parts 533 us, in
+// one 1179 (the 128 workgroups of one part leave half of the chip idle and differ in length); 2999 x 2999, 12 / 4 of 80 in four documents: in eight
+// 87, in one 267; 8192 x 8192, 16 of 128 in documents: in one 339, in four 400 (the partials' traffic).
 ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap_q, int cap_kv) {
+  const bool documents = r.ranges && r.heads_per_set == d.heads;
   const WalkKeys w = walk_keys(d, r);
-  const double most = w.most, mean = w.mean, rows_mean = (double)d.nq * r.group * (mean / d.nkv);
-  ScoredBwdPlan best{1, 1, 1};
-  double least = 0;
-  const double part_q = (double)d.heads * d.nq * d.hdim * 8 / 4.5e6, part_kv = (double)(d.heads / r.group) * d.nkv * d.hdim * 16 / 4.5e6;
-  for (int lanes = 1; lanes <= 2; ++lanes) {
-    const int bm = 256 / lanes;
-    const WalkModel m{(int64_t)d.heads * ((d.nq + bm - 1) / bm), cus, mean / (64 * lanes) + 0.2, most / (64 * lanes) + 0.2,
-                      lanes == 1 ? 2.6 : 2.9, 5.0, 0, 0, nullptr, 0, 0.5};
-    double t;
-    const int parts = best_parts(m, cap_q, 4.5, part_q, &t);
-    if (lanes == 1 || t < 0.98 * least) {
-      least = t;
-      best.lanes = lanes;
-      best.parts_q = parts;
+  const int rules = (r.cap != 0.f) + (r.slopes != nullptr);
+  const double most = documents ? 0.65 * w.most : w.most, mean = documents ? 0.35 * w.mean : w.mean, by_head = d.hdim / 128.0;
+  const double all_rows = (double)d.nq * r.group, rows_most = documents ? 0.65 * all_rows : all_rows, rows_mean = all_rows * (mean / d.nkv);
+  const double part_q = (double)d.heads * d.nq * d.hdim * 8 / 6e6, part_kv = (double)(d.heads / r.group) * d.nkv * d.hdim * 16 / 6e6;
+  const auto plan = [&](bool split, double* time) {
+    ScoredBwdPlan p{1, 1, 1};
+    double t, least = 0;
+    for (int lanes = 1; lanes <= 2; ++lanes) {
+      const int bm = 256 / lanes;
+      const double step = lanes == 1 ? 0.4 + 1.4 * by_head + 0.2 * rules : 0.75 + 1.4 * by_head + 0.1 * rules;
+      const WalkModel m{(int64_t)d.heads * ((d.nq + bm - 1) / bm), cus, mean / (64 * lanes) + 0.2, most / (64 * lanes) + 0.2,
+                        step, lanes == 1 ? 3.5 : 5.0, 0, 0, nullptr, 0, 0.0};
+      const int parts = best_parts(m, split ? cap_q : 1, 0, part_q, &t);
+      if (lanes == 1 || t < least) {
+        least = t;
+        p.lanes = lanes;
+        p.parts_q = parts;
+      }
     }
-  }
-  const WalkModel m{(int64_t)(d.heads / r.group) * ((d.nkv + WK_KEYS - 1) / WK_KEYS), cus, rows_mean / WK_ROWS + 0.2,
-                    (double)d.nq * r.group / WK_ROWS + 0.2, 3.4, 5.0, 0, 0, nullptr, 0, 0.5};
-  best.parts_kv = best_parts(m, cap_kv, 4.5, part_kv, nullptr);
-  return best;
+    const WalkModel m{(int64_t)(d.heads / r.group) * ((d.nkv + WK_KEYS - 1) / WK_KEYS), cus, rows_mean / WK_ROWS + 0.2,
+                      rows_most / WK_ROWS + 0.2, 1.1 + by_head + 0.5 * rules, 7.5, 0, 0, nullptr, 0, 0.0};
+    p.parts_kv = best_parts(m, split ? cap_kv : 1, 0, part_kv, &t);
+    *time = least + t + (split ? 6.5 : 0);
+    return p;
+  };
+  double whole_us, split_us;
+  const ScoredBwdPlan whole = plan(false, &whole_us), split = plan(true, &split_us);
+  return split_us < whole_us ? split : whole;
 }
 
 hipError_t launch_scored_bwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K,
