@@ -700,8 +700,9 @@ int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0); }
 
 // as cap_of, of dQ, dK or dV of a backward call under score rules: grouped heads over long rows leave half of the chip without dK / dV
 // workgroups, and a partial of theirs is already tens of MiB
+constexpr size_t kScoredParts = (size_t)128 << 20;
 int scored_cap(int64_t floats) {
-  const int64_t n = ((int64_t)128 << 20) / (int64_t)sizeof(float) / floats;
+  const int64_t n = (int64_t)(kScoredParts / sizeof(float)) / floats;
   return n < 1 ? 1 : n > A2D_MAX_PARTS ? A2D_MAX_PARTS : (int)n;
 }
 
@@ -849,26 +850,35 @@ a2d_status a2d_partial_bwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, c
     a2d::trace_mark(s);
     return hip_result(a2d::launch_scored_bwd_generic(dd, r, Q, K, V, O, dO, lse, static_cast<float*>(workspace), dQ, dK, dV, s), who);
   }
-  const int64_t nq = (int64_t)dd.heads * dd.nq * dd.hdim, nk = (int64_t)kv_heads * dd.nkv * dd.hdim;
   int cus = 0;
   A2D_TRY(hip_result(a2d::device_cus(&cus), who));
-  const bool offered = a2d::scratch_offered(), f32 = dd.dtype == A2D_F32;
-  const auto plan_of = f32 ? a2d::plan_scored_bwd_f32 : a2d::plan_scored_bwd;
-  const auto launch = f32 ? a2d::launch_scored_bwd_f32 : a2d::launch_scored_bwd;
-  a2d::ScoredBwdPlan plan = plan_of(dd, r, cus, offered ? scored_cap(nq) : 1, offered ? scored_cap(nk) : 1);
-  const int64_t dq_floats = plan.parts_q > 1 ? plan.parts_q * nq : 0, kv_floats = plan.parts_kv > 1 ? plan.parts_kv * nk : 0;
+  const bool offered = a2d::scratch_offered();
+  if (dd.dtype == A2D_BF16) {
+    a2d::ScoredBwdPlan plan = a2d::plan_scored_bwd(dd, r, cus, offered ? kScoredParts : 0);
+    const size_t bytes = a2d::scored_bwd_scratch(dd, r, plan);
+    void* more = nullptr;
+    if (bytes && !(more = a2d::scratch_get(bytes))) plan = a2d::plan_scored_bwd(dd, r, cus, 0);
+    A2D_TRY(hip_result(a2d::launch_scored_bwd(a2d::PREPARE, dd, r, plan, Q, K, V, O, dO, lse, workspace, more, dQ, dK, dV, s), who));
+    a2d::trace_mark(s);
+    return hip_result(a2d::launch_scored_bwd(a2d::LAUNCH, dd, r, plan, Q, K, V, O, dO, lse, workspace, more, dQ, dK, dV, s), who);
+  }
+  const int64_t nq = (int64_t)dd.heads * dd.nq * dd.hdim, nk = (int64_t)kv_heads * dd.nkv * dd.hdim;
+  a2d::ScoredBwdPlan plan = a2d::plan_scored_bwd_f32(dd, r, cus, offered ? scored_cap(nq) : 1, offered ? scored_cap(nk) : 1);
+  const int64_t dq_floats = plan.q > 1 ? plan.q * nq : 0, kv_floats = plan.kv > 1 ? plan.kv * nk : 0;
   float* more = nullptr;
   if (dq_floats + kv_floats > 0 && !(more = static_cast<float*>(a2d::scratch_get((size_t)(dq_floats + 2 * kv_floats) * sizeof(float)))))
-    plan = plan_of(dd, r, cus, 1, 1);
-  float* const dq = plan.parts_q > 1 ? more : static_cast<float*>(dQ);
-  float* const dk = plan.parts_kv > 1 ? more + dq_floats : static_cast<float*>(dK);
-  float* const dv = plan.parts_kv > 1 ? dk + kv_floats : static_cast<float*>(dV);
-  A2D_TRY(hip_result(launch(a2d::PREPARE, dd, r, plan, Q, K, V, O, dO, lse, workspace, dq, dk, dv, s), who));
+    plan = a2d::plan_scored_bwd_f32(dd, r, cus, 1, 1);
+  float* const dq = plan.q > 1 ? more : static_cast<float*>(dQ);
+  float* const dk = plan.kv > 1 ? more + dq_floats : static_cast<float*>(dK);
+  float* const dv = plan.kv > 1 ? dk + kv_floats : static_cast<float*>(dV);
+  A2D_TRY(hip_result(a2d::launch_scored_bwd_f32(a2d::PREPARE, dd, r, plan, Q, K, V, O, dO, lse, workspace, dq, dk, dv, s), who));
   a2d::trace_mark(s);
-  A2D_TRY(hip_result(launch(a2d::LAUNCH, dd, r, plan, Q, K, V, O, dO, lse, workspace, dq, dk, dv, s), who));
-  const a2d::PartSet sets[3] = {{dk, dK, nk, plan.parts_kv, 0}, {dv, dV, nk, plan.parts_kv, 0}, {dq, dQ, nq, plan.parts_q, r.acc}};
-  const int at = plan.parts_kv > 1 ? 0 : 2, n = (plan.parts_kv > 1 ? 2 : 0) + (plan.parts_q > 1 ? 1 : 0);
-  return n ? hip_result(a2d::launch_sum_parts(n, sets + at, s, r.norm && !f32), who) : A2D_OK;
+  A2D_TRY(hip_result(a2d::launch_scored_bwd_f32(a2d::LAUNCH, dd, r, plan, Q, K, V, O, dO, lse, workspace, dq, dk, dv, s), who));
+  const a2d::PartSet sets[3] = {{dk, static_cast<float*>(dK), nk, plan.kv, 0},
+                                {dv, static_cast<float*>(dV), nk, plan.kv, 0},
+                                {dq, static_cast<float*>(dQ), nq, plan.q, r.acc}};
+  const int at = plan.kv > 1 ? 0 : 2, n = (plan.kv > 1 ? 2 : 0) + (plan.q > 1 ? 1 : 0);
+  return n ? hip_result(a2d::launch_sum_parts(n, sets + at, s), who) : A2D_OK;
 }
 
 a2d_status a2d_document_ranges(int32_t documents, const int32_t* starts, const int32_t* prefix, int causal, int64_t first,

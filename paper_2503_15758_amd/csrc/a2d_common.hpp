@@ -354,15 +354,14 @@ struct SumSet {
   a2d_layout lo;
 };
 hipError_t launch_sum_grid(int nsets, const SumSet* sets, int hdim, int out_dtype, hipStream_t s);
-// out[i] (+)= sum of k partials of n floats that follow one another, up to three sets in one launch; rounded: out is bf16 and
-// not added to
+// out[i] (+)= sum of k partials of n floats that follow one another, up to three sets in one launch
 struct PartSet {
   const float* p;
-  void* out;
+  float* out;
   int64_t n;
   int k, add;
 };
-hipError_t launch_sum_parts(int nsets, const PartSet* sets, hipStream_t s, bool rounded = false);
+hipError_t launch_sum_parts(int nsets, const PartSet* sets, hipStream_t s);
 
 hipError_t launch_fix(int k, int64_t rows, int hdim, int out_dtype, const FixPtrs& p, const OutMap& om, void* O,
                       float* lse, hipStream_t s);

@@ -415,14 +415,13 @@ __global__ __launch_bounds__(256) void sum_grid_kernel(SumSets a, int hv) {
 struct PartSets {
   PartSet s[3];
 };
-template <bool ROUNDED>
 __global__ __launch_bounds__(256) void sum_parts_kernel(PartSets a) {
   const PartSet& s = a.s[blockIdx.y];
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n4 = s.n / 4;
   if (i >= n4) return;
   const f32x4* p = reinterpret_cast<const f32x4*>(s.p) + i;
-  f32x4* out = static_cast<f32x4*>(s.out) + i;
-  f32x4 acc = !ROUNDED && s.add ? *out : f32x4{0.f, 0.f, 0.f, 0.f};
+  f32x4* out = reinterpret_cast<f32x4*>(s.out) + i;
+  f32x4 acc = s.add ? *out : f32x4{0.f, 0.f, 0.f, 0.f};
   int z = 0;
   for (; z + 4 <= s.k; z += 4) {
     f32x4 v[4];
@@ -437,8 +436,7 @@ __global__ __launch_bounds__(256) void sum_parts_kernel(PartSets a) {
     const f32x4 v = p[z * n4];
     acc[0] += v[0]; acc[1] += v[1]; acc[2] += v[2]; acc[3] += v[3];
   }
-  if constexpr (ROUNDED) static_cast<bf16x4*>(s.out)[i] = bf16x4{(bf16_t)acc[0], (bf16_t)acc[1], (bf16_t)acc[2], (bf16_t)acc[3]};
-  else *out = acc;
+  *out = acc;
 }
 
 // (go(std::integral_constant<int, CPT>, first group, grid): launches)
@@ -608,16 +606,14 @@ hipError_t launch_sum_grid(int nsets, const SumSet* sets, int hdim, int out_dtyp
   return hipGetLastError();
 }
 
-hipError_t launch_sum_parts(int nsets, const PartSet* sets, hipStream_t s, bool rounded) {
+hipError_t launch_sum_parts(int nsets, const PartSet* sets, hipStream_t s) {
   PartSets a;
   int64_t most = 0;
   for (int x = 0; x < 3; ++x) {
     a.s[x] = sets[x < nsets ? x : 0];
     if (a.s[x].n > most) most = a.s[x].n;
   }
-  const dim3 grid((unsigned)((most / 4 + 255) / 256), nsets);
-  if (rounded) A2D_LAUNCH(sum_parts_kernel<true>, grid, dim3(256), 0, s, a);
-  else A2D_LAUNCH(sum_parts_kernel<false>, grid, dim3(256), 0, s, a);
+  A2D_LAUNCH(sum_parts_kernel, dim3((unsigned)((most / 4 + 255) / 256), nsets), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -104,17 +104,20 @@ ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus,
 hipError_t launch_scored_fwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, const void* Q, const void* K,
                              const void* V, float* out0, float* out1, float* out2, const FwdInput& in, hipStream_t s);
 
-// bf16 backward (a2d_scored_bwd.hip).  ws: scored_bwd_bytes(d); parts > 1: dQ, or dK and dV, are partials [parts][heads][rows][H] in fp32,
-// to be summed; else r.norm writes bf16 and r.acc adds to dQ.
+// bf16 backward (a2d_scored_bwd.hip).  ws: scored_bwd_bytes(d); more: scored_bwd_scratch(...) bytes for the fp32 partials of blocks that
+// workgroups share.  r.norm writes bf16, r.acc adds to dQ.
 struct ScoredBwdPlan {
-  int lanes, parts_q, parts_kv;                      // key lanes of a dQ workgroup (1: 256 rows, 2: 128); workgroups that share a walk
+  int lanes;             // key lanes of a dQ workgroup (1: 256 rows, 2: 128)
+  int q, kv;             // fp32: workgroups that share a walk; bf16: workgroups of a query head for dQ, of a key/value head for dK / dV
+  bool share_q, share_kv;  // bf16: shared out in proportion to the blocks' walks (Cut in a2d_scored_rows.hpp); else evenly
 };
 constexpr int SCORED_MOST_BITS = 16384;              // bytes: a bit a step of 64 rows of each query head of a group, group * nq <= 2^22
 size_t scored_bwd_bytes(const a2d_tile_desc& d);
-ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap_q, int cap_kv);
+ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, size_t most_bytes);  // most_bytes: of a result's partials
+size_t scored_bwd_scratch(const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan);
 hipError_t launch_scored_bwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K,
-                             const void* V, const void* O, const void* dO, const float* lse, void* ws, float* dQ, float* dK, float* dV,
-                             hipStream_t s);
+                             const void* V, const void* O, const void* dO, const float* lse, void* ws, void* more, void* dQ, void* dK,
+                             void* dV, hipStream_t s);
 
 // the same for fp32 (a2d_scored_f32.hip; plan.form: 1 or 2 tiles of 16 rows a workgroup)
 ScoredPlan plan_scored_fwd_f32(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap);

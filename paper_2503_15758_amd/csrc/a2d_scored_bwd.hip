@@ -51,23 +51,25 @@ __host__ __device__ constexpr int dq_ring(int hd) { return hd == 64 ? 4 : 2; }
 // KL = 1: 256 rows, KL = 2: 128 rows in two key lanes (see scored_fwd_kernel)
 template <int HR, int KL, bool CAP, bool BIAS>
 __device__ __forceinline__ void scored_dq_rows(
-    int id, char* const lds_all, int* const hull, const Ranks& ranks, const a2d_tile_desc& d, const ScoreRules& r, int by_size, int parts,
+    int id, char* const lds_all, int* const hull, Shares& shares, const a2d_tile_desc& d, const ScoreRules& r, const Cut& cut, int in_order,
     const RowTable& tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V,
-    const bf16_t* __restrict__ O, const bf16_t* __restrict__ dO, const float* __restrict__ lse, float* dQ, int rounded) {
+    const bf16_t* __restrict__ O, const bf16_t* __restrict__ dO, const float* __restrict__ lse, void* dQ, float* __restrict__ more,
+    int2* __restrict__ table) {
   constexpr int WAVES = 8, RW = WAVES / KL, BM = 32 * RW, kThreads = 64 * RW;
   constexpr int HD = padded_head(HR), H = HR, KS = HD / 32, HT = HR / 16, DQ_BUF = dq_buf(HD), RING = dq_ring(HD);
   const int kl = KL == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads);
   char* const lds = lds_all + kl * (2 * DQ_BUF);
   const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  const int nqb = (d.nq + BM - 1) / BM;
-  int unit, blk;
-  if (!xcd_map(id, d.heads / r.group * parts, r.group * nqb, by_size != 0, unit, blk, kXcdCus)) return;
-  const Split up = split_by(unit, parts);
-  const int kvh = up.q, part = up.r;
-  const Split in_group = query_head(blk, r.group, nqb, by_size != 0);
+  int kvh, at_unit;
+  if (!xcd_map(id, d.heads / r.group, r.group * cut.units, in_order, kvh, at_unit, kXcdCus)) return;
+  const Split in_group = query_head(at_unit, r.group, cut.units, in_order);
   const int head = kvh * r.group + in_group.r;
   // longest walks first, as far as they are known (late rows)
-  const int q0 = (by_size == BY_RANK ? __builtin_amdgcn_readfirstlane((int)ranks.order[in_group.q]) : nqb - 1 - in_group.q) * BM;
+  if (cut.parts == 0) weigh_rows(shares.ranks, d, r, d.nq, BM, 512);
+  const Share mine = cut.parts == 0 ? share_out(shares, cut, in_group.q) : share_evenly(cut, in_group.q, true);
+  if (mine.parts == 0) return;
+  const int q0 = mine.block * BM, part = mine.part, parts = mine.parts;
+  if (table && head == 0 && part == 0 && threadIdx.x == 0) table[mine.block] = int2{mine.slot, parts};
   const int tid = (int)threadIdx.x - kl * kThreads;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, grp = lane >> 4;
   Q += (int64_t)head * d.lq.head;
@@ -298,23 +300,22 @@ __device__ __forceinline__ void scored_dq_rows(
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     const int row = w0 + 16 * q;
-    const int64_t at = (((int64_t)part * d.heads + head) * d.nq + row) * H;
-    if (rounded) store_acc16(reinterpret_cast<bf16_t*>(dQ) + at, H, d.nq - row, area, dq, q, lane, d.scale);
-    else store_acc16(dQ + at, H, d.nq - row, area, dq, q, lane, d.scale, parts == 1 && r.acc != 0);
+    const int64_t at = ((int64_t)head * d.nq + row) * H;
+    if (parts > 1) store_acc16(more + (((int64_t)head * cut.units + mine.slot + part) * BM + row - q0) * H, H, d.nq - row, area, dq, q, lane, d.scale);
+    else if (r.norm) store_acc16(static_cast<bf16_t*>(dQ) + at, H, d.nq - row, area, dq, q, lane, d.scale);
+    else store_acc16(static_cast<float*>(dQ) + at, H, d.nq - row, area, dq, q, lane, d.scale, r.acc != 0);
   }
 }
 
 template <int HR, int KL, bool CAP, bool BIAS>
 __global__ __launch_bounds__(512, 1) void scored_dq_kernel(
-    a2d_tile_desc d, ScoreRules r, int by_size, int parts, RowTable tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
+    a2d_tile_desc d, ScoreRules r, Cut cut, int in_order, RowTable tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
     const bf16_t* __restrict__ V, const bf16_t* __restrict__ O, const bf16_t* __restrict__ dO, const float* __restrict__ lse,
-    float* dQ, int rounded) {
+    void* dQ, float* __restrict__ more, int2* __restrict__ table) {
   extern __shared__ __attribute__((aligned(1024))) char lds_all[];
   __shared__ int hull[16];
-  __shared__ Ranks ranks;
-  constexpr int BM = 256 / KL;
-  if (by_size == BY_RANK) rank_rows(ranks, d, r, d.nq, BM, 512);
-  scored_dq_rows<HR, KL, CAP, BIAS>(blockIdx.x, lds_all, hull, ranks, d, r, by_size, parts, tab, Q, K, V, O, dO, lse, dQ, rounded);
+  __shared__ Shares shares;
+  scored_dq_rows<HR, KL, CAP, BIAS>(blockIdx.x, lds_all, hull, shares, d, r, cut, in_order, tab, Q, K, V, O, dO, lse, dQ, more, table);
 }
 
 // --------------------------------------------------------------------------------------------- dK, dV
@@ -334,22 +335,43 @@ __host__ __device__ constexpr int wk_bits(int hd) {
 __host__ __device__ constexpr int wk_park(int hd) { return hd == 128 ? 1 : 0; }
 __host__ __device__ constexpr int wk_lds(int hd) { return wk_bits(hd) + SCORED_MOST_BITS + wk_park(hd) * 8 * 4 * BLOCK; }
 
+// weights of the key blocks (the same for all heads): row tiles that see one, +1 at the first block of a tile's hull, -1 behind its last, summed up
+__device__ __forceinline__ void weigh_keys(Ranks& ranks, const ScoreRules& r, const Cut& cut, const RowTable& tab) {
+  const int tid = threadIdx.x;
+  for (int i = tid; i < cut.blocks; i += WK_THREADS) ranks.weight[i] = 0;
+  __syncthreads();
+  for (int i = tid; i < tab.padded / 32; i += WK_THREADS) {
+    const int lo = tab.tiles[i].lo, hi = tab.tiles[i].hi;
+    if (lo >= hi) continue;
+    atomicAdd(&ranks.weight[lo / WK_KEYS], r.group);
+    if ((hi - 1) / WK_KEYS + 1 < cut.blocks) atomicAdd(&ranks.weight[(hi - 1) / WK_KEYS + 1], -r.group);
+  }
+  __syncthreads();
+  int sum = 0;
+  if (tid < cut.blocks)
+    for (int j = 0; j <= tid; ++j) sum += ranks.weight[j];
+  __syncthreads();
+  if (tid < cut.blocks) ranks.weight[tid] = sum;
+}
+
 template <int HR, bool CAP, bool BIAS>
 __device__ __forceinline__ void scored_dkdv_keys(
-    int id, char* const lds, const Ranks& ranks, const a2d_tile_desc& d, const ScoreRules& r, int by_size, int parts, const RowTable& tab,
+    int id, char* const lds, Shares& shares, const a2d_tile_desc& d, const ScoreRules& r, const Cut& cut, int in_order, const RowTable& tab,
     const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
-    float* __restrict__ dK, float* __restrict__ dV, int rounded) {
+    void* __restrict__ dK, void* __restrict__ dV, float* __restrict__ more, int2* __restrict__ table) {
   const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   constexpr int HD = padded_head(HR), H = HR, TILE = wk_tile(HD), BUF = 2 * TILE;
   constexpr int KS = HD / 32, HT = HR / 16;
   constexpr bool TIGHT = HD == 128;                  // registers (see dkdv_wide)
-  const int kv_heads = d.heads / r.group, nkb = (d.nkv + WK_KEYS - 1) / WK_KEYS;
-  int unit, blk;
-  if (!xcd_map(id, kv_heads * parts, nkb, by_size != 0, unit, blk)) return;
-  if (by_size == BY_RANK) blk = __builtin_amdgcn_readfirstlane((int)ranks.order[blk]);
-  const Split up = split_by(unit, parts);
-  const int head = up.q, part = up.r, qh0 = head * r.group;
-  const int k0 = blk * WK_KEYS;
+  const int kv_heads = d.heads / r.group;
+  int head, at_unit;
+  if (!xcd_map(id, kv_heads, cut.units, in_order, head, at_unit)) return;
+  if (cut.parts == 0) weigh_keys(shares.ranks, r, cut, tab);
+  const Share mine = cut.parts == 0 ? share_out(shares, cut, at_unit) : share_evenly(cut, at_unit, false);
+  if (mine.parts == 0) return;
+  const int part = mine.part, parts = mine.parts, qh0 = head * r.group;
+  const int k0 = mine.block * WK_KEYS;
+  if (table && head == 0 && part == 0 && threadIdx.x == 0) table[mine.block] = int2{mine.slot, parts};
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int l16 = lane & 15, grp = lane >> 4;
   Q += (int64_t)qh0 * d.lq.head;
@@ -644,70 +666,128 @@ __device__ __forceinline__ void scored_dkdv_keys(
 #pragma unroll
   for (int kt = 0; kt < 2; ++kt) {
     const int first = wk + 16 * kt, n = d.nkv - first;
-    const int64_t at = (((int64_t)part * kv_heads + head) * d.nkv + first) * H;
-    if (rounded) {
-      store_acc16(reinterpret_cast<bf16_t*>(dV) + at, H, n, area, dv, kt, ln, 1.0f);
-      store_acc16(reinterpret_cast<bf16_t*>(dK) + at, H, n, area, dk, kt, ln, d.scale);
+    const int64_t at = ((int64_t)head * d.nkv + first) * H;
+    if (parts > 1) {
+      float* const to = more + (((int64_t)head * cut.units + mine.slot + part) * WK_KEYS + first - k0) * H;
+      store_acc16(to + (int64_t)kv_heads * cut.units * WK_KEYS * H, H, n, area, dv, kt, ln, 1.0f);
+      store_acc16(to, H, n, area, dk, kt, ln, d.scale);
+    } else if (r.norm) {
+      store_acc16(static_cast<bf16_t*>(dV) + at, H, n, area, dv, kt, ln, 1.0f);
+      store_acc16(static_cast<bf16_t*>(dK) + at, H, n, area, dk, kt, ln, d.scale);
     } else {
-      store_acc16(dV + at, H, n, area, dv, kt, ln, 1.0f);
-      store_acc16(dK + at, H, n, area, dk, kt, ln, d.scale);
+      store_acc16(static_cast<float*>(dV) + at, H, n, area, dv, kt, ln, 1.0f);
+      store_acc16(static_cast<float*>(dK) + at, H, n, area, dk, kt, ln, d.scale);
     }
   }
 }
 
 template <int HR, bool CAP, bool BIAS>
 __global__ __launch_bounds__(WK_THREADS) void scored_dkdv_kernel(
-    a2d_tile_desc d, ScoreRules r, int by_size, int parts, RowTable tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
-    const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO, float* __restrict__ dK, float* __restrict__ dV, int rounded) {
+    a2d_tile_desc d, ScoreRules r, Cut cut, int in_order, RowTable tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
+    const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO, void* __restrict__ dK, void* __restrict__ dV, float* __restrict__ more,
+    int2* __restrict__ table) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  __shared__ Ranks ranks;
-  const int nkb = (d.nkv + WK_KEYS - 1) / WK_KEYS;
-  if (by_size == BY_RANK) {
-    // (the same for all heads) row tiles that see a block: +1 at the first block of a tile's hull, -1 behind its last, summed up
-    for (int i = threadIdx.x; i < nkb; i += WK_THREADS) ranks.weight[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < tab.padded / 32; i += WK_THREADS) {
-      const int lo = tab.tiles[i].lo, hi = tab.tiles[i].hi;
-      if (lo >= hi) continue;
-      atomicAdd(&ranks.weight[lo / WK_KEYS], 1);
-      if ((hi - 1) / WK_KEYS + 1 < nkb) atomicAdd(&ranks.weight[(hi - 1) / WK_KEYS + 1], -1);
-    }
-    __syncthreads();
-    int sum = 0;
-    if ((int)threadIdx.x < nkb)
-      for (int j = 0; j <= (int)threadIdx.x; ++j) sum += ranks.weight[j];
-    __syncthreads();
-    if ((int)threadIdx.x < nkb) ranks.weight[threadIdx.x] = sum;
-    rank_blocks(ranks, nkb, WK_THREADS);
-  }
-  scored_dkdv_keys<HR, CAP, BIAS>(blockIdx.x, lds, ranks, d, r, by_size, parts, tab, Q, K, V, dO, dK, dV, rounded);
+  __shared__ Shares shares;
+  scored_dkdv_keys<HR, CAP, BIAS>(blockIdx.x, lds, shares, d, r, cut, in_order, tab, Q, K, V, dO, dK, dV, more, table);
 }
 static_assert(MAX_RANKED <= WK_THREADS, "a thread a block");
 
+// ---- sums of the partials, blocks of one part left out (theirs are written already): four floats a thread, the parts in their order
+struct SumOf {
+  const float* p;        // [heads][cut.units][bm][hdim]
+  void* out;             // [heads][rows][hdim]
+  const int2* table;     // shared out: slot and parts of each block
+  Cut cut;
+  int heads, rows, bm;
+};
+struct SumsOf {
+  SumOf s[3];
+};
+template <bool ROUNDED>
+__global__ __launch_bounds__(256) void scored_sum_kernel(SumsOf sums, int hdim, int add) {
+  const SumOf& s = sums.s[blockIdx.z];               // (dK, dV, dQ: the last is added to)
+  const int per = s.bm * hdim / 1024;                // workgroups a block: bm is 128 or 256, hdim a multiple of 16
+  if ((int)blockIdx.x >= s.cut.blocks * per || (int)blockIdx.y >= s.heads) return;
+  const int block = blockIdx.x / per, in = (blockIdx.x - block * per) * 1024 + 4 * threadIdx.x;
+  const int2 at = s.table ? s.table[block] : int2{block * s.cut.parts, s.cut.parts};
+  const int64_t to = ((int64_t)blockIdx.y * s.rows + (int64_t)block * s.bm) * hdim + in;
+  if (at.y == 1 || in >= (s.rows - block * s.bm) * hdim) return;
+  const int64_t part = (int64_t)s.bm * hdim;
+  const float* p = s.p + ((int64_t)blockIdx.y * s.cut.units + at.x) * part + in;
+  f32x4 acc{0.f, 0.f, 0.f, 0.f};
+  if (!ROUNDED && add && blockIdx.z == 2) acc = *reinterpret_cast<const f32x4*>(static_cast<float*>(s.out) + to);
+  int z = 0;
+  for (; z + 4 <= at.y; z += 4) {
+    f32x4 v[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) v[x] = *reinterpret_cast<const f32x4*>(p + (z + x) * part);
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += v[x][e];
+  }
+  for (; z < at.y; ++z) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p + z * part);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += v[e];
+  }
+  if constexpr (ROUNDED) *reinterpret_cast<bf16x4*>(static_cast<bf16_t*>(s.out) + to) = bf16x4{(bf16_t)acc[0], (bf16_t)acc[1], (bf16_t)acc[2], (bf16_t)acc[3]};
+  else *reinterpret_cast<f32x4*>(static_cast<float*>(s.out) + to) = acc;
+}
+
+constexpr int LEAST_Q = 1, LEAST_KV = 2;             // a step: 64 keys; two tiles of 32 rows
+// in_order: heaviest blocks first over all heads (see xcd_map)
+Cut cut_of(const a2d_tile_desc& d, const ScoreRules& r, int n, int units, bool share, int least, int* in_order) {
+  *in_order = share || blocks_by_size(d, r, n) == BY_ROWS;
+  return share ? Cut{n, units, 0, least} : Cut{n, units / n * n, units / n, least};
+}
+struct BwdCuts {
+  Cut q, kv;
+  int bm, q_in_order, kv_in_order;
+  int64_t q_floats, kv_floats;                       // of partials, each result's
+  BwdCuts(const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan) : bm(256 / plan.lanes) {
+    q = cut_of(d, r, (d.nq + bm - 1) / bm, plan.q, plan.share_q, LEAST_Q, &q_in_order);
+    kv = cut_of(d, r, (d.nkv + WK_KEYS - 1) / WK_KEYS, plan.kv, plan.share_kv, LEAST_KV, &kv_in_order);
+    q_floats = q.units > q.blocks ? (int64_t)d.heads * q.units * bm * d.hdim : 0;
+    kv_floats = kv.units > kv.blocks ? (int64_t)(d.heads / r.group) * kv.units * WK_KEYS * d.hdim : 0;
+  }
+};
+
 template <int HR, bool CAP, bool BIAS>
 hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K, const void* V,
-              const void* O, const void* dO, const float* lse, void* ws, float* dQ, float* dK, float* dV, hipStream_t s) {
+              const void* O, const void* dO, const float* lse, void* ws, void* more, void* dQ, void* dK, void* dV, hipStream_t s) {
   constexpr int HD = padded_head(HR);
   const RowTable tab = row_table(d, ws);
+  const BwdCuts c(d, r, plan);
   const int kvh = d.heads / r.group, dq_bytes = dq_launch_lds(HD, plan.lanes);
   const int words = (tab.padded / WK_ROWS * r.group + 63) / 64, wk_bytes = wk_park(HD) ? wk_lds(HD) : wk_bits(HD) + 8 * words;
+  float* const q_more = static_cast<float*>(more);
+  float* const kv_more = q_more + c.q_floats;
+  int2* const q_table = reinterpret_cast<int2*>(kv_more + 2 * c.kv_floats);
+  int2* const kv_table = q_table + c.q.blocks;
+  const bool q_shared = c.q_floats && c.q.parts == 0, kv_shared = c.kv_floats && c.kv.parts == 0;
   const auto dq = [&](auto* kernel) {
     if (ph == PREPARE) return ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), dq_bytes);
-    const int bm = plan.lanes == 2 ? 128 : 256;
-    const int nqb = (d.nq + bm - 1) / bm, by_size = blocks_by_size(d, r, nqb);
-    A2D_LAUNCH(kernel, dim3(xcd_grid(kvh * plan.parts_q, r.group * nqb)), dim3(512), dq_bytes, s, d, r, by_size,
-               plan.parts_q, tab, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, (const bf16_t*)O, (const bf16_t*)dO, lse, dQ,
-               (int)(r.norm && plan.parts_q == 1));
+    A2D_LAUNCH(kernel, dim3(xcd_grid(kvh, r.group * c.q.units)), dim3(512), dq_bytes, s, d, r, c.q, c.q_in_order, tab, (const bf16_t*)Q,
+               (const bf16_t*)K, (const bf16_t*)V, (const bf16_t*)O, (const bf16_t*)dO, lse, dQ, q_more, q_shared ? q_table : nullptr);
     return hipGetLastError();
   };
   hipError_t e = plan.lanes == 2 ? dq(scored_dq_kernel<HR, 2, CAP, BIAS>) : dq(scored_dq_kernel<HR, 1, CAP, BIAS>);
   if (e != hipSuccess) return e;
   // (the most a call can ask for: ensure_dynamic_lds is asked once for a kernel)
   if (ph == PREPARE) return ensure_dynamic_lds(reinterpret_cast<const void*>(scored_dkdv_kernel<HR, CAP, BIAS>), wk_lds(HD));
-  const int nkb = (d.nkv + WK_KEYS - 1) / WK_KEYS, by_size = blocks_by_size(d, r, nkb);
-  A2D_LAUNCH((scored_dkdv_kernel<HR, CAP, BIAS>), dim3(xcd_grid(kvh * plan.parts_kv, nkb)), dim3(WK_THREADS),
-             wk_bytes, s, d, r, by_size, plan.parts_kv, tab, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, (const bf16_t*)dO, dK, dV,
-             (int)(r.norm && plan.parts_kv == 1));
+  A2D_LAUNCH((scored_dkdv_kernel<HR, CAP, BIAS>), dim3(xcd_grid(kvh, c.kv.units)), dim3(WK_THREADS), wk_bytes, s, d, r, c.kv, c.kv_in_order, tab,
+             (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, (const bf16_t*)dO, dK, dV, kv_more, kv_shared ? kv_table : nullptr);
+  if ((e = hipGetLastError()) != hipSuccess || c.q_floats + c.kv_floats == 0) return e;
+  Cut none{};
+  const SumsOf sums{{{kv_more, dK, kv_shared ? kv_table : nullptr, c.kv_floats ? c.kv : none, kvh, d.nkv, WK_KEYS},
+                     {kv_more + c.kv_floats, dV, kv_shared ? kv_table : nullptr, c.kv_floats ? c.kv : none, kvh, d.nkv, WK_KEYS},
+                     {q_more, dQ, q_shared ? q_table : nullptr, c.q_floats ? c.q : none, d.heads, d.nq, c.bm}}};
+  int wide = 0;
+  for (const SumOf& x : sums.s) wide = std::max(wide, x.cut.blocks * (x.bm * d.hdim / 1024));
+  const dim3 grid(wide, c.q_floats ? d.heads : kvh, c.q_floats ? 3 : 2);
+  if (r.norm) A2D_LAUNCH(scored_sum_kernel<true>, grid, dim3(256), 0, s, sums, d.hdim, 0);
+  else A2D_LAUNCH(scored_sum_kernel<false>, grid, dim3(256), 0, s, sums, d.hdim, (int)r.acc);
   return hipGetLastError();
 }
 
@@ -718,37 +798,70 @@ size_t scored_bwd_bytes(const a2d_tile_desc& d) {
   return 16 * n + n / 32 * sizeof(RowTile);
 }
 
-// As plan_scored_fwd: steps in us, fitted to 40 calls timed with each number of key lanes and parts; one launch sums up every result that is
-// split.  What they choose between, measured: 4096 x 4096, 32 / 8 heads of 128, causal under a cap: dK / dV in four parts 533 us, in
-// one 1179 (the 128 workgroups of one part leave half of the chip idle and differ in length); 2999 x 2999, 12 / 4 of 80 in four documents: in eight
-// 87, in one 267; 8192 x 8192, 16 of 128 in documents: in one 339, in four 400 (the partials' traffic).
-ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap_q, int cap_kv) {
+size_t scored_bwd_scratch(const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan) {
+  const BwdCuts c(d, r, plan);
+  if (c.q_floats + c.kv_floats == 0) return 0;
+  return (size_t)(c.q_floats + 2 * c.kv_floats) * sizeof(float) + (size_t)(c.q.blocks + c.kv.blocks) * sizeof(int2);
+}
+
+// Every way's time from its turns of the chip, the quickest; one launch sums up every result that is cut.  Steps in us, fitted to 45 calls
+// timed in each of 120 ways.  Documents, which the host cannot see, are taken to have their tokens in the rows and the keys alike and for
+// walks of a third of them.  What it chooses between, measured: 4096 x 4096, 32 / 8 heads of 128, causal under a cap: dK / dV of four
+// parts a block 540 us, of one 1179 (128 workgroups, of any length); 8192 x 8192, 16 of 128 in documents: whole blocks, the longest first 349,
+// in their own order 425, four parts 400; 427 x 5532, 16 / 4 of 64 in documents: dK / dV of three units a block on average, shared out, 43,
+// of four even parts 56; 746 x 895, 4 / 1 of 64: shared out 28, even 22 (finding out the shares takes some 3 us).
+ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, size_t most_bytes) {
+  constexpr double kFindOut = 3.0, kSum = 5.0, kBytes = 6e6;             // us; bytes of partials a us, out and back
   const bool documents = r.ranges && r.heads_per_set == d.heads;
+  const int rules = (r.cap != 0.f) + (r.slopes != nullptr), kvh = d.heads / r.group;
+  const double by_head = d.hdim / 128.0, all_rows = (double)d.nq * r.group, alike = std::min(1.0, (double)d.nkv / d.nq);
   const WalkKeys w = walk_keys(d, r);
-  const int rules = (r.cap != 0.f) + (r.slopes != nullptr);
-  const double most = documents ? 0.65 * w.most : w.most, mean = documents ? 0.35 * w.mean : w.mean, by_head = d.hdim / 128.0;
-  const double all_rows = (double)d.nq * r.group, rows_most = documents ? 0.65 * all_rows : all_rows, rows_mean = all_rows * (mean / d.nkv);
-  const double part_q = (double)d.heads * d.nq * d.hdim * 8 / 6e6, part_kv = (double)(d.heads / r.group) * d.nkv * d.hdim * 16 / 6e6;
-  const auto plan = [&](bool split, double* time) {
-    ScoredBwdPlan p{1, 1, 1};
-    double t, least = 0;
-    for (int lanes = 1; lanes <= 2; ++lanes) {
-      const int bm = 256 / lanes;
-      const double step = lanes == 1 ? 0.4 + 1.4 * by_head + 0.2 * rules : 0.75 + 1.4 * by_head + 0.1 * rules;
-      const WalkModel m{(int64_t)d.heads * ((d.nq + bm - 1) / bm), cus, mean / (64 * lanes) + 0.2, most / (64 * lanes) + 0.2,
-                        step, lanes == 1 ? 3.5 : 5.0, 0, 0, nullptr, 0, 0.0};
-      const int parts = best_parts(m, split ? cap_q : 1, 0, part_q, &t);
-      if (lanes == 1 || t < least) {
-        least = t;
-        p.lanes = lanes;
-        p.parts_q = parts;
+  struct Walks {
+    double mean, most;
+  } keys{w.mean, w.most}, rows{all_rows * (w.mean / d.nkv), all_rows};
+  if (documents) {
+    const double part = std::sqrt(std::min(1.0, (double)d.nq / d.nkv));
+    keys = Walks{0.35 * part * keys.mean, 0.65 * part * keys.most};
+    rows = Walks{0.35 * alike * rows.mean, 0.65 * alike * rows.most};
+  }
+  struct Way {
+    int units;
+    bool share;
+    double us;
+  };
+  // n blocks of `bm` rows or keys of each of `heads` heads, which walk in steps of `of` keys or rows
+  const auto cut = [&](int n, int heads, int bm, int results, Walks walks, int of, double step, double fixed, bool split) {
+    const double mean = walks.mean / of + 0.2, most = walks.most / of + 0.2, unit_us = bm * d.hdim * 8.0 * results / kBytes;
+    const double blind = documents ? 1.2 : 1.0;                          // walks in no order
+    const int64_t room = split ? (int64_t)(most_bytes / ((size_t)heads * bm * d.hdim * sizeof(float))) : 0;
+    const bool uneven = n > 1 && n <= MAX_RANKED && blocks_by_size(d, r, n) != 0;
+    const WalkModel whole{(int64_t)heads * n, cus, mean, most, step, fixed, 0, 0, nullptr, 0, 0.1};
+    Way best{n, false, walk_time(whole, 1) * blind};
+    for (int x = 4; x <= 128; x += x < 8 ? 1 : x < 32 ? 4 : 16) {        // quarters of n
+      const int u = (int)((int64_t)n * x / 4);
+      if (u > n && u > room) break;
+      if (u > n && x % 4 == 0) {
+        const double us = walk_time(whole, x / 4) * blind + (double)heads * u * unit_us;
+        if (us < best.us) best = Way{u, false, us};
+      }
+      if (uneven) {
+        const double each = u > n ? std::max(1.0, n * mean / (u - n)) : most, split_units = u > n ? std::min<double>(u, 0.5 * n + n * mean / each) : 0;
+        const double one = std::min(each, most) * step + fixed + kFindOut;
+        const double even = heads * (n * mean * step + std::max<double>(n, split_units) * (fixed + kFindOut)) / cus + 0.15 * one;
+        const double turns = u > n ? std::ceil(heads * std::min<double>(u - n, n * mean) / cus) : 1;   // of units of that weight
+        const double us = std::max(turns * one, even) + heads * split_units * unit_us;
+        if (us < best.us) best = Way{u, true, us};
       }
     }
-    const WalkModel m{(int64_t)(d.heads / r.group) * ((d.nkv + WK_KEYS - 1) / WK_KEYS), cus, rows_mean / WK_ROWS + 0.2,
-                      rows_most / WK_ROWS + 0.2, 1.1 + by_head + 0.5 * rules, 7.5, 0, 0, nullptr, 0, 0.0};
-    p.parts_kv = best_parts(m, split ? cap_kv : 1, 0, part_kv, &t);
-    *time = least + t + (split ? 6.5 : 0);
-    return p;
+    return best;
+  };
+  const auto plan = [&](bool split, double* us) {
+    const Way one = cut((d.nq + 255) / 256, d.heads, 256, 1, keys, 64, 0.35 + 1.4 * by_head + 0.2 * rules, 3.6, split);
+    const Way two = cut((d.nq + 127) / 128, d.heads, 128, 1, keys, 128, 0.75 + 1.4 * by_head + 0.1 * rules, 5.3, split);
+    const Way kv = cut((d.nkv + WK_KEYS - 1) / WK_KEYS, kvh, WK_KEYS, 2, rows, WK_ROWS, 1.3 + 1.1 * by_head + 0.55 * rules, 7.5, split);
+    const Way& q = two.us < one.us ? two : one;
+    *us = q.us + kv.us + (split ? kSum : 0);
+    return ScoredBwdPlan{two.us < one.us ? 2 : 1, q.units, kv.units, q.share, kv.share};
   };
   double whole_us, split_us;
   const ScoredBwdPlan whole = plan(false, &whole_us), split = plan(true, &split_us);
@@ -756,13 +869,13 @@ ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int c
 }
 
 hipError_t launch_scored_bwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K,
-                             const void* V, const void* O, const void* dO, const float* lse, void* ws, float* dQ, float* dK, float* dV,
-                             hipStream_t s) {
+                             const void* V, const void* O, const void* dO, const float* lse, void* ws, void* more, void* dQ, void* dK,
+                             void* dV, hipStream_t s) {
 #define A2D_RULES(HR)                                                                                                \
-  return r.cap != 0.f ? (r.slopes ? go<HR, true, true>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, dQ, dK, dV, s)       \
-                                  : go<HR, true, false>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, dQ, dK, dV, s))     \
-                      : (r.slopes ? go<HR, false, true>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, dQ, dK, dV, s)      \
-                                  : go<HR, false, false>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, dQ, dK, dV, s))
+  return r.cap != 0.f ? (r.slopes ? go<HR, true, true>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, more, dQ, dK, dV, s)       \
+                                  : go<HR, true, false>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, more, dQ, dK, dV, s))     \
+                      : (r.slopes ? go<HR, false, true>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, more, dQ, dK, dV, s)      \
+                                  : go<HR, false, false>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, more, dQ, dK, dV, s))
   if (d.hdim == 128) { A2D_RULES(128); }
   if (d.hdim == 96) { A2D_RULES(96); }
   if (d.hdim == 80) { A2D_RULES(80); }

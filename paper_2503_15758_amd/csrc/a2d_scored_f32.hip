@@ -515,12 +515,12 @@ hipError_t bwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const Scor
   }
   const RowTable tab = row_table(d, ws);
   const int by_size = blocks_by_size(d, r, 1) != 0, kvh = d.heads / r.group, words = (tab.padded / 32 * r.group + 63) / 64;
-  A2D_LAUNCH((scored_dq_f32_kernel<H>), dim3(xcd_grid(kvh * plan.parts_q, r.group * ((d.nq + 31) / 32))), dim3(64 * KL), lds, s, d, r, by_size,
-             plan.parts_q, tab, (const float*)Q, (const float*)K, (const float*)V, (const float*)O, (const float*)dO, lse, dQ);
+  A2D_LAUNCH((scored_dq_f32_kernel<H>), dim3(xcd_grid(kvh * plan.q, r.group * ((d.nq + 31) / 32))), dim3(64 * KL), lds, s, d, r, by_size,
+             plan.q, tab, (const float*)Q, (const float*)K, (const float*)V, (const float*)O, (const float*)dO, lse, dQ);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  A2D_LAUNCH((scored_dkdv_f32_kernel<H>), dim3(xcd_grid(kvh * plan.parts_kv, (d.nkv + BLK - 1) / BLK)), dim3(64 * KL), lds + 8 * words, s, d, r,
-             by_size, plan.parts_kv, tab, lds, (const float*)Q, (const float*)K, (const float*)V, (const float*)dO, dK, dV);
+  A2D_LAUNCH((scored_dkdv_f32_kernel<H>), dim3(xcd_grid(kvh * plan.kv, (d.nkv + BLK - 1) / BLK)), dim3(64 * KL), lds + 8 * words, s, d, r,
+             by_size, plan.kv, tab, lds, (const float*)Q, (const float*)K, (const float*)V, (const float*)dO, dK, dV);
   return hipGetLastError();
 }
 

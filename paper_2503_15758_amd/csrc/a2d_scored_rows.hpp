@@ -32,15 +32,71 @@ __device__ __forceinline__ void rank_blocks(Ranks& r, int n, int threads) {
   }
   __syncthreads();
 }
-// of bm query rows each: by the hull of a block's first and last row
-__device__ __forceinline__ void rank_rows(Ranks& ranks, const a2d_tile_desc& d, const ScoreRules& r, int rows, int bm, int threads) {
+// of bm query rows each: by the steps of 64 keys in the hull of a block's first and last row
+__device__ __forceinline__ void weigh_rows(Ranks& ranks, const a2d_tile_desc& d, const ScoreRules& r, int rows, int bm, int threads) {
   const int n = (rows + bm - 1) / bm;
   for (int i = threadIdx.x; i < n; i += threads) {
     const Run a = visible_run(d, r, 0, i * bm), b = visible_run(d, r, 0, min((i + 1) * bm, rows) - 1);
     const int lo = min(a.n ? a.lo : INT_MAX, b.n ? b.lo : INT_MAX), hi = max(a.lo + a.n, b.lo + b.n);
-    ranks.weight[i] = lo < hi ? hi - lo : 0;
+    ranks.weight[i] = lo < hi ? (hi - lo + 63) / 64 : 0;
   }
-  rank_blocks(ranks, n, threads);
+}
+__device__ __forceinline__ void rank_rows(Ranks& ranks, const a2d_tile_desc& d, const ScoreRules& r, int rows, int bm, int threads) {
+  weigh_rows(ranks, d, r, rows, bm, threads);
+  rank_blocks(ranks, (rows + bm - 1) / bm, threads);
+}
+
+// How the blocks of a head (row blocks of dQ, key blocks of dK / dV) are cut into units, a workgroup each: uniform, every block into
+// `parts`; or (parts = 0) in proportion to the blocks' walks, which again the workgroups find out for themselves: a causal mask
+// and documents leave walks of any length, and what an even cut of them costs is the traffic of the short ones' partials.
+struct Cut {
+  int blocks, units;     // a head; units: at most, where they are shared out
+  int parts;             // 0: shared out
+  int least;             // weight of the smallest unit that is worth its partial (shared out)
+};
+// a unit: one of the `parts` of a block, whose partials stand from `slot` on (of the head's)
+struct Share {
+  int block, part, parts, slot;
+};
+struct Shares {
+  Ranks ranks;
+  int total, wave[8];
+  Share mine;
+};
+// Unit u where they are shared out: a unit takes `each` of the blocks' weights at most, blocks of at least one unit, so that
+// sum_b max(1, ceil(w_b / each)) <= W / each + blocks <= cut.units; the heaviest blocks' units first.  parts = 0: there are fewer units.
+// ranks.weight is set; 512 threads, cut.blocks <= MAX_RANKED
+__device__ __forceinline__ Share share_out(Shares& s, const Cut& cut, int u) {
+  const int i = threadIdx.x, n = cut.blocks;
+  if (i == 0) {
+    s.total = 0;
+    s.mine = Share{0, 0, 0, 0};
+  }
+  rank_blocks(s.ranks, n, 512);
+  const int block = i < n ? s.ranks.order[i] : 0, w = i < n ? s.ranks.weight[block] : 0;
+  if (w > 0) atomicAdd(&s.total, w);
+  __syncthreads();
+  const int room = cut.units - n, each = room > 0 ? max(cut.least, s.total / room + 1) : INT_MAX;
+  const int parts = i >= n ? 0 : max(1, (int)(((int64_t)w + each - 1) / each));
+  int upto = parts;                                  // of this rank and those before it
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(upto, o, 64);
+    if ((i & 63) >= o) upto += x;
+  }
+  if ((i & 63) == 63) s.wave[i >> 6] = upto;
+  __syncthreads();
+  for (int x = 0; x < i >> 6; ++x) upto += s.wave[x];
+  if (u < upto && u >= upto - parts) s.mine = Share{block, u - (upto - parts), parts, upto - parts};
+  __syncthreads();
+  return Share{__builtin_amdgcn_readfirstlane(s.mine.block), __builtin_amdgcn_readfirstlane(s.mine.part),
+               __builtin_amdgcn_readfirstlane(s.mine.parts), __builtin_amdgcn_readfirstlane(s.mine.slot)};
+}
+// the same where every block is cut alike; the last block first
+__device__ __forceinline__ Share share_evenly(const Cut& cut, int u, bool last_first) {
+  const mfma::Split at = mfma::split_by(u, cut.parts);
+  const int block = last_first ? cut.blocks - 1 - at.q : at.q;
+  return Share{block, at.r, cut.parts, block * cut.parts};
 }
 
 // what a wavefront knows of its NT tiles of 16 rows; of the lane's row in each
