@@ -811,7 +811,7 @@ size_t scored_bwd_scratch(const a2d_tile_desc& d, const ScoreRules& r, const Sco
 // in their own order 425, four parts 400; 427 x 5532, 16 / 4 of 64 in documents: dK / dV of three units a block on average, shared out, 43,
 // of four even parts 56; 746 x 895, 4 / 1 of 64: shared out 28, even 22 (finding out the shares takes some 3 us).
 ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, size_t most_bytes) {
-  constexpr double kFindOut = 3.0, kSum = 5.0, kBytes = 6e6;             // us; bytes of partials a us, out and back
+  constexpr double kFindOut = 4.0, kSum = 5.0, kBytes = 6e6;             // us; bytes of partials a us, out and back
   const bool documents = r.ranges && r.heads_per_set == d.heads;
   const int rules = (r.cap != 0.f) + (r.slopes != nullptr), kvh = d.heads / r.group;
   const double by_head = d.hdim / 128.0, all_rows = (double)d.nq * r.group, alike = std::min(1.0, (double)d.nkv / d.nq);
@@ -845,11 +845,11 @@ ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int c
         if (us < best.us) best = Way{u, false, us};
       }
       if (uneven) {
-        const double each = u > n ? std::max(1.0, n * mean / (u - n)) : most, split_units = u > n ? std::min<double>(u, 0.5 * n + n * mean / each) : 0;
+        const double each = u > n ? std::max(1.0, n * mean / (u - 0.5 * n)) : most, made = u > n ? std::min<double>(u, 0.5 * n + n * mean / each) : n;
         const double one = std::min(each, most) * step + fixed + kFindOut;
-        const double even = heads * (n * mean * step + std::max<double>(n, split_units) * (fixed + kFindOut)) / cus + 0.15 * one;
-        const double turns = u > n ? std::ceil(heads * std::min<double>(u - n, n * mean) / cus) : 1;   // of units of that weight
-        const double us = std::max(turns * one, even) + heads * split_units * unit_us;
+        const double even = heads * (n * mean * step + made * (fixed + kFindOut)) / cus + 0.15 * one;
+        const double turns = u > n ? std::ceil(heads * made / cus) : 1;
+        const double us = std::max(turns * one, even) + (u > n ? heads * made * unit_us : 0);
         if (us < best.us) best = Way{u, true, us};
       }
     }

@@ -60,31 +60,46 @@ struct Share {
 };
 struct Shares {
   Ranks ranks;
-  int total, wave[8];
+  int each[8], wave[8];
   Share mine;
 };
-// Unit u where they are shared out: a unit takes `each` of the blocks' weights at most, blocks of at least one unit, so that
-// sum_b max(1, ceil(w_b / each)) <= W / each + blocks <= cut.units; the heaviest blocks' units first.  parts = 0: there are fewer units.
-// ranks.weight is set; 512 threads, cut.blocks <= MAX_RANKED
+// Unit u where they are shared out: a unit takes `each` of the blocks' weights at most, blocks of at least one unit, the heaviest blocks'
+// units first; the least `each` of eight, a wavefront each, that makes no more than cut.units of them.  They lie between W / units, which no
+// cut can undercut, and W / (units - blocks) + 1, which always does: sum_b max(1, ceil(w_b / each)) < W / each + blocks.
+// parts = 0: there are fewer units.  ranks.weight is set; 512 threads, cut.blocks <= MAX_RANKED
 __device__ __forceinline__ Share share_out(Shares& s, const Cut& cut, int u) {
-  const int i = threadIdx.x, n = cut.blocks;
-  if (i == 0) {
-    s.total = 0;
-    s.mine = Share{0, 0, 0, 0};
-  }
-  rank_blocks(s.ranks, n, 512);
-  const int block = i < n ? s.ranks.order[i] : 0, w = i < n ? s.ranks.weight[block] : 0;
-  if (w > 0) atomicAdd(&s.total, w);
+  const int i = threadIdx.x, n = cut.blocks, lane = i & 63;
+  const auto units = [](int w, int each) { return max(1, (int)(((unsigned)w + each - 1) / (unsigned)each)); };
+  const auto sum = [](int x) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o, 64);
+    return x;
+  };
   __syncthreads();
-  const int room = cut.units - n, each = room > 0 ? max(cut.least, s.total / room + 1) : INT_MAX;
-  const int parts = i >= n ? 0 : max(1, (int)(((int64_t)w + each - 1) / each));
+  int each = INT_MAX;
+  if (cut.units > n) {
+    int total = 0, made = 0;
+    for (int b = lane; b < n; b += 64) total += s.ranks.weight[b];
+    total = sum(total);
+    const int lo = total / cut.units, hi = total / (cut.units - n) + 1;
+    each = max(cut.least, lo + (int)((int64_t)(hi - lo) * ((i >> 6) + 1) / 8));
+    for (int b = lane; b < n; b += 64) made += units(s.ranks.weight[b], each);
+    if (sum(made) > cut.units) each = INT_MAX;
+  }
+  if (lane == 0) s.each[i >> 6] = each;
+  if (i == 0) s.mine = Share{0, 0, 0, 0};
+  rank_blocks(s.ranks, n, 512);
+#pragma unroll
+  for (int x = 0; x < 8; ++x) each = min(each, s.each[x]);
+  const int block = i < n ? s.ranks.order[i] : 0;
+  const int parts = i < n ? units(s.ranks.weight[block], each) : 0;
   int upto = parts;                                  // of this rank and those before it
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int x = __shfl_up(upto, o, 64);
-    if ((i & 63) >= o) upto += x;
+    if (lane >= o) upto += x;
   }
-  if ((i & 63) == 63) s.wave[i >> 6] = upto;
+  if (lane == 63) s.wave[i >> 6] = upto;
   __syncthreads();
   for (int x = 0; x < i >> 6; ++x) upto += s.wave[x];
   if (u < upto && u >= upto - parts) s.mine = Share{block, u - (upto - parts), parts, upto - parts};
