@@ -350,7 +350,7 @@ a2d_status a2d_partial_bwd_gqa(const a2d_tile_desc* desc, int32_t kv_heads, int 
  * tokens for each row (a2d_document_ranges writes those of packed documents).  A row without a visible key has the empty partial.
  */
 typedef struct {
-  float softcap;         /* finite, >= 0; 0: no cap                                                             */
+  float softcap;         /* 0: no cap; else 1e-6 .. 1e6, and scale / softcap at most 1e4 (A2D_ERR_UNSUPPORTED)   */
   int32_t token_step;    /* tokens between rows, and between keys; 1 .. 2^20                                    */
   int32_t range_sets;    /* 1, or sets of ranges: one for each run of heads / range_sets query heads (a batch's
                             sequences); must divide kv_heads                                                    */
@@ -372,6 +372,7 @@ typedef struct {
  * Rows of Q, O, dO that see no key, and keys in front of the first or behind the last one that any row sees, may hold
  * anything (NaN, uninitialised cache): they are not read or have no effect, and their gradients are 0.
  * With slopes no distance |t_i - u_k| of the tile may exceed 2^24 (A2D_ERR_UNSUPPORTED): they are exact in fp32 up to there.
+ * desc->scale below 1e-20 is refused (A2D_ERR_UNSUPPORTED).  slopes: any finite values, negative ones too.
  * group * nq may not exceed 2^22 rows.
  */
 a2d_status a2d_partial_fwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, const a2d_score_rules* rules, int flags,

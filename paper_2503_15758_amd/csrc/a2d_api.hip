@@ -711,9 +711,10 @@ a2d_status make_rules(const a2d_tile_desc* d, int32_t kv_heads, const a2d_score_
   if (!in) return fail(A2D_ERR_INVALID_ARG, "%s: rules is NULL", who);
   if (!(in->softcap >= 0.f) || !std::isfinite(in->softcap))
     return fail(A2D_ERR_INVALID_ARG, "%s: softcap must be finite and >= 0", who);
-  // (below, scale / softcap or its square is no normal number any more)
-  if (in->softcap != 0.f && (in->softcap < 1e-6f || in->softcap > 1e6f || d->scale / in->softcap > 1e4f || d->scale < 1e-20f))
-    return fail(A2D_ERR_UNSUPPORTED, "%s: softcap=%g outside 1e-6 .. 1e6 or below scale / 1e4, or scale=%g below 1e-20 with it", who, in->softcap, d->scale);
+  // (below, scale / softcap or its square, or lse / scale, is no normal number any more)
+  if (d->scale < 1e-20f) return fail(A2D_ERR_UNSUPPORTED, "%s: scale=%g below 1e-20", who, d->scale);
+  if (in->softcap != 0.f && (in->softcap < 1e-6f || in->softcap > 1e6f || d->scale / in->softcap > 1e4f))
+    return fail(A2D_ERR_UNSUPPORTED, "%s: softcap=%g outside 1e-6 .. 1e6 or below scale / 1e4 (scale=%g)", who, in->softcap, d->scale);
   if (in->token_step < 1 || in->token_step > (1 << 20))
     return fail(A2D_ERR_INVALID_ARG, "%s: token_step=%d outside 1..2^20", who, in->token_step);
   if (in->pad != 0) return fail(A2D_ERR_INVALID_ARG, "%s: rules->pad must be 0", who);

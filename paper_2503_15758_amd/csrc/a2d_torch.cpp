@@ -101,7 +101,8 @@ a2d_layout layout(const at::Tensor& t) {
   if (t.is_contiguous()) return a2d_layout{0, 0};
   const int64_t heads = t.size(0), rows = t.size(1), H = t.size(2);
   const int64_t row = rows > 1 ? t.stride(1) : H;      // a stride over a dimension of extent 1 is arbitrary
-  return a2d_layout{heads > 1 ? t.stride(0) : rows * row, row};
+  const int64_t head = heads > 1 ? t.stride(0) : rows * row;
+  return head == 0 && row == 0 ? a2d_layout{-1, -1} : a2d_layout{head, row};   // (an expanded row: {0, 0} would read as plain)
 }
 
 template <class T>

@@ -68,6 +68,12 @@ def test_bad_tiles_and_pointers(b):
     assert bwd(b, desc(b, flags=b.DESC_KEEP_DS), r) == UNSUPPORTED
 
 
+def test_scales_too_small(b):
+    """lse / scale is formed in fp32"""
+    assert fwd(b, desc(b, scale=9e-21), rules(b)) == UNSUPPORTED and bwd(b, desc(b, scale=1e-38), rules(b, softcap=0.0)) == UNSUPPORTED
+    assert fwd(b, desc(b, scale=1.1e-20), rules(b, softcap=0.0), q=ODD) == MISALIGNED
+
+
 def test_distances_of_a_bias(b):
     """Up to 2^24 tokens: they are fp32 in the kernels."""
     for change in (dict(q_off=(1 << 24) - 126), dict(kv_off=(1 << 24) - 126)):
