@@ -835,7 +835,7 @@ PyObject* rotary(Args a) {
   d.out_dtype = dtype_code(ot);
   Outputs o;
   if (a[6] == Py_None) {
-    for (int i = 0; i < n; ++i) o.add(at::empty_like(xs[i], xs[i].options().dtype(ot).requires_grad(false)));
+    for (int i = 0; i < n; ++i) o.add(empty_like_shape(xs[i], xs[i].sizes(), ot));
   } else if (one) {
     o.n = 1;
     o.given[0] = a[6];

@@ -320,3 +320,33 @@ def test_refusals(a2d):
         with pytest.raises(refused):
             a2d.document_ranges(*args, **kw)
     torch.cuda.synchronize()
+
+
+def test_frequencies_of_any_size(a2d):
+    """Parts of a turn from frequencies of either sign, from ones that never get anywhere to some turns a position, against angles from
+    rational arithmetic: position times frequency is exact there, and 2 pi is good to 300 bits."""
+    import math
+    from fractions import Fraction
+
+    def arctan(x):                                   # of 1 / x, in units of 2^-300
+        total = term = (1 << 300) // x
+        n, sign = 3, -1
+        while term:
+            term //= x * x
+            total += sign * (term // n)
+            n, sign = n + 2, -sign
+        return total
+
+    turn = Fraction(8 * (4 * arctan(5) - arctan(239)), 1 << 300)
+    f = [1.0, -1.0, 0.1, -1e-4, 1e-30, -5e-324, 6.283185307179586, 1e3, -123456.789, 1e9, 0.0, 2.0 ** -33]
+    rows = [0, 1, -1, 77, 2 ** 31 - 1, -2 ** 31]
+    X = torch.zeros(1, len(rows), 32, device="cuda")
+    X[:, :, :16] = 1.0
+    got = a2d.rotary(X, int32([rows]), torch.tensor(f, dtype=torch.float64)).cpu().double()
+    for i, n in enumerate(rows):
+        for p, freq in enumerate(f):
+            part = float((n * Fraction(freq) / turn) % 1)
+            want = (math.cos(2 * math.pi * part), math.sin(2 * math.pi * part))
+            # 2^-64 turns a position, the angle's 2^-32 turns and its fp32 rounding (half a turn at most), 4 half steps of the sine
+            bound = 2 * math.pi * (abs(n) * 2.0 ** -64 + 2.0 ** -32 + 2.0 ** -25) + 4 * U
+            assert abs(got[0, i, p] - want[0]) <= bound and abs(got[0, i, 16 + p] - want[1]) <= bound, (n, freq)
