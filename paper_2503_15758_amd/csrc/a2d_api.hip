@@ -744,6 +744,7 @@ a2d_status make_rules(const a2d_tile_desc* d, int32_t kv_heads, const a2d_score_
   r->heads_per_set = d->heads / in->range_sets;
   r->group = g.group;
   for (int i = 0; i < 6; ++i) r->steps[i] = (float)(in->token_step * (i < 3 ? i + 1 : 16 * (i - 2)));
+  for (int e = 0; e < 16; ++e) r->all_steps[e] = (float)in->token_step * (16 * (e / 4) + e % 4);
   r->rel = d->q_off - d->kv_off;
   r->kv_off = d->kv_off;
   r->slopes = in->slopes;

@@ -22,6 +22,7 @@ struct ScoreRules {
   int acc, norm;        // as in SegList
   int64_t rel, kv_off;  // tokens: of row 0 behind key 0; of key 0
   float steps[6];       // step times 1, 2, 3, 16, 32, 48: between the scores that a lane holds
+  float all_steps[16];  // step times 16 (e / 4) + e % 4: of score e behind a lane's first
   const float* slopes;
   const int2* ranges;
 };

@@ -2,9 +2,11 @@
 //
 // The contractions are those of fwd_mfma_kernel and fwd_small_kernel: S^T = K Q^T with a lane holding four keys of one query
 // row in each tile of 16 x 16, and P^T as it stands as an operand of O^T += V^T P^T.  Between them the scores are brought into log2
-// units (z -> cap -> minus the bias), so that 2^x follows directly; without cap and bias they stay raw and the exponent
-// takes them in with its multiply-add.  The rules cost vector instructions a score: the cap 4.5 (a polynomial, see CapArgs; where some
-// score of a wavefront's block is beyond its range 12, two of them of a quarter of the rate), the bias 2.3.
+// units (z -> cap -> minus the bias) relative to the row's reference, so that 2^x follows directly.  The rules cost vector instructions a
+// score: the cap 4.5 (a polynomial, see CapArgs; where some score of a wavefront's block is beyond its range 12, two of them of a quarter of the
+// rate), the bias 1, near the diagonal 2.3.  Bound: the vector instructions (of 64 keys and 32 rows of a wavefront at H = 64, 512 clocks of
+// exponentials and 600 to 900 of others stand beside 512 of matrix instructions), which two wavefronts of a SIMD share.  16 heads of 64,
+// 8192 x 8192, not causal: 265 us without rules, 317 with a bias, 379 with a cap; 32 / 8 of 128, 4096 x 4096, causal: 137, 132, 147.
 //
 // Masks: whatever they are made of, a query row sees one run of keys (visible_run).  A workgroup walks the hull of
 // its rows' runs; a wavefront leaves out the blocks that none of its rows sees, and compares keys only in blocks that some row does not see
@@ -26,13 +28,17 @@ constexpr float kRescaleThreshold = 8.0f;            // log2 units (as in a2d_fw
 // ---- Scores in log2 units, relative to the row's reference from the start: the multiply-add that ends the cap or takes in the raw product takes
 // the reference too, so that 2^x follows directly (a subtraction of its own was a tenth of the vector instructions).
 // Score e of a lane's: tile of 16 keys e >> 2, key e & 3 of its four.  raw: log2 units of a raw product.  from: distance of the lane's first
-// key.  BEYOND: products beyond the polynomial's range too
-template <bool CAP, bool BIAS, bool BEYOND>
-__device__ __forceinline__ float to_score(float z, float ref, const ScoreRules& r, float raw, float slope, float from, int e) {
+// key.  BEYOND: products beyond the polynomial's range too.  ASIDE: the keys stand on one side of the row, all of them ASIDE_STEPS off at
+// least, so that the bias is linear (slope < 0: keys ahead) and its multiply-add takes in the reference: start = -ref - slope from.  (What
+// `start` is rounded by is 2^-24 of ref and of the first key's bias, which is 3 times the score's own at most.)
+constexpr int ASIDE_STEPS = 32;
+template <bool CAP, bool BIAS, bool BEYOND, bool ASIDE>
+__device__ __forceinline__ float to_score(float z, float ref, const ScoreRules& r, float raw, float slope, float from, float start, int e) {
+  const float less = ASIDE ? (e == 0 ? start : fmaf(slope, r.all_steps[e], start)) : -ref;
   float x;
-  if constexpr (CAP) x = BEYOND ? cap_log2(r.capped, z) - ref : fmaf(z, cap_factor(r.capped, z), -ref);
-  else x = fmaf(z, raw, -ref);
-  if constexpr (BIAS) x = fmaf(-slope, fabsf(distance<-1>(r, from, e >> 2, e & 3)), x);
+  if constexpr (CAP) x = BEYOND ? cap_log2(r.capped, z) + less : fmaf(z, cap_factor(r.capped, z), less);
+  else x = fmaf(z, raw, less);
+  if constexpr (BIAS && !ASIDE) x = fmaf(-slope, fabsf(distance<-1>(r, from, e >> 2, e & 3)), x);
   return x;
 }
 // whether some score of the wavefront's is beyond the polynomial's range (a NaN is left out, and comes through it as NaN)
@@ -67,28 +73,36 @@ struct Softmax {
     f = none ? 0.f : fast_exp2(-m_row);
     if (!none) m_row += ref[q];
   }
-  // Takes in the maxima of new scores.  The reference follows the running maximum only when a score exceeds it by more than 2^8, or
+  // take: the maxima of new scores.  The reference follows the running maximum only when a score exceeds it by more than 2^8, or
   // with the first keys that a lane sees (as in fwd_softmax): a rare branch, and the only place where the lanes of a row talk.
-  template <int NT, int HT>
-  __device__ __forceinline__ void follow(f32x4 (&s)[NT][2], f32x4 (&o)[HT][2]) {
-    const float was[2] = {m_lane[0], m_lane[1]};
+  // follow is true where a row left a reference that it had: its scores are rounded to 2^-24 of their distance from that, which may be many
+  // times their own size (a bias, met far keys first), so they are made again, from the products, and taken.
+  template <int NT>
+  __device__ __forceinline__ bool take(const f32x4 (&s)[NT][2], float (&was)[2]) {       // whether the reference is to follow
     bool grow = false;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      float mx = was[q];
+      float mx = was[q] = m_lane[q];
 #pragma unroll
       for (int e = 0; e < 4 * NT; ++e) mx = fmaxf(mx, s[e >> 2][q][e & 3]);
       m_lane[q] = mx;
       grow |= mx > kRescaleThreshold || (was[q] == -INFINITY && mx > -INFINITY);         // (NaN: false)
     }
-    if (A2D_OFTEN(__builtin_amdgcn_ballot_w64(grow) == 0)) return;
-    asm volatile("" ::: "memory");                   // keep this a branch
+    return __builtin_amdgcn_ballot_w64(grow) != 0;
+  }
+  template <int NT, int HT>
+  __device__ __forceinline__ bool follow(f32x4 (&s)[NT][2], f32x4 (&o)[HT][2], const float (&was)[2]) {
+    bool left = false;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const float m_row = row_max(m_lane[q]), by = m_row == -INFINITY ? 0.f : m_row;
-      const float alpha = row_max(was[q]) == -INFINITY ? 0.f : fast_exp2(-by);           // (nothing is held yet)
-      ref[q] += by;
-      m_lane[q] -= by;
+      const float m_row = row_max(m_lane[q]);
+      const bool held = row_max(was[q]) > -INFINITY;
+      const float next = m_row == -INFINITY ? ref[q] : ref[q] + m_row, by = next - ref[q];
+      const float alpha = held ? fast_exp2(-by) : 0.f;
+      const bool made = held && by > kRescaleThreshold;
+      left |= made;
+      ref[q] = next;
+      m_lane[q] = made ? was[q] - by : m_lane[q] - by;
       l[q] *= alpha;
 #pragma unroll
       for (int e = 0; e < 4 * NT; ++e) s[e >> 2][q][e & 3] -= by;
@@ -97,6 +111,7 @@ struct Softmax {
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[t][q][e] *= alpha;
     }
+    return __builtin_amdgcn_ballot_w64(left) != 0;
   }
   // P^T in bf16 (nearest-even, for the contraction); the sums take the probabilities before their rounding
   template <int NT>
@@ -116,24 +131,31 @@ struct Softmax {
 };
 
 // Raw products of NT tiles of 16 keys from k0 on -> scores
-template <int NT, bool CAP, bool BIAS>
+// (ONE_WAY: of whatever size and place, which every product may go)
+template <int NT, bool CAP, bool BIAS, bool ONE_WAY = false>
 __device__ __forceinline__ void to_scores(f32x4 (&s)[NT][2], const Softmax& sm, const ScoreRules& r, const RowState<2>& rs, bool masked, int k0,
                                           int grp, float raw) {
-  const auto all = [&](auto beyond) {
+  const auto all = [&](auto beyond, auto aside, bool ahead) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const float from = first_distance<BIAS>(r, rs, q, k0, grp);
+      const float from = first_distance<BIAS>(r, rs, q, k0, grp), slope = !BIAS ? 0.f : ahead ? -rs.slope[q] : rs.slope[q], start = fmaf(-slope, from, -sm.ref[q]);
 #pragma unroll
       for (int e = 0; e < 4 * NT; ++e)
         s[e >> 2][q][e & 3] =
-            to_score<CAP, BIAS, decltype(beyond)::value>(s[e >> 2][q][e & 3], sm.ref[q], r, raw, BIAS ? rs.slope[q] : 0.f, from, e);
+            to_score<CAP, BIAS, decltype(beyond)::value, decltype(aside)::value>(s[e >> 2][q][e & 3], sm.ref[q], r, raw, slope, from, start, e);
     }
   };
-  if (CAP && A2D_SELDOM(some_beyond(s, r.capped))) {
+  const bool ahead = BIAS && rs.farthest <= (k0 - ASIDE_STEPS) * r.step;
+  if constexpr (ONE_WAY) {
+    all(std::true_type{}, std::false_type{}, false);
+  } else if (CAP && A2D_SELDOM(some_beyond(s, r.capped))) {
     asm volatile("" ::: "memory");                   // keep this a branch
-    all(std::true_type{});
+    all(std::true_type{}, std::false_type{}, false);
+  } else if (BIAS && A2D_SELDOM(!ahead && rs.nearest < (k0 + 16 * NT - 1 + ASIDE_STEPS) * r.step)) {
+    asm volatile("" ::: "memory");
+    all(std::false_type{}, std::false_type{}, false);
   } else {
-    all(std::false_type{});
+    all(std::false_type{}, std::bool_constant<BIAS>{}, ahead);
   }
   if (A2D_SELDOM(masked)) {
     asm volatile("" ::: "memory");                   // keep this a branch
@@ -255,28 +277,45 @@ __device__ __forceinline__ void scored_fwd_rows(
   };
   Blocks16 rd;
   rd.init(lane, lds_base);
-  // From the last block down: under a bias the nearest keys of a causal row score highest, and met last they would move its reference again and
-  // again (16 heads of 64, 8192 x 8192: 225 us from the first block up, 177 down; 32 of 128, 4096 x 4096: 164, 141)
-  const int stride = KL * map.parts;
-  int lead = end - 1 - part * KL, j = lead - kl;      // key lane 0's block; this lane's
-  if (j >= first) load_tile(j, 0);
+  // Under a bias the nearest keys score highest, and met last they would move a row's reference again and again: from the block of the
+  // last row's own token down, then up from there (16 heads of 64, 8192 x 8192: causal 225 us from the first block up, 177 down; not
+  // causal 410 from the last block down, 317 from the row's own)
+  int turn = end - 1;
+  if constexpr (BIAS) {
+    const int64_t key = floor_div(r.rel + (int64_t)((map.rows > d.nq ? d.nq : min(q0 + BM, d.nq)) - 1) * r.step, r.step);
+    turn = max(min(turn, (int)(max(key, (int64_t)0) / BN)), first);
+  }
+  const auto block_at = [&](int i) { return i <= turn - first ? turn - i : first + i; };
+  const int blocks = end - first, stride = KL * map.parts;
+  int lead = part * KL, i = lead + kl, j = block_at(i);      // key lane 0's place in the walk; this lane's, and its block
+  if (i < blocks) load_tile(j, 0);
   wait_vmem_all();                                    // (the Q rows and the first tiles together)
 #pragma unroll
   for (int q = 0; q < 2; ++q) sm.start(q, m_in[q]);
   __syncthreads();
 
   int boff = 0;
-  for (; lead >= first; lead -= stride) {
-    if (A2D_OFTEN(j - stride >= first)) load_tile(j - stride, BUF_BYTES - boff);
-    const int k0 = j * BN;
-    if (j >= first && k0 + BN > rs.lo && k0 < rs.hi) {
+  for (; lead < blocks; lead += stride) {
+    const int next = block_at(i + stride), k0 = j * BN;
+    if (A2D_OFTEN(i + stride < blocks)) load_tile(next, BUF_BYTES - boff);
+    if (i < blocks && k0 + BN > rs.lo && k0 < rs.hi) {
       Scores s;
       Ring kr, vr;
       bf16x8 pb[2][2];
       fwd_first_keys<HR>(kr, rd, boff);
       fwd_scores<HR>(s, kr, qf, rd, boff);
-      to_scores<4, CAP, BIAS>(s, sm, r, rs, k0 < rs.all_lo || k0 + BN > rs.all_hi, k0, grp, raw);
-      sm.follow(s, o);
+      const bool masked = k0 < rs.all_lo || k0 + BN > rs.all_hi;
+      to_scores<4, CAP, BIAS>(s, sm, r, rs, masked, k0, grp, raw);
+      float was[2];
+      if (A2D_SELDOM(sm.take(s, was))) {
+        asm volatile("" ::: "memory");               // keep this a branch
+        if (sm.follow(s, o, was)) {
+          fwd_first_keys<HR>(kr, rd, boff);
+          fwd_scores<HR>(s, kr, qf, rd, boff);
+          to_scores<4, CAP, BIAS, true>(s, sm, r, rs, masked, k0, grp, raw);
+          sm.take(s, was);
+        }
+      }
       fwd_first_values<HR>(vr, rd, boff);
       sm.probabilities(s, pb);
       __builtin_amdgcn_sched_barrier(0);
@@ -284,7 +323,8 @@ __device__ __forceinline__ void scored_fwd_rows(
     }
     wait_vmem_all();
     __syncthreads();
-    j -= stride;
+    i += stride;
+    j = next;
     boff = BUF_BYTES - boff;
   }
 
@@ -485,8 +525,21 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
       }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) load(false, j - stride);
-    to_scores<2, CAP, BIAS>(s, sm, r, rs, k0 < rs.all_lo || k0 + SB > rs.all_hi, k0, grp, raw);
-    sm.follow(s, o);
+    const f32x4 z[2][2] = {{s[0][0], s[0][1]}, {s[1][0], s[1][1]}};
+    const bool masked = k0 < rs.all_lo || k0 + SB > rs.all_hi;
+    to_scores<2, CAP, BIAS>(s, sm, r, rs, masked, k0, grp, raw);
+    float was[2];
+    if (A2D_SELDOM(sm.take(s, was))) {
+      asm volatile("" ::: "memory");                 // keep this a branch
+      if (sm.follow(s, o, was)) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) s[k][q] = z[k][q];
+        to_scores<2, CAP, BIAS, true>(s, sm, r, rs, masked, k0, grp, raw);
+        sm.take(s, was);
+      }
+    }
     bf16x8 pb[1][2];
     sm.probabilities(s, pb);
     __builtin_amdgcn_sched_barrier(0);

@@ -122,6 +122,7 @@ struct RowState {
   float at[NT], slope[NT]; // tokens behind key 0; slope in log2 units
   int lo, hi;            // hull of the wavefront's runs; lo > hi: nothing seen
   int all_lo, all_hi;    // keys that all of its rows see
+  int nearest, farthest; // `at` of its rows, the least and the most
 };
 
 // min or max over the 16 lanes of a lane's tile (every 16 lanes hold the same rows)
@@ -138,7 +139,7 @@ __device__ __forceinline__ void look_up_rows(RowState<NT>& rs, const a2d_tile_de
                                              int lane) {
   const auto least = [](int a, int b) { return min(a, b); };
   const auto most = [](int a, int b) { return max(a, b); };
-  int lo = INT_MAX, hi = 0, all_lo = 0, all_hi = INT_MAX;
+  int lo = INT_MAX, hi = 0, all_lo = 0, all_hi = INT_MAX, nearest = INT_MAX, farthest = INT_MIN;
 #pragma unroll
   for (int q = 0; q < NT; ++q) {
     const int row = w0 + 16 * q + (lane & 15), in = min(row, map.rows - 1);
@@ -146,7 +147,10 @@ __device__ __forceinline__ void look_up_rows(RowState<NT>& rs, const a2d_tile_de
     rs.q_at[q] = hd.q * d.lq.head + hd.r * d.lq.row;
     rs.run[q] = visible_run(d, r, head + hd.q, hd.r);
     if constexpr (BIAS) {
-      rs.at[q] = (float)(int)(r.rel + (int64_t)hd.r * r.step);
+      const int at = (int)(r.rel + (int64_t)hd.r * r.step);
+      rs.at[q] = (float)at;
+      nearest = min(nearest, at);
+      farthest = max(farthest, at);
       rs.slope[q] = r.slopes[head + hd.q] * kLog2e;
     }
     if (row >= map.rows) rs.run[q] = Run{0, 0};                // (never stored; asks for nothing)
@@ -163,6 +167,8 @@ __device__ __forceinline__ void look_up_rows(RowState<NT>& rs, const a2d_tile_de
   rs.hi = over16(hi, most);
   rs.all_lo = over16(all_lo, most);
   rs.all_hi = over16(all_hi, least);
+  rs.nearest = BIAS ? over16(nearest, least) : 0;
+  rs.farthest = BIAS ? over16(farthest, most) : 0;
 }
 
 // how the blocks of a tile are ordered, of which there are n a head

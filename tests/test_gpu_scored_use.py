@@ -350,3 +350,18 @@ def test_frequencies_of_any_size(a2d):
             # 2^-64 turns a position, the angle's 2^-32 turns and its fp32 rounding (half a turn at most), 4 half steps of the sine
             bound = 2 * math.pi * (abs(n) * 2.0 ** -64 + 2.0 ** -32 + 2.0 ** -25) + 4 * U
             assert abs(got[0, i, p] - want[0]) <= bound and abs(got[0, i, 16 + p] - want[1]) <= bound, (n, freq)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("step, slopes", [(1, [8.0, 0.5, -0.01, 1e-6]), (1000, [0.01, 1e-4, 3.0, 0.0]), (4, [30.0, -0.25, 0.0, 0.125])])
+def test_steep_and_rising_slopes(a2d, dt, step, slopes):
+    """Rows with keys on both sides, and a bias that changes within a block by more than fp32 could forget, or rises with distance."""
+    Q, K, V, dO = inputs(4, 2, 330, 470, 64, dt)
+    rules = dict(slopes=torch.tensor(slopes, device="cuda"), token_step=step, q_off=70 * step + step // 2)
+    s = Scored(Q, K, V, **rules)
+    f = s.partial()
+    check_fwd(a2d.partial_fwd_scored(Q, K, V, normalised=True, **rules), f, True, Q.dtype, "slopes")
+    O, lse = f["O"].to(Q.dtype).cuda(), f["lse"].float().cuda()
+    want = s.gradients(O, dO, lse)
+    for x, n in zip(a2d.partial_bwd_scored(Q, K, V, O, dO, lse, **rules), ("dQ", "dK", "dV")):
+        within(x, want[n], want["e_" + n], "slopes %s" % n)
