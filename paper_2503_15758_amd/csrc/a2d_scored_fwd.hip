@@ -24,6 +24,7 @@ namespace {
 using namespace mfma;
 
 constexpr float kRescaleThreshold = 8.0f;            // log2 units (as in a2d_fwd_mfma.hip)
+constexpr float kFarReference = 64.0f;               // (see Softmax::follow)
 
 // ---- Scores in log2 units, relative to the row's reference from the start: the multiply-add that ends the cap or takes in the raw product takes
 // the reference too, so that 2^x follows directly (a subtraction of its own was a tenth of the vector instructions).
@@ -38,7 +39,7 @@ __device__ __forceinline__ float to_score(float z, float ref, const ScoreRules& 
   float x;
   if constexpr (CAP) x = BEYOND ? cap_log2(r.capped, z) + less : fmaf(z, cap_factor(r.capped, z), less);
   else x = fmaf(z, raw, less);
-  if constexpr (BIAS && !ASIDE) x = fmaf(-slope, fabsf(distance<-1>(r, from, e >> 2, e & 3)), x);
+  if constexpr (BIAS && !ASIDE) x = fmaf(-slope, fabsf(from - r.all_steps[e]), x);
   return x;
 }
 // whether some score of the wavefront's is beyond the polynomial's range (a NaN is left out, and comes through it as NaN)
@@ -75,8 +76,10 @@ struct Softmax {
   }
   // take: the maxima of new scores.  The reference follows the running maximum only when a score exceeds it by more than 2^8, or
   // with the first keys that a lane sees (as in fwd_softmax): a rare branch, and the only place where the lanes of a row talk.
-  // follow is true where a row left a reference that it had: its scores are rounded to 2^-24 of their distance from that, which may be many
-  // times their own size (a bias, met far keys first), so they are made again, from the products, and taken.
+  // follow is true where a row left a reference far behind: its scores are rounded to 2^-24 of their distance from that, which may be many
+  // times their own size (a steep bias, met far keys first), so they are made again, from the products, and taken.  Up to 2^64, whose
+  // logarithm's rounding is 4e-6 of a probability, a thousandth of its own to bf16, they stay: rows that saw but a few keys
+  // of their first block leave its reference often (32 / 8 heads of 128, 4096 x 4096, capped: 178 us with every one made again, 153 with these).
   template <int NT>
   __device__ __forceinline__ bool take(const f32x4 (&s)[NT][2], float (&was)[2]) {       // whether the reference is to follow
     bool grow = false;
@@ -99,7 +102,7 @@ struct Softmax {
       const bool held = row_max(was[q]) > -INFINITY;
       const float next = m_row == -INFINITY ? ref[q] : ref[q] + m_row, by = next - ref[q];
       const float alpha = held ? fast_exp2(-by) : 0.f;
-      const bool made = held && by > kRescaleThreshold;
+      const bool made = held && by > kFarReference;
       left |= made;
       ref[q] = next;
       m_lane[q] = made ? was[q] - by : m_lane[q] - by;
@@ -388,8 +391,10 @@ __device__ __forceinline__ void scored_fwd_rows(
   }
 }
 
+// (pairs of workgroups at H = 64 are three, with 168 registers, where the rules leave room for that: 8192 x 8192, 16 heads, causal, 165 us under
+// a bias and 205 under a cap; 189 and 216 as two)
 template <int WAVES, int HR, int KL, bool CAP, bool BIAS>
-__global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void scored_fwd_kernel(
+__global__ __launch_bounds__(64 * WAVES, WAVES == 4 && HR == 64 && !(CAP && BIAS) ? 3 : 8 / WAVES) void scored_fwd_kernel(
     a2d_tile_desc d, ScoreRules r, RowMap map, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
     const bf16_t* __restrict__ V, float* out0, float* out1, float* out2, FwdInput in) {
   extern __shared__ __attribute__((aligned(1024))) char lds_all[];
