@@ -365,3 +365,38 @@ def test_steep_and_rising_slopes(a2d, dt, step, slopes):
     want = s.gradients(O, dO, lse)
     for x, n in zip(a2d.partial_bwd_scored(Q, K, V, O, dO, lse, **rules), ("dQ", "dK", "dV")):
         within(x, want[n], want["e_" + n], "slopes %s" % n)
+
+
+@pytest.mark.parametrize("dt, kvh, nq", [("bf16", 5, 1), ("bf16", 2, 40), ("f32", 2, 3)])
+def test_a_long_cache(a2d, dt, kvh, nq):
+    """4 million keys a head, so that heads begin beyond 4 GiB: sequences that see runs at its start, across its middle and at its end, and
+    the rest of it as it was allocated; the gradients of what no row sees are zeros."""
+    nkv, H, group = (1 << 22) - 3, 128, 2
+    dtype = torch.bfloat16 if dt == "bf16" else torch.float32
+    gen = torch.Generator().manual_seed(2)
+    rand = lambda *shape: torch.randn(*shape, generator=gen).to(dtype).cuda()
+    K, V = (torch.empty(kvh, nkv, H, dtype=dtype, device="cuda") for _ in range(2))
+    Q, dO = rand(kvh * group, nq, H), rand(kvh * group, nq, H)
+    seen = [((i * (nkv - 300)) // max(kvh - 1, 1), (i * (nkv - 300)) // max(kvh - 1, 1) + 300) for i in range(kvh)]
+    for i, (a, b) in enumerate(seen):
+        K[i, a:b], V[i, a:b] = rand(b - a, H), rand(b - a, H)
+    rules = dict(softcap=9.0)
+    ranges = int32([[list(x)] * nq for x in seen])
+    O, lse = a2d.partial_fwd_scored(Q, K, V, ranges=ranges, normalised=True, **rules)
+    refs = [Scored(Q[i * group: (i + 1) * group], K[i: i + 1, a:b], V[i: i + 1, a:b], **rules) for i, (a, b) in enumerate(seen)]
+    for i, s in enumerate(refs):
+        h = slice(i * group, (i + 1) * group)
+        check_fwd((O[h], lse[h]), s.partial(), True, dtype, "sequence %d" % i)
+    if kvh > 2:
+        return
+    dQ, dK, dV = a2d.partial_bwd_scored(Q, K, V, O, dO, lse, ranges=ranges, rounded=True, **rules)
+    for i, (a, b) in enumerate(seen):
+        h = slice(i * group, (i + 1) * group)
+        want = refs[i].gradients(O[h], dO[h], lse[h])
+        for got, n in ((dQ[h], "dQ"), (dK[i: i + 1, a:b], "dK"), (dV[i: i + 1, a:b], "dV")):
+            within(got, want[n], want["e_" + n], n, half_step(dtype) or U)
+        for x in (dK, dV):
+            assert not x[i, :a].any() and not x[i, b:].any()
+    with pytest.raises(a2d.A2DError):                # rows of a head that span 4 GiB
+        a2d.partial_fwd_scored(Q, torch.empty(nkv, 5, H, dtype=dtype, device="cuda").permute(1, 0, 2)[:kvh],
+                               torch.empty(nkv, 5, H, dtype=dtype, device="cuda").permute(1, 0, 2)[:kvh])
