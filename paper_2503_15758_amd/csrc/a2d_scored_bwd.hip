@@ -10,6 +10,11 @@
 // all of them see.  From the hulls a dK / dV workgroup makes a bit for every step of 64 query rows, and walks the set ones: documents cost
 // nothing but their own scores, wherever they lie.  Rows that see nothing are not loaded (zeros in their place), nor are keys
 // outside a hull: they may hold anything.
+//
+// Bound: vector and matrix instructions of two wavefronts a SIMD that share its issue, 8192 x 8192, 16 heads of 128 in four documents 350 us
+// (660 TFLOP/s of the five contractions; matrix units busy 41 % of dQ's time, 35 % of dK / dV's), 4096 x 4096, 32 / 8 of 128, causal under a cap
+// 527 (44 % and 38 %, vector ALUs 62 % and 48 %); below some hundred million scores by uneven walks, what a workgroup costs besides, and
+// launches: 2999 x 2999, 12 / 4 of 80 in four documents 76.
 #include "a2d_bwd.hpp"
 #include "a2d_scored_rows.hpp"
 
@@ -49,7 +54,7 @@ __host__ __device__ constexpr int dq_launch_lds(int hd, int kl) {
 __host__ __device__ constexpr int dq_ring(int hd) { return hd == 64 ? 4 : 2; }
 
 // KL = 1: 256 rows, KL = 2: 128 rows in two key lanes (see scored_fwd_kernel)
-template <int HR, int KL, bool CAP, bool BIAS>
+template <int HR, int KL, bool CAP, bool BIAS, bool FINE>
 __device__ __forceinline__ void scored_dq_rows(
     int id, char* const lds_all, int* const hull, Shares& shares, const a2d_tile_desc& d, const ScoreRules& r, const Cut& cut, int in_order,
     const RowTable& tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V,
@@ -247,16 +252,22 @@ __device__ __forceinline__ void scored_dq_rows(
           s[e >> 2][q][e & 3] = (unsigned)key < (unsigned)run[q].n ? s[e >> 2][q][e & 3] : 0.f;
         }
     }
-    bf16x8 dsb[2];                                     // dZ is rounded to the inputs' type, as P is
+    bf16x8 dsb[2], rest[2];                            // dZ is rounded to the inputs' type, as P is (FINE: see fine_call)
 #pragma unroll
     for (int q = 0; q < 2; ++q)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) dsb[q][e] = (bf16_t)s[e >> 2][q][e & 3];
+      for (int e = 0; e < 8; ++e) {
+        dsb[q][e] = (bf16_t)s[e >> 2][q][e & 3];
+        if constexpr (FINE) rest[q][e] = (bf16_t)(s[e >> 2][q][e & 3] - (float)dsb[q][e]);
+      }
     __builtin_amdgcn_sched_barrier(0);
     static_for<0, HT>([&](auto I) {
       constexpr int i = decltype(I)::value;
 #pragma unroll
-      for (int q = 0; q < 2; ++q) dq[i][q] = mma16(kt[i % RING], dsb[q], dq[i][q]);
+      for (int q = 0; q < 2; ++q) {
+        dq[i][q] = mma16(kt[i % RING], dsb[q], dq[i][q]);
+        if constexpr (FINE) dq[i][q] = mma16(kt[i % RING], rest[q], dq[i][q]);
+      }
       if constexpr (i + RING < HT) ld2(std::integral_constant<int, i + RING>{});
     });
   };
@@ -307,7 +318,7 @@ __device__ __forceinline__ void scored_dq_rows(
   }
 }
 
-template <int HR, int KL, bool CAP, bool BIAS>
+template <int HR, int KL, bool CAP, bool BIAS, bool FINE>
 __global__ __launch_bounds__(512, 1) void scored_dq_kernel(
     a2d_tile_desc d, ScoreRules r, Cut cut, int in_order, RowTable tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
     const bf16_t* __restrict__ V, const bf16_t* __restrict__ O, const bf16_t* __restrict__ dO, const float* __restrict__ lse,
@@ -315,7 +326,7 @@ __global__ __launch_bounds__(512, 1) void scored_dq_kernel(
   extern __shared__ __attribute__((aligned(1024))) char lds_all[];
   __shared__ int hull[16];
   __shared__ Shares shares;
-  scored_dq_rows<HR, KL, CAP, BIAS>(blockIdx.x, lds_all, hull, shares, d, r, cut, in_order, tab, Q, K, V, O, dO, lse, dQ, more, table);
+  scored_dq_rows<HR, KL, CAP, BIAS, FINE>(blockIdx.x, lds_all, hull, shares, d, r, cut, in_order, tab, Q, K, V, O, dO, lse, dQ, more, table);
 }
 
 // --------------------------------------------------------------------------------------------- dK, dV
@@ -354,7 +365,7 @@ __device__ __forceinline__ void weigh_keys(Ranks& ranks, const ScoreRules& r, co
   if (tid < cut.blocks) ranks.weight[tid] = sum;
 }
 
-template <int HR, bool CAP, bool BIAS>
+template <int HR, bool CAP, bool BIAS, bool FINE>
 __device__ __forceinline__ void scored_dkdv_keys(
     int id, char* const lds, Shares& shares, const a2d_tile_desc& d, const ScoreRules& r, const Cut& cut, int in_order, const RowTable& tab,
     const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
@@ -554,7 +565,7 @@ __device__ __forceinline__ void scored_dkdv_keys(
       for (int kt = 0; kt < 2; ++kt)
         base[kt] = (float)(int)(r.rel + (int64_t)(i0 + 4 * (ln >> 4) - (wk + (ln & 15) + 16 * kt)) * r.step);
     }
-    bf16x8 pb[2], sb[2];
+    bf16x8 pb[2], sb[2], p_rest[2], s_rest[2];
     // score e of the lane's 16: row tile e >> 3, key tile (e >> 2) & 1, row e & 3 of the lane's four.  P to pb, P (1 - t^2) stays in s
     auto prob = [&](int e) {
       const int t = e >> 3, kt = (e >> 2) & 1, i = e & 3;
@@ -563,6 +574,7 @@ __device__ __forceinline__ void scored_dkdv_keys(
       if constexpr (BIAS) x = fmaf(-slope, fabsf(distance<1>(r, base[kt], t, i)), x);
       const float p = fast_exp2(x);
       pb[kt][4 * t + i] = (bf16_t)p;
+      if constexpr (FINE) p_rest[kt][4 * t + i] = (bf16_t)(p - (float)pb[kt][4 * t + i]);
       if constexpr (CAP) {
         const float u = y * inv_top;
         s[t][kt][i] = fmaf(-p * u, u, p);
@@ -592,7 +604,9 @@ __device__ __forceinline__ void scored_dkdv_keys(
     };
     auto dscore = [&](int e) {
       const int t = e >> 3, kt = (e >> 2) & 1, i = e & 3;
-      sb[kt][4 * t + i] = (bf16_t)(s[t][kt][i] * dp[t][kt][i]);
+      const float z = s[t][kt][i] * dp[t][kt][i];
+      sb[kt][4 * t + i] = (bf16_t)z;
+      if constexpr (FINE) s_rest[kt][4 * t + i] = (bf16_t)(z - (float)sb[kt][4 * t + i]);
     };
     mask();
     static_for<0, N1>([&](auto I) {
@@ -617,7 +631,10 @@ __device__ __forceinline__ void scored_dkdv_keys(
     static_for<0, HT>([&](auto Y) {
       constexpr int y = decltype(Y)::value;
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) dv[y][kt] = mma16(a[(N2 + y) % RING], pb[kt], dv[y][kt]);
+      for (int kt = 0; kt < 2; ++kt) {
+        dv[y][kt] = mma16(a[(N2 + y) % RING], pb[kt], dv[y][kt]);
+        if constexpr (FINE) dv[y][kt] = mma16(a[(N2 + y) % RING], p_rest[kt], dv[y][kt]);
+      }
 #pragma unroll
       for (int e = 16 * y / HT; e < 16 * (y + 1) / HT; ++e) dscore(e);
       ld(std::integral_constant<int, N2 + y + RING>{});
@@ -626,7 +643,10 @@ __device__ __forceinline__ void scored_dkdv_keys(
     static_for<0, HT>([&](auto Y) {
       constexpr int y = decltype(Y)::value;
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) dk[y][kt] = mma16(a[(N3 + y) % RING], sb[kt], dk[y][kt]);
+      for (int kt = 0; kt < 2; ++kt) {
+        dk[y][kt] = mma16(a[(N3 + y) % RING], sb[kt], dk[y][kt]);
+        if constexpr (FINE) dk[y][kt] = mma16(a[(N3 + y) % RING], s_rest[kt], dk[y][kt]);
+      }
       ld(std::integral_constant<int, N3 + y + RING>{});
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -681,14 +701,14 @@ __device__ __forceinline__ void scored_dkdv_keys(
   }
 }
 
-template <int HR, bool CAP, bool BIAS>
+template <int HR, bool CAP, bool BIAS, bool FINE>
 __global__ __launch_bounds__(WK_THREADS) void scored_dkdv_kernel(
     a2d_tile_desc d, ScoreRules r, Cut cut, int in_order, RowTable tab, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
     const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO, void* __restrict__ dK, void* __restrict__ dV, float* __restrict__ more,
     int2* __restrict__ table) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   __shared__ Shares shares;
-  scored_dkdv_keys<HR, CAP, BIAS>(blockIdx.x, lds, shares, d, r, cut, in_order, tab, Q, K, V, dO, dK, dV, more, table);
+  scored_dkdv_keys<HR, CAP, BIAS, FINE>(blockIdx.x, lds, shares, d, r, cut, in_order, tab, Q, K, V, dO, dK, dV, more, table);
 }
 static_assert(MAX_RANKED <= WK_THREADS, "a thread a block");
 
@@ -753,7 +773,7 @@ struct BwdCuts {
   }
 };
 
-template <int HR, bool CAP, bool BIAS>
+template <int HR, bool CAP, bool BIAS, bool FINE>
 hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K, const void* V,
               const void* O, const void* dO, const float* lse, void* ws, void* more, void* dQ, void* dK, void* dV, hipStream_t s) {
   constexpr int HD = padded_head(HR);
@@ -772,11 +792,11 @@ hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const Score
                (const bf16_t*)K, (const bf16_t*)V, (const bf16_t*)O, (const bf16_t*)dO, lse, dQ, q_more, q_shared ? q_table : nullptr);
     return hipGetLastError();
   };
-  hipError_t e = plan.lanes == 2 ? dq(scored_dq_kernel<HR, 2, CAP, BIAS>) : dq(scored_dq_kernel<HR, 1, CAP, BIAS>);
+  hipError_t e = plan.lanes == 2 ? dq(scored_dq_kernel<HR, 2, CAP, BIAS, FINE>) : dq(scored_dq_kernel<HR, 1, CAP, BIAS, FINE>);
   if (e != hipSuccess) return e;
   // (the most a call can ask for: ensure_dynamic_lds is asked once for a kernel)
-  if (ph == PREPARE) return ensure_dynamic_lds(reinterpret_cast<const void*>(scored_dkdv_kernel<HR, CAP, BIAS>), wk_lds(HD));
-  A2D_LAUNCH((scored_dkdv_kernel<HR, CAP, BIAS>), dim3(xcd_grid(kvh, c.kv.units)), dim3(WK_THREADS), wk_bytes, s, d, r, c.kv, c.kv_in_order, tab,
+  if (ph == PREPARE) return ensure_dynamic_lds(reinterpret_cast<const void*>(scored_dkdv_kernel<HR, CAP, BIAS, FINE>), wk_lds(HD));
+  A2D_LAUNCH((scored_dkdv_kernel<HR, CAP, BIAS, FINE>), dim3(xcd_grid(kvh, c.kv.units)), dim3(WK_THREADS), wk_bytes, s, d, r, c.kv, c.kv_in_order, tab,
              (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, (const bf16_t*)dO, dK, dV, kv_more, kv_shared ? kv_table : nullptr);
   if ((e = hipGetLastError()) != hipSuccess || c.q_floats + c.kv_floats == 0) return e;
   Cut none{};
@@ -868,19 +888,28 @@ ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int c
   return split_us < whole_us ? split : whole;
 }
 
+// Calls of few scores contract P and dZ as two bf16 numbers each (hi + lo, 2^-17 off).  One rounding to bf16 leaves gradients off by 1.41
+// times what the rounding of the outputs alone does, as sums of many independent errors; of short sums, which cancel by chance, by up to 1.5 times
+// (349 x 193, 4 / 1 heads of 80: 1.47).  These calls wait for launches and first loads: 637 x 260, 4 / 2 of 96, 31 -> 33 us.  Of
+// 2^22 scores and more it was 1.46 at the most (250 calls), and 4619 x 543, 2 of 80, would take 46 us for 41.
+static bool fine_call(const a2d_tile_desc& d) { return (int64_t)d.heads * d.nq * d.nkv <= (int64_t)1 << 22; }
+
 hipError_t launch_scored_bwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K,
                              const void* V, const void* O, const void* dO, const float* lse, void* ws, void* more, void* dQ, void* dK,
                              void* dV, hipStream_t s) {
-#define A2D_RULES(HR)                                                                                                \
-  return r.cap != 0.f ? (r.slopes ? go<HR, true, true>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, more, dQ, dK, dV, s)       \
-                                  : go<HR, true, false>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, more, dQ, dK, dV, s))     \
-                      : (r.slopes ? go<HR, false, true>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, more, dQ, dK, dV, s)      \
-                                  : go<HR, false, false>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, more, dQ, dK, dV, s))
+  const bool fine = fine_call(d);
+#define A2D_FINE(HR, CAP, BIAS)                                                                              \
+  (fine ? go<HR, CAP, BIAS, true>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, more, dQ, dK, dV, s)                \
+        : go<HR, CAP, BIAS, false>(ph, d, r, plan, Q, K, V, O, dO, lse, ws, more, dQ, dK, dV, s))
+#define A2D_RULES(HR)                                                                                        \
+  return r.cap != 0.f ? (r.slopes ? A2D_FINE(HR, true, true) : A2D_FINE(HR, true, false))                     \
+                      : (r.slopes ? A2D_FINE(HR, false, true) : A2D_FINE(HR, false, false))
   if (d.hdim == 128) { A2D_RULES(128); }
   if (d.hdim == 96) { A2D_RULES(96); }
   if (d.hdim == 80) { A2D_RULES(80); }
   A2D_RULES(64);
 #undef A2D_RULES
+#undef A2D_FINE
 }
 
 }  // namespace a2d

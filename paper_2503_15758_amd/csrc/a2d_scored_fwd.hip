@@ -131,6 +131,22 @@ struct Softmax {
       l[q] += sum;
     }
   }
+  // P^T as the sum of two bf16 numbers, 2^-17 of it off
+  template <int NT>
+  __device__ __forceinline__ void probabilities(const f32x4 (&s)[NT][2], bf16x8 (&pb)[NT / 2][2], bf16x8 (&rest)[NT / 2][2]) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4 * NT; ++e) {
+        const float p = fast_exp2(s[e >> 2][q][e & 3]);
+        sum += p;
+        pb[e >> 3][q][e & 7] = (bf16_t)p;
+        rest[e >> 3][q][e & 7] = (bf16_t)(p - (float)pb[e >> 3][q][e & 7]);
+      }
+      l[q] += sum;
+    }
+  }
 };
 
 // Raw products of NT tiles of 16 keys from k0 on -> scores
@@ -545,8 +561,9 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
         sm.take(s, was);
       }
     }
-    bf16x8 pb[1][2];
-    sm.probabilities(s, pb);
+    // (a row of few keys' weight shows their rounding, and the walk waits for memory: both halves of P are contracted)
+    bf16x8 pb[1][2], rest[1][2];
+    sm.probabilities(s, pb, rest);
     __builtin_amdgcn_sched_barrier(0);
     if (more) wait_dma<LOADS>(); else wait_dma();    // V has arrived
 #pragma unroll
@@ -554,7 +571,10 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
       const unsigned at = (t & 1 ? rd.tr_o : rd.tr_e) + V_AT + (t >> 1) * BLOCK;
       const bf16x8 a = lds_load_tr(at, at + KS * BLOCK);
 #pragma unroll
-      for (int q = 0; q < 2; ++q) o[t][q] = mma16(a, pb[0][q], o[t][q]);
+      for (int q = 0; q < 2; ++q) {
+        o[t][q] = mma16(a, pb[0][q], o[t][q]);
+        o[t][q] = mma16(a, rest[0][q], o[t][q]);
+      }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) {
