@@ -8,7 +8,8 @@
 // the result); fp32 results take sincospif.
 //
 // Bound: HBM, each value read and written once.  A thread owns eight pairs of a row (two 16-byte pieces a head in bf16):
-// it makes their sines and cosines once and walks over heads, as many as still leave the chip full of wavefronts.
+// it makes their sines and cosines once and walks over heads, as many as still leave the chip full of wavefronts.  32 + 8 heads of 128, 16384
+// rows, packed: 69 us, 4.86 TB/s; 24 + 24 of 80, 2999 rows, fp32 to bf16: 14.7 us, 4.7 TB/s; a token of 256 + 64 heads: 3.3 us, host 6.7.
 #include "a2d_scored.hpp"
 
 namespace a2d {

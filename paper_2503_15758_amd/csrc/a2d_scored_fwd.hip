@@ -561,7 +561,8 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
         sm.take(s, was);
       }
     }
-    // (a row of few keys' weight shows their rounding, and the walk waits for memory: both halves of P are contracted)
+    // (a row of few keys' weight shows their rounding, and the walk waits for memory: both halves of P are contracted.  A token against 1133
+    // keys: off by 1.49 times what rounding the output alone does with one half; 256 / 64 heads of 128 against up to 16384: 67 us with either)
     bf16x8 pb[1][2], rest[1][2];
     sm.probabilities(s, pb, rest);
     __builtin_amdgcn_sched_barrier(0);

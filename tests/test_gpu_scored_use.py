@@ -400,3 +400,23 @@ def test_a_long_cache(a2d, dt, kvh, nq):
     with pytest.raises(a2d.A2DError):                # rows of a head that span 4 GiB
         a2d.partial_fwd_scored(Q, torch.empty(nkv, 5, H, dtype=dtype, device="cuda").permute(1, 0, 2)[:kvh],
                                torch.empty(nkv, 5, H, dtype=dtype, device="cuda").permute(1, 0, 2)[:kvh])
+
+
+@pytest.mark.parametrize("case", [c for c in FORMS if c[3] < 10000 and c[4] > 1], ids=lambda c: c[0].replace(" ", "_"))
+def test_every_form_accumulated(a2d, case):
+    """Two tiles of keys, views of one cache, the second continuing the first's partial: the whole's, at every form."""
+    name, heads, kvh, nq, nkv, H, more = case
+    print("scored forms accumulated", case, flush=True)
+    Q, K, V, _ = inputs(heads, kvh, nq, nkv, H, "bf16")
+    rules = {k: v for k, v in more.items() if k not in ("docs", "lens")}
+    if rules.get("slopes"):
+        rules["slopes"] = slopes_of(heads)
+    if "docs" in more:
+        rules["ranges"] = documents(a2d, nq, *more["docs"], first=rules.get("q_off", 0))
+    if "lens" in more:
+        rules["ranges"] = int32([[[0, n]] * nq for n in more["lens"]])
+    cut = nkv // 3 + 5
+    out = a2d.partial_fwd_scored(Q, K[:, cut:], V[:, cut:], kv_off=cut, **rules)
+    a2d.partial_fwd_scored(Q, K[:, :cut], V[:, :cut], out=out, accumulate=True, **rules)
+    ref = Scored(Q, K, V, **rules).partial()
+    check_fwd(out, {k: v * 2 if k.startswith("e_") else v for k, v in ref.items()}, False, Q.dtype, name)
