@@ -420,3 +420,41 @@ def test_every_form_accumulated(a2d, case):
     a2d.partial_fwd_scored(Q, K[:, :cut], V[:, :cut], out=out, accumulate=True, **rules)
     ref = Scored(Q, K, V, **rules).partial()
     check_fwd(out, {k: v * 2 if k.startswith("e_") else v for k, v in ref.items()}, False, Q.dtype, name)
+
+
+@pytest.mark.parametrize("dt, nq, kvh", [("bf16", 200, 2), ("f32", 200, 2), ("bf16", 7, 1), ("bf16", 300, 4)])
+@pytest.mark.parametrize("step, q_off, kv_off", [(1, 0, 0), (3, 1, 2), (1, -40, -20), (7, 1 << 20, (1 << 20) - 300)])
+def test_ranges_of_any_kind(a2d, dt, nq, kvh, step, q_off, kv_off):
+    """Ranges that end before they begin, hold nothing, lie in front of or behind all keys, or span every token there is."""
+    heads, nkv = 4, 333
+    Q, K, V, dO = inputs(heads, kvh, nq, nkv, 64, dt)
+    end = kv_off + nkv * step
+    kinds = [(-2 ** 31, 2 ** 31 - 1), (kv_off + 10, kv_off + 5), (-50, kv_off + 20), (end + 5, end + 90), (kv_off + 11, kv_off + 12), (0, 0),
+             (kv_off - 9, kv_off), (end - step, 2 ** 31 - 1), (2 ** 31 - 1, -2 ** 31), (kv_off + 30, end - 40), (-1, 2 ** 31 - 1)]
+    gen = torch.Generator().manual_seed(nq)
+    sets = torch.tensor(kinds, dtype=torch.int32)[torch.randint(0, len(kinds), (kvh, nq), generator=gen)].cuda()
+    for ranges, causal in ((sets, False), (sets[0].contiguous(), True)):
+        rules = dict(ranges=ranges, causal=causal, q_off=q_off, kv_off=kv_off, token_step=step, softcap=12.0, slopes=slopes_of(heads) / step)
+        s = Scored(Q, K, V, **rules)
+        f = s.partial()
+        check_fwd(a2d.partial_fwd_scored(Q, K, V, normalised=True, **rules), f, True, Q.dtype, "ranges")
+        O, lse = f["O"].to(Q.dtype).cuda(), f["lse"].float().cuda()
+        want = s.gradients(O, dO, lse)
+        for x, n in zip(a2d.partial_bwd_scored(Q, K, V, O, dO, lse, **rules), ("dQ", "dK", "dV")):
+            within(x, want[n], want["e_" + n], "ranges %s" % n)
+
+
+@pytest.mark.parametrize("dt, heads, kvh, nq", [("bf16", 65535, 65535, 1), ("bf16", 65535, 13107, 2), ("f32", 65535, 21845, 2), ("bf16", 65520, 65520, 40)])
+def test_as_many_heads_as_there_may_be(a2d, dt, heads, kvh, nq):
+    Q, K, V, dO = inputs(heads, kvh, nq, 3, 64, dt)
+    rules = dict(softcap=5.0, slopes=torch.rand(heads, generator=torch.Generator().manual_seed(1)).cuda(), causal=True, q_off=1)
+    s = Scored(Q, K, V, **rules)
+    f = s.partial()
+    check_fwd(a2d.partial_fwd_scored(Q, K, V, normalised=True, **rules), f, True, Q.dtype, "heads")
+    O, lse = f["O"].to(Q.dtype).cuda(), f["lse"].float().cuda()
+    want = s.gradients(O, dO, lse)
+    for x, n in zip(a2d.partial_bwd_scored(Q, K, V, O, dO, lse, rounded=True, **rules), ("dQ", "dK", "dV")):
+        within(x, want[n], want["e_" + n], "heads %s" % n, half_step(Q.dtype) or U)
+    freqs, axis = a2d.rotary_frequencies(64, (16, 16))
+    pos = torch.arange(2 * nq, dtype=torch.int32, device="cuda").view(2, nq)
+    check(a2d.rotary(Q, pos, freqs, axis), *turned(Q, pos, freqs, axis, False, False), Q.dtype, "turned")
