@@ -432,6 +432,19 @@ def tile_route(heads, nq, nkv, hdim, dtype=torch.bfloat16, kv_heads=None, q_off=
                              compute_units)
 
 
+def scored_route(heads, nq, nkv, hdim, dtype=torch.bfloat16, kv_heads=None, q_off=0, kv_off=0, causal=False, softcap=0.0, slopes=False,
+                 range_sets=0, token_step=1, backward=False, scratch=True, compute_units=0):
+    """Diagnostic: as tile_route, for partial_fwd_scored and partial_bwd_scored; slopes: whether there are any; range_sets: 0: no ranges.
+    A dict: "kernels" in launch order; "rows", "lanes" (key lanes) and "waves" of a forward or dQ workgroup; "order" of a forward's
+    blocks (0: the heads one after another, 1: late rows first, 2: by the lengths of the documents); "blocks_q" and "units_q", the
+    row blocks of a head (of a group's heads in a forward) and the workgroups for them, "blocks_kv" and "units_kv", the same of a
+    backward's keys; "shared_q" and "shared_kv": in proportion to the blocks' walks; "fine": P (and dZ) contracted as
+    two bf16 numbers each."""
+    flags = 1 * bool(backward) | 8 * bool(scratch)
+    return _ext().scored_route(heads, kv_heads or heads, nq, nkv, hdim, dtype, q_off, kv_off, causal, softcap, slopes, range_sets,
+                               token_step, flags, compute_units)
+
+
 def force_generic(on):
     """a2d_debug_force_generic: route every tile call to the vector-ALU kernels (debugging aid)."""
     lib().a2d_debug_force_generic(int(bool(on)))

@@ -759,6 +759,17 @@ a2d_status make_rules(const a2d_tile_desc* d, int32_t kv_heads, const a2d_score_
   return A2D_OK;
 }
 
+// The plans of a call, scratch: whether there is memory for partial results
+a2d::ScoredPlan plan_scored_fwd_of(const a2d_tile_desc& d, const a2d::ScoreRules& r, int cus, bool scratch) {
+  const int cap = scratch ? cap_of((int64_t)d.heads * d.nq * (d.hdim + 2)) : 1;
+  return d.dtype == A2D_F32 ? a2d::plan_scored_fwd_f32(d, r, cus, cap) : a2d::plan_scored_fwd(d, r, cus, cap);
+}
+a2d::ScoredBwdPlan plan_scored_bwd_of(const a2d_tile_desc& d, const a2d::ScoreRules& r, int cus, bool scratch) {
+  if (d.dtype == A2D_BF16) return a2d::plan_scored_bwd(d, r, cus, scratch ? kScoredParts : 0);
+  const int64_t nq = (int64_t)d.heads * d.nq * d.hdim, nk = (int64_t)(d.heads / r.group) * d.nkv * d.hdim;
+  return a2d::plan_scored_bwd_f32(d, r, cus, scratch ? scored_cap(nq) : 1, scratch ? scored_cap(nk) : 1);
+}
+
 }  // namespace
 
 a2d_status a2d_partial_fwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, const a2d_score_rules* rules, int flags,
@@ -792,9 +803,8 @@ a2d_status a2d_partial_fwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, c
   int cus = 0;
   A2D_TRY(hip_result(a2d::device_cus(&cus), who));
   const bool f32 = dd.dtype == A2D_F32;
-  const auto plan_of = f32 ? a2d::plan_scored_fwd_f32 : a2d::plan_scored_fwd;
   const auto launch = f32 ? a2d::launch_scored_fwd_f32 : a2d::launch_scored_fwd;
-  a2d::ScoredPlan plan = plan_of(dd, r, cus, a2d::scratch_offered() ? cap_of(rows * (H + 2)) : 1);
+  a2d::ScoredPlan plan = plan_scored_fwd_of(dd, r, cus, a2d::scratch_offered());
   if (plan.parts > 1) {
     N = static_cast<float*>(a2d::scratch_get((size_t)plan.parts * rows * (H + 2) * sizeof(float)));
     if (N) {
@@ -802,7 +812,7 @@ a2d_status a2d_partial_fwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, c
       tl = tm + plan.parts * rows;
     } else {
       N = static_cast<float*>(out0);
-      plan = plan_of(dd, r, cus, 1);
+      plan = plan_scored_fwd_of(dd, r, cus, false);
     }
   }
   const a2d::FwdInput in{static_cast<const float*>(out0), out1, out2};
@@ -855,21 +865,20 @@ a2d_status a2d_partial_bwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, c
   int cus = 0;
   A2D_TRY(hip_result(a2d::device_cus(&cus), who));
   const bool offered = a2d::scratch_offered();
+  a2d::ScoredBwdPlan plan = plan_scored_bwd_of(dd, r, cus, offered);
   if (dd.dtype == A2D_BF16) {
-    a2d::ScoredBwdPlan plan = a2d::plan_scored_bwd(dd, r, cus, offered ? kScoredParts : 0);
     const size_t bytes = a2d::scored_bwd_scratch(dd, r, plan);
     void* more = nullptr;
-    if (bytes && !(more = a2d::scratch_get(bytes))) plan = a2d::plan_scored_bwd(dd, r, cus, 0);
+    if (bytes && !(more = a2d::scratch_get(bytes))) plan = plan_scored_bwd_of(dd, r, cus, false);
     A2D_TRY(hip_result(a2d::launch_scored_bwd(a2d::PREPARE, dd, r, plan, Q, K, V, O, dO, lse, workspace, more, dQ, dK, dV, s), who));
     a2d::trace_mark(s);
     return hip_result(a2d::launch_scored_bwd(a2d::LAUNCH, dd, r, plan, Q, K, V, O, dO, lse, workspace, more, dQ, dK, dV, s), who);
   }
   const int64_t nq = (int64_t)dd.heads * dd.nq * dd.hdim, nk = (int64_t)kv_heads * dd.nkv * dd.hdim;
-  a2d::ScoredBwdPlan plan = a2d::plan_scored_bwd_f32(dd, r, cus, offered ? scored_cap(nq) : 1, offered ? scored_cap(nk) : 1);
   const int64_t dq_floats = plan.q > 1 ? plan.q * nq : 0, kv_floats = plan.kv > 1 ? plan.kv * nk : 0;
   float* more = nullptr;
   if (dq_floats + kv_floats > 0 && !(more = static_cast<float*>(a2d::scratch_get((size_t)(dq_floats + 2 * kv_floats) * sizeof(float)))))
-    plan = a2d::plan_scored_bwd_f32(dd, r, cus, 1, 1);
+    plan = plan_scored_bwd_of(dd, r, cus, false);
   float* const dq = plan.q > 1 ? more : static_cast<float*>(dQ);
   float* const dk = plan.kv > 1 ? more + dq_floats : static_cast<float*>(dK);
   float* const dv = plan.kv > 1 ? dk + kv_floats : static_cast<float*>(dV);
@@ -1085,6 +1094,23 @@ a2d_status tile_route(const a2d_tile_desc& desc, int kv_heads, int nseg, const a
   const BwdPlan p = plan_bwd(desc, g, ds, cus, scratch, (flags & ROUTE_SPLIT_GROUPS) != 0 ? split_cap(g.group) : 1);
   route_bwd(desc, p.parts, out);
   if (p.parts.kv > 1 || p.parts.q > 1) out->kernel[out->kernels++] = "sum_parts_kernel";
+  return A2D_OK;
+}
+
+a2d_status scored_route(const a2d_tile_desc& desc, int kv_heads, const a2d_score_rules& rules, int flags, int cus, ScoredRoute* out) {
+  const char* who = "scored_route";
+  A2D_TRY(check_desc(&desc, who));
+  ScoreRules r;
+  A2D_TRY(make_rules(&desc, kv_heads, &rules, who, &r));
+  if (cus == 0) A2D_TRY(hip_result(device_cus(&cus), who));
+  const bool f32 = desc.dtype == A2D_F32, scratch = (flags & ROUTE_SCRATCH) != 0;
+  if ((flags & ROUTE_BACKWARD) == 0) {
+    const ScoredPlan plan = plan_scored_fwd_of(desc, r, cus, scratch);
+    (f32 ? route_scored_fwd_f32 : route_scored_fwd)(desc, r, plan, out);
+    if (plan.parts > 1) out->kernel[out->kernels++] = "fix_kernel";
+  } else {
+    (f32 ? route_scored_bwd_f32 : route_scored_bwd)(desc, r, plan_scored_bwd_of(desc, r, cus, scratch), out);
+  }
   return A2D_OK;
 }
 

@@ -35,6 +35,20 @@ enum RouteFlags { ROUTE_BACKWARD = 1, ROUTE_KEEP_DS = 2, ROUTE_SPLIT_GROUPS = 4,
 a2d_status tile_route(const a2d_tile_desc& desc, int kv_heads, int nseg, const a2d_kv_segment* segs, int flags, int cus,
                       Route* out);
 
+// How a tile call under score rules goes out
+struct ScoredRoute {
+  const char* kernel[4];
+  int kernels;
+  int rows, lanes, waves;        // of a forward or dQ workgroup: query rows, key lanes, wavefronts
+  int order;                     // a forward's blocks: 0 the heads one after another, 1 late rows first, 2 by the documents' lengths
+  int blocks_q, units_q;         // row blocks of a head; workgroups for them
+  int blocks_kv, units_kv;       // a backward's key blocks of a key/value head; workgroups for them
+  int shared_q, shared_kv;       // the units in proportion to the blocks' walks
+  int fine;                      // P (and dZ) contracted as two bf16 numbers each
+};
+// rules: its pointers say only what is there, they are not read.  flags: ROUTE_BACKWARD, ROUTE_SCRATCH
+a2d_status scored_route(const a2d_tile_desc& desc, int kv_heads, const a2d_score_rules& rules, int flags, int cus, ScoredRoute* out);
+
 struct GridProblem {
   int heads, kv_heads, seq, side, hdim, causal, cyclic;
   float scale;

@@ -2,6 +2,7 @@
 // of keys that a query row sees, and their launchers.
 #pragma once
 #include "a2d_common.hpp"
+#include "a2d_grid.hpp"
 
 namespace a2d {
 
@@ -119,6 +120,12 @@ size_t scored_bwd_scratch(const a2d_tile_desc& d, const ScoreRules& r, const Sco
 hipError_t launch_scored_bwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K,
                              const void* V, const void* O, const void* dO, const float* lse, void* ws, void* more, void* dQ, void* dK,
                              void* dV, hipStream_t s);
+
+// what a call's plan makes of it (kernels and launches of these files alone)
+void route_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, ScoredRoute* out);
+void route_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, ScoredRoute* out);
+void route_scored_fwd_f32(const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, ScoredRoute* out);
+void route_scored_bwd_f32(const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, ScoredRoute* out);
 
 // the same for fp32 (a2d_scored_f32.hip; plan.form: 1 or 2 tiles of 16 rows a workgroup)
 ScoredPlan plan_scored_fwd_f32(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap);

@@ -894,6 +894,23 @@ ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int c
 // 2^22 scores and more it was 1.46 at the most (250 calls), and 4619 x 543, 2 of 80, would take 46 us for 41.
 static bool fine_call(const a2d_tile_desc& d) { return (int64_t)d.heads * d.nq * d.nkv <= (int64_t)1 << 22; }
 
+void route_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, ScoredRoute* out) {
+  const BwdCuts c(d, r, plan);
+  *out = ScoredRoute{};
+  for (const char* k : {"scored_dq_kernel", "scored_dkdv_kernel"}) out->kernel[out->kernels++] = k;
+  if (c.q_floats + c.kv_floats) out->kernel[out->kernels++] = "scored_sum_kernel";
+  out->rows = c.bm;
+  out->lanes = plan.lanes;
+  out->waves = 8;
+  out->blocks_q = c.q.blocks;
+  out->units_q = c.q.units;
+  out->blocks_kv = c.kv.blocks;
+  out->units_kv = c.kv.units;
+  out->shared_q = plan.share_q;
+  out->shared_kv = plan.share_kv;
+  out->fine = fine_call(d);
+}
+
 hipError_t launch_scored_bwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, const void* Q, const void* K,
                              const void* V, const void* O, const void* dO, const float* lse, void* ws, void* more, void* dQ, void* dK,
                              void* dV, hipStream_t s) {

@@ -553,6 +553,30 @@ ScoredBwdPlan plan_scored_bwd_f32(const a2d_tile_desc& d, const ScoreRules& r, i
                        best_parts(k, cap_kv, 4.6, (double)(d.heads / r.group) * d.nkv * d.hdim * 16 / 4.9e6, nullptr)};
 }
 
+void route_scored_fwd_f32(const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, ScoredRoute* out) {
+  const int bm = BLK * plan.form;
+  const RowMap map = row_map(d, r, bm, plan.parts);
+  *out = ScoredRoute{};
+  out->kernel[out->kernels++] = "scored_fwd_f32_kernel";
+  out->rows = bm;
+  out->lanes = out->waves = KL;
+  out->order = map.by_size ? BY_ROWS : 0;
+  out->blocks_q = map.sub * ((map.rows + bm - 1) / bm);
+  out->units_q = out->blocks_q * plan.parts;
+}
+void route_scored_bwd_f32(const a2d_tile_desc& d, const ScoreRules&, const ScoredBwdPlan& plan, ScoredRoute* out) {
+  *out = ScoredRoute{};
+  for (const char* k : {"scored_dq_f32_kernel", "scored_dkdv_f32_kernel"}) out->kernel[out->kernels++] = k;
+  out->rows = 2 * BLK;
+  out->lanes = 2;
+  out->waves = KL;
+  out->blocks_q = (d.nq + 31) / 32;
+  out->units_q = out->blocks_q * plan.q;
+  out->blocks_kv = (d.nkv + BLK - 1) / BLK;
+  out->units_kv = out->blocks_kv * plan.kv;
+  if (plan.q > 1 || plan.kv > 1) out->kernel[out->kernels++] = "sum_parts_kernel";
+}
+
 #define A2D_HEADS(CALL)              \
   switch (d.hdim) {                  \
     case 128: return CALL(128);      \

@@ -715,6 +715,20 @@ ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus,
   return best;
 }
 
+void route_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, ScoredRoute* out) {
+  const int bm = kRows[plan.form];
+  const RowMap map = row_map(d, r, bm, plan.parts);
+  *out = ScoredRoute{};
+  out->kernel[out->kernels++] = plan.form == SCORED_32 ? "scored_fwd_small_kernel" : "scored_fwd_kernel";
+  out->rows = bm;
+  out->lanes = plan.form == SCORED_32 ? 8 : plan.form == SCORED_LANES ? 2 : 1;
+  out->waves = plan.form == SCORED_PAIRS ? 4 : 8;
+  out->order = plan.form == SCORED_32 && map.by_size ? BY_ROWS : map.by_size;
+  out->blocks_q = map.sub * ((map.rows + bm - 1) / bm);
+  out->units_q = out->blocks_q * plan.parts;
+  out->fine = plan.form == SCORED_32;
+}
+
 hipError_t launch_scored_fwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, const void* Q, const void* K,
                              const void* V, float* out0, float* out1, float* out2, const FwdInput& in, hipStream_t s) {
 #define A2D_RULES(HR)                                                                                  \

@@ -971,6 +971,46 @@ PyObject* tile_route(Args a) {
   return route_dict(r);
 }
 
+// heads, kv_heads, nq, nkv, hdim, dtype, q_off, kv_off, causal, softcap, slopes, range_sets, token_step, flags, compute_units
+PyObject* scored_route(Args a) {
+  a2d_tile_desc d{};
+  d.heads = (int32_t)integer(a[0]);
+  d.nq = (int32_t)integer(a[2]);
+  d.nkv = (int32_t)integer(a[3]);
+  d.hdim = (int32_t)integer(a[4]);
+  d.dtype = dtype_code(dtype_arg(a[5]));
+  d.q_off = integer(a[6]);
+  d.kv_off = integer(a[7]);
+  d.causal = truth(a[8]);
+  d.scale = scale_of(Py_None, d.hdim);
+  static const int32_t some[4] __attribute__((aligned(16))) = {};      // (in place of what a call would give; never read)
+  a2d_score_rules r{};
+  r.softcap = (float)number(a[9]);
+  r.slopes = truth(a[10]) ? reinterpret_cast<const float*>(some) : nullptr;
+  r.range_sets = int32_of(a[11], "range_sets");
+  r.ranges = r.range_sets ? some : nullptr;
+  if (!r.ranges) r.range_sets = 1;
+  r.token_step = int32_of(a[12], "token_step");
+  a2d::ScoredRoute o;
+  check(a2d::scored_route(d, (int)integer(a[1]), r, (int)integer(a[13]), (int)integer(a[14]), &o));
+  PyObject* k = PyTuple_New(o.kernels);
+  if (!k) throw PythonError();
+  for (int i = 0; i < o.kernels; ++i) {
+    PyObject* name = PyUnicode_FromString(o.kernel[i]);
+    if (!name) {
+      Py_DECREF(k);
+      throw PythonError();
+    }
+    PyTuple_SET_ITEM(k, i, name);
+  }
+  PyObject* m = Py_BuildValue("{s:N,s:i,s:i,s:i,s:i,s:i,s:i,s:i,s:i,s:N,s:N,s:N}", "kernels", k, "rows", o.rows, "lanes", o.lanes,
+                              "waves", o.waves, "order", o.order, "blocks_q", o.blocks_q, "units_q", o.units_q, "blocks_kv", o.blocks_kv,
+                              "units_kv", o.units_kv, "shared_q", PyBool_FromLong(o.shared_q), "shared_kv", PyBool_FromLong(o.shared_kv),
+                              "fine", PyBool_FromLong(o.fine));
+  if (!m) throw PythonError();
+  return m;
+}
+
 // heads, kv_heads, seq, side, hdim, causal, cyclic, backward, compute_units
 PyObject* grid_route(Args a) {
   const int64_t heads = integer(a[0]), kv_heads = integer(a[1]), seq = integer(a[2]), hdim = integer(a[4]);
@@ -1018,7 +1058,7 @@ PyMethodDef g_methods[] = {
     A2D_ENTRY(attnfix, 4),         A2D_ENTRY(fix_bwd, 3),          A2D_ENTRY(grid_forward, 7),
     A2D_ENTRY(grid_backward, 10),  A2D_ENTRY(tile_route, 12),      A2D_ENTRY(grid_route, 9),
     A2D_ENTRY(partial_fwd_scored, 14), A2D_ENTRY(partial_bwd_scored, 18), A2D_ENTRY(document_ranges, 7),
-    A2D_ENTRY(rotary, 8),
+    A2D_ENTRY(rotary, 8),           A2D_ENTRY(scored_route, 15),
     {"set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

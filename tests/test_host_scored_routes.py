@@ -1,0 +1,59 @@
+"""How calls under score rules go out (binding.scored_route: the library's own plans, on the CPU), and that the GPU tests' cases take the
+forms that they are there for.  256 compute units, as on MI355X."""
+import random
+
+import pytest
+
+from test_gpu_scored_forms import BACKWARD, FORWARD, name_of
+
+CUS = 256
+
+
+@pytest.fixture(scope="module")
+def a2d():
+    from paper_2503_15758_amd import binding
+    binding._ext()
+    return binding
+
+
+def route(a2d, heads, kvh, nq, nkv, H, more, **kw):
+    rules = {k: more[k] for k in ("q_off", "kv_off", "causal", "softcap") if k in more}
+    return a2d.scored_route(heads, nq, nkv, H, kv_heads=kvh, slopes="slopes" in more, range_sets=int("docs" in more), compute_units=CUS, **rules, **kw)
+
+
+@pytest.mark.parametrize("case", FORWARD, ids=name_of)
+def test_forward_forms(a2d, case):
+    form, order, split = case[6:]
+    r = route(a2d, *case[:6])
+    assert (r["rows"], r["lanes"], r["waves"]) == form and r["order"] == order
+    assert (r["units_q"] > r["blocks_q"]) == split and r["kernels"] == ("scored_fwd_kernel",) + ("fix_kernel",) * split
+
+
+@pytest.mark.parametrize("case", BACKWARD, ids=name_of)
+def test_backward_forms(a2d, case):
+    lanes, shared_q, cut_q, shared_kv, cut_kv = case[6:]
+    r = route(a2d, *case[:6], backward=True)
+    assert (r["lanes"], r["rows"]) == (lanes, 256 // lanes)
+    assert (r["shared_q"], r["units_q"] > r["blocks_q"]) == (shared_q, cut_q)
+    assert (r["shared_kv"], r["units_kv"] > r["blocks_kv"]) == (shared_kv, cut_kv)
+    assert ("scored_sum_kernel" in r["kernels"]) == (cut_q or cut_kv)
+
+
+def test_every_form_is_there():
+    forms = {c[6] for c in FORWARD}
+    assert len(forms) == 3 and len({(c[6], c[8]) for c in FORWARD}) == 6
+    assert len({(c[6], c[4]) for c in FORWARD}) == 12                              # head sizes
+    for rule in ("slopes", "softcap"):
+        assert len({(c[6], rule in c[5]) for c in FORWARD}) == 6
+
+
+def test_without_memory_nothing_is_in_parts(a2d):
+    rng = random.Random(2)
+    for _ in range(300):
+        kv = int(2 ** rng.uniform(0, 5))
+        heads = kv * rng.choice([1, 1, 4])
+        nq, nkv = (int(2 ** rng.uniform(0, 13)) for _ in range(2))
+        more = dict(causal=rng.random() < 0.5, **(dict(docs=()) if rng.random() < 0.4 else {}))
+        for backward in (False, True):
+            r = route(a2d, heads, kv, nq, nkv, 128, more, backward=backward, scratch=False)
+            assert r["units_q"] == r["blocks_q"] and r["units_kv"] == r["blocks_kv"], (heads, kv, nq, nkv, more)
