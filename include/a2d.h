@@ -368,8 +368,10 @@ typedef struct {
  *     desc->flags must be 0.  workspace: at least a2d_workspace_bytes(desc, A2D_OP_PARTIAL_BWD_SCORED, 0) bytes.
  *     Neither the slopes nor the ranges have gradients.
  * Partials merge as those of the plain calls do (a2d_fix, a2d_attnfix, a2d_fix_norm; lse and O of the merged rows go into the
- * backward call).  bf16 inputs: the probabilities and dZ are rounded to bf16 in front of their contractions
- * (a forward call of few rows, a backward call of few scores: taken as two bf16 numbers each), all else is fp32.
+ * backward call).  bf16 inputs: the probabilities and dZ are rounded to bf16 in front of their contractions, all else is fp32.
+ * Taken as two bf16 numbers each (2^-17 off) are those of a forward call of up to 32 query rows for each key/value head, and of
+ * a backward call of heads * nq * nkv <= 2^22; of larger forward calls, those that go to workgroups of 32 rows, which goes
+ * by sizes and rules alone, not by the memory for partial results.
  * Rows of Q, O, dO that see no key, and keys in front of the first or behind the last one that any row sees, may hold
  * anything (NaN, uninitialised cache): they are not read or have no effect, and their gradients are 0.
  * With slopes no distance |t_i - u_k| of the tile may exceed 2^24 (A2D_ERR_UNSUPPORTED): they are exact in fp32 up to there.

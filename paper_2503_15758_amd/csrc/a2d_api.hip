@@ -761,8 +761,8 @@ a2d_status make_rules(const a2d_tile_desc* d, int32_t kv_heads, const a2d_score_
 
 // The plans of a call, scratch: whether there is memory for partial results
 a2d::ScoredPlan plan_scored_fwd_of(const a2d_tile_desc& d, const a2d::ScoreRules& r, int cus, bool scratch) {
-  const int cap = scratch ? cap_of((int64_t)d.heads * d.nq * (d.hdim + 2)) : 1;
-  return d.dtype == A2D_F32 ? a2d::plan_scored_fwd_f32(d, r, cus, cap) : a2d::plan_scored_fwd(d, r, cus, cap);
+  const int cap = cap_of((int64_t)d.heads * d.nq * (d.hdim + 2));
+  return d.dtype == A2D_F32 ? a2d::plan_scored_fwd_f32(d, r, cus, scratch ? cap : 1) : a2d::plan_scored_fwd(d, r, cus, cap, scratch);
 }
 a2d::ScoredBwdPlan plan_scored_bwd_of(const a2d_tile_desc& d, const a2d::ScoreRules& r, int cus, bool scratch) {
   if (d.dtype == A2D_BF16) return a2d::plan_scored_bwd(d, r, cus, scratch ? kScoredParts : 0);

@@ -96,13 +96,14 @@ inline WalkKeys walk_keys(const a2d_tile_desc& d, const ScoreRules& r) {
 }
 
 // bf16 forward on the matrix units (a2d_scored_fwd.hip).  How a call goes out: the form of its workgroups, and how many
-// share a walk of the keys (their partials [parts][heads][nq] in place of the outputs, to be merged).
+// share a walk of the keys (their partials [parts][heads][nq] in place of the outputs, to be merged): `cap` at most, one without `scratch`.
 struct ScoredPlan {
   int form, parts;
+  bool fine;             // 32 rows: P as two bf16 numbers
 };
 enum { SCORED_256, SCORED_LANES, SCORED_PAIRS, SCORED_32 };   // 256 rows; 128 rows in two key lanes; 128 rows in four wavefronts, two
                                                               // workgroups a compute unit; 32 rows in eight key lanes
-ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap);
+ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap, bool scratch);
 hipError_t launch_scored_fwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, const void* Q, const void* K,
                              const void* V, float* out0, float* out1, float* out2, const FwdInput& in, hipStream_t s);
 

@@ -534,11 +534,11 @@ ScoredPlan plan_scored_fwd_f32(const a2d_tile_desc& d, const ScoreRules& r, int 
     const RowMap map = row_map(d, r, bm, 1);
     return (int64_t)(d.heads / r.group) * map.sub * ((map.rows + bm - 1) / bm);
   };
-  if (blocks(32) >= 4 * (int64_t)cus) return ScoredPlan{2, 1};
+  if (blocks(32) >= 4 * (int64_t)cus) return ScoredPlan{2, 1, false};
   constexpr double kStep[4] = {0.93, 1.11, 1.49, 1.99};
   const WalkKeys w = walk_keys(d, r);
   const WalkModel m{blocks(16), 2 * cus, w.mean / (BLK * KL) + 0.2, w.most / (BLK * KL) + 0.2, kStep[head_index(d.hdim)], 2.4, 0, 0, nullptr, 0, 0.5};
-  return ScoredPlan{1, best_parts(m, cap, 5.0, (double)d.heads * d.nq * (d.hdim + 2) * 8 / 4.6e6, nullptr)};
+  return ScoredPlan{1, best_parts(m, cap, 5.0, (double)d.heads * d.nq * (d.hdim + 2) * 8 / 4.6e6, nullptr), false};
 }
 
 ScoredBwdPlan plan_scored_bwd_f32(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap_q, int cap_kv) {

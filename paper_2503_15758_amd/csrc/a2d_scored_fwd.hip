@@ -428,7 +428,11 @@ constexpr int SB = 32;
 constexpr int STAT = 8 * 16 * 1024;                  // (slabs, at the end every wavefront's results) | m, l of every wavefront's rows
 constexpr int SMALL_LDS = STAT + 2 * 8 * SB * 4;
 
-template <int HR, bool CAP, bool BIAS>
+//
+// FINE: both halves of P are contracted, as two bf16 numbers (2^-17 off).  A row of few keys' weight shows the rounding of one: a token
+// against 1133 keys is off by 1.49 times what rounding the output alone does, and by 1.0 with two; the walk waits for memory meanwhile
+// (256 / 64 heads of 128 against up to 16384 keys: 67 us with either).
+template <int HR, bool CAP, bool BIAS, bool FINE>
 __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
     a2d_tile_desc d, ScoreRules r, RowMap map, const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
     const bf16_t* __restrict__ V, float* out0, float* out1, float* out2, FwdInput in) {
@@ -561,10 +565,9 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
         sm.take(s, was);
       }
     }
-    // (a row of few keys' weight shows their rounding, and the walk waits for memory: both halves of P are contracted.  A token against 1133
-    // keys: off by 1.49 times what rounding the output alone does with one half; 256 / 64 heads of 128 against up to 16384: 67 us with either)
     bf16x8 pb[1][2], rest[1][2];
-    sm.probabilities(s, pb, rest);
+    if constexpr (FINE) sm.probabilities(s, pb, rest);
+    else sm.probabilities(s, pb);
     __builtin_amdgcn_sched_barrier(0);
     if (more) wait_dma<LOADS>(); else wait_dma();    // V has arrived
 #pragma unroll
@@ -574,7 +577,7 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         o[t][q] = mma16(a, pb[0][q], o[t][q]);
-        o[t][q] = mma16(a, rest[0][q], o[t][q]);
+        if constexpr (FINE) o[t][q] = mma16(a, rest[0][q], o[t][q]);
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -669,7 +672,8 @@ hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const Score
   return plan.form == SCORED_256     ? run(scored_fwd_kernel<8, HR, 1, CAP, BIAS>)
          : plan.form == SCORED_LANES ? run(scored_fwd_kernel<8, HR, 2, CAP, BIAS>)
          : plan.form == SCORED_PAIRS ? run(scored_fwd_kernel<4, HR, 1, CAP, BIAS>)
-                                     : run(scored_fwd_small_kernel<HR, CAP, BIAS>);
+         : plan.fine                 ? run(scored_fwd_small_kernel<HR, CAP, BIAS, true>)
+                                     : run(scored_fwd_small_kernel<HR, CAP, BIAS, false>);
 }
 
 }  // namespace
@@ -681,7 +685,7 @@ hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const Score
 // a token of 256 heads of 64 against 16384 of 64: 67 with 32 rows in four parts, 180 in one, 330 with 256.  Ranges that the
 // host cannot see: one for all heads is taken for documents, which see a part of the keys each (749 x 9939: 13 us in one part, 21 where a plan
 // for whole walks split them); one a sequence for its filled length.
-ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap) {
+static ScoredPlan best_form(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap, bool rows_of_32) {
   constexpr struct {
     double step, by_head, fixed, pair;                // pair: both workgroups of a compute unit, of one's time
     int keys;
@@ -690,8 +694,9 @@ ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus,
   const WalkKeys walk = walk_keys(d, r);
   const double part_us = (double)d.heads * d.nq * (d.hdim + 2) * 8 / 4.5e6;
   double least = 0;
-  ScoredPlan best{SCORED_256, 1};
-  for (int f = 0; f < 4; ++f) {
+  ScoredPlan best{SCORED_32, 1, false};
+  const int only = rows_of_32 ? SCORED_32 : SCORED_256;
+  for (int f = only; f < 4; ++f) {
     const auto& form = kForms[f];
     const int bm = kRows[f];
     const bool packed = r.group > 1 && d.nq < bm;
@@ -707,12 +712,24 @@ ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus,
                       form.pair != 0 ? form.fixed : 0, nullptr, 0, 0.4};
     double t;
     const int parts = best_parts(m, cap, 4.5, part_us, &t);
-    if (f == 0 || t < least) {
+    if (f == only || t < least) {
       least = t;
-      best = ScoredPlan{f, parts};
+      best = ScoredPlan{f, parts, false};
     }
   }
   return best;
+}
+
+// How P is rounded is a matter of the call, not of the memory that there happens to be: fine are calls of few rows - a workgroup's 32 for
+// a key/value head, whatever is quickest - and those that go to 32 rows with memory for their parts.
+ScoredPlan plan_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap, bool scratch) {
+  const bool few = (r.group > 1 ? (int64_t)r.group * d.nq : d.nq) <= kRows[SCORED_32];
+  ScoredPlan plan = best_form(d, r, cus, cap, few);
+  plan.fine = plan.form == SCORED_32;
+  if (scratch || plan.parts == 1) return plan;
+  ScoredPlan whole = best_form(d, r, cus, 1, plan.fine);
+  whole.fine = plan.fine;
+  return whole;
 }
 
 void route_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, ScoredRoute* out) {
@@ -726,7 +743,7 @@ void route_scored_fwd(const a2d_tile_desc& d, const ScoreRules& r, const ScoredP
   out->order = plan.form == SCORED_32 && map.by_size ? BY_ROWS : map.by_size;
   out->blocks_q = map.sub * ((map.rows + bm - 1) / bm);
   out->units_q = out->blocks_q * plan.parts;
-  out->fine = plan.form == SCORED_32;
+  out->fine = plan.fine;
 }
 
 hipError_t launch_scored_fwd(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const ScoredPlan& plan, const void* Q, const void* K,

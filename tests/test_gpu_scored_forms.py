@@ -5,6 +5,7 @@ tests/scored_reference.py."""
 import pytest
 import torch
 
+import scored_reference
 from scored_reference import Scored, half_step, within
 from test_gpu_scored import check_fwd, documents, inputs, int32, slopes_of
 
@@ -132,3 +133,71 @@ def test_backward(a2d, case):
     # (1 is added first, or last: each of up to 33 partial sums is rounded next to it)
     within(out[0], plain[0].cpu().double() + 1.0, 40 * U * (1.0 + plain[0].cpu().double().abs()), "accumulated")
     assert torch.equal(out[1], plain[1]) and torch.equal(out[2], plain[2])
+
+
+# ---- P and dZ as two bf16 numbers each: h = x rounded to bf16, x - h is exact and below 2^-8 of x's power of two, so rounded it is off by
+# 2^-17 of x.  The sums' other errors as ever.
+TWO = 2.0 ** -17
+
+# heads, kv_heads, nq, nkv, H, rules ("lens": the lengths of caches, one for each run of heads)
+FINE = [
+    (32, 8, 1, 1133, 128, dict(softcap=30.0, lens=[1133])),
+    (32, 8, 1, 1133, 128, dict(softcap=30.0)),
+    (8, 2, 1, 2048, 128, dict(lens=[2048])),
+    (8, 8, 1, 4096, 96, dict(lens=[4001], slopes=True, q_off=4000)),
+    (12, 12, 5, 1300, 64, dict(lens=[1300, 40, 777])),
+    (2, 2, 1, 104, 64, dict(lens=[104])),
+    (16, 4, 8, 900, 80, dict(causal=True, q_off=892, softcap=8.0, slopes=True)),
+    (1, 1, 32, 5000, 128, dict(slopes=STEEP[4:5], q_off=4968)),
+    (2, 1, 130, 1000, 80, dict(softcap=20.0)),
+]
+
+
+def fine_rules(heads, nq, more):
+    rules = rules_of(None, heads, nq, {k: v for k, v in more.items() if k != "lens"})
+    if "lens" in more:
+        rules["ranges"] = int32([[[0, n]] * nq for n in more["lens"]])
+    return rules
+
+
+@pytest.mark.parametrize("case", FINE, ids=name_of)
+def test_probabilities_as_two_numbers(a2d, monkeypatch, case):
+    heads, kvh, nq, nkv, H, more = case
+    print("two numbers", case, flush=True)
+    Q, K, V, _ = inputs(heads, kvh, nq, nkv, H, "bf16", sigma=3.0 if "softcap" in more else 1.0)
+    rules = fine_rules(heads, nq, more)
+    s = Scored(Q, K, V, **rules)
+    with monkeypatch.context() as m:
+        m.setattr(scored_reference, "half_step", lambda dtype: TWO)
+        ref = s.partial()
+    # (one number would be outside; a row whose weight one key has holds 1, which is one)
+    w = torch.exp(s.s - ref["m"].unsqueeze(2))
+    once = w.bfloat16().double() @ s.V / ref["l"].unsqueeze(2)
+    assert ((once - ref["O"]).abs() > ref["e_O"]).any() or ref["l"].max() < 1 + 2.0 ** -20
+    check_fwd(a2d.partial_fwd_scored(Q, K, V, **rules), ref, False, Q.dtype, str(case))
+    out = (torch.zeros(heads, nq, H, device="cuda"), torch.full((heads, nq), -float("inf"), device="cuda"), torch.zeros(heads, nq, device="cuda"))
+    check_fwd(a2d.partial_fwd_scored(Q, K, V, out=out, accumulate=True, **rules), ref, False, Q.dtype, str(case))
+
+
+@pytest.mark.parametrize("case", [(32, 8, 40, 100, 128, dict(softcap=30.0)), (4, 1, 349, 193, 80, dict(slopes=True, q_off=20)), (2, 2, 1000, 700, 64, dict(causal=True)),
+                                  (3, 3, 300, 290, 96, dict(docs=DOCS, softcap=9.0, slopes=True))], ids=name_of)
+def test_gradients_as_two_numbers(a2d, monkeypatch, case):
+    heads, kvh, nq, nkv, H, more = case
+    print("two numbers, gradients", case, flush=True)
+    Q, K, V, dO = inputs(heads, kvh, nq, nkv, H, "bf16")
+    rules = rules_of(a2d, heads, nq, more)
+    s = Scored(Q, K, V, **rules)
+    f = s.partial()
+    O, lse = f["O"].to(Q.dtype).cuda(), f["lse"].float().cuda()
+    with monkeypatch.context() as m:
+        m.setattr(scored_reference, "half_step", lambda dtype: TWO)
+        want = s.gradients(O, dO, lse)
+    g, L = dO.cpu().double(), lse.cpu().double().unsqueeze(2)
+    p = torch.exp(s.s - L).nan_to_num(0.0)
+    dz = s.scale * p * (g @ s.V.transpose(1, 2) - (g * O.cpu().double()).sum(2, keepdim=True)) * s.dy
+    by_kv = lambda x: x.view(-1, s.group, *x.shape[1:]).sum(1)
+    for n, once in (("dQ", dz.bfloat16().double() @ s.K), ("dK", by_kv(dz.bfloat16().double().transpose(1, 2) @ s.Q)),
+                    ("dV", by_kv(p.bfloat16().double().transpose(1, 2) @ g))):
+        assert ((once - want[n]).abs() > want["e_" + n]).any(), n
+    for x, n in zip(a2d.partial_bwd_scored(Q, K, V, O, dO, lse, **rules), ("dQ", "dK", "dV")):
+        within(x, want[n], want["e_" + n], "%s %s" % (case, n))

@@ -4,7 +4,7 @@ import random
 
 import pytest
 
-from test_gpu_scored_forms import BACKWARD, FORWARD, name_of
+from test_gpu_scored_forms import BACKWARD, FINE, FORWARD, name_of
 
 CUS = 256
 
@@ -18,7 +18,8 @@ def a2d():
 
 def route(a2d, heads, kvh, nq, nkv, H, more, **kw):
     rules = {k: more[k] for k in ("q_off", "kv_off", "causal", "softcap") if k in more}
-    return a2d.scored_route(heads, nq, nkv, H, kv_heads=kvh, slopes="slopes" in more, range_sets=int("docs" in more), compute_units=CUS, **rules, **kw)
+    return a2d.scored_route(heads, nq, nkv, H, kv_heads=kvh, slopes="slopes" in more,
+                            range_sets=len(more["lens"]) if "lens" in more else int("docs" in more), compute_units=CUS, **rules, **kw)
 
 
 @pytest.mark.parametrize("case", FORWARD, ids=name_of)
@@ -57,3 +58,32 @@ def test_without_memory_nothing_is_in_parts(a2d):
         for backward in (False, True):
             r = route(a2d, heads, kv, nq, nkv, 128, more, backward=backward, scratch=False)
             assert r["units_q"] == r["blocks_q"] and r["units_kv"] == r["blocks_kv"], (heads, kv, nq, nkv, more)
+
+
+@pytest.mark.parametrize("case", FINE, ids=name_of)
+def test_two_numbers(a2d, case):
+    for scratch in (False, True):
+        r = route(a2d, *case, scratch=scratch)
+        assert r["fine"] and r["kernels"][0] == "scored_fwd_small_kernel"
+
+
+def test_rounding_does_not_go_by_memory(a2d):
+    """The results of a call without memory for partial results are the same up to the order of fp32 sums: P and dZ are rounded alike.  Up to 32
+    rows for each key/value head are taken as two numbers, in a forward, and up to 2^22 scores in a backward."""
+    rng, kinds = random.Random(3), set()
+    for _ in range(3000):
+        kv = int(2 ** rng.uniform(0, 6))
+        heads = kv * rng.choice([1, 1, 2, 4, 8])
+        nq, nkv = int(2 ** rng.uniform(0, rng.choice([5, 13]))), int(2 ** rng.uniform(4, 14))
+        more = dict(causal=rng.random() < 0.4, q_off=rng.randint(0, nkv), **(dict(slopes=True) if rng.random() < 0.5 else {}),
+                    **rng.choice([dict(), dict(docs=()), dict(lens=[1] * kv)]))
+        case = (heads, kv, nq, nkv, rng.choice([64, 80, 96, 128]), more)
+        with_, without = (route(a2d, *case, scratch=x) for x in (True, False))
+        assert with_["fine"] == without["fine"], case
+        assert with_["fine"] == (with_["kernels"][0] == "scored_fwd_small_kernel"), case
+        if (heads // kv if heads > kv else 1) * nq <= 32:
+            assert with_["fine"], case
+        kinds.add((with_["fine"], with_["kernels"][0] == without["kernels"][0], without["kernels"][0]))
+        if nkv > 1:
+            assert route(a2d, *case, backward=True)["fine"] == (heads * nq * nkv <= 1 << 22)
+    assert len(kinds) == 3, kinds                                                   # (other forms without memory among them)
