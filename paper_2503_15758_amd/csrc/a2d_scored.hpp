@@ -84,6 +84,12 @@ __device__ __forceinline__ float cap_log2_f32(const CapArgs& a, float z) {
   return fabsf(z) <= a.small ? y : cap_beyond(a, z);
 }
 
+// Ranges that the host cannot see: one set for all heads is taken for documents, which see a part of the keys each, where a head's rows are
+// more than a workgroup's.  Fewer (new tokens against a cache) lie in one document or two, and the set may as well be a cache's
+// filled length, which they see all of.  One sequence's 16384 keys, heads of 128, planned for all of them and for documents: 100 rows of 32 / 8
+// heads 41 us and 63, their gradients 127 and 142; those of a token of 8 heads 56 and 429.
+inline bool taken_for_documents(const a2d_tile_desc& d, const ScoreRules& r) { return r.ranges && r.heads_per_set == d.heads && d.nq > 128; }
+
 // keys of a row's walk, on average and at most, as far as sizes and the causal mask tell
 struct WalkKeys {
   double mean, most;

@@ -832,7 +832,7 @@ size_t scored_bwd_scratch(const a2d_tile_desc& d, const ScoreRules& r, const Sco
 // of four even parts 56; 746 x 895, 4 / 1 of 64: shared out 28, even 22 (finding out the shares takes some 3 us).
 ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, size_t most_bytes) {
   constexpr double kFindOut = 4.0, kSum = 5.0, kBytes = 6e6;             // us; bytes of partials a us, out and back
-  const bool documents = r.ranges && r.heads_per_set == d.heads;
+  const bool documents = taken_for_documents(d, r);
   const int rules = (r.cap != 0.f) + (r.slopes != nullptr), kvh = d.heads / r.group;
   const double by_head = d.hdim / 128.0, all_rows = (double)d.nq * r.group, alike = std::min(1.0, (double)d.nkv / d.nq);
   const WalkKeys w = walk_keys(d, r);
@@ -854,7 +854,7 @@ ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int c
     const double mean = walks.mean / of + 0.2, most = walks.most / of + 0.2, unit_us = bm * d.hdim * 8.0 * results / kBytes;
     const double blind = documents ? 1.2 : 1.0;                          // walks in no order
     const int64_t room = split ? (int64_t)(most_bytes / ((size_t)heads * bm * d.hdim * sizeof(float))) : 0;
-    const bool uneven = n > 1 && n <= MAX_RANKED && blocks_by_size(d, r, n) != 0;
+    const bool uneven = n > 1 && n <= MAX_RANKED && (documents || !r.ranges) && blocks_by_size(d, r, n) != 0;
     const WalkModel whole{(int64_t)heads * n, cus, mean, most, step, fixed, 0, 0, nullptr, 0, 0.1};
     Way best{n, false, walk_time(whole, 1) * blind};
     for (int x = 4; x <= 128; x += x < 8 ? 1 : x < 32 ? 4 : 16) {        // quarters of n

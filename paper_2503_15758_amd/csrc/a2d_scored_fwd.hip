@@ -703,7 +703,7 @@ static ScoredPlan best_form(const a2d_tile_desc& d, const ScoreRules& r, int cus
     const int64_t blocks = packed ? (int64_t)kv_heads * (((int64_t)r.group * d.nq + bm - 1) / bm)
                                   : (int64_t)d.heads * ((d.nq + bm - 1) / bm);
     double most = walk.most, mean = packed ? most : walk.mean;
-    if (r.ranges && r.heads_per_set == d.heads && !packed) {
+    if (taken_for_documents(d, r) && !packed) {
       most *= 0.35;
       mean *= 0.25;
     }

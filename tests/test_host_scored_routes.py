@@ -87,3 +87,17 @@ def test_rounding_does_not_go_by_memory(a2d):
         if nkv > 1:
             assert route(a2d, *case, backward=True)["fine"] == (heads * nq * nkv <= 1 << 22)
     assert len(kinds) == 3, kinds                                                   # (other forms without memory among them)
+
+
+def test_one_sequence_is_no_documents(a2d):
+    """A set of ranges for a few new rows is a cache's filled length as well: they are planned for all of it, as without ranges, or in a batch
+    with another sequence."""
+    rng = random.Random(4)
+    same = ("kernels", "rows", "lanes", "waves", "blocks_q", "units_q", "blocks_kv", "units_kv", "shared_q", "shared_kv")
+    for _ in range(500):
+        kv = 2 * int(2 ** rng.uniform(0, 5))
+        case = (kv * rng.choice([1, 1, 4]), kv, int(2 ** rng.uniform(0, 7)), int(2 ** rng.uniform(4, 14)), rng.choice([64, 80, 96, 128]))
+        for backward in (False, True):
+            one, none, two = (route(a2d, *case, dict(lens=[case[3]] * n) if n else {}, backward=backward) for n in (1, 0, 2))
+            for k in same:
+                assert one[k] == none[k] == two[k], (case, backward, k)
