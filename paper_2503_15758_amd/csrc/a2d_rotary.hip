@@ -3,13 +3,14 @@
 // The angle of a pair is a position times a frequency.  Taken as a part of a turn it needs only what is left of the product
 // behind its whole turns, so the frequency comes as a 64-bit fixed-point part of a turn (2^-64 units, made on the host)
 // and the product is formed modulo 2^64: one wrapping multiplication, no reduction, and a position of 2^31 is off by
-// 2^-33 turns at most.  The top 32 bits, read as a signed number, are the angle in -1/2 .. 1/2 turns.  Results of 16
-// bits take the hardware's sine and cosine, whose argument is in turns (their error, some 2^-20, is far below half a step of
-// the result); fp32 results take sincospif.
+// 2^-33 turns at most.  Of the product, what is left of the nearest quarter turn becomes an fp32 number, so that it loses 2^-24 of
+// itself, wherever the angle is: a sine near half a turn is as good as one near none.  Sine and cosine of up to an eighth
+// of a turn are the first terms of their series (see sine_cosine).
 //
 // Bound: HBM, each value read and written once.  A thread owns eight pairs of a row (two 16-byte pieces a head in bf16):
 // it makes their sines and cosines once and walks over heads, as many as still leave the chip full of wavefronts.  32 + 8 heads of 128, 16384
-// rows, packed: 69 us, 4.86 TB/s; 24 + 24 of 80, 2999 rows, fp32 to bf16: 14.7 us, 4.7 TB/s; a token of 256 + 64 heads: 3.3 us, host 6.7.
+// rows, packed: 70 us, 4.8 TB/s; 24 + 24 of 80, 2999 rows, fp32 to bf16: 14.9 us, 4.6 TB/s; a token of 256 + 64 heads: 3.3 us, host 6.2 to
+// 7.2.  (With the hardware's sine and cosine, some 2^-20 of a whole one off, where a low frequency's is 2^-13: 69.6 and 14.7.)
 #include "a2d_scored.hpp"
 
 namespace a2d {
@@ -57,6 +58,19 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
 }
 
+// Sine and cosine of `part` 2^-64 turns: a number of quarter turns, and t = -pi/4 .. pi/4 beyond, as fp32.  The series end at t^9 / 9! and
+// t^10 / 10!: what is left off is 2^-28 of the sine and 2^-32 of the cosine at the most; with the roundings 4 half steps of either.
+__device__ __forceinline__ void sine_cosine(uint64_t part, float& sn, float& cs) {
+  const unsigned quarter = (unsigned)((part + ((uint64_t)1 << 61)) >> 62);
+  const float t = (float)(int64_t)(part - ((uint64_t)quarter << 62)) * 0x1.921fb6p-62f, u = t * t;     // 2 pi 2^-64
+  const float s = fmaf(t * u, fmaf(u, fmaf(u, fmaf(u, 1 / 362880.f, -1 / 5040.f), 1 / 120.f), -1 / 6.f), t);
+  const float c = fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, -1 / 3628800.f, 1 / 40320.f), -1 / 720.f), 1 / 24.f), -0.5f), 1.f);
+  sn = quarter & 1 ? c : s;
+  cs = quarter & 1 ? s : c;
+  if (quarter & 2) sn = -sn;
+  if ((quarter + 1) & 2) cs = -cs;
+}
+
 // (x and y may be the same memory: a thread reads its pieces of a head before it writes them, and no other thread touches them)
 template <typename TI, typename TO, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Turns turns) {
@@ -71,14 +85,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Turns turns) 
   for (int i = 0; i < 8; ++i) {
     const int p = min(p0 + i, a.pairs - 1);
     const int64_t at = pos[(int64_t)turns.axis[p] * a.rows];
-    const int part = (int)(uint32_t)(((uint64_t)at * turns.step[p]) >> 32);
-    const float turn = (float)part * 0x1p-32f;
-    if constexpr (sizeof(TO) == 2) {
-      sn[i] = __builtin_amdgcn_sinf(turn);
-      cs[i] = __builtin_amdgcn_cosf(turn);
-    } else {
-      sincospif(2.f * turn, &sn[i], &cs[i]);
-    }
+    sine_cosine((uint64_t)at * turns.step[p], sn[i], cs[i]);
     if (a.inverse) sn[i] = -sn[i];
   }
   const int at0 = INTERLEAVED ? 2 * p0 : p0, at1 = INTERLEAVED ? 2 * p0 + 8 : p0 + a.half;
