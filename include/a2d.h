@@ -415,7 +415,7 @@ typedef struct {
   int32_t interleaved;      /* 0 or 1 */
   int32_t inverse;          /* 0 or 1 */
   int32_t pad;              /* must be 0 */
-  const double* freqs;      /* HOST [pairs], finite                                                                  */
+  const double* freqs;      /* HOST [pairs], each below 2^64 in size                                                 */
   const uint8_t* axis;      /* HOST [pairs], each < axes; NULL: all 0                                                */
   const int32_t* positions; /* DEVICE [sets][axes][rows]; any sign                                                   */
 } a2d_rotary_desc;

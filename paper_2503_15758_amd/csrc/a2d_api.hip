@@ -928,7 +928,7 @@ a2d_status a2d_rotary(const a2d_rotary_desc* desc, int n, const a2d_rotary_tenso
     return fail(A2D_ERR_INVALID_ARG, "%s: interleaved and inverse must be 0 or 1, pad 0", who);
   A2D_TRY(check_ptr(d.positions, who, "positions"));
   for (int p = 0; p < d.pairs; ++p) {
-    if (!std::isfinite(d.freqs[p])) return fail(A2D_ERR_INVALID_ARG, "%s: freqs[%d] is not finite", who, p);
+    if (!(std::fabs(d.freqs[p]) < 0x1p64)) return fail(A2D_ERR_INVALID_ARG, "%s: freqs[%d]=%g is not below 2^64", who, p, d.freqs[p]);
     if (d.axis && d.axis[p] >= d.axes) return fail(A2D_ERR_INVALID_ARG, "%s: axis[%d]=%d, axes=%d", who, p, d.axis[p], d.axes);
   }
   a2d_rotary_tensor t[A2D_ROTARY_MAX_TENSORS];

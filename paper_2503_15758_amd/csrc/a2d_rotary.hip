@@ -121,7 +121,7 @@ hipError_t go(const RotaryArgs& a, const Turns& t, dim3 grid, bool interleaved, 
 
 // freq / (2 pi) modulo 1, in 2^-64 units: the product of freq's 53 bits and the first 128 of 1 / (2 pi) behind the point, in integers (a call
 // makes one for each pair: as divisions and floors of 80-bit numbers they took 8.7 us of the host's time for 64 pairs).
-// From 2^64 radians on nothing is left of a fraction.
+// |freq| < 2^64: beyond, 128 bits do not reach the fraction.
 uint64_t part_of_turn(double freq) {
   constexpr uint64_t kHi = 0x28BE60DB9391054Aull, kLo = 0x7F09D5F47D4D3770ull;
   uint64_t bits;
@@ -129,7 +129,7 @@ uint64_t part_of_turn(double freq) {
   const int biased = (int)(bits >> 52) & 0x7FF, e = biased ? biased - 1075 : -1074;        // |freq| = m 2^e
   const uint64_t m = (bits & (((uint64_t)1 << 52) - 1)) | (biased ? (uint64_t)1 << 52 : 0);
   const int shift = 64 - e;                                              // of m / (2 pi) in 2^-128 units, down
-  if (e > 11 || shift >= 192) return 0;
+  if (shift >= 192) return 0;
   const unsigned __int128 low = (unsigned __int128)m * kLo, high = (unsigned __int128)m * kHi + (uint64_t)(low >> 64);
   const uint64_t w[4] = {(uint64_t)low, (uint64_t)high, (uint64_t)(high >> 64), 0};
   const int at = shift / 64, by = shift % 64;
