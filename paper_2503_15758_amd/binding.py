@@ -11,8 +11,10 @@ among several workgroups and takes up to 32 MiB for each result it shares (forwa
 dQ; dK and dV; 128 MiB for each in partial_bwd_scored) from torch's allocator while it runs, also where `out` and `workspace`
 are given.  Under torch.cuda.graph that is the graph's own pool.  On a stream that the
 program captures by other means, no memory is taken and no walk is shared: the same
-results up to the order of fp32 sums.  The same where there is no memory, with a
-RuntimeWarning.
+results up to the order of fp32 sums (in bf16 probabilities are rounded relative to
+the maximum of a shared walk's part, so each anew).  The same where there is no memory,
+with a RuntimeWarning.  Slopes, ranges, starts, prefix and positions that begin at no
+multiple of 16 bytes (views) are copied first; in such a capture they are refused.
 """
 import ctypes
 import math

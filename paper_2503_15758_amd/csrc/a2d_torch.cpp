@@ -281,6 +281,23 @@ bool torch_captures(const at::Device& device) noexcept {
   }
 }
 
+// Does memory that torch's allocator gives for a call on the stream stay the call's?
+bool may_allocate(const at::Device& device, hipStream_t stream) noexcept {
+  hipStreamCaptureStatus now = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(stream, &now) != hipSuccess) {
+    (void)hipGetLastError();                         // (not an error of the launches to come)
+    return false;
+  }
+  return now == hipStreamCaptureStatusNone || torch_captures(device);
+}
+
+// The few numbers that a call reads besides its tensors (slopes, ranges, starts), at an address that the library takes: a view may begin
+// at any of them (a rank's slopes of a model's), and is copied then.
+at::Tensor at_16_bytes(const at::Tensor& t) {
+  if ((reinterpret_cast<uintptr_t>(t.data_ptr()) & 15) == 0 || !may_allocate(t.device(), static_cast<hipStream_t>(stream()))) return t;
+  return t.detach().clone();
+}
+
 // Offers the library memory for the partial results of shared walks while it lives: from torch's allocator (the
 // blocks go back when it dies; the allocator orders their reuse on the stream) or, for the static calls, the
 // library's own device array.  A foreign capture gets none: its graph would replay into memory that has been
@@ -292,16 +309,8 @@ class Scratch {
   size_t missing_ = 0;
   a2d::ScratchSource source_;
 
-  bool capturable() const {
-    hipStreamCaptureStatus now = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(stream_, &now) != hipSuccess) {
-      (void)hipGetLastError();                       // (not an error of the launches to come)
-      return false;
-    }
-    return now == hipStreamCaptureStatusNone || torch_captures(like_->device());
-  }
   void* allocate(size_t bytes) {
-    if (!capturable()) return nullptr;
+    if (!may_allocate(like_->device(), stream_)) return nullptr;
     try {
       held_.push_back(at::empty({(int64_t)bytes}, like_->options().dtype(at::kByte).requires_grad(false)));
       return held_.back().data_ptr();
@@ -653,8 +662,13 @@ int32_t int32_of(PyObject* o, const char* name) {
 }
 
 // softcap, slopes, ranges, token_step
-a2d_score_rules score_rules(const at::Tensor& Q, const at::Tensor& K, Args a) {
+struct Rules {
   a2d_score_rules r;
+  at::Tensor slopes, ranges;
+};
+Rules score_rules(const at::Tensor& Q, const at::Tensor& K, Args a) {
+  Rules all;
+  a2d_score_rules& r = all.r;
   r.softcap = (float)number(a[0]);
   r.token_step = int32_of(a[3], "token_step");
   r.range_sets = 1;
@@ -664,7 +678,8 @@ a2d_score_rules score_rules(const at::Tensor& Q, const at::Tensor& K, Args a) {
   if (a[1] != Py_None) {
     const at::Tensor& t = tensor(a[1], "slopes");
     exactly(t, {Q.size(0)}, at::kFloat, "slopes (fp32 [heads])");
-    r.slopes = data<float>(t);
+    all.slopes = at_16_bytes(t);
+    r.slopes = data<float>(all.slopes);
   }
   if (a[2] != Py_None) {
     const at::Tensor& t = tensor(a[2], "ranges");
@@ -672,11 +687,12 @@ a2d_score_rules score_rules(const at::Tensor& Q, const at::Tensor& K, Args a) {
     if (t.dim() == 3) r.range_sets = (int32_t)t.size(0);
     if (t.dim() == 3) exactly(t, {t.size(0), Q.size(1), 2}, at::kInt, what);
     else exactly(t, {Q.size(1), 2}, at::kInt, what);
-    r.ranges = data<int32_t>(t);
+    all.ranges = at_16_bytes(t);
+    r.ranges = data<int32_t>(all.ranges);
   }
   here(Q, "Q");
   here(K, "K");
-  return r;
+  return all;
 }
 
 // Q, K, V, q_off, kv_off, causal, scale, softcap, slopes, ranges, token_step, out, accumulate, normalised
@@ -685,7 +701,7 @@ PyObject* partial_fwd_scored(Args a) {
   qkv(Q, K, V);
   here(V, "V");
   const a2d_tile_desc d = descriptor(Q, K, V, a + 3, 0);
-  const a2d_score_rules r = score_rules(Q, K, a + 7);
+  const Rules rules = score_rules(Q, K, a + 7);
   const bool acc = truth(a[12]), norm = truth(a[13]);
   if (acc && norm) fail(A2D_ERR_INVALID_ARG, "a normalised partial is not accumulated into");
   if (acc && a[11] == Py_None) fail(A2D_ERR_INVALID_ARG, "accumulate needs out=(O_part, m, l)");
@@ -707,7 +723,7 @@ PyObject* partial_fwd_scored(Args a) {
   const int kvh = (int)K.size(0);
   const Scratch scratch(Q, s);
   check(unlocked([&] {
-    return a2d_partial_fwd_scored(&d, kvh, &r, acc ? A2D_TILE_ACCUMULATE : norm ? A2D_TILE_NORMALISED : 0, q, k, v, N, m, l,
+    return a2d_partial_fwd_scored(&d, kvh, &rules.r, acc ? A2D_TILE_ACCUMULATE : norm ? A2D_TILE_NORMALISED : 0, q, k, v, N, m, l,
                                   nullptr, 0, s);
   }));
   scratch.tell();
@@ -723,7 +739,7 @@ PyObject* partial_bwd_scored(Args a) {
   a2d_tile_desc d = descriptor(x.Q, x.K, x.V, a + 6, 0);
   d.lo = layout(x.O);
   d.ldo = layout(x.dO);
-  const a2d_score_rules r = score_rules(x.Q, x.K, a + 10);
+  const Rules rules = score_rules(x.Q, x.K, a + 10);
   const bool acc = truth(a[16]), rounded = truth(a[17]);
   if (acc && rounded) fail(A2D_ERR_INVALID_ARG, "rounded gradients are not accumulated into");
   if (acc && a[14] == Py_None) fail(A2D_ERR_INVALID_ARG, "accumulate needs out=(dQ_part, dK_part, dV_part)");
@@ -753,7 +769,7 @@ PyObject* partial_bwd_scored(Args a) {
   const int kvh = (int)x.K.size(0);
   const Scratch scratch(x.Q, s);
   check(unlocked([&] {
-    return a2d_partial_bwd_scored(&d, kvh, &r, acc ? A2D_TILE_ACCUMULATE : rounded ? A2D_TILE_NORMALISED : 0, q, k, v, O, g, lse,
+    return a2d_partial_bwd_scored(&d, kvh, &rules.r, acc ? A2D_TILE_ACCUMULATE : rounded ? A2D_TILE_NORMALISED : 0, q, k, v, O, g, lse,
                                   dq, dk, dv, w, wb, s);
   }));
   scratch.tell();
@@ -762,16 +778,18 @@ PyObject* partial_bwd_scored(Args a) {
 
 // starts, rows, prefix, first, step, causal, out
 PyObject* document_ranges(Args a) {
-  const at::Tensor& starts = tensor(a[0], "starts");
+  at::Tensor starts = tensor(a[0], "starts"), prefixes;
   const char* what = "starts (int32 [documents + 1])";
   if (starts.dim() != 1 || starts.size(0) < 2) fail(A2D_ERR_INVALID_ARG, std::string(what) + ": one document at least");
   exactly(starts, starts.sizes(), at::kInt, what);
+  starts = at_16_bytes(starts);
   const int32_t documents = (int32_t)(starts.size(0) - 1), rows = int32_of(a[1], "rows");
   const int32_t* prefix = nullptr;
   if (a[2] != Py_None) {
     const at::Tensor& t = tensor(a[2], "prefix");
     exactly(t, {documents}, at::kInt, "prefix (int32 [documents])");
-    prefix = data<int32_t>(t);
+    prefixes = at_16_bytes(t);
+    prefix = data<int32_t>(prefixes);
   }
   const int64_t first = integer(a[3]);
   const int32_t step = int32_of(a[4], "step");
@@ -806,7 +824,8 @@ PyObject* rotary(Args a) {
   }
   const int n = (int)xs.size();
   if (n < 1 || n > A2D_ROTARY_MAX_TENSORS) fail(A2D_ERR_INVALID_ARG, "X must be one or two tensors");
-  const at::Tensor &positions = tensor(a[1], "positions"), &freqs = tensor(a[2], "freqs");
+  at::Tensor positions = tensor(a[1], "positions");
+  const at::Tensor& freqs = tensor(a[2], "freqs");
   if (!freqs.device().is_cpu() || freqs.scalar_type() != at::kDouble || freqs.dim() != 1 || !freqs.is_contiguous())
     fail(A2D_ERR_INVALID_ARG, "freqs must be a contiguous fp64 tensor [pairs] on the host");
   a2d_rotary_desc d{};
@@ -827,6 +846,7 @@ PyObject* rotary(Args a) {
   if (positions.size(-1) != d.rows) fail(A2D_ERR_INVALID_ARG, std::string(what) + ": as many rows as X expected");
   d.axes = (int32_t)std::min<int64_t>(positions.size(-2), 1 << 20);
   d.sets = positions.dim() == 3 ? (int32_t)std::min<int64_t>(positions.size(0), 1 << 20) : 1;
+  positions = at_16_bytes(positions);
   d.positions = data<int32_t>(positions);
   d.interleaved = truth(a[4]);
   d.inverse = truth(a[5]);
