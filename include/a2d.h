@@ -348,6 +348,10 @@ a2d_status a2d_partial_bwd_gqa(const a2d_tile_desc* desc, int32_t kv_heads, int 
  * and the key is visible iff (not desc->causal or t_i >= u_k) and first_i <= u_k < end_i, where (first_i, end_i) is the
  * row's pair in `ranges`: documents, prefixes, windows, the lengths of a batch's sequences - whatever is one run of
  * tokens for each row (a2d_document_ranges writes those of packed documents).  A row without a visible key has the empty partial.
+ * The sets of a batch differ in their ranges alone: t_i and u_k are the same tokens for all of them.  So under slopes, or causal, the
+ * caches of sequences of different lengths end together, each at its row's token (a sequence of n tokens: keys nkv - n .. nkv - 1).
+ * With caches that begin together, and q_off at or behind every sequence's last key, a bias is off by one number a row: O is right,
+ * m and lse are slopes[h] times the difference too low.
  */
 typedef struct {
   float softcap;         /* 0: no cap; else 1e-6 .. 1e6, and scale / softcap at most 1e4 (A2D_ERR_UNSUPPORTED)   */
@@ -375,7 +379,8 @@ typedef struct {
  * Rows of Q, O, dO that see no key, and keys in front of the first or behind the last one that any row sees, may hold
  * anything (NaN, uninitialised cache): they are not read or have no effect, and their gradients are 0.
  * With slopes no distance |t_i - u_k| of the tile may exceed 2^24 (A2D_ERR_UNSUPPORTED): they are exact in fp32 up to there.
- * desc->scale below 1e-20 is refused (A2D_ERR_UNSUPPORTED).  slopes: any finite values, negative ones too.
+ * desc->scale below 1e-20 is refused (A2D_ERR_UNSUPPORTED).  slopes: negative ones too; slopes[h] times the
+ * largest distance stays below 1e29 in size.
  * group * nq may not exceed 2^22 rows.
  */
 a2d_status a2d_partial_fwd_scored(const a2d_tile_desc* desc, int32_t kv_heads, const a2d_score_rules* rules, int flags,
@@ -401,7 +406,8 @@ a2d_status a2d_document_ranges(int32_t documents, const int32_t* starts, const i
  * Rotary positions with several axes (time, height, width): every pair of columns follows one axis and is turned by
  *   angle = positions[axis of the pair][row] * freqs[pair]   radians:   (x, y) -> (x cos - y sin, x sin + y cos),
  * by -angle with inverse != 0: its inverse, and the gradient of the turned tensor on its way back.  Pair p is the columns
- * (2 p, 2 p + 1) with interleaved != 0, else (p, p + hdim / 2); columns of no pair stay as they are.
+ * (2 p, 2 p + 1) with interleaved != 0, else (p, p + hdim / 2); columns of no pair stay as they are.  A model that turns the first
+ * r columns of its heads, in pairs (p, p + r / 2), passes hdim = r and layouts with its own row stride (in place: the others stay).
  * The angle is formed in 64-bit fixed point as a part of a turn, so that far positions lose nothing; values are rounded once.
  */
 typedef struct {

@@ -329,7 +329,7 @@ def partial_fwd_scored(Q, K, V, q_off=0, kv_off=0, causal=False, scale=None, sof
     """a2d_partial_fwd_scored: partial_fwd (grouped heads too) with rules on the scores.  softcap: s = softcap tanh(s / softcap)
     of the scaled scores, 0: none; slopes: fp32 [heads], s -= slope |distance in tokens|; ranges: int32 [nq][2] (or
     [sets][nq][2], a set for each run of heads / sets query heads), the tokens that each row may see, first and behind the last
-    (see document_ranges); token_step: tokens between rows and between keys (the grid side in the cyclic layout, with
+    (see document_ranges; the tokens of rows and keys are the same in every set, so with slopes or causal a batch's caches end together); token_step: tokens between rows and between keys (the grid side in the cyclic layout, with
     q_off, kv_off the blocks' first tokens).  Returns (O_part, m, l) fp32, or with normalised=True (O in Q's dtype, lse)."""
     return (_native or _ext()).partial_fwd_scored(Q, K, V, q_off, kv_off, causal, scale, softcap, slopes, ranges, token_step,
                                                   out, accumulate, normalised)
@@ -354,7 +354,8 @@ def document_ranges(starts, rows, prefix=None, first=0, step=1, causal=True, out
 
 def rotary_frequencies(hdim, sections, base=10000.0, restart=False):
     """(freqs, axis) for rotary(), on the host: sections[a] pairs of columns follow axis a, one after another.  Pair p turns by
-    base ** (-2 p / hdim) radians a position; restart=True: each axis has its own falling sequence, base ** (-2 j / (2 n)) for
+    base ** (-2 p / hdim) radians a position (of heads that turn their first r columns: rotary_frequencies(r, ..), rotary(X[..., :r],
+    .., out=X[..., :r])); restart=True: each axis has its own falling sequence, base ** (-2 j / (2 n)) for
     pair j of its n."""
     sections = [int(n) for n in sections]
     if not sections or min(sections) < 0 or not 0 < sum(sections) <= hdim // 2:

@@ -99,3 +99,23 @@ def test_without_memory(a2d, shape):
     # scores' 2^x beside them are 2^-17 too: nkv + 160 roundings, and 2^-24 of scores up to 20 log2(e), twice)
     step = (2.0 ** -17 if fine else 2.0 ** -8) + (nkv + 160 + 60) * 2.0 ** -24
     assert ((a - b).norm() / b.norm()).item() <= 2 * step
+
+
+def test_a_batch_under_a_bias(a2d):
+    """Caches that end together: each sequence's own distances.  Caches that begin together, asked from behind the longest: every bias of a
+    shorter one is too large by the same tokens, O is right and lse lower by slope times them."""
+    heads, kvh, H, lens = 4, 2, 64, [200, 77]
+    Q, K, V, _ = inputs(2 * heads, 2 * kvh, 1, 200, H, "bf16")
+    slopes = slopes_of(heads).repeat(2)
+    ends = a2d.partial_fwd_scored(Q, K, V, q_off=199, slopes=slopes, ranges=int32([[[200 - n, 200]] for n in lens]), normalised=True)
+    begins = a2d.partial_fwd_scored(Q, K, V, q_off=199, slopes=slopes, ranges=int32([[[0, n]] for n in lens]), normalised=True)
+    for i, n in enumerate(lens):
+        h, k = slice(i * heads, (i + 1) * heads), slice(i * kvh, (i + 1) * kvh)
+        s = Scored(Q[h], K[k, 200 - n:], V[k, 200 - n:], q_off=n - 1, slopes=slopes[h]).partial()
+        check_fwd((ends[0][h], ends[1][h]), s, True, Q.dtype, "ending together")
+        s = Scored(Q[h], K[k, :n], V[k, :n], q_off=n - 1, slopes=slopes[h]).partial()
+        s["lse"] = s["lse"] - slopes[h].cpu().double().unsqueeze(1) * (200 - n)
+        # (the scores are rounded next to a bias that is larger by slope times up to 123 tokens)
+        more = 32 * 2.0 ** -24 * slopes[h].max().item() * 200
+        s["e_O"], s["e_lse"] = s["e_O"] + more * V[k].abs().max().item(), s["e_lse"] + more
+        check_fwd((begins[0][h], begins[1][h]), s, True, Q.dtype, "beginning together")
