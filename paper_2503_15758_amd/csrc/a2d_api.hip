@@ -730,7 +730,14 @@ a2d_status make_rules(const a2d_tile_desc* d, int32_t kv_heads, const a2d_score_
     // fit on Chebyshev points, weights moved to where the error is largest until it is even.  Taken at x = scale z / cap, times cap log2(e).
     const double tanh_of[4] = {0.999999456, -0.333263179, 0.131902963, -0.0444022184};
     const double finer[5] = {0.999999987, -0.333330694, 0.133247793, -0.0529860738, 0.0171350036};
-    const double a = (double)d->scale / r->cap, top = (double)r->cap * 1.4426950408889634;
+    const double top = (double)r->cap * 1.4426950408889634;
+    double a = (double)d->scale / r->cap;
+    r->capped.lift = 1.f;
+    if (finer[4] * std::pow(a, 9) * top < 1e-30) {
+      int e;
+      a = std::frexp(a, &e);
+      r->capped.lift = (float)std::ldexp(1.0, e);
+    }
     double power = a * top;
     for (int i = 0; i < 5; ++i, power *= a * a) {
       if (i < 4) r->capped.c[i] = (float)(tanh_of[i] * power);

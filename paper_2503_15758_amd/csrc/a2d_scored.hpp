@@ -10,8 +10,10 @@ namespace a2d {
 // z (c0 + .. + c3 z^6), fitted to tanh with 5e-7 of it; beyond, top (1 - 2 / (1 + 2^(rate z))), whose error, some 2^-22 of top, is relative to
 // a y of 0.46 top and more.  (That form alone would be off by 2^-22 of the cap everywhere: as much as y itself for a wide cap.)
 // fine: one coefficient more (1e-8 and the roundings), for fp32 inputs.
+// lift: a power of two that the kernels' Q (dK / dV: K) comes multiplied with, where the coefficients, up to (scale / cap)^9, or z^2 would leave
+// fp32's range otherwise (a scale of 1e-8 under a cap of 30); all of these are of that z then.  1: as it is.
 struct CapArgs {
-  float small, rate, top, c[4], fine[5];
+  float small, rate, top, c[4], fine[5], lift;
 };
 struct ScoreRules {
   float cap;            // 0: none

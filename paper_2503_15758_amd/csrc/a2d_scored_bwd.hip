@@ -120,6 +120,10 @@ __device__ __forceinline__ void scored_dq_rows(
 #pragma unroll
       for (int x = 0; x < KS; ++x) qf[x][q] = gf[x][q] = bf16x8{};
     }
+    if (CAP && A2D_SELDOM(r.capped.lift != 1.f)) {
+#pragma unroll
+      for (int x = 0; x < KS; ++x) lift(qf[x][q], r.capped.lift);
+    }
     start[q] = f32x4{-del, -del, -del, -del};
     if (BIAS) from[q] = (float)(int)(r.rel + (int64_t)in * r.step);
     if (live) {
@@ -424,6 +428,7 @@ __device__ __forceinline__ void scored_dkdv_keys(
       bf16x8 kx = *reinterpret_cast<const bf16x8*>(K + at_row * d.lk.row + ld);
       bf16x8 vx = *reinterpret_cast<const bf16x8*>(V + at_row * d.lv.row + ld);
       if (32 * x + 32 > H && at >= H) kx = vx = bf16x8{};
+      if (CAP && A2D_SELDOM(r.capped.lift != 1.f)) lift(kx, r.capped.lift);
       if (x < PARK) {
         auto* const p = reinterpret_cast<__attribute__((address_space(3))) bf16x8*>((uintptr_t)(park + 16 * lane));
         p[64 * kt] = kx;

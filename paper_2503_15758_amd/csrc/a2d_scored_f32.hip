@@ -43,6 +43,15 @@ __device__ __forceinline__ void load_at(Nat<H>& x, gptr_t base, unsigned off, in
   for (int y = 0; y < H / 16; ++y) x.v[y] = gload<f32x4>(base, off + 16 * g4 + 64 * y);
 }
 
+// (see CapArgs)
+template <int H>
+__device__ __forceinline__ void lift(Nat<H>& x, const ScoreRules& r) {
+  if (r.cap != 0.f && A2D_SELDOM(r.capped.lift != 1.f)) {
+#pragma unroll
+    for (int y = 0; y < H / 16; ++y) x.v[y] *= r.capped.lift;
+  }
+}
+
 // ------------------------------------------------------------------------------------------- forward
 // 16 RT rows a workgroup of four key lanes, 16 keys a step (as fwd_f32_kernel)
 // (out0, out1, out2 are not __restrict__: an accumulating call's `in` is the same memory)
@@ -74,6 +83,7 @@ __global__ __launch_bounds__(64 * KL, 2) void scored_fwd_f32_kernel(
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     load_at<H>(qf[t], qb, (unsigned)rs.q_at[t] * 4, g4);
+    lift(qf[t], r);
     o[t].zero();
     m_lane[t] = -INFINITY;
     l_run[t] = 0.f;
@@ -231,6 +241,7 @@ __global__ __launch_bounds__(64 * KL, 2) void scored_dq_f32_kernel(
 #pragma unroll
     for (int y = 0; y < H / 16; ++y) qf.v[y] = gf.v[y] = zero4();
   }
+  lift(qf, r);
   const float lse2 = live ? L * kLog2e : INFINITY;    // +inf: P = 0
   const float slope = r.slopes ? r.slopes[head] * kLog2e : 0.f;
   const float at = (float)(int)(r.rel + (int64_t)in * r.step);
@@ -375,6 +386,7 @@ __global__ __launch_bounds__(64 * KL, 2) void scored_dkdv_f32_kernel(
   Nat<H> kf, vf;
   kf.load(uniform_gptr(K + (int64_t)head * d.lk.head), k_ld, (unsigned)d.lk.row * 4, g4);
   vf.load(uniform_gptr(V + (int64_t)head * d.lv.head), k_ld, (unsigned)d.lv.row * 4, g4);
+  lift(kf, r);
   Out<H> dk, dv;
   dk.zero();
   dv.zero();

@@ -233,6 +233,12 @@ __device__ __forceinline__ void scored_fwd_rows(
       qf[x][q] = *reinterpret_cast<const bf16x8*>(Q + rs.q_at[q] + min(at, H - 8));
       if (32 * x + 32 > H && at >= H) qf[x][q] = bf16x8{};
     }
+  if (CAP && A2D_SELDOM(r.capped.lift != 1.f)) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int x = 0; x < KS; ++x) lift(qf[x][q], r.capped.lift);
+  }
   if ((KL == 1 || kl == 0) && lane == 0) {
     hull[2 * wave] = rs.lo;
     hull[2 * wave + 1] = rs.hi;
@@ -475,6 +481,12 @@ __global__ __launch_bounds__(512, 1) void scored_fwd_small_kernel(
       qf[x][q] = *reinterpret_cast<const bf16x8*>(Q + rs.q_at[q] + min(at, H - 8));
       if (32 * x + 32 > H && at >= H) qf[x][q] = bf16x8{};
     }
+  if (CAP && A2D_SELDOM(r.capped.lift != 1.f)) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int x = 0; x < KS; ++x) lift(qf[x][q], r.capped.lift);
+  }
   const int lo = rs.lo, hi = rs.hi;
   const int first = hi > lo ? lo / SB : 1, end = hi > lo ? (hi + SB - 1) / SB : 1;
 

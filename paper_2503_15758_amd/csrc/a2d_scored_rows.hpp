@@ -125,6 +125,12 @@ struct RowState {
   int nearest, farthest; // `at` of its rows, the least and the most
 };
 
+// (exact: a power of two)
+__device__ __forceinline__ void lift(bf16x8& v, float by) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = (bf16_t)((float)v[e] * by);
+}
+
 // min or max over the 16 lanes of a lane's tile (every 16 lanes hold the same rows)
 template <class F>
 __device__ __forceinline__ int over16(int x, F&& f) {
