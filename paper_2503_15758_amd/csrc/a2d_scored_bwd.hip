@@ -8,13 +8,15 @@
 // Masks.  The dQ kernel looks up what each row sees and leaves it for the other one: per row its run of keys, lse and delta in the
 // units that are used (a row that sees nothing: lse = +inf, so that its P is 0), per 32 rows the hull of their runs and the keys that
 // all of them see.  From the hulls a dK / dV workgroup makes a bit for every step of 64 query rows, and walks the set ones: documents cost
-// nothing but their own scores, wherever they lie.  Rows that see nothing are not loaded (zeros in their place), nor are keys
-// outside a hull: they may hold anything.
+// nothing but their own scores, wherever they lie.  Rows that see nothing are zeros in front of every product, so they may hold anything;
+// so may keys that no row sees: dQ reads none outside a block's hull, dK / dV hold those of every block (asked for before the steps that see
+// one are known) and leave out what an unseen one would take part in.
 //
-// Bound: vector and matrix instructions of two wavefronts a SIMD that share its issue, 8192 x 8192, 16 heads of 128 in four documents 350 us
-// (660 TFLOP/s of the five contractions; matrix units busy 41 % of dQ's time, 35 % of dK / dV's), 4096 x 4096, 32 / 8 of 128, causal under a cap
-// 527 (44 % and 38 %, vector ALUs 62 % and 48 %); below some hundred million scores by uneven walks, what a workgroup costs besides, and
-// launches: 2999 x 2999, 12 / 4 of 80 in four documents 76.
+// Bound: of 4096 x 4096, 32 / 8 of 128, causal under a cap, 535 us, vector and matrix instructions of two wavefronts a SIMD that share its issue
+// (matrix units busy 43 % of dQ's time and 38 % of dK / dV's, vector ALUs 62 % and 48 %).  Documents, by their longest walk: 8192 x 8192, 16 heads of
+// 128 in four, 347 us (660 TFLOP/s of the five contractions; 41 % and 35 %, 31 % and 27 %; 1.6 wavefronts a SIMD: up to 66 steps where an even
+// share were 51); below some hundred million scores also by what a workgroup costs besides, and launches: 2999 x 2999, 12 / 4 of
+// 80 in four documents 76.
 #include "a2d_bwd.hpp"
 #include "a2d_scored_rows.hpp"
 
@@ -832,9 +834,10 @@ size_t scored_bwd_scratch(const a2d_tile_desc& d, const ScoreRules& r, const Sco
 // Every way's time from its turns of the chip, the quickest; one launch sums up every result that is cut.  Steps in us, fitted to 45 calls
 // timed in each of 120 ways.  Documents, which the host cannot see, are taken to have their tokens in the rows and the keys alike and for
 // walks of a third of them.  What it chooses between, measured: 4096 x 4096, 32 / 8 heads of 128, causal under a cap: dK / dV of four
-// parts a block 540 us, of one 1179 (128 workgroups, of any length); 8192 x 8192, 16 of 128 in documents: whole blocks, the longest first 349,
-// in their own order 425, four parts 400; 427 x 5532, 16 / 4 of 64 in documents: dK / dV of three units a block on average, shared out, 43,
-// of four even parts 56; 746 x 895, 4 / 1 of 64: shared out 28, even 22 (finding out the shares takes some 3 us).
+// parts a block 532 us, of one 1169 (128 workgroups, of any length); 8192 x 8192, 16 of 128 in documents: whole blocks, the longest first 343,
+// in their own order 427, dK / dV in four parts besides 520; of the fit's calls, as they were timed for it: 427 x 5532, 16 / 4 of 64 in documents,
+// dK / dV of three units a block on average, shared out, 43, of four even parts 56; 746 x 895, 4 / 1 of 64, shared out 28, even 22
+// (finding out the shares takes some 3 us).
 ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int cus, size_t most_bytes) {
   constexpr double kFindOut = 4.0, kSum = 5.0, kBytes = 6e6;             // us; bytes of partials a us, out and back
   const bool documents = taken_for_documents(d, r);
@@ -894,9 +897,10 @@ ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int c
 }
 
 // Calls of few scores contract P and dZ as two bf16 numbers each (hi + lo, 2^-17 off).  One rounding to bf16 leaves gradients off by 1.41
-// times what the rounding of the outputs alone does, as sums of many independent errors; of short sums, which cancel by chance, by up to 1.5 times
-// (349 x 193, 4 / 1 heads of 80: 1.47).  These calls wait for launches and first loads: 637 x 260, 4 / 2 of 96, 31 -> 33 us.  Of
-// 2^22 scores and more it was 1.46 at the most (250 calls), and 4619 x 543, 2 of 80, would take 46 us for 41.
+// times what the rounding of the outputs alone does - two roundings of one size -, however long the sums are (4096 rows in documents of 16 to
+// 4096 tokens: 1.41 to 1.43), in small results by chance up to 1.5 times (349 x 193, 4 / 1 heads of 80: 1.47).  Up to 2^22 scores the
+// second number is nearly free, as calls wait for launches and first loads: 637 x 260, 4 / 2 of 96, 31 -> 33 us.  Beyond it is not: 4619 x 543, 2
+// of 80, 41 -> 46; 2999 x 2999, 12 / 4 of 80 in documents 76 -> 89; 4096 x 4096, 32 / 8 of 128 under a cap 532 -> 667.
 static bool fine_call(const a2d_tile_desc& d) { return (int64_t)d.heads * d.nq * d.nkv <= (int64_t)1 << 22; }
 
 void route_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, const ScoredBwdPlan& plan, ScoredRoute* out) {

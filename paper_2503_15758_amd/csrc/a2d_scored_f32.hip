@@ -6,7 +6,7 @@
 // lanes take alike: their few vector instructions a score are a small part of a step.  Scores are kept in log2 units.
 //
 // Bound by the fp32 matrix rate where there are many rows, by the chip's idle units, first loads and launches where there are few: backward of
-// 8 heads of 96, 700 x 900, causal, 77 us (matrix units busy 30 % of the time, one wavefront a SIMD); forward of 2 x 128 x 128 6 us.
+// 8 heads of 96, 700 x 900, causal, 78 us (matrix units busy 30 % of the time, one wavefront a SIMD); forward of 2 x 128 x 128 7 us.
 #include "a2d_f32.hpp"
 #include "a2d_scored_rows.hpp"
 

@@ -5,8 +5,10 @@
 // units (z -> cap -> minus the bias) relative to the row's reference, so that 2^x follows directly.  The rules cost vector instructions a
 // score: the cap 4.5 (a polynomial, see CapArgs; where some score of a wavefront's block is beyond its range 12, two of them of a quarter of the
 // rate), the bias 1, near the diagonal 2.3.  Bound: the vector instructions (of 64 keys and 32 rows of a wavefront at H = 64, 512 clocks of
-// exponentials and 600 to 900 of others stand beside 512 of matrix instructions), which two wavefronts of a SIMD share.  16 heads of 64,
-// 8192 x 8192, not causal: 265 us without rules, 317 with a bias, 379 with a cap; 32 / 8 of 128, 4096 x 4096, causal: 137, 132, 147.
+// exponentials and 600 to 900 of others stand beside 512 of matrix instructions), which the two (H = 64: up to three) wavefronts of a SIMD share;
+// 32 / 8 heads of 128, 4096 x 4096, causal under a cap: vector instructions 58 % of the time, matrix instructions 35 %.  Documents end with
+// their longest walk instead: six of 8192 tokens, H = 64, 53 % and 22 %, up to 50 steps where an even share were 30.  16 heads of 64,
+// 8192 x 8192, not causal: 295 us without rules, 326 with a bias, 390 with a cap; 32 / 8 of 128, 4096 x 4096, causal: 139, 132, 155.
 //
 // Masks: whatever they are made of, a query row sees one run of keys (visible_run).  A workgroup walks the hull of
 // its rows' runs; a wavefront leaves out the blocks that none of its rows sees, and compares keys only in blocks that some row does not see
@@ -116,7 +118,9 @@ struct Softmax {
     }
     return __builtin_amdgcn_ballot_w64(left) != 0;
   }
-  // P^T in bf16 (nearest-even, for the contraction); the sums take the probabilities before their rounding
+  // P^T in bf16 (nearest-even, for the contraction); the sums take the probabilities before their rounding.  O is off by 1.41 times what its
+  // own rounding does: two roundings of one size.  Two numbers, as below, would double the contraction with V: 32 / 8 heads of
+  // 128, 4096 x 4096, capped 205 us for 154, six documents of 8192 tokens 96 for 75, 16384 x 16384 652 for 482.
   template <int NT>
   __device__ __forceinline__ void probabilities(const f32x4 (&s)[NT][2], bf16x8 (&pb)[NT / 2][2]) {
 #pragma unroll
@@ -692,11 +696,11 @@ hipError_t go(Phase ph, const a2d_tile_desc& d, const ScoreRules& r, const Score
 
 // Every form's time from its turns of the chip (walk_time), the quickest.  Steps in us, of 64 keys (of 128 and 256 in the forms with key
 // lanes), by head size and rules, fitted to 40 calls timed in every form.  What they choose between, measured: 8192 x 8192 rows of
-// 16 heads of 64 in six documents 83 us in pairs, 102 with 256 rows (the pairs' turns are half as long); 16384 x 16384, 8 heads of 128: 574
-// with 256 rows, 612 in pairs; 13611 x 14346, 4 of 80, causal: 206 in two key lanes, 281 in pairs, 382 with 256 rows;
-// a token of 256 heads of 64 against 16384 of 64: 67 with 32 rows in four parts, 180 in one, 330 with 256.  Ranges that the
-// host cannot see: one for all heads is taken for documents, which see a part of the keys each (749 x 9939: 13 us in one part, 21 where a plan
-// for whole walks split them); one a sequence for its filled length.
+// 16 heads of 64 in six documents 76 us in pairs, 90 with 256 rows (the pairs' turns are half as long), 102 in two key lanes; 16384 x 16384, 8
+// heads of 128: 491 with 256 rows, 512 in pairs; 13611 x 14346, 4 of 80, causal: 156 in two key lanes, 207 in pairs, 273 with 256 rows;
+// a token of 256 / 64 heads of 64 against up to 16384 keys: 30 with 32 rows in four parts, 67 in one, 196 with 256.  Ranges that the
+// host cannot see: one set for all heads is taken for documents, which see a part of the keys each (749 x 9939: 13 us in one part, 21 where
+// a plan for whole walks split them; see taken_for_documents); one a sequence for its filled length.
 static ScoredPlan best_form(const a2d_tile_desc& d, const ScoreRules& r, int cus, int cap, bool rows_of_32) {
   constexpr struct {
     double step, by_head, fixed, pair;                // pair: both workgroups of a compute unit, of one's time
