@@ -3,7 +3,8 @@
 // Tiles of 16 rows in LDS of a wavefront's own, fragments, contractions and the merge of the four key lanes as in
 // a2d_f32_mfma.hip; masks, hulls and the row table as in a2d_scored_fwd.hip and a2d_scored_bwd.hip.  A step of 16 x 16 scores is
 // H / 4 matrix instructions of 32 cycles for each contraction and four scores a lane, so the rules are branches of the one kernel that all
-// lanes take alike: their few vector instructions a score are a small part of a step.  Scores are kept in log2 units.
+// lanes take alike: their few vector instructions a score are a small part of a step.  Scores are kept in log2 units.  In the backward a bias
+// and lse, which may be thousands where their difference is a few units, meet in natural units in one multiply-add, rounded once.
 //
 // Bound by the fp32 matrix rate where there are many rows, by the chip's idle units, first loads and launches where there are few: backward of
 // 8 heads of 96, 700 x 900, causal, 78 us (matrix units busy 30 % of the time, one wavefront a SIMD); forward of 2 x 128 x 128 7 us.
@@ -242,8 +243,8 @@ __global__ __launch_bounds__(64 * KL, 2) void scored_dq_f32_kernel(
     for (int y = 0; y < H / 16; ++y) qf.v[y] = gf.v[y] = zero4();
   }
   lift(qf, r);
-  const float lse2 = live ? L * kLog2e : INFINITY;    // +inf: P = 0
-  const float slope = r.slopes ? r.slopes[head] * kLog2e : 0.f;
+  const float from = live ? L : INFINITY;             // +inf: P = 0
+  const float slope = r.slopes ? r.slopes[head] : 0.f;
   const float at = (float)(int)(r.rel + (int64_t)in * r.step);
   const auto least = [](int a, int b) { return min(a, b); };
   const auto most = [](int a, int b) { return max(a, b); };
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(64 * KL, 2) void scored_dq_f32_kernel(
   if (part == 0 && kl == 0) {
     if (g4 == 0 && row < tab.padded) {
       const int64_t to = (int64_t)head * tab.padded + row;
-      tab.from[to] = lse2;
+      tab.from[to] = from;
       tab.delta[to] = -del;
       tab.lo[to] = run.lo;
       tab.n[to] = run.n;
@@ -314,10 +315,8 @@ __global__ __launch_bounds__(64 * KL, 2) void scored_dq_f32_kernel(
     const float far = fmaf((float)-(k0 + 4 * g4), r.steps[0], at);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float x = y[i] - lse2;
-      if (r.slopes) x = fmaf(-slope, fabsf(distance<-1>(r, far, 0, i)), x);
-      const float t = y[i] * inv_top;
-      ds[i] = fast_exp2(x) * (ds[i] - del) * fmaf(-t, t, 1.f);
+      const float less = r.slopes ? fmaf(slope, fabsf(distance<-1>(r, far, 0, i)), from) : from, t = y[i] * inv_top;
+      ds[i] = fast_exp2(fmaf(-less, kLog2e, y[i])) * (ds[i] - del) * fmaf(-t, t, 1.f);
       ds[i] = (unsigned)(k0 + 4 * g4 + i - run.lo) < (unsigned)run.n ? ds[i] : 0.f;
     }
     static_for<0, 4>([&](auto R) {
@@ -439,7 +438,7 @@ __global__ __launch_bounds__(64 * KL, 2) void scored_dkdv_f32_kernel(
   Cols<H> ring[2];
   while (more) {
     i0 = (tile - qh * ntiles) * 32 + 16 * h;
-    if (r.slopes) slope = r.slopes[qh0 + qh] * kLog2e;
+    if (r.slopes) slope = r.slopes[qh0 + qh];
     f32x4 p, ds;
     mfma::wait_dma();
     reads_done();                                     // (zeros written in place of rows)
@@ -470,9 +469,8 @@ __global__ __launch_bounds__(64 * KL, 2) void scored_dkdv_f32_kernel(
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const bool vis = (unsigned)key - ll[i] < nn[i];
-      float x = y[i] - fr[i];
-      if (r.slopes) x = fmaf(-slope, fabsf(distance<1>(r, far, 0, i)), x);
-      const float t = y[i] * inv_top, e = fast_exp2(x);
+      const float less = r.slopes ? fmaf(slope, fabsf(distance<1>(r, far, 0, i)), fr[i]) : fr[i];
+      const float t = y[i] * inv_top, e = fast_exp2(fmaf(-less, kLog2e, y[i]));
       p[i] = vis ? e : 0.f;
       ds[i] = vis ? e * (ds[i] + de[i]) * fmaf(-t, t, 1.f) : 0.f;
     }

@@ -34,9 +34,9 @@ __device__ __forceinline__ void capped(float cap, float z, float& y, float& dy) 
     dy = 1.f - t * t;
   }
 }
-__device__ __forceinline__ float bias(const ScoreRules& r, float slope, int i, int k) {
+__device__ __forceinline__ float tokens_apart(const ScoreRules& r, int i, int k) {
   const int64_t far = r.rel + (int64_t)(i - k) * r.step;
-  return slope * (float)(far < 0 ? -far : far);
+  return (float)(far < 0 ? -far : far);
 }
 __device__ __forceinline__ float slope_of(const ScoreRules& r, int head) { return r.slopes ? r.slopes[head] : 0.f; }
 
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(LANES) void scored_fwd_generic_kernel(a2d_tile_desc
     float s = -INFINITY, dy;
     if (lane < keys) {
       capped(r.cap, d.scale * dot(Q, K + k * d.lk.row, H), s, dy);
-      s -= bias(r, slope, i, k);
+      s = fmaf(-slope, tokens_apart(r, i, k), s);
     }
     const float m_new = fmaxf(m, max_of(s)), use = m_new == -INFINITY ? 0.f : m_new;
     const float p = expf(s - use), alpha = expf(m - use);
@@ -95,7 +95,7 @@ __device__ __forceinline__ void gradient(const a2d_tile_desc& d, const ScoreRule
                                          float lse, float delta, float slope, int i, int key, float& p, float& dz) {
   float y, dy;
   capped(r.cap, d.scale * dot(q, k, d.hdim), y, dy);
-  p = expf(y - bias(r, slope, i, key) - lse);
+  p = expf(y - fmaf(slope, tokens_apart(r, i, key), lse));      // (bias and lse may be thousands where their difference is a few units)
   dz = p * (dot(g, v, d.hdim) - delta) * dy;
 }
 

@@ -197,7 +197,7 @@ struct RowTile {
 };
 struct RowTable {
   int padded;
-  float *from, *delta;   // lse in log2 units, with a cap; without one -lse in units of raw products: what the scores start from.  -(dO . O)
+  float *from, *delta;   // bf16: lse in log2 units, with a cap; without one -lse in units of raw products: what the scores start from; fp32: lse.  -(dO . O)
   int *lo, *n;           // run of keys
   RowTile* tiles;        // [heads][padded / 32]
 };

@@ -44,3 +44,22 @@ def test_scales(a2d, shape, sizes):
         want = s.gradients(O, dO, lse)
         for x, n in zip(a2d.partial_bwd_scored(Q, K, V, O, dO, lse, **rules), ("dQ", "dK", "dV")):
             within(x, want[n], want["e_" + n], "scale %s" % n)
+
+
+@pytest.mark.parametrize("step, slope, nq, nkv", [(4, 0.7, 300, 187), (1, 8.0, 200, 90), (1000, 0.01, 77, 300), (1, 0.0, 150, 203)])
+def test_fp32_gradients_far_from_the_keys(a2d, step, slope, nq, nkv):
+    """Rows thousands of units of bias behind their keys: bias and lse cancel, and P is off by the roundings of what is left.  Scores of nothing but
+    the bias, so that P = exp(-slope d - lse) is known from fp32 numbers: dV = P^T dO.  Each P is off by 2^-24 of |slope d + lse|
+    twice (that sum's rounding, and log2(e) times it) and some 8 half steps, the sum over rows by (nq + 16) more."""
+    H, u = 64, 2.0 ** -24
+    gen = torch.Generator().manual_seed(4)
+    K, V, dO = (torch.randn(2, n, H, generator=gen).cuda() for n in (nkv, nkv, nq))
+    Q, slopes, off = torch.zeros(2, nq, H, device="cuda"), torch.tensor([slope, slope / 3], device="cuda"), 700 * step
+    s = Scored(Q, K, V, slopes=slopes, q_off=off, token_step=step)
+    lse = s.partial()["lse"].float().cuda()
+    rest = s.s - lse.cpu().double().unsqueeze(2)
+    p = torch.exp(rest)
+    _, _, dV = a2d.partial_bwd_scored(Q, K, V, torch.zeros_like(Q), dO, lse, slopes=slopes, q_off=off, token_step=step)
+    g = dO.cpu().double()
+    bound = (p * ((nq + 24) * u + 4 * u * rest.abs())).transpose(1, 2) @ g.abs()
+    within(dV, p.transpose(1, 2) @ g, bound, "dV")
