@@ -897,8 +897,8 @@ ScoredBwdPlan plan_scored_bwd(const a2d_tile_desc& d, const ScoreRules& r, int c
 }
 
 // Calls of few scores contract P and dZ as two bf16 numbers each (hi + lo, 2^-17 off).  One rounding to bf16 leaves gradients off by 1.41
-// times what the rounding of the outputs alone does - two roundings of one size -, however long the sums are (4096 rows in documents of 16 to
-// 4096 tokens: 1.41 to 1.43), in small results by chance up to 1.5 times (349 x 193, 4 / 1 heads of 80: 1.47).  Up to 2^22 scores the
+// times what the rounding of the outputs alone does - two roundings of one size -, however long the sums are (4096 rows in documents of 2 to
+// 4096 tokens: 1.25 to 1.43), where few scores make the result by chance more (349 x 193, 4 / 1 heads of 80: 1.47).  Up to 2^22 scores the
 // second number is nearly free, as calls wait for launches and first loads: 637 x 260, 4 / 2 of 96, 31 -> 33 us.  Beyond it is not: 4619 x 543, 2
 // of 80, 41 -> 46; 2999 x 2999, 12 / 4 of 80 in documents 76 -> 89; 4096 x 4096, 32 / 8 of 128 under a cap 532 -> 667.
 static bool fine_call(const a2d_tile_desc& d) { return (int64_t)d.heads * d.nq * d.nkv <= (int64_t)1 << 22; }

@@ -5,7 +5,7 @@ import ctypes
 import pytest
 import torch
 
-from scored_reference import Scored
+from scored_reference import Scored, within
 from test_gpu_rotary import check, turned
 from test_gpu_scored import check_fwd, inputs, int32, slopes_of
 
@@ -119,3 +119,52 @@ def test_a_batch_under_a_bias(a2d):
         more = 32 * 2.0 ** -24 * slopes[h].max().item() * 200
         s["e_O"], s["e_lse"] = s["e_O"] + more * V[k].abs().max().item(), s["e_lse"] + more
         check_fwd((begins[0][h], begins[1][h]), s, True, Q.dtype, "beginning together")
+
+
+# heads, kv_heads, rows, H, type, window
+WINDOWS = [(4, 2, 1500, 128, "bf16", 200), (16, 16, 700, 64, "bf16", 64), (2, 1, 300, 80, "f32", 33), (6, 3, 150, 96, "bf16", 1)]
+
+
+@pytest.mark.parametrize("case", WINDOWS, ids=lambda c: "%dx%dx%d_H%d_%s_window%d" % c)
+def test_sliding_windows(a2d, case):
+    """Each row sees the last `window` tokens up to itself: ranges that move by a token a row, under a cap, with a bias too."""
+    heads, kvh, n, H, dt, window = case
+    print("window", case, flush=True)
+    Q, K, V, dO = inputs(heads, kvh, n, n, H, dt)
+    t = torch.arange(n, dtype=torch.int32, device="cuda")
+    ranges = torch.stack([(t - window + 1).clamp(min=0), t + 1], 1).contiguous()
+    for rules in (dict(softcap=8.0), dict(softcap=8.0, slopes=slopes_of(heads))):
+        s = Scored(Q, K, V, ranges=ranges, **rules)
+        f = s.partial()
+        check_fwd(a2d.partial_fwd_scored(Q, K, V, ranges=ranges, normalised=True, **rules), f, True, Q.dtype, "window")
+        O, lse = f["O"].to(Q.dtype).cuda(), f["lse"].float().cuda()
+        want = s.gradients(O, dO, lse)
+        for x, name in zip(a2d.partial_bwd_scored(Q, K, V, O, dO, lse, ranges=ranges, **rules), ("dQ", "dK", "dV")):
+            within(x, want[name], want["e_" + name], "window %s" % name)
+        # (a range that begins in front of the first token, and the mask instead of its end, say the same)
+        open_ = torch.stack([t - window + 1, torch.full_like(t, 2 ** 31 - 1)], 1).contiguous()
+        a = a2d.partial_fwd_scored(Q, K, V, ranges=open_, causal=True, normalised=True, **rules)
+        check_fwd(a, f, True, Q.dtype, "window")
+
+
+@pytest.mark.parametrize("dt, rows", [("bf16", 333), ("bf16", 40), ("f32", 130)])
+def test_a_batch_of_prompts(a2d, dt, rows):
+    """Sequences of different lengths whose last rows are asked for at once, caches ending together: one of them shorter than the rows."""
+    heads, kvh, H, lens, nkv = 4, 2, 64, [500, 90, 333], 500
+    print("prompts", dt, rows, flush=True)
+    Q, K, V, dO = inputs(3 * heads, 3 * kvh, rows, nkv, H, dt)
+    first = nkv - rows
+    ranges = torch.zeros(3, rows, 2, dtype=torch.int32)
+    for b, n in enumerate(lens):
+        for i in range(rows):
+            ranges[b, i] = torch.tensor([nkv - n, first + i + 1])
+    rules = dict(softcap=9.0, slopes=slopes_of(heads).repeat(3), ranges=ranges.cuda(), q_off=first)
+    s = Scored(Q, K, V, **rules)
+    f = s.partial()
+    got = a2d.partial_fwd_scored(Q, K, V, normalised=True, **rules)
+    check_fwd(got, f, True, Q.dtype, "prompts")
+    assert rows < 90 or not got[0][heads: 2 * heads, : rows - 90].any()
+    O, lse = f["O"].to(Q.dtype).cuda(), f["lse"].float().cuda()
+    want = s.gradients(O, dO, lse)
+    for x, name in zip(a2d.partial_bwd_scored(Q, K, V, O, dO, lse, **rules), ("dQ", "dK", "dV")):
+        within(x, want[name], want["e_" + name], "prompts %s" % name)
