@@ -440,6 +440,103 @@ typedef struct {
 a2d_status a2d_rotary(const a2d_rotary_desc* desc, int n, const a2d_rotary_tensor* x, void* stream);
 
 /*
+ * A paged cache of keys and values in 16, 8 or 4 bits.
+ * Pages of page_rows tokens hold K and V of every key/value head: codes [pages][kv_heads][page_rows][hdim], and for the 8- and 4-bit
+ * formats scales [pages][kv_heads][page_rows][4], a byte for each 32 values of a row (hdim = 80: the third has 16; bytes of no
+ * block are not touched).  Token t of sequence b is row t % page_rows of page table[b][t / page_rows].  A contiguous cache is one with a
+ * page for each sequence.
+ *   A2D_CACHE_BF16  the values, rounded to bf16
+ *   A2D_CACHE_E4M3  8-bit codes: sign, 4 bits of exponent, 3 bits behind the point, up to 448 (the format without infinities)
+ *   A2D_CACHE_E2M1  4-bit codes, 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign; of a byte the low half is the even column
+ * A value is its code times 2^(scale byte - 127).  The exponent s of a block is the smallest integer >= -100 with max |x| <= M 2^s
+ * (M = 448; 6), and a code is x / 2^s, to the nearest, ties to even: nothing saturates, the sign of a zero stays, and what a block holds follows from
+ * its values alone.  Values that round to 2^128 read back as infinite.  A block with a NaN or an infinity has the scale byte 255 and reads back
+ * as NaN.
+ */
+typedef enum { A2D_CACHE_BF16 = 0, A2D_CACHE_E4M3 = 1, A2D_CACHE_E2M1 = 2 } a2d_cache_format;
+
+typedef struct {
+  int32_t format;        /* a2d_cache_format                                                                     */
+  int32_t kv_heads;      /* 1 .. 65535                                                                           */
+  int32_t hdim;          /* 64, 80, 96 or 128                                                                    */
+  int32_t page_rows;     /* tokens of a page: a multiple of 16, 16 .. 2^22                                       */
+  int32_t pages;         /* that K and V hold; pages * kv_heads * page_rows < 2^36                               */
+  int32_t sequences;     /* rows of the table, 1 .. 65535                                                        */
+  int32_t max_pages;     /* its columns; max_pages * page_rows <= 2^30                                           */
+  int32_t pad;           /* must be 0                                                                            */
+  void* K;               /* codes, DEVICE                                                                        */
+  void* V;
+  uint8_t* K_scales;     /* DEVICE; NULL for A2D_CACHE_BF16                                                      */
+  uint8_t* V_scales;
+  const int32_t* table;  /* DEVICE [sequences][max_pages].  A number that is no page's: its tokens are neither written nor
+                            seen, and read as zeros.  Entries of tokens that a call does not touch are not looked at          */
+} a2d_cache;
+
+/*
+ * Where the rows of a [sequences][heads][rows][H] tensor lie: strides in elements, as in a2d_layout, with one more.  {0, 0, 0}: plain.
+ * Else all >= 1 and multiples of 16 bytes, row >= H, a head's rows within 4 GiB of the first; the rows of an output must not overlap.
+ */
+typedef struct {
+  int64_t sequence;
+  int64_t head;
+  int64_t row;
+} a2d_batch_layout;
+
+/*
+ * Writes rows of K and V [sequences][kv_heads][rows][H] (dtype: A2D_F32 or A2D_BF16) into the cache: token starts[b] + j of sequence b, j = 0 ..
+ * count - 1, becomes row index[b][j] (index: DEVICE [sequences][count]; NULL: row j, count = rows).  Where index[b][j] is no row
+ * (-1: a draft that was not accepted, padding), the token lies outside the table, or its page is none, nothing is written.
+ * Pages that several sequences share are to be written by one of them at a time.  1 <= rows, count <= 2^22.
+ */
+a2d_status a2d_cache_write(const a2d_cache* cache, int32_t rows, int32_t count, int32_t dtype, const void* K, const a2d_batch_layout* lk,
+                           const void* V, const a2d_batch_layout* lv, const int32_t* starts, const int32_t* index, void* stream);
+
+/*
+ * Reads the tokens first .. first + rows - 1 of every sequence back, to K and V [sequences][kv_heads][rows][H] in dtype (bf16 holds every value
+ * exactly); tokens from lens[b] on (lens: DEVICE [sequences]) are zeros.  first >= 0, 1 <= rows <= 2^22.
+ */
+a2d_status a2d_cache_read(const a2d_cache* cache, const int32_t* lens, int32_t first, int32_t rows, int32_t dtype, void* K,
+                          const a2d_batch_layout* lk, void* V, const a2d_batch_layout* lv, void* stream);
+
+/*
+ * The rows of a tree of drafted tokens: parents [sequences][rows], DEVICE: the row that a row follows, which comes before it, or -1 where it
+ * follows the text.  Anything else marks a row that is no token (padding), and the rows that follow it are none either.
+ *   masks [sequences][rows][ceil(rows / 64)]: bit j % 64 of word j / 64 is set iff row i sees row j: itself and its ancestors; no token: 0
+ *   positions [sequences][rows]: lens[b] (NULL: 0; a negative one counts as 0) and the number of ancestors; no token: 0.
+ *     The positions of a2d_rotary with one axis and a set for each sequence.
+ * 1 <= rows <= A2D_TREE_MAX_ROWS, 1 <= sequences <= 65535.
+ */
+#define A2D_TREE_MAX_ROWS 256
+a2d_status a2d_tree_masks(int32_t sequences, int32_t rows, const int32_t* parents, const int32_t* lens, uint64_t* masks, int32_t* positions,
+                          void* stream);
+
+/*
+ * Attention of new rows (a token, a chain or a tree of drafted tokens of every sequence) against the cache, bf16.
+ *   in : Q [sequences][heads][rows][H]; K, V [sequences][kv_heads][rows][H]: the rows' own keys and values, not in the cache yet, or both NULL
+ *   Row i of sequence b sees the tokens 0 .. lens[b] - 1 of the cache and, of the rows' own K and V, row j if bit j of its mask is set (masks as of
+ *   a2d_tree_masks; NULL: j <= i).  A row whose own bit is not set is no token: it has the empty partial.  Scores are scale <q, k>.
+ *   out: flags 0: out0 = N [sequences][heads][rows][H] fp32 (plain), out1 = m, out2 = l [sequences][heads][rows] fp32: the partial triple of
+ *   a2d_partial_fwd, to be merged by a2d_fix with those of other shares of the text;
+ *   A2D_TILE_NORMALISED: out0 = O in bf16 (layout lo), out1 = lse fp32, out2 is ignored.
+ * Codes enter the products exactly; P is taken as two bf16 numbers (2^-17 off), all else is fp32.
+ * What no row sees - tokens behind lens[b], rows whose bit no mask of the sequence has, Q, K and V of rows that are no tokens - may hold anything.
+ * workspace: NULL, or at least a2d_cached_workspace_bytes(cache, desc) bytes, through which workgroups share long walks; calls that share one
+ * must be ordered on one stream.  The same sizes, lengths and workspace (or none) give the same bits.
+ */
+typedef struct {
+  int32_t heads;         /* query heads of a sequence, a multiple of kv_heads; 1 .. 65535                        */
+  int32_t rows;          /* 1 .. 2^20; with masks 1 .. A2D_TREE_MAX_ROWS; heads / kv_heads * rows <= 2^22        */
+  int32_t max_tokens;    /* the host's bound on the lengths: a longer lens[b] counts as this.  0: what the table holds */
+  float scale;           /* > 0, at most 1e30 */
+  a2d_batch_layout lq, lk, lv, lo;
+  const int32_t* lens;   /* DEVICE [sequences]; a negative one counts as 0                                       */
+  const uint64_t* masks; /* DEVICE [sequences][rows][ceil(rows / 64)], or NULL                                   */
+} a2d_cached_desc;
+size_t a2d_cached_workspace_bytes(const a2d_cache* cache, const a2d_cached_desc* desc);
+a2d_status a2d_partial_fwd_cached(const a2d_cache* cache, const a2d_cached_desc* desc, int flags, const void* Q, const void* K, const void* V,
+                                  void* out0, float* out1, float* out2, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Sum of k gradient partials (the reduce-scatters of Alg. 3 lines 4-5 use plain
  * summation): out[i] = sum_k parts[k][i], added in index order in fp32, rounded
  * once to out_dtype.  parts: HOST array of k device pointers to n fp32 values;

@@ -36,6 +36,7 @@ EXPORTS = ("a2d_workspace_bytes", "a2d_partial_fwd", "a2d_fix", "a2d_attnfix", "
            "a2d_partial_fwd_norm", "a2d_fix_norm", "a2d_partial_fwd_gqa", "a2d_partial_bwd_gqa",
            "a2d_fix_strided", "a2d_fix_bwd_strided", "a2d_fix_norm_strided",
            "a2d_partial_fwd_scored", "a2d_partial_bwd_scored", "a2d_document_ranges", "a2d_rotary",
+           "a2d_cache_write", "a2d_cache_read", "a2d_tree_masks", "a2d_cached_workspace_bytes", "a2d_partial_fwd_cached",
            "a2d_mfma_ceiling_scratch_bytes", "a2d_mfma_ceiling", "a2d_forward_mix_ceiling", "a2d_backward_mix_ceiling", "a2d_lds_read_ceiling", "a2d_debug_force_generic",
            "a2d_debug_trace", "a2d_debug_trace_count", "a2d_copy_probe",
            "a2d_status_str", "a2d_last_error", "a2d_version")
@@ -77,6 +78,26 @@ class RotaryTensor(ctypes.Structure):
                 ("heads", ctypes.c_int32), ("pad", ctypes.c_int32)]
 
 
+class BatchLayout(ctypes.Structure):
+    """a2d_batch_layout: element strides of a [sequences][heads][rows][H] tensor; (0, 0, 0) = plain."""
+    _fields_ = [("sequence", ctypes.c_int64), ("head", ctypes.c_int64), ("row", ctypes.c_int64)]
+
+
+class CacheDesc(ctypes.Structure):
+    """a2d_cache"""
+    _fields_ = [(n, ctypes.c_int32) for n in ("format", "kv_heads", "hdim", "page_rows", "pages", "sequences", "max_pages", "pad")] + \
+               [(n, ctypes.c_void_p) for n in ("K", "V", "K_scales", "V_scales", "table")]
+
+
+class CachedDesc(ctypes.Structure):
+    """a2d_cached_desc"""
+    _fields_ = [("heads", ctypes.c_int32), ("rows", ctypes.c_int32), ("max_tokens", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("lq", BatchLayout), ("lk", BatchLayout), ("lv", BatchLayout), ("lo", BatchLayout),
+                ("lens", ctypes.c_void_p), ("masks", ctypes.c_void_p)]
+
+
+CACHE_BF16, CACHE_E4M3, CACHE_E2M1 = 0, 1, 2
+TREE_MAX_ROWS = 256
 MAX_SEGMENTS = 32
 TILE_ACCUMULATE, TILE_NORMALISED, TILE_SPLIT_GROUPS = 1, 2, 4
 DESC_KEEP_DS = 1
@@ -168,6 +189,20 @@ def lib():
                                           ctypes.c_int32, vp, vp]
         L.a2d_rotary.restype = ctypes.c_int
         L.a2d_rotary.argtypes = [ctypes.POINTER(RotaryDesc), ctypes.c_int, ctypes.POINTER(RotaryTensor), vp]
+        batch = ctypes.POINTER(BatchLayout)
+        L.a2d_cache_write.restype = ctypes.c_int
+        L.a2d_cache_write.argtypes = [ctypes.POINTER(CacheDesc), ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, batch, vp, batch,
+                                      vp, vp, vp]
+        L.a2d_cache_read.restype = ctypes.c_int
+        L.a2d_cache_read.argtypes = [ctypes.POINTER(CacheDesc), vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, batch, vp, batch,
+                                     vp]
+        L.a2d_tree_masks.restype = ctypes.c_int
+        L.a2d_tree_masks.argtypes = [ctypes.c_int32, ctypes.c_int32, vp, vp, vp, vp, vp]
+        L.a2d_cached_workspace_bytes.restype = ctypes.c_size_t
+        L.a2d_cached_workspace_bytes.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(CachedDesc)]
+        L.a2d_partial_fwd_cached.restype = ctypes.c_int
+        L.a2d_partial_fwd_cached.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(CachedDesc), ctypes.c_int, vp, vp, vp, vp, fp, fp,
+                                             vp, ctypes.c_size_t, vp]
         L.a2d_mfma_ceiling_scratch_bytes.restype = ctypes.c_size_t
         L.a2d_mfma_ceiling_scratch_bytes.argtypes = []
         L.a2d_mfma_ceiling.restype = ctypes.c_int
@@ -376,6 +411,53 @@ def rotary(X, positions, freqs, axis=None, interleaved=False, inverse=False, out
     gradient with respect to X of the gradient with respect to the turned X.  out: as X, may be X itself; else new tensors in
     out_dtype (X's, or bf16 for fp32 gradient partials)."""
     return (_native or _ext()).rotary(X, positions, freqs, axis, interleaved, inverse, out, out_dtype)
+
+
+def cache_empty(pages, kv_heads, page_rows, hdim, format=CACHE_E4M3, device=None):
+    """The tensors of a paged cache with nothing in it, as the calls below take them: (K, V), bfloat16 [pages][kv_heads][page_rows][hdim]
+    (CACHE_BF16), or (K, V, K_scales, V_scales) with codes float8_e4m3fn of that shape (CACHE_E4M3) or two to a byte, uint8
+    [pages][kv_heads][page_rows][hdim / 2] (CACHE_E2M1), and scales uint8 [pages][kv_heads][page_rows][4]: 32 values of a row are
+    their codes times 2 ** (byte - 127).  page_rows: a multiple of 16."""
+    dtypes = {CACHE_BF16: torch.bfloat16, CACHE_E4M3: torch.float8_e4m3fn, CACHE_E2M1: torch.uint8}
+    if format not in dtypes:
+        raise A2DError(-2, "cache format %s not supported" % (format,))
+    device = torch.device("cuda") if device is None else device
+    columns = hdim // 2 if format == CACHE_E2M1 else hdim
+    new = [torch.empty((pages, kv_heads, page_rows, columns), dtype=dtypes[format], device=device) for _ in range(2)]
+    if format != CACHE_BF16:
+        new += [torch.full((pages, kv_heads, page_rows, 4), 127, dtype=torch.uint8, device=device) for _ in range(2)]
+    return tuple(new)
+
+
+def cache_write(cache, table, K, V, starts, index=None):
+    """a2d_cache_write: rows of K and V ([sequences][kv_heads][rows][H] tensors or views, bf16 or fp32) into the pages that table
+    (int32 [sequences][pages], on the device) names: token starts[b] + j of sequence b becomes row index[b][j] (int32
+    [sequences][count]; -1: not written), or row j without an index.  8- and 4-bit codes are rounded to nearest, ties to even, under a power
+    of two for each 32 values that none of them exceeds."""
+    (_native or _ext()).cache_write(cache, table, K, V, starts, index)
+
+
+def cache_read(cache, table, lens, rows, first=0, out=None, out_dtype=torch.bfloat16):
+    """a2d_cache_read: (K, V) [sequences][kv_heads][rows][H] of the tokens first .. first + rows - 1 of every sequence, zeros from lens[b]
+    on; new tensors in out_dtype (bf16 and fp32 hold every value exactly), or out=(K, V), of any strides.  For the tile calls: they take
+    a sequence's [kv_heads][rows][H]."""
+    return (_native or _ext()).cache_read(cache, table, lens, rows, first, out, out_dtype)
+
+
+def tree_masks(parents, lens=None, out=None):
+    """a2d_tree_masks: (masks int64 [sequences][rows][ceil(rows / 64)], positions int32 [sequences][1][rows]) of drafted tokens.  parents
+    (int32 [sequences][rows], on the device): the earlier row that a row follows, -1 the text; anything else: no token.  A row's mask has the
+    bits of itself and its ancestors; its position, lens[b] plus the number of these, is as rotary() takes it."""
+    return (_native or _ext()).tree_masks(parents, lens, out)
+
+
+def partial_fwd_cached(Q, cache, table, lens, K=None, V=None, masks=None, scale=None, max_tokens=0, out=None, normalised=False):
+    """a2d_partial_fwd_cached: the rows Q [sequences][heads][rows][H] (bf16, any strides; grouped heads too) of every sequence against the
+    first lens[b] tokens of its cache and against K, V [sequences][kv_heads][rows][H], the rows' own, which are not in the cache yet: row i
+    sees row j if its mask (tree_masks) has bit j, without masks if j <= i.  Rows that are no tokens get the empty partial.  max_tokens: the
+    host's bound on lens (longer ones count as this), by which the call is planned.  Returns the partial (N, m, l) fp32, or with
+    normalised=True (O in bf16, lse).  Takes up to 35 MiB from torch's allocator while it runs, as the tile calls do."""
+    return (_native or _ext()).partial_fwd_cached(Q, cache, table, lens, K, V, masks, scale, max_tokens, out, normalised)
 
 
 def mfma_ceiling(iters=20000, random_data=True):

@@ -17,7 +17,8 @@ LIB = os.path.join(PKG, "liba2d.so")
 EXT = os.path.join(PKG, "_native.so")
 SOURCES = ["a2d_api.hip", "a2d_device.hip", "a2d_fix.hip", "a2d_generic.hip", "a2d_f32_mfma.hip",
            "a2d_fwd_mfma.hip", "a2d_fwd_small.hip", "a2d_bwd_mfma.hip", "a2d_bwd_wide.hip", "a2d_bwd_one.hip", "a2d_bwd_small.hip", "a2d_grid.hip", "a2d_static.hip",
-           "a2d_scored_fwd.hip", "a2d_scored_bwd.hip", "a2d_scored_f32.hip", "a2d_scored_generic.hip", "a2d_rotary.hip", "a2d_probe.hip"]
+           "a2d_scored_fwd.hip", "a2d_scored_bwd.hip", "a2d_scored_f32.hip", "a2d_scored_generic.hip", "a2d_rotary.hip",
+           "a2d_cache.hip", "a2d_cached.hip", "a2d_cached_bf16.hip", "a2d_cached_e4m3.hip", "a2d_cached_e2m1.hip", "a2d_probe.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC,
@@ -59,7 +60,8 @@ def build(force=False, verbose=True):
                os.path.join(CSRC, "a2d_bwd.hpp"), os.path.join(CSRC, "a2d_bwd_dq.hpp"),
                os.path.join(CSRC, "a2d_bwd_pairs.hpp"), os.path.join(CSRC, "a2d_bwd_wide.hpp"),
                os.path.join(CSRC, "a2d_grid.hpp"), os.path.join(CSRC, "a2d_scored.hpp"), os.path.join(CSRC, "a2d_fwd.hpp"), os.path.join(CSRC, "a2d_scored_rows.hpp"),
-               os.path.join(CSRC, "a2d_f32.hpp"), os.path.join(ROOT, "include", "a2d.h")]
+               os.path.join(CSRC, "a2d_f32.hpp"), os.path.join(CSRC, "a2d_cache.hpp"), os.path.join(CSRC, "a2d_cached_cut.hpp"),
+               os.path.join(CSRC, "a2d_cached_fwd.hpp"), os.path.join(ROOT, "include", "a2d.h")]
     jobs, objs = [], []
     for src in SOURCES:
         s = os.path.join(CSRC, src)

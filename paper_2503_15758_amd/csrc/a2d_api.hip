@@ -1,11 +1,13 @@
 // C-ABI layer of liba2d: argument validation, kernel selection, error reporting.
 // No arithmetic happens here; see include/a2d.h for the contract of every call.
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
 
+#include "a2d_cache.hpp"
 #include "a2d_scored.hpp"
 
 namespace {
@@ -961,6 +963,244 @@ a2d_status a2d_rotary(const a2d_rotary_desc* desc, int n, const a2d_rotary_tenso
   hipStream_t s = static_cast<hipStream_t>(stream);
   a2d::trace_mark(s);
   return hip_result(a2d::launch_rotary(d, n, t, cus, s), who);
+}
+
+}  // extern "C"
+
+// ---- the paged cache
+
+namespace {
+
+a2d_status check_cache(const a2d_cache* c, const char* who) {
+  if (!c) return fail(A2D_ERR_INVALID_ARG, "%s: cache is NULL", who);
+  if (c->format != A2D_CACHE_BF16 && c->format != A2D_CACHE_E4M3 && c->format != A2D_CACHE_E2M1)
+    return fail(A2D_ERR_UNSUPPORTED, "%s: cache format %d not supported", who, c->format);
+  if (c->hdim != 64 && c->hdim != 80 && c->hdim != 96 && c->hdim != 128)
+    return fail(A2D_ERR_UNSUPPORTED, "%s: head size %d not supported (64, 80, 96 or 128)", who, c->hdim);
+  if (c->kv_heads < 1 || c->kv_heads > 65535 || c->sequences < 1 || c->sequences > 65535)
+    return fail(A2D_ERR_INVALID_ARG, "%s: kv_heads=%d, sequences=%d must be 1..65535", who, c->kv_heads, c->sequences);
+  if (c->page_rows < 16 || c->page_rows > (1 << 22) || c->page_rows % 16 != 0)
+    return fail(A2D_ERR_INVALID_ARG, "%s: page_rows=%d must be a multiple of 16 in 16..2^22", who, c->page_rows);
+  // (units of 16 rows are numbered in 32 bits, one number stands for none)
+  if (c->pages < 1 || (double)c->pages * c->kv_heads * c->page_rows >= 0x1p36)
+    return fail(A2D_ERR_INVALID_ARG, "%s: pages=%d: pages * kv_heads * page_rows must be 16..2^36", who, c->pages);
+  if (c->max_pages < 1 || (int64_t)c->max_pages * c->page_rows > (1 << 30))
+    return fail(A2D_ERR_INVALID_ARG, "%s: max_pages=%d: a sequence has 1 to 2^30 tokens", who, c->max_pages);
+  if (c->pad != 0) return fail(A2D_ERR_INVALID_ARG, "%s: pad must be 0", who);
+  A2D_TRY(check_ptr(c->K, who, "the cache's K"));
+  A2D_TRY(check_ptr(c->V, who, "the cache's V"));
+  A2D_TRY(check_ptr(c->table, who, "table"));
+  if (c->format != A2D_CACHE_BF16) {
+    A2D_TRY(check_ptr(c->K_scales, who, "K_scales"));
+    A2D_TRY(check_ptr(c->V_scales, who, "V_scales"));
+  }
+  return A2D_OK;
+}
+
+a2d::CacheView view_of(const a2d_cache& c) {
+  return a2d::CacheView{static_cast<char*>(c.K), static_cast<char*>(c.V), reinterpret_cast<char*>(c.K_scales),
+                        reinterpret_cast<char*>(c.V_scales), c.table, c.kv_heads, c.page_rows / 16, c.pages, c.max_pages};
+}
+
+// A layout with {0, 0, 0} filled in.  output: its rows must not overlap - the dimensions, by their strides, reach past all smaller ones
+a2d_status batch_layout(const a2d_batch_layout* l, const char* name, int64_t sequences, int64_t heads, int64_t rows, int hdim, int esize,
+                        bool output, const char* who, a2d::BatchLayout* out) {
+  if (!l) return fail(A2D_ERR_INVALID_ARG, "%s: layout of %s is NULL", who, name);
+  *out = a2d::BatchLayout{l->sequence, l->head, l->row};
+  if (l->sequence == 0 && l->head == 0 && l->row == 0) {
+    *out = a2d::BatchLayout{heads * rows * hdim, rows * hdim, hdim};
+  }
+  const int64_t unit = 16 / esize, most = (int64_t)1 << 40;
+  if (out->sequence < 1 || out->head < 1 || out->row < hdim || out->sequence > most || out->head > most || out->row > most)
+    return fail(A2D_ERR_INVALID_ARG, "%s: layout of %s: sequence=%lld head=%lld row=%lld (row >= H, the others >= 1 needed)", who, name,
+                (long long)out->sequence, (long long)out->head, (long long)out->row);
+  if (out->sequence % unit || out->head % unit || out->row % unit)
+    return fail(A2D_ERR_MISALIGNED, "%s: layout of %s: sequence=%lld head=%lld row=%lld must be multiples of %lld elements", who, name,
+                (long long)out->sequence, (long long)out->head, (long long)out->row, (long long)unit);
+  if (((rows - 1) * out->row + hdim) * esize >= ((int64_t)1 << 32))
+    return fail(A2D_ERR_UNSUPPORTED, "%s: layout of %s: a head's rows span 4 GiB or more", who, name);
+  if (output) {
+    struct Dim { int64_t n, stride; } d[3] = {{sequences, out->sequence}, {heads, out->head}, {rows, out->row}};
+    std::sort(d, d + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+    int64_t reach = hdim;
+    for (const Dim& x : d) {
+      if (x.n == 1) continue;
+      if (x.stride < reach) return fail(A2D_ERR_INVALID_ARG, "%s: layout of %s: its rows overlap", who, name);
+      reach += (x.n - 1) * x.stride;
+    }
+  }
+  return A2D_OK;
+}
+
+int dtype_bytes(int dtype) { return dtype == A2D_F32 ? 4 : 2; }
+
+a2d_status cache_rows(const a2d_cache* cache, int32_t rows, int32_t count, int32_t dtype, const void* K, const a2d_batch_layout* lk,
+                      const void* V, const a2d_batch_layout* lv, bool output, const char* who, a2d::CacheRows* a) {
+  A2D_TRY(check_cache(cache, who));
+  if (rows < 1 || rows > (1 << 22) || count < 1 || count > (1 << 22))
+    return fail(A2D_ERR_INVALID_ARG, "%s: rows=%d, count=%d must be 1..2^22", who, rows, count);
+  if (dtype != A2D_F32 && dtype != A2D_BF16) return fail(A2D_ERR_UNSUPPORTED, "%s: dtype %d is neither A2D_F32 nor A2D_BF16", who, dtype);
+  A2D_TRY(check_ptr(K, who, "K"));
+  A2D_TRY(check_ptr(V, who, "V"));
+  if (output && K == V) return fail(A2D_ERR_INVALID_ARG, "%s: K and V are the same output", who);
+  if (!output && cache->K == cache->V) return fail(A2D_ERR_INVALID_ARG, "%s: the cache's K and V are the same memory", who);
+  *a = a2d::CacheRows{};
+  a->c = view_of(*cache);
+  a->sequences = cache->sequences;
+  a->rows = rows;
+  a->count = count;
+  a->K = static_cast<const char*>(K);
+  a->V = static_cast<const char*>(V);
+  A2D_TRY(batch_layout(lk, "K", cache->sequences, cache->kv_heads, rows, cache->hdim, dtype_bytes(dtype), output, who, &a->lk));
+  return batch_layout(lv, "V", cache->sequences, cache->kv_heads, rows, cache->hdim, dtype_bytes(dtype), output, who, &a->lv);
+}
+
+// What the call goes by, all but its tensors
+a2d_status cached_args(const a2d_cache* cache, const a2d_cached_desc* d, bool drafts, const char* who, a2d::CachedArgs* a) {
+  A2D_TRY(check_cache(cache, who));
+  if (!d) return fail(A2D_ERR_INVALID_ARG, "%s: descriptor is NULL", who);
+  if (d->heads < 1 || d->heads > 65535 || d->heads % cache->kv_heads != 0)
+    return fail(A2D_ERR_INVALID_ARG, "%s: heads=%d must be 1..65535 and a multiple of kv_heads=%d", who, d->heads, cache->kv_heads);
+  const int group = d->heads / cache->kv_heads;
+  if (d->rows < 1 || d->rows > (1 << 20) || (int64_t)group * d->rows > (1 << 22))
+    return fail(A2D_ERR_INVALID_ARG, "%s: rows=%d outside 1..2^20, or heads / kv_heads * rows above 2^22", who, d->rows);
+  if (d->masks && d->rows > A2D_TREE_MAX_ROWS)
+    return fail(A2D_ERR_UNSUPPORTED, "%s: rows=%d with masks (at most %d)", who, d->rows, A2D_TREE_MAX_ROWS);
+  if (d->max_tokens < 0) return fail(A2D_ERR_INVALID_ARG, "%s: max_tokens=%d is negative", who, d->max_tokens);
+  if (!(d->scale > 0.f) || !std::isfinite(d->scale)) return fail(A2D_ERR_INVALID_ARG, "%s: scale must be finite and > 0", who);
+  if (d->scale > 1e30f) return fail(A2D_ERR_UNSUPPORTED, "%s: scale=%g is above 1e30", who, d->scale);
+  if (d->masks) A2D_TRY(check_ptr(d->masks, who, "masks"));
+  A2D_TRY(check_ptr(d->lens, who, "lens"));
+  *a = a2d::CachedArgs{};
+  a->c = view_of(*cache);
+  a->sequences = cache->sequences;
+  a->heads = d->heads;
+  a->group = group;
+  a->rows = d->rows;
+  const int32_t room = cache->max_pages * cache->page_rows;
+  a->max_tokens = d->max_tokens == 0 || d->max_tokens > room ? room : d->max_tokens;
+  a->words = (d->rows + 63) / 64;
+  a->scale = d->scale;
+  a->c2 = d->scale * a2d::kLog2e;
+  a->lens = d->lens;
+  a->masks = d->masks;
+  if (drafts) a->K = a->V = reinterpret_cast<const char*>(cache);          // (for the plan: there are some)
+  A2D_TRY(batch_layout(&d->lq, "Q", cache->sequences, d->heads, d->rows, cache->hdim, 2, false, who, &a->lq));
+  A2D_TRY(batch_layout(&d->lk, "K", cache->sequences, cache->kv_heads, d->rows, cache->hdim, 2, false, who, &a->lk));
+  A2D_TRY(batch_layout(&d->lv, "V", cache->sequences, cache->kv_heads, d->rows, cache->hdim, 2, false, who, &a->lv));
+  A2D_TRY(batch_layout(&d->lo, "O", cache->sequences, d->heads, d->rows, cache->hdim, 2, true, who, &a->lo));
+  const a2d::CachedPlan p = a2d::plan_cached(cache->format, cache->hdim, *a, 1, false);
+  a->tiles = p.tiles;
+  a->blocks = p.blocks;
+  // (steps are numbered through in 32 bits, workgroups in 31)
+  const double walks = (double)cache->sequences * cache->kv_heads * p.blocks;
+  if (walks * ((a->max_tokens + 31) / 32 + (d->rows + 31) / 32) >= 0x1p31 || (double)cache->sequences * d->heads * d->rows >= 0x1p31)
+    return fail(A2D_ERR_UNSUPPORTED, "%s: more than 2^31 steps of 32 keys, or rows of all heads, in one call", who);
+  return A2D_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+a2d_status a2d_cache_write(const a2d_cache* cache, int32_t rows, int32_t count, int32_t dtype, const void* K, const a2d_batch_layout* lk,
+                           const void* V, const a2d_batch_layout* lv, const int32_t* starts, const int32_t* index, void* stream) {
+  const char* who = "a2d_cache_write";
+  a2d::CacheRows a;
+  A2D_TRY(cache_rows(cache, rows, count, dtype, K, lk, V, lv, false, who, &a));
+  if (!index && count != rows) return fail(A2D_ERR_INVALID_ARG, "%s: count=%d of rows=%d without an index", who, count, rows);
+  A2D_TRY(check_ptr(starts, who, "starts"));
+  if (index) A2D_TRY(check_ptr(index, who, "index"));
+  a.starts = starts;
+  a.index = index;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  a2d::trace_mark(s);
+  return hip_result(a2d::launch_cache_write(cache->format, cache->hdim, dtype, a, s), who);
+}
+
+a2d_status a2d_cache_read(const a2d_cache* cache, const int32_t* lens, int32_t first, int32_t rows, int32_t dtype, void* K,
+                          const a2d_batch_layout* lk, void* V, const a2d_batch_layout* lv, void* stream) {
+  const char* who = "a2d_cache_read";
+  a2d::CacheRows a;
+  A2D_TRY(cache_rows(cache, rows, rows, dtype, K, lk, V, lv, true, who, &a));
+  if (first < 0) return fail(A2D_ERR_INVALID_ARG, "%s: first=%d is negative", who, first);
+  A2D_TRY(check_ptr(lens, who, "lens"));
+  a.first = first;
+  a.starts = lens;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  a2d::trace_mark(s);
+  return hip_result(a2d::launch_cache_read(cache->format, cache->hdim, dtype, a, s), who);
+}
+
+a2d_status a2d_tree_masks(int32_t sequences, int32_t rows, const int32_t* parents, const int32_t* lens, uint64_t* masks, int32_t* positions,
+                          void* stream) {
+  const char* who = "a2d_tree_masks";
+  if (sequences < 1 || sequences > 65535) return fail(A2D_ERR_INVALID_ARG, "%s: sequences=%d outside 1..65535", who, sequences);
+  if (rows < 1) return fail(A2D_ERR_INVALID_ARG, "%s: rows=%d must be >= 1", who, rows);
+  if (rows > A2D_TREE_MAX_ROWS) return fail(A2D_ERR_UNSUPPORTED, "%s: rows=%d (at most %d)", who, rows, A2D_TREE_MAX_ROWS);
+  A2D_TRY(check_ptr(parents, who, "parents"));
+  if (lens) A2D_TRY(check_ptr(lens, who, "lens"));
+  A2D_TRY(check_ptr(masks, who, "masks"));
+  A2D_TRY(check_ptr(positions, who, "positions"));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  a2d::trace_mark(s);
+  return hip_result(a2d::launch_tree_masks(sequences, rows, parents, lens, masks, positions, s), who);
+}
+
+size_t a2d_cached_workspace_bytes(const a2d_cache* cache, const a2d_cached_desc* desc) {
+  a2d::CachedArgs a;
+  int cus = 0;
+  if (cached_args(cache, desc, true, "a2d_cached_workspace_bytes", &a) != A2D_OK || a2d::device_cus(&cus) != hipSuccess) return 0;
+  const a2d::CachedPlan p = a2d::plan_cached(cache->format, cache->hdim, a, cus, true);
+  a.K = a.V = nullptr;                               // (with or without drafted rows)
+  const a2d::CachedPlan q = a2d::plan_cached(cache->format, cache->hdim, a, cus, true);
+  return p.bytes > q.bytes ? p.bytes : q.bytes;
+}
+
+a2d_status a2d_partial_fwd_cached(const a2d_cache* cache, const a2d_cached_desc* desc, int flags, const void* Q, const void* K, const void* V,
+                                  void* out0, float* out1, float* out2, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "a2d_partial_fwd_cached";
+  a2d::CachedArgs a;
+  A2D_TRY(cached_args(cache, desc, K != nullptr, who, &a));
+  if (flags != 0 && flags != A2D_TILE_NORMALISED) return fail(A2D_ERR_INVALID_ARG, "%s: flags=%d (0 or A2D_TILE_NORMALISED)", who, flags);
+  a.norm = flags == A2D_TILE_NORMALISED;
+  if (!K != !V) return fail(A2D_ERR_INVALID_ARG, "%s: K and V of the rows come together", who);
+  A2D_TRY(check_ptr(Q, who, "Q"));
+  if (K) {
+    A2D_TRY(check_ptr(K, who, "K"));
+    A2D_TRY(check_ptr(V, who, "V"));
+  }
+  A2D_TRY(check_ptr(out0, who, a.norm ? "O" : "N"));
+  A2D_TRY(check_ptr(out1, who, a.norm ? "lse" : "m"));
+  if (!a.norm) A2D_TRY(check_ptr(out2, who, "l"));
+  if (out0 == Q || out0 == K || out0 == V || out0 == out1 || (!a.norm && (out0 == out2 || out1 == out2)))
+    return fail(A2D_ERR_INVALID_ARG, "%s: an output is an input or another output", who);
+  a.Q = static_cast<const char*>(Q);
+  a.K = static_cast<const char*>(K);
+  a.V = static_cast<const char*>(V);
+  a.out0 = out0;
+  a.out1 = out1;
+  a.out2 = out2;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (a2d::force_generic()) {
+    a2d::trace_mark(s);
+    return hip_result(a2d::launch_cached_generic(cache->format, cache->hdim, a, s), who);
+  }
+  if (workspace) {
+    if (workspace_bytes > ((size_t)1 << 46))
+      return fail(A2D_ERR_INVALID_ARG, "%s: workspace_bytes = %zu is not a plausible size (size_t expected)", who, workspace_bytes);
+    int cus = 0;
+    A2D_TRY(hip_result(a2d::device_cus(&cus), who));
+    const a2d::CachedPlan p = a2d::plan_cached(cache->format, cache->hdim, a, cus, true);
+    if (workspace_bytes < p.bytes)
+      return fail(A2D_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given (or none)", who, p.bytes, workspace_bytes);
+    if (!aligned16(workspace)) return fail(A2D_ERR_MISALIGNED, "%s: workspace is not 16-byte aligned", who);
+    a.workers = p.workers;
+    a.parts = static_cast<float*>(workspace);
+  }
+  A2D_TRY(hip_result(a2d::launch_cached(a2d::PREPARE, cache->format, cache->hdim, a, s), who));
+  a2d::trace_mark(s);
+  return hip_result(a2d::launch_cached(a2d::LAUNCH, cache->format, cache->hdim, a, s), who);
 }
 
 const char* a2d_status_str(a2d_status status) {

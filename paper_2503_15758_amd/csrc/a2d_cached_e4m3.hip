@@ -1,0 +1,8 @@
+// The kernels of a2d_cached_fwd.hpp over a cache in e4m3.
+#include "a2d_cached_fwd.hpp"
+
+namespace a2d {
+hipError_t launch_cached_e4m3(Phase ph, int hdim, const CachedArgs& a, hipStream_t s) {
+  return cached::go_format<A2D_CACHE_E4M3>(ph, hdim, a, s);
+}
+}  // namespace a2d

@@ -1,0 +1,614 @@
+// Attention of a few rows of each sequence - new tokens, a tree of drafted ones - against the paged cache, bf16 on the matrix units.
+//
+//   s = scale <q, k>;  row i sees all cached tokens of its sequence and the drafted rows j whose bit is set in its mask (no masks: j <= i);
+//   N = sum 2^(s' - m') v, l = sum 2^(s' - m') in log2 units, one pass over the keys.
+//
+// A workgroup has a block of 16, 32 or 64 rows (query heads of a group and rows of a sequence, numbered through) of one key/value head, and
+// a run of its keys in steps of 32, dealt in turn to its four wavefronts.  Each wavefront keeps (N, m, l) of all the block's rows to itself: no
+// barrier on the walk, the four are joined through LDS at its end.
+//  - S^T = K Q^T: a lane's part of K comes straight from memory, 16 values in a piece (16 bytes of e4m3): the order in which the columns
+//    are contracted is the one in which pieces lie (half a row apart they fill whole lines), and Q is held in the same.
+//  - O^T += V^T P^T: V goes through LDS of the wavefront's own, decoded, for the transposing reads.
+//  - Codes are decoded with their scales by the conversion itself, exactly (a2d_cache.hpp); so only P is rounded, to two bf16
+//    numbers (2^-17): these calls wait for memory.
+//  - Pages: 64 page numbers at a time are in the lanes of a register, and a step's two are read from there as scalars.
+#pragma once
+#include "a2d_cached_cut.hpp"
+
+namespace a2d {
+namespace cached {
+
+using namespace mfma;
+
+constexpr int WAVES = 4;
+constexpr float LOW = -3.0e38f;                      // a reference below every score
+
+template <int N>
+struct Words { unsigned w[N]; };
+// N = 1, 2, 4, 8 dwords
+template <int N>
+__device__ __forceinline__ Words<N> load_words(gptr_t base, unsigned off) {
+  Words<N> r;
+  if constexpr (N == 1) {
+    r.w[0] = *reinterpret_cast<const __attribute__((address_space(1))) unsigned*>(base + off);
+  } else if constexpr (N == 2) {
+    const u32x2 x = *reinterpret_cast<const __attribute__((address_space(1))) u32x2*>(base + off);
+    r.w[0] = x[0];
+    r.w[1] = x[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const u32x4 x = gload_b128(base, off + 16 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.w[4 * i + e] = x[e];
+    }
+  }
+  return r;
+}
+
+// How a head size's columns fall into a lane's pieces.  Lane group g = lane / 16 has the columns 64 j + 16 g .. + 15 (slices 2 j and
+// 2 j + 1 of the contraction) and, of the rest, 64 JF + 8 g .. + 7 (the last slice; H = 80: groups 0 and 1).
+template <int H>
+struct Head {
+  static constexpr int HD = padded_head(H), KS = HD / 32, HT = H / 16, JF = H / 64, REST = (H % 64) / 8;
+  static constexpr int PIECES = H / 16, NV = (16 * PIECES + 63) / 64;      // of a row of V; loads of a tile
+  static constexpr int AREA = 2 * KS * BLOCK;                              // of a wavefront in LDS
+};
+
+// a lane's codes of 16 keys as they come from memory
+template <int H, int FMT>
+struct Codes {
+  using G = Head<H>;
+  static constexpr int W = code_bytes<FMT>(16) / 4;
+  Words<W> k[G::JF], v[G::NV];
+  Words<(W + 1) / 2> rest;
+  unsigned ks, vs[G::NV];
+};
+
+// where a lane's pieces lie in a tile of 16 rows
+template <int H>
+struct Lane {
+  using G = Head<H>;
+  int row, g, vrow[G::NV];
+  unsigned lds[G::NV];
+  bool has_rest, vlive[G::NV];
+  unsigned vpiece[G::NV];
+  __device__ __forceinline__ void init(int lane) {
+    row = lane & 15;
+    g = lane >> 4;
+    has_rest = g < G::REST;
+#pragma unroll
+    for (int n = 0; n < G::NV; ++n) {
+      const int at = min(64 * n + lane, 16 * G::PIECES - 1);
+      vlive[n] = 64 * n + lane < 16 * G::PIECES;
+      vrow[n] = at / G::PIECES;
+      vpiece[n] = at % G::PIECES;
+      lds[n] = (vpiece[n] >> 1) * BLOCK + vrow[n] * 64 + 16 * ((2 * (vpiece[n] & 1)) ^ block_swap(vrow[n] >> 2));
+    }
+  }
+};
+
+// The codes of one unit of the cache
+template <int H, int FMT>
+__device__ __forceinline__ void load_unit(Codes<H, FMT>& c, const CacheView& view, unsigned unit, const Lane<H>& l) {
+  using G = Head<H>;
+  constexpr int ROW = code_bytes<FMT>(H), W = Codes<H, FMT>::W;
+  const gptr_t k = uniform_gptr(view.K + (uint64_t)unit * (16 * ROW)), v = uniform_gptr(view.V + (uint64_t)unit * (16 * ROW));
+#pragma unroll
+  for (int j = 0; j < G::JF; ++j) c.k[j] = load_words<W>(k, l.row * ROW + l.g * code_bytes<FMT>(16) + j * code_bytes<FMT>(64));
+  if constexpr (G::REST)       // (lanes without columns there take the row's first)
+    c.rest = load_words<(W + 1) / 2>(k, l.row * ROW + (l.has_rest ? code_bytes<FMT>(64) * G::JF + l.g * code_bytes<FMT>(8) : 0));
+#pragma unroll
+  for (int n = 0; n < G::NV; ++n) c.v[n] = load_words<W>(v, l.vrow[n] * ROW + l.vpiece[n] * code_bytes<FMT>(16));
+  if constexpr (FMT != A2D_CACHE_BF16) {
+    const gptr_t ks = uniform_gptr(view.Ks + (uint64_t)unit * 64), vs = uniform_gptr(view.Vs + (uint64_t)unit * 64);
+    c.ks = load_words<1>(ks, l.row * 4).w[0];
+#pragma unroll
+    for (int n = 0; n < G::NV; ++n) c.vs[n] = load_words<1>(vs, l.vrow[n] * 4).w[0];
+  }
+}
+
+// 16 drafted rows from `first` on (the last row in place of those behind it)
+template <int H>
+__device__ __forceinline__ void load_drafts(Codes<H, A2D_CACHE_BF16>& c, const CachedArgs& a, int b, int h, int first, const Lane<H>& l) {
+  using G = Head<H>;
+  const gptr_t k = uniform_gptr(a.K + 2 * at_row(a.lk, b, h, 0)), v = uniform_gptr(a.V + 2 * at_row(a.lv, b, h, 0));
+  const unsigned kr = (unsigned)min(first + l.row, a.rows - 1) * (unsigned)(2 * a.lk.row);
+#pragma unroll
+  for (int j = 0; j < G::JF; ++j) c.k[j] = load_words<8>(k, kr + l.g * 32 + j * 128);
+  if constexpr (G::REST) c.rest = load_words<4>(k, kr + (l.has_rest ? 128 * G::JF + l.g * 16 : 0));
+#pragma unroll
+  for (int n = 0; n < G::NV; ++n)
+    c.v[n] = load_words<8>(v, (unsigned)min(first + l.vrow[n], a.rows - 1) * (unsigned)(2 * a.lv.row) + l.vpiece[n] * 32);
+}
+
+template <int FMT, int N>
+__device__ __forceinline__ bf16x8 decode_half(const Words<N>& w, int half, float scale) {
+  if constexpr (FMT == A2D_CACHE_BF16) {
+    return __builtin_bit_cast(bf16x8, u32x4{w.w[4 * half], w.w[4 * half + 1], w.w[4 * half + 2], w.w[4 * half + 3]});
+  } else if constexpr (FMT == A2D_CACHE_E4M3) {
+    return decode8<FMT>(w.w[2 * half], w.w[2 * half + 1], scale);
+  } else {
+    return decode8<FMT>(w.w[half], 0, scale);
+  }
+}
+__device__ __forceinline__ void lds_store(unsigned at, bf16x8 x) {
+  *reinterpret_cast<__attribute__((address_space(3))) bf16x8*>((uintptr_t)at) = x;
+}
+__device__ __forceinline__ float lds_number(unsigned at) {
+  return (float)*reinterpret_cast<const __attribute__((address_space(3))) bf16_t*>((uintptr_t)at);
+}
+__device__ __forceinline__ bf16x8 zero8() { return __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0}); }
+
+// K of a tile as fragments
+template <int H, int FMT>
+__device__ __forceinline__ void decode_keys(bf16x8 (&kf)[Head<H>::KS], const Codes<H, FMT>& c, const Lane<H>& l) {
+  using G = Head<H>;
+#pragma unroll
+  for (int j = 0; j < G::JF; ++j) {
+    float scale = 1.f;
+    if constexpr (FMT != A2D_CACHE_BF16) scale = scale_number(c.ks >> (16 * j + 8 * (l.g >> 1)) & 255);
+    kf[2 * j] = decode_half<FMT>(c.k[j], 0, scale);
+    kf[2 * j + 1] = decode_half<FMT>(c.k[j], 1, scale);
+  }
+  if constexpr (G::REST) {
+    float scale = 1.f;
+    if constexpr (FMT != A2D_CACHE_BF16) scale = scale_number(c.ks >> (16 * G::JF) & 255);
+    kf[2 * G::JF] = decode_half<FMT>(c.rest, 0, scale);
+    if (G::REST < 4 && !l.has_rest) kf[2 * G::JF] = zero8();
+  }
+}
+// V of it into LDS at `at` (of the tile's blocks), rows whose bit in `vis` is not set as zeros
+template <int H, int FMT>
+__device__ __forceinline__ void decode_values(const Codes<H, FMT>& c, const Lane<H>& l, unsigned at, unsigned vis) {
+  using G = Head<H>;
+#pragma unroll
+  for (int n = 0; n < G::NV; ++n) {
+    float scale = 1.f;
+    if constexpr (FMT != A2D_CACHE_BF16) scale = scale_number(c.vs[n] >> (8 * (l.vpiece[n] >> 1)) & 255);
+    bf16x8 x = decode_half<FMT>(c.v[n], 0, scale), y = decode_half<FMT>(c.v[n], 1, scale);
+    if (A2D_SELDOM(vis != 0xFFFFu)) {
+      const bool keep = vis >> l.vrow[n] & 1;
+      x = keep ? x : zero8();
+      y = keep ? y : zero8();
+    }
+    if (64 * n + 64 <= 16 * G::PIECES || l.vlive[n]) {
+      lds_store(at + l.lds[n], x);
+      lds_store(at + (l.lds[n] ^ 16), y);
+    }
+  }
+}
+
+// What a wavefront keeps of RT tiles of 16 rows; a lane: row lane & 15 of each, of which it has a quarter of the keys and of O's columns
+template <int H, int RT>
+struct State {
+  f32x4 o[Head<H>::HT][RT];
+  float m[RT];          // largest score the lane has seen, as it comes from the matrix unit
+  float ref[RT];        // log2 units: what the exponentials are relative to, the same in the four lanes of a row
+  float l[RT];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      m[t] = -INFINITY;
+      ref[t] = LOW;
+      l[t] = 0.f;
+#pragma unroll
+      for (int h = 0; h < Head<H>::HT; ++h) o[h][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+};
+
+// Scores to probabilities: s becomes P
+template <int H, int RT>
+__device__ __forceinline__ void soften(State<H, RT>& st, f32x4 (&s)[2][RT], float c2) {
+  float top[RT];
+  bool far = false;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    float x = fmaxf(s[0][t][0], s[1][t][0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) x = fmaxf(x, fmaxf(s[0][t][i], s[1][t][i]));
+    top[t] = x;
+    st.m[t] = fmaxf(st.m[t], x);
+    far |= x * c2 > st.ref[t] + 8.f;
+  }
+  if (A2D_SELDOM(__any(far))) {                      // a reference is only moved by more than 2^8
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const float ref = fmaxf(st.ref[t], row_max(top[t]) * c2);
+      const float f = ref == st.ref[t] ? 1.f : fast_exp2(st.ref[t] - ref);
+      st.ref[t] = ref;
+      st.l[t] *= f;
+#pragma unroll
+      for (int h = 0; h < Head<H>::HT; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.o[h][t][i] *= f;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[k][t][i] = fast_exp2(fmaf(s[k][t][i], c2, -st.ref[t]));
+        st.l[t] += s[k][t][i];
+      }
+}
+
+template <int H, int RT>
+__device__ __forceinline__ void products(State<H, RT>& st, const f32x4 (&s)[2][RT], const Blocks16& rd) {
+  using G = Head<H>;
+  bf16x8 hi[RT], lo[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float p = s[e >> 2][t][e & 3];
+      hi[t][e] = (bf16_t)p;
+      lo[t][e] = (bf16_t)(p - (float)hi[t][e]);
+    }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int h = 0; h < G::HT; ++h) {
+    const unsigned at = (h & 1 ? rd.tr_o : rd.tr_e) + (h >> 1) * BLOCK;
+    const bf16x8 v = lds_load_tr(at, at + G::KS * BLOCK);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      st.o[h][t] = mma16(v, hi[t], st.o[h][t]);
+      st.o[h][t] = mma16(v, lo[t], st.o[h][t]);
+    }
+  }
+}
+
+// of the 16 keys of a tile
+template <int H, int RT>
+__device__ __forceinline__ void scores(f32x4 (&s)[RT], const bf16x8 (&kf)[Head<H>::KS], const bf16x8 (&qf)[Head<H>::KS][RT]) {
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < Head<H>::KS; ++x) s[t] = mma16(kf[x], qf[x][t], s[t]);
+  }
+}
+
+// Is any of the eight numbers a NaN or an infinity?
+__device__ __forceinline__ bool not_finite(bf16x8 x) {
+  const u32x4 w = __builtin_bit_cast(u32x4, x);
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bad |= (w[i] & 0x7F80u) == 0x7F80u || (w[i] & 0x7F800000u) == 0x7F800000u;
+  return bad;
+}
+
+// bits of 32 drafted rows from 32 * step on that row i of sequence b sees
+__device__ __forceinline__ unsigned seen_rows(const CachedArgs& a, int b, int i, int step) {
+  if (a.masks) {
+    const uint64_t w = a.masks[((int64_t)b * a.rows + i) * a.words + (step >> 1)];
+    const unsigned x = (unsigned)(w >> (32 * (step & 1)));
+    const int left = a.rows - STEP * step;            // (bits of no row)
+    return left < 32 ? x & ((1u << left) - 1) : x;
+  }
+  const int n = i - STEP * step;
+  return n < 0 ? 0 : n >= 31 ? ~0u : (2u << n) - 1;
+}
+// is row i a token (its own bit is set)?
+__device__ __forceinline__ bool is_token(const CachedArgs& a, int b, int i) {
+  return !a.masks || (a.masks[((int64_t)b * a.rows + i) * a.words + (i >> 6)] >> (i & 63) & 1);
+}
+
+template <int H, int FMT, int RT>
+struct Walk {
+  using G = Head<H>;
+  const CachedArgs& a;
+  const Lane<H>& ln;
+  const Blocks16& rd;
+  unsigned area;                                     // LDS: the wavefront's V
+  int lane, wave;
+  State<H, RT> st;
+  bf16x8 qf[G::KS][RT];
+  int row_of[RT];                                    // the row within its sequence of the lane's row in a tile
+  bool live[RT];
+
+  // steps s0 .. s1 - 1 of block `block` of head h of sequence b
+  __device__ __forceinline__ void run(int b, int h, int block, int s0, int s1) {
+    const int rows = a.group * a.rows;
+    Lane<H> ln;
+    ln.init(lane_again());
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int at = (block * RT + t) * 16 + ln.row, r = min(at, rows - 1);
+      const Split sp = split_by(r, a.rows);
+      const int head = a.rows == 1 ? r : sp.q, i = a.rows == 1 ? 0 : sp.r;
+      row_of[t] = i;
+      live[t] = at < rows && is_token(a, b, i);
+      const bf16_t* q = reinterpret_cast<const bf16_t*>(a.Q) + at_row(a.lq, b, h * a.group + head, i);
+#pragma unroll
+      for (int x = 0; x < 2 * G::JF; ++x) qf[x][t] = *reinterpret_cast<const bf16x8*>(q + 64 * (x >> 1) + 16 * ln.g + 8 * (x & 1));
+      if constexpr (G::REST) {
+        qf[2 * G::JF][t] = *reinterpret_cast<const bf16x8*>(q + (ln.has_rest ? 64 * G::JF + 8 * ln.g : 0));
+        if (G::REST < 4 && !ln.has_rest) qf[2 * G::JF][t] = zero8();
+      }
+    }
+    st.clear();
+    const int tokens = cached_tokens(a, b), cached = (tokens + STEP - 1) / STEP;
+    const int last = min(s1, cached);
+    if (s0 + wave < last) cache_steps(b, h, s0 + wave, last, tokens);
+    if (a.K) {
+      // (those in front of the first drafted step are behind the wavefront's last cached one)
+      int s = s0 + wave;
+      if (s < cached) s += (cached - s + WAVES - 1) / WAVES * WAVES;
+      for (; s < s1; s += WAVES) draft_step(b, h, s - cached);
+    }
+  }
+
+  __device__ __forceinline__ void cache_steps(int b, int h, int first, int last, int tokens) {
+    Codes<H, FMT> c[2];
+    unsigned units = 0;                              // of tile lane & 1 of the wavefront's step lane >> 1, of 32
+    const auto look_up = [&](int s) {
+      const int tile = 2 * (s + WAVES * (lane >> 1)) + (lane & 1);
+      units = tile * 16 < tokens ? unit_of(a.c, b, h, tile) : NO_UNIT;
+    };
+    unsigned vis = 0;
+    const auto load = [&](int n, int s) {            // the wavefront's n-th step, s
+      vis = 0;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const unsigned u = __builtin_amdgcn_readlane((int)units, 2 * (n & 31) + k);
+        const int there = min(max(tokens - STEP * s - 16 * k, 0), 16);
+        if (u != NO_UNIT) vis |= ((1u << there) - 1) << (16 * k);
+        load_unit<H, FMT>(c[k], a.c, u == NO_UNIT ? 0 : u, ln);
+      }
+    };
+    look_up(first);
+    load(0, first);
+    for (int s = first, n = 0; s < last; s += WAVES, ++n) {
+      f32x4 sc[2][RT];
+      const unsigned now = vis;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        bf16x8 kf[G::KS];
+        decode_values<H, FMT>(c[k], ln, area + k * G::KS * BLOCK, k ? now >> 16 : now & 0xFFFF);
+        decode_keys<H, FMT>(kf, c[k], ln);
+        scores<H, RT>(sc[k], kf, qf);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      // the next step's codes, while this one is worked on (behind the last: the last again)
+      const bool more = s + WAVES < last;
+      if (A2D_SELDOM((n & 31) == 31 && more)) look_up(s + WAVES);
+      load(more ? n + 1 : n, more ? s + WAVES : s);
+      if (A2D_SELDOM(now != ~0u)) {
+        const unsigned mine = now >> (4 * ln.g);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[k][t][i] = mine >> (16 * k + i) & 1 ? sc[k][t][i] : -INFINITY;
+      }
+      soften<H, RT>(st, sc, a.c2);
+      products<H, RT>(st, sc, rd);
+    }
+  }
+
+  // (the lane's places are computed anew: kept beside the walk over the cache, they would take its registers)
+  __device__ __forceinline__ void draft_step(int b, int h, int step) {
+    Lane<H> ln;
+    ln.init(lane_again());
+    unsigned seen[RT], all = 0;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      seen[t] = live[t] ? seen_rows(a, b, row_of[t], step) : 0;
+      all |= seen[t];
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) all |= (unsigned)__shfl_xor((int)all, d);
+    all = __builtin_amdgcn_readfirstlane((int)all);
+    if (all == 0) return;
+    f32x4 sc[2][RT];
+    unsigned bad = 0;                                // drafted rows of the step whose V is not finite
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      Codes<H, A2D_CACHE_BF16> c;
+      load_drafts<H>(c, a, b, h, STEP * step + 16 * k, ln);
+#pragma unroll
+      for (int n = 0; n < G::NV; ++n) {
+        const bool odd = ln.vlive[n] && (all >> (16 * k + ln.vrow[n]) & 1) &&
+                         (not_finite(decode_half<A2D_CACHE_BF16>(c.v[n], 0, 1.f)) || not_finite(decode_half<A2D_CACHE_BF16>(c.v[n], 1, 1.f)));
+        bad |= odd ? 1u << (16 * k + ln.vrow[n]) : 0;
+      }
+      // (rows that none of the block's rows see are zeros: they may hold anything)
+      decode_values<H, A2D_CACHE_BF16>(c, ln, area + k * G::KS * BLOCK, all >> (16 * k) & 0xFFFF);
+      bf16x8 kf[G::KS];
+      decode_keys<H, A2D_CACHE_BF16>(kf, c, ln);
+      scores<H, RT>(sc[k], kf, qf);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[k][t][i] = seen[t] >> (16 * k + 4 * ln.g + i) & 1 ? sc[k][t][i] : -INFINITY;
+    soften<H, RT>(st, sc, a.c2);
+    if (A2D_SELDOM(__any(bad != 0))) apart(sc, seen, bad);
+    products<H, RT>(st, sc, rd);
+  }
+
+  // A drafted row's V with a NaN or an infinity may be added to those rows only that see it, and a product with P = 0 is not 0 then: such
+  // keys are added one at a time and become zeros in LDS.
+  __device__ __forceinline__ void apart(const f32x4 (&sc)[2][RT], const unsigned (&seen)[RT], unsigned bad) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) bad |= (unsigned)__shfl_xor((int)bad, d);
+    bad = __builtin_amdgcn_readfirstlane((int)bad);
+    const int lane = lane_again();
+    while (bad) {
+      const int key = __builtin_ctz(bad), k = key >> 4, r = key & 15;
+      bad &= bad - 1;
+      // column c of the key: block c / 32, chunk c / 8 % 4 of its row
+      const unsigned row = area + k * G::KS * BLOCK + r * 64;
+      const auto column = [&](int c) { return row + (c >> 5) * BLOCK + 16 * ((c >> 3 & 3) ^ block_swap(r >> 2)) + 2 * (c & 7); };
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        float p = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p = 4 * (e >> 2) + (e & 3) == 4 * k + (r & 3) ? sc[e >> 2][t][e & 3] : p;
+        p = __shfl(p, 16 * (r >> 2) + (lane & 15));
+        if (!(seen[t] >> key & 1)) continue;
+#pragma unroll
+        for (int h = 0; h < G::HT; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st.o[h][t][i] = fmaf(p, lds_number(column(16 * h + 4 * (lane >> 4) + i)), st.o[h][t][i]);
+      }
+      if (lane < H / 8) lds_store(column(8 * lane), zero8());
+    }
+  }
+};
+
+template <int H, int FMT, int RT>
+__global__ __launch_bounds__(64 * WAVES, RT == 1 ? 3 : RT == 2 ? 2 : 1) void cached_kernel(CachedArgs a) {
+  using G = Head<H>;
+  constexpr int ROWS = 16 * RT, QUADS = H / 4;
+  __shared__ __align__(1024) char area[WAVES][G::AREA];
+  __shared__ f32x4 stat[WAVES][ROWS];                // m (log2 units), ref, l of a wavefront's row
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Lane<H> ln;
+  ln.init(lane);
+  Blocks16 rd;
+  const unsigned mine = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)area[wave];
+  rd.init(lane, mine);
+  Walk<H, FMT, RT> w{a, ln, rd, mine, lane, wave};
+
+  // the workgroup's run of the line of steps
+  const int per_sequence = a.c.kv_heads * a.blocks;
+  int b, unit, s0;
+  unsigned left;
+  int worker = -1;
+  if (a.workers == 0) {
+    b = blockIdx.x / per_sequence;
+    unit = blockIdx.x - b * per_sequence;
+    s0 = 0;
+    left = walk_steps(a, b);
+  } else {
+    const Cut cut = make_cut(a, lane);
+    // neighbours on the line, which share keys where a head has several blocks, to one XCD
+    const unsigned per = (cut.workers + 7) / 8, n = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= per || n >= cut.workers) return;
+    worker = (int)n;
+    unsigned at = cut.begin(n);
+    left = cut.begin(n + 1) - at;
+    unsigned before = 0;                             // of the sequences in front of the chunk
+    int first = 0;
+    unsigned sum;
+    for (;; first += 64) {
+      sum = sequence_sum(a, first, lane);
+      const unsigned all = __builtin_amdgcn_readlane((int)sum, 63);
+      if (at < before + all || first + 64 >= a.sequences) break;
+      before += all;
+    }
+    const int in = __popcll(__ballot(before + sum <= at));       // sequences of the chunk that end in front of it
+    b = first + in;
+    if (in > 0) before += __builtin_amdgcn_readlane((int)sum, in - 1);
+    const int steps = walk_steps(a, b);
+    at -= before;
+    unit = at / steps;
+    s0 = at - unit * steps;
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  unit = __builtin_amdgcn_readfirstlane(unit);
+  s0 = __builtin_amdgcn_readfirstlane(s0);
+
+  while (left > 0) {
+    const int steps = walk_steps(a, b), s1 = (int)min((unsigned)steps, s0 + left);
+    const int h = unit / a.blocks, block = unit - h * a.blocks;
+    w.run(b, h, block, s0, s1);
+
+    // the four wavefronts' results become one, 16 rows at a time
+    const int lane = lane_again(), thread = 64 * wave + lane;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const float l = row_reduce(w.st.l[t], [](float x, float y) { return x + y; });
+      const float m = row_max(w.st.m[t]) * a.c2;
+      if (lane < 16) stat[wave][16 * t + lane] = f32x4{m, w.st.ref[t], w.live[t] ? l : 0.f, w.live[t] ? 1.f : 0.f};
+    }
+    __syncthreads();
+    const bool whole = s0 == 0 && s1 == steps;
+    float* part = whole ? nullptr : a.parts + (size_t)(2 * worker + (s0 == 0)) * part_floats(ROWS, H);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      {
+        const int r = 16 * t + (lane & 15);
+        float top = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) top = fmaxf(top, stat[v][r][0]);
+        const float f = top == -INFINITY ? 0.f : fast_exp2(w.st.ref[t] - top);
+#pragma unroll
+        for (int x = 0; x < G::HT; ++x) {
+          f32x4 o = w.st.o[x][t];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] *= f;
+          *reinterpret_cast<f32x4*>(area[wave] + 4 * H * (lane & 15) + 16 * ((4 * x + (lane >> 4)) ^ (lane & 3))) = o;
+        }
+      }
+      __syncthreads();
+      for (int at = thread; at < 16 * QUADS; at += 64 * WAVES) {
+        const int row = at / QUADS, quad = at - row * QUADS, r = 16 * t + row;
+        const int index = (block * RT + t) * 16 + row;
+        if (index >= a.group * a.rows) continue;
+        float top = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) top = fmaxf(top, stat[v][r][0]);
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) {
+          const f32x4 s = stat[v][r];
+          l += s[2] * (top == -INFINITY ? 0.f : fast_exp2(s[1] - top));
+          const f32x4 x = *reinterpret_cast<const f32x4*>(area[v] + 4 * H * row + 16 * (quad ^ (row & 3)));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] += x[i];
+        }
+        const bool empty = stat[0][r][3] == 0.f || l == 0.f;
+        if (empty) {
+          top = -INFINITY;
+          l = 0.f;
+          o = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        if (whole) {
+          const int g = index / a.rows, i = index - g * a.rows;
+          finish(a, b, h * a.group + g, i, H, quad, o, top, l);
+        } else {
+          *reinterpret_cast<f32x4*>(part + 2 * ROWS + (size_t)r * H + 4 * quad) = o;
+          if (quad == 0) {
+            part[r] = top;
+            part[ROWS + r] = l;
+          }
+        }
+      }
+      __syncthreads();
+    }
+    left -= s1 - s0;
+    s0 = 0;
+    if (++unit == per_sequence) {
+      unit = 0;
+      ++b;
+    }
+  }
+}
+
+template <int H, int FMT>
+hipError_t go_tiles(Phase ph, const CachedArgs& a, hipStream_t s) {
+  if (ph == PREPARE) return hipSuccess;              // (no dynamic LDS)
+  const dim3 grid(a.workers ? (unsigned)((a.workers + 7) / 8 * 8) : (unsigned)(a.sequences * a.c.kv_heads * a.blocks));
+  if (a.tiles == 1) A2D_LAUNCH((cached_kernel<H, FMT, 1>), grid, dim3(64 * WAVES), 0, s, a);
+  else if (a.tiles == 2) A2D_LAUNCH((cached_kernel<H, FMT, 2>), grid, dim3(64 * WAVES), 0, s, a);
+  else A2D_LAUNCH((cached_kernel<H, FMT, 4>), grid, dim3(64 * WAVES), 0, s, a);
+  return hipGetLastError();
+}
+template <int FMT>
+hipError_t go_format(Phase ph, int hdim, const CachedArgs& a, hipStream_t s) {
+  return hdim == 64 ? go_tiles<64, FMT>(ph, a, s) : hdim == 80 ? go_tiles<80, FMT>(ph, a, s) : hdim == 96 ? go_tiles<96, FMT>(ph, a, s)
+                                                                                              : go_tiles<128, FMT>(ph, a, s);
+}
+
+}  // namespace cached
+}  // namespace a2d

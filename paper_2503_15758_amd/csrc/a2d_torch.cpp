@@ -344,6 +344,29 @@ class Scratch {
   }
 };
 
+// Memory that a call may do without (its walks are not shared then), where Scratch has some
+class Workspace {
+  at::Tensor t_;
+  size_t missing_ = 0;
+
+ public:
+  Workspace(const at::Tensor& like, size_t bytes, void* stream) {
+    if (!bytes || !may_allocate(like.device(), static_cast<hipStream_t>(stream))) return;
+    try {
+      t_ = at::empty({(int64_t)bytes}, like.options().dtype(at::kByte).requires_grad(false));
+    } catch (...) {
+      missing_ = bytes;
+    }
+  }
+  void* get() const { return t_.defined() ? t_.data_ptr() : nullptr; }
+  void tell() const {
+    if (missing_ && PyErr_WarnFormat(PyExc_RuntimeWarning, 1,
+                                     "no memory for partial results (%zu bytes): the call did not share its walks among "
+                                     "workgroups, its sums are added in another order", missing_) != 0)
+      throw PythonError();
+  }
+};
+
 // runs f with the GIL released
 template <class F>
 a2d_status unlocked(F&& f) {
@@ -880,6 +903,223 @@ PyObject* rotary(Args a) {
   return one ? o.one(0) : o.give();
 }
 
+// ---- the paged cache
+
+// The strides of a [sequences][heads][rows][H] device tensor or view whose rows are contiguous
+a2d_batch_layout batch_strides(const at::Tensor& t) {
+  if (t.is_contiguous()) return a2d_batch_layout{0, 0, 0};
+  const int64_t n = t.size(0), heads = t.size(1), rows = t.size(2), H = t.size(3);
+  const int64_t row = rows > 1 ? t.stride(2) : H;      // a stride over a dimension of extent 1 is arbitrary
+  // (an expanded dimension, of stride 0, is refused by the library; {0, 0, 0} would read as plain)
+  const auto some = [](int64_t x) { return x == 0 ? (int64_t)-1 : x; };
+  // of an extent of 1: any that overlaps nothing
+  const int64_t head = heads > 1 ? t.stride(1) : rows > 1 ? (row < 0 ? 1 : row) * rows : H;
+  return a2d_batch_layout{some(n > 1 ? t.stride(0) : (head < 0 ? 1 : head) * heads), some(head), some(row)};
+}
+const at::Tensor& dev4(PyObject* o, const char* name) {
+  const at::Tensor& t = tensor(o, name);
+  if (!(t.is_cuda() && t.dim() == 4 && (t.stride(3) == 1 || t.size(3) == 1)) || t.numel() == 0)
+    fail(A2D_ERR_INVALID_ARG, std::string(name) + " must be a [sequences][heads][rows][H] device tensor with contiguous rows");
+  here(t, name);
+  return t;
+}
+int32_t extent(int64_t n) { return (int32_t)std::min<int64_t>(n, INT32_MAX); }
+
+// The tensors of a cache, and its table
+struct Cache {
+  a2d_cache c{};
+  at::Tensor table;
+  Cache(PyObject* o, PyObject* table_of) {
+    const Parts p(o, "cache");
+    if (p.k() != 2 && p.k() != 4) fail(A2D_ERR_INVALID_ARG, "cache must be (K, V) or (K, V, K_scales, V_scales)");
+    const at::Tensor &K = *p.t[0], &V = *p.t[1];
+    const at::ScalarType type = K.scalar_type();
+    c.format = type == at::kBFloat16 ? A2D_CACHE_BF16 : type == at::kFloat8_e4m3fn ? A2D_CACHE_E4M3 : A2D_CACHE_E2M1;
+    if (c.format == A2D_CACHE_E2M1 && type != at::kByte)
+      fail(A2D_ERR_UNSUPPORTED, std::string("a cache of ") + c10::toString(type) + " (bfloat16, float8_e4m3fn, or uint8 for e2m1 codes)");
+    const char* what = "cache: K, V ([pages][kv_heads][page_rows][H], of e2m1 codes [H / 2])";
+    if (K.dim() != 4) fail(A2D_ERR_INVALID_ARG, std::string(what) + " expected");
+    for (int i = 0; i < 4; ++i) c.pad |= K.size(i) > INT32_MAX;
+    if (c.pad || K.numel() == 0) fail(A2D_ERR_INVALID_ARG, std::string(what) + ": size out of range");
+    exactly(K, K.sizes(), type, what);
+    exactly(V, K.sizes(), type, what);
+    if (p.k() != (c.format == A2D_CACHE_BF16 ? 2 : 4))
+      fail(A2D_ERR_INVALID_ARG, "cache: 8- and 4-bit codes come with K_scales and V_scales, bf16 without");
+    if (p.k() == 4) {
+      const std::vector<int64_t> shape{K.size(0), K.size(1), K.size(2), 4};
+      for (int i = 2; i < 4; ++i) exactly(*p.t[i], shape, at::kByte, "cache: scales (uint8 [pages][kv_heads][page_rows][4])");
+      c.K_scales = data<uint8_t>(*p.t[2]);
+      c.V_scales = data<uint8_t>(*p.t[3]);
+    }
+    c.pages = (int32_t)K.size(0);
+    c.kv_heads = (int32_t)K.size(1);
+    c.page_rows = (int32_t)K.size(2);
+    c.hdim = c.format == A2D_CACHE_E2M1 ? extent(2 * K.size(3)) : (int32_t)K.size(3);
+    c.K = K.data_ptr();
+    c.V = V.data_ptr();
+    const at::Tensor& t = tensor(table_of, "table");
+    if (t.dim() != 2 || t.numel() == 0) fail(A2D_ERR_INVALID_ARG, "table (int32 [sequences][pages]) expected");
+    exactly(t, t.sizes(), at::kInt, "table (int32 [sequences][pages])");
+    table = at_16_bytes(t);
+    c.table = data<int32_t>(table);
+    c.sequences = extent(t.size(0));
+    c.max_pages = extent(t.size(1));
+  }
+  // a tensor of the batch: [sequences][heads][rows][H]
+  void fits(const at::Tensor& t, int64_t heads, int64_t rows, const char* name) const {
+    if (t.size(0) != c.sequences || t.size(1) != heads || t.size(2) != rows || t.size(3) != c.hdim || rows > INT32_MAX)
+      fail(A2D_ERR_INVALID_ARG, std::string(name) + " does not match the cache, the table or the other tensors: [sequences][heads][rows][H]");
+  }
+};
+// int32 [sequences] (or of the shape given)
+at::Tensor numbers(PyObject* o, at::IntArrayRef shape, const char* what) {
+  const at::Tensor& t = tensor(o, what);
+  exactly(t, shape, at::kInt, what);
+  return at_16_bytes(t);
+}
+
+// cache, table, K, V, starts, index
+PyObject* cache_write(Args a) {
+  const Cache cache(a[0], a[1]);
+  const at::Tensor &K = dev4(a[2], "K"), &V = dev4(a[3], "V");
+  cache.fits(K, cache.c.kv_heads, K.size(2), "K");
+  cache.fits(V, cache.c.kv_heads, K.size(2), "V");
+  if (V.scalar_type() != K.scalar_type()) fail(A2D_ERR_INVALID_ARG, "K and V must be of one type");
+  const int dt = dtype_code(K.scalar_type());
+  const at::Tensor starts = numbers(a[4], {cache.c.sequences}, "starts (int32 [sequences])");
+  at::Tensor index;
+  int32_t count = (int32_t)K.size(2);
+  if (a[5] != Py_None) {
+    const at::Tensor& t = tensor(a[5], "index");
+    if (t.dim() != 2 || t.numel() == 0) fail(A2D_ERR_INVALID_ARG, "index (int32 [sequences][count]) expected");
+    count = extent(t.size(1));
+    index = numbers(a[5], {cache.c.sequences, t.size(1)}, "index (int32 [sequences][count])");
+  }
+  const a2d_batch_layout lk = batch_strides(K), lv = batch_strides(V);
+  const void *k = K.data_ptr(), *v = V.data_ptr();
+  const int32_t *from = data<int32_t>(starts), *which = a[5] == Py_None ? nullptr : data<int32_t>(index);
+  const int32_t rows = (int32_t)K.size(2);
+  void* s = stream();
+  check(unlocked([&] { return a2d_cache_write(&cache.c, rows, count, dt, k, &lk, v, &lv, from, which, s); }));
+  Py_RETURN_NONE;
+}
+
+// cache, table, lens, rows, first, out, out_dtype
+PyObject* cache_read(Args a) {
+  const Cache cache(a[0], a[1]);
+  const at::Tensor lens = numbers(a[2], {cache.c.sequences}, "lens (int32 [sequences])");
+  const int32_t rows = int32_of(a[3], "rows"), first = int32_of(a[4], "first");
+  if (rows < 1) fail(A2D_ERR_INVALID_ARG, "rows must be >= 1");
+  Outputs o;
+  const std::vector<int64_t> shape{cache.c.sequences, cache.c.kv_heads, rows, cache.c.hdim};
+  if (a[5] == Py_None) {
+    const at::ScalarType t = dtype_arg(a[6]);
+    (void)dtype_code(t);
+    for (int i = 0; i < 2; ++i) o.add(empty_like_shape(lens, shape, t));
+  } else {
+    o.take(a[5], 2, "out=(K, V)", false);
+    for (int i = 0; i < 2; ++i) cache.fits(dev4(o.given[i], "out"), cache.c.kv_heads, rows, "out");
+    if (o.t[0].scalar_type() != o.t[1].scalar_type()) fail(A2D_ERR_INVALID_ARG, "out: K and V must be of one type");
+  }
+  const int dt = dtype_code(o.t[0].scalar_type());
+  const a2d_batch_layout lk = batch_strides(o.t[0]), lv = batch_strides(o.t[1]);
+  void *k = o.t[0].data_ptr(), *v = o.t[1].data_ptr(), *s = stream();
+  const int32_t* n = data<int32_t>(lens);
+  check(unlocked([&] { return a2d_cache_read(&cache.c, n, first, rows, dt, k, &lk, v, &lv, s); }));
+  return o.give();
+}
+
+// parents, lens, out
+PyObject* tree_masks(Args a) {
+  const at::Tensor& p = tensor(a[0], "parents");
+  if (p.dim() != 2 || p.numel() == 0) fail(A2D_ERR_INVALID_ARG, "parents (int32 [sequences][rows]) expected");
+  exactly(p, p.sizes(), at::kInt, "parents (int32 [sequences][rows])");
+  const at::Tensor parents = at_16_bytes(p);
+  const int32_t sequences = extent(p.size(0)), rows = extent(p.size(1));
+  at::Tensor lens;
+  if (a[1] != Py_None) lens = numbers(a[1], {p.size(0)}, "lens (int32 [sequences])");
+  Outputs o;
+  const std::vector<int64_t> masks{p.size(0), p.size(1), (p.size(1) + 63) / 64}, positions{p.size(0), 1, p.size(1)};
+  if (a[2] == Py_None) {
+    o.add(empty_like_shape(p, masks, at::kLong));
+    o.add(empty_like_shape(p, positions, at::kInt));
+  } else {
+    o.take(a[2], 2, "out=(masks, positions)");
+    exactly(o.t[0], masks, at::kLong, "out: masks (int64 [sequences][rows][words])");
+    exactly(o.t[1], positions, at::kInt, "out: positions (int32 [sequences][1][rows])");
+  }
+  void* s = stream();
+  check(unlocked([&] {
+    return a2d_tree_masks(sequences, rows, data<int32_t>(parents), a[1] == Py_None ? nullptr : data<int32_t>(lens), data<uint64_t>(o.t[0]),
+                          data<int32_t>(o.t[1]), s);
+  }));
+  return o.give();
+}
+
+// Q, cache, table, lens, K, V, masks, scale, max_tokens, out, normalised
+PyObject* partial_fwd_cached(Args a) {
+  const at::Tensor& Q = dev4(a[0], "Q");
+  const Cache cache(a[1], a[2]);
+  const int64_t n = cache.c.sequences, rows = Q.size(2);
+  cache.fits(Q, Q.size(1), rows, "Q");
+  if (Q.scalar_type() != at::kBFloat16)
+    fail(A2D_ERR_UNSUPPORTED, std::string("Q of ") + c10::toString(Q.scalar_type()) + ": bfloat16 only (cache_read for the tile calls)");
+  const at::Tensor lens = numbers(a[3], {n}, "lens (int32 [sequences])");
+  a2d_cached_desc d{};
+  d.heads = extent(Q.size(1));
+  d.rows = (int32_t)rows;
+  d.scale = scale_of(a[7], cache.c.hdim);
+  d.max_tokens = int32_of(a[8], "max_tokens");
+  d.lens = data<int32_t>(lens);
+  d.lq = batch_strides(Q);
+  const void *k = nullptr, *v = nullptr;
+  if ((a[4] == Py_None) != (a[5] == Py_None)) fail(A2D_ERR_INVALID_ARG, "K and V of the rows come together");
+  if (a[4] != Py_None) {
+    const at::Tensor &K = dev4(a[4], "K"), &V = dev4(a[5], "V");
+    cache.fits(K, cache.c.kv_heads, rows, "K");
+    cache.fits(V, cache.c.kv_heads, rows, "V");
+    if (K.scalar_type() != Q.scalar_type() || V.scalar_type() != Q.scalar_type()) fail(A2D_ERR_INVALID_ARG, "Q, K and V must be of one type");
+    d.lk = batch_strides(K);
+    d.lv = batch_strides(V);
+    k = K.data_ptr();
+    v = V.data_ptr();
+  }
+  at::Tensor masks;
+  if (a[6] != Py_None) {
+    const at::Tensor& t = tensor(a[6], "masks");
+    exactly(t, {n, rows, (rows + 63) / 64}, at::kLong, "masks (int64 [sequences][rows][words])");
+    masks = at_16_bytes(t);
+    d.masks = data<uint64_t>(masks);
+  }
+  const bool norm = truth(a[10]);
+  Outputs o;
+  const at::ScalarType ot = norm ? Q.scalar_type() : at::kFloat;
+  const std::vector<int64_t> stats{n, Q.size(1), rows};
+  if (a[9] == Py_None) {
+    o.add(empty_like_shape(Q, Q.sizes(), ot));
+    for (int i = norm ? 1 : 0; i < 2; ++i) o.add(empty_like_shape(Q, stats, at::kFloat));
+  } else {
+    const char* what = norm ? "out=(O, lse)" : "out=(N, m, l)";
+    o.take(a[9], norm ? 2 : 3, what, false);
+    cache.fits(dev4(o.given[0], "out"), Q.size(1), rows, "out");
+    if (o.t[0].scalar_type() != ot) fail(A2D_ERR_INVALID_ARG, std::string(what) + ": O in bfloat16, N in float32");
+    if (norm) d.lo = batch_strides(o.t[0]);
+    else plain(o.t[0], what);
+    for (int i = 1; i < o.n; ++i) exactly(o.t[i], stats, at::kFloat, what);
+  }
+  void* s = stream();
+  const void* q = Q.data_ptr();
+  void* out0 = o.t[0].data_ptr();
+  float *out1 = data<float>(o.t[1]), *out2 = norm ? nullptr : data<float>(o.t[2]);
+  const size_t bytes = a2d_cached_workspace_bytes(&cache.c, &d);
+  const Workspace ws(Q, bytes, s);
+  check(unlocked([&] {
+    return a2d_partial_fwd_cached(&cache.c, &d, norm ? A2D_TILE_NORMALISED : 0, q, k, v, out0, out1, out2, ws.get(), ws.get() ? bytes : 0, s);
+  }));
+  ws.tell();
+  return o.give();
+}
+
 // the layout with its strides written out
 a2d_layout full(const at::Tensor& t) {
   const a2d_layout l = layout(t);
@@ -1079,6 +1319,8 @@ PyMethodDef g_methods[] = {
     A2D_ENTRY(grid_backward, 10),  A2D_ENTRY(tile_route, 12),      A2D_ENTRY(grid_route, 9),
     A2D_ENTRY(partial_fwd_scored, 14), A2D_ENTRY(partial_bwd_scored, 18), A2D_ENTRY(document_ranges, 7),
     A2D_ENTRY(rotary, 8),           A2D_ENTRY(scored_route, 15),
+    A2D_ENTRY(cache_write, 6),      A2D_ENTRY(cache_read, 7),      A2D_ENTRY(tree_masks, 3),
+    A2D_ENTRY(partial_fwd_cached, 11),
     {"set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
