@@ -14,10 +14,20 @@ __global__ __launch_bounds__(256) void cached_merge_kernel(CachedArgs a, int per
   const int lane = threadIdx.x & 63, group = threadIdx.x >> 5, quad = threadIdx.x & 31;
   const int u = blockIdx.x / groups, from = (blockIdx.x - u * groups) * per, per_sequence = a.c.kv_heads * a.blocks;
   const int b = u / per_sequence, unit = u - b * per_sequence;
-  unsigned before = 0;
-  const Cut cut = make_cut(a, lane, b, &before);
-  const unsigned steps = walk_steps(a, b), begin = before + unit * steps;
-  const unsigned w0 = cut.worker_of(begin), parts = cut.worker_of(begin + steps - 1) - w0 + 1;
+  Batch batch;
+  Cut cut;
+  unsigned places = 0, begin = 0, last = 0;            // of the walk's first step and its last
+  for (int first = 0; first < a.sequences; first += 64) {
+    batch.look(a, first, lane);
+    if (b >= first && b < first + 64) {
+      const unsigned steps = steps_of(a, batch.tokens_at(b));
+      begin = places + batch.before(b) + unit * (START + steps) + START;
+      last = begin + steps - 1;
+    }
+    places += batch.all();
+  }
+  cut.make(a, places);
+  const unsigned w0 = cut.worker_of(begin), parts = cut.worker_of(last) - w0 + 1;
   if (parts == 1) return;
   const int rows = 16 * a.tiles, h = unit / a.blocks, block = unit - h * a.blocks;
   for (int r = from; r < from + per; ++r) {
@@ -87,7 +97,7 @@ __global__ __launch_bounds__(64) void cached_generic_kernel(CachedArgs a, int hd
   const int i = (int)(x % a.rows), head = (int)(x / a.rows % a.heads), b = (int)(x / a.rows / a.heads), h = head / a.group;
   for (int c = lane; c < hdim; c += 64) q[c] = (float)(reinterpret_cast<const bf16_t*>(a.Q) + at_row(a.lq, b, head, i))[c];
   const bool token = !a.masks || (a.masks[((int64_t)b * a.rows + i) * a.words + (i >> 6)] >> (i & 63) & 1);
-  const int tokens = token ? cached_tokens(a, b) : 0, drafts = token && a.K ? a.rows : 0;
+  const int tokens = token ? tokens_of(a, a.lens[b]) : 0, drafts = token && a.K ? a.rows : 0;
   float m = -INFINITY, l = 0.f, o[2] = {0.f, 0.f};
   const int64_t cached = (tokens + 63) / 64, all = cached + (drafts + 63) / 64;
   for (int64_t s = 0; s < all; ++s) {
@@ -155,11 +165,11 @@ void go_merge(const CachedArgs& a, hipStream_t s) {
 CachedPlan plan_cached(int format, int hdim, const CachedArgs& a, int cus, bool workspace) {
   CachedPlan p{};
   const int64_t rows = (int64_t)a.group * a.rows;
-  p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  p.tiles = rows <= 16 ? 1 : 2;
   p.blocks = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
   const int64_t steps = ((int64_t)a.max_tokens + STEP - 1) / STEP + (a.K ? (a.rows + STEP - 1) / STEP : 0);
-  if (!workspace || steps <= (int64_t)(2 * LEAST_STEPS)) return p;
-  p.workers = (p.tiles == 4 ? 1 : 2) * cus;
+  if (!workspace || steps <= 16) return p;
+  p.workers = 2 * cus;
   p.bytes = 2 * (size_t)p.workers * part_floats(16 * p.tiles, hdim) * sizeof(float);
   return p;
 }

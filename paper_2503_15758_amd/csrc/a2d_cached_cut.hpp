@@ -6,57 +6,63 @@
 namespace a2d {
 
 // The walk of a block of rows: steps of 32 keys, those of the cached tokens first, then those of the drafted rows.  Sequence b has
-// kv_heads * blocks such walks of the same length; all walks, one after another, are a line of steps, cut into equal runs, one for each
-// worker, whatever the lengths are (which the host does not know).
+// kv_heads * blocks such walks of the same length; all walks, one after another, are a line, cut into equal runs, one for each worker,
+// whatever the lengths are (which the host does not know).  On the line a walk is START places longer than its steps: what it costs
+// besides (Q, the table, the first codes, the join of the wavefronts: 8 sequences, one of them of a token alone, without 61 us, with 41).
 constexpr int STEP = 32;
-__device__ __forceinline__ int cached_tokens(const CachedArgs& a, int b) { return min(max(a.lens[b], 0), a.max_tokens); }
+constexpr unsigned START = 8;
+constexpr unsigned LEAST = 16;         // places of a worker
 __device__ __forceinline__ int draft_steps(const CachedArgs& a) { return a.K ? (a.rows + STEP - 1) / STEP : 0; }
+__device__ __forceinline__ int tokens_of(const CachedArgs& a, int length) { return min(max(length, 0), a.max_tokens); }
 // (a walk of nothing is one step all the same: its results have to be written)
-__device__ __forceinline__ int walk_steps(const CachedArgs& a, int b) {
-  return max(1, (cached_tokens(a, b) + STEP - 1) / STEP + draft_steps(a));
-}
+__device__ __forceinline__ int steps_of(const CachedArgs& a, int tokens) { return max(1, (tokens + STEP - 1) / STEP + draft_steps(a)); }
 
 // sum over the lanes up to this one
-__device__ __forceinline__ unsigned lanes_sum(unsigned x, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const unsigned y = __shfl_up(x, d);
-    x += lane >= d ? y : 0;
-  }
+__device__ __forceinline__ unsigned lanes_sum(unsigned x) {
+  const auto add = [&](auto C, auto R) {
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, decltype(C)::value, decltype(R)::value, 0xF, false);
+  };
+  using std::integral_constant;
+  add(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});    // within 16 lanes: shifted by 1, 2, 4, 8
+  add(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
+  add(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
+  add(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
+  add(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});    // the last of 16 lanes to the next 16
+  add(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});    // lane 31 to the upper half
   return x;
 }
 
-struct Cut {
-  unsigned total, each, more;          // steps; of a worker; the first `more` workers have one more
-  unsigned workers;
-  __device__ __forceinline__ unsigned begin(unsigned w) const { return w * each + min(w, more); }
-  __device__ __forceinline__ unsigned worker_of(unsigned step) const {
-    const unsigned far = more * (each + 1);
-    return step < far ? step / (each + 1) : more + (step - far) / each;
+// 64 sequences of the batch: a lane's tokens, and the places of the walks of the sequences up to it (behind the last: no more)
+struct Batch {
+  int first;
+  int tokens;
+  unsigned sum;
+  __device__ __forceinline__ void look(const CachedArgs& a, int from, int lane) {
+    first = from;
+    const int b = from + lane;
+    tokens = b < a.sequences ? tokens_of(a, a.lens[b]) : 0;
+    sum = lanes_sum(b < a.sequences ? (steps_of(a, tokens) + START) * (unsigned)(a.c.kv_heads * a.blocks) : 0);
   }
+  __device__ __forceinline__ int tokens_at(int b) const { return __builtin_amdgcn_readlane(tokens, b - first); }
+  __device__ __forceinline__ unsigned before(int b) const { return b > first ? (unsigned)__builtin_amdgcn_readlane((int)sum, b - first - 1) : 0; }
+  __device__ __forceinline__ unsigned all() const { return (unsigned)__builtin_amdgcn_readlane((int)sum, 63); }
 };
 
-constexpr unsigned LEAST_STEPS = 8;    // of a worker: two for each wavefront
-
-// steps of all walks of sequences first .. first + 63, the lane's and those in front of it; 0 behind the last
-__device__ __forceinline__ unsigned sequence_sum(const CachedArgs& a, int first, int lane) {
-  const int b = first + lane;
-  return lanes_sum(b < a.sequences ? (unsigned)walk_steps(a, b) * (unsigned)(a.c.kv_heads * a.blocks) : 0, lane);
-}
-// (before: steps of the sequences in front of b)
-__device__ __forceinline__ Cut make_cut(const CachedArgs& a, int lane, int b = 0, unsigned* before = nullptr) {
-  Cut c;
-  c.total = 0;
-  for (int first = 0; first < a.sequences; first += 64) {
-    const unsigned sum = sequence_sum(a, first, lane);
-    if (before && b >= first && b < first + 64) *before = c.total + (b > first ? (unsigned)__builtin_amdgcn_readlane((int)sum, b - first - 1) : 0);
-    c.total += (unsigned)__builtin_amdgcn_readlane((int)sum, 63);
+struct Cut {
+  unsigned total, each, more;          // places; of a worker; the first `more` workers have one more
+  unsigned workers;
+  __device__ __forceinline__ void make(const CachedArgs& a, unsigned places) {
+    total = places;
+    workers = min((unsigned)a.workers, max(1u, total / LEAST));
+    each = total / workers;
+    more = total - each * workers;
   }
-  c.workers = min((unsigned)a.workers, max(1u, c.total / LEAST_STEPS));
-  c.each = c.total / c.workers;
-  c.more = c.total - c.each * c.workers;
-  return c;
-}
+  __device__ __forceinline__ unsigned begin(unsigned w) const { return w * each + min(w, more); }
+  __device__ __forceinline__ unsigned worker_of(unsigned place) const {
+    const unsigned far = more * (each + 1);
+    return place < far ? place / (each + 1) : more + (place - far) / each;
+  }
+};
 
 // Results that are parts of a block's: m (log2 units), l, N of `rows` = 16 * tiles rows; a worker leaves at most one of a walk that
 // began before it (slot 2 w) and one of a walk that goes on behind it (slot 2 w + 1).

@@ -3,7 +3,7 @@
 //   s = scale <q, k>;  row i sees all cached tokens of its sequence and the drafted rows j whose bit is set in its mask (no masks: j <= i);
 //   N = sum 2^(s' - m') v, l = sum 2^(s' - m') in log2 units, one pass over the keys.
 //
-// A workgroup has a block of 16, 32 or 64 rows (query heads of a group and rows of a sequence, numbered through) of one key/value head, and
+// A workgroup has a block of 16 or 32 rows (query heads of a group and rows of a sequence, numbered through) of one key/value head, and
 // a run of its keys in steps of 32, dealt in turn to its four wavefronts.  Each wavefront keeps (N, m, l) of all the block's rows to itself: no
 // barrier on the walk, the four are joined through LDS at its end.
 //  - S^T = K Q^T: a lane's part of K comes straight from memory, 16 values in a piece (16 bytes of e4m3): the order in which the columns
@@ -292,11 +292,6 @@ __device__ __forceinline__ unsigned seen_rows(const CachedArgs& a, int b, int i,
   const int n = i - STEP * step;
   return n < 0 ? 0 : n >= 31 ? ~0u : (2u << n) - 1;
 }
-// is row i a token (its own bit is set)?
-__device__ __forceinline__ bool is_token(const CachedArgs& a, int b, int i) {
-  return !a.masks || (a.masks[((int64_t)b * a.rows + i) * a.words + (i >> 6)] >> (i & 63) & 1);
-}
-
 template <int H, int FMT, int RT>
 struct Walk {
   using G = Head<H>;
@@ -307,48 +302,53 @@ struct Walk {
   int lane, wave;
   State<H, RT> st;
   bf16x8 qf[G::KS][RT];
-  int row_of[RT];                                    // the row within its sequence of the lane's row in a tile
-  bool live[RT];
+  int row_of[RT];                                    // the lane's row of a tile within its sequence; -1: there is none
+  uint64_t own[RT];                                  // the word of its mask with its own bit
+  unsigned units;
 
-  // steps s0 .. s1 - 1 of block `block` of head h of sequence b
-  __device__ __forceinline__ void run(int b, int h, int block, int s0, int s1) {
+  // steps s0 .. s1 - 1 of block `block` of head h of sequence b, which has `tokens` cached ones
+  __device__ __forceinline__ void run(int b, int h, int block, int s0, int s1, int tokens) {
     const int rows = a.group * a.rows;
-    Lane<H> ln;
-    ln.init(lane_again());
+    const int cached = (tokens + STEP - 1) / STEP, last = min(s1, cached), first = s0 + wave;
+    if (first < last) look_up(b, h, first, tokens);
+    {
+      Lane<H> ln;
+      ln.init(lane_again());
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const int at = (block * RT + t) * 16 + ln.row, r = min(at, rows - 1);
-      const Split sp = split_by(r, a.rows);
-      const int head = a.rows == 1 ? r : sp.q, i = a.rows == 1 ? 0 : sp.r;
-      row_of[t] = i;
-      live[t] = at < rows && is_token(a, b, i);
-      const bf16_t* q = reinterpret_cast<const bf16_t*>(a.Q) + at_row(a.lq, b, h * a.group + head, i);
+      for (int t = 0; t < RT; ++t) {
+        const int at = (block * RT + t) * 16 + ln.row, r = min(at, rows - 1);
+        const int head = a.rows == 1 ? r : r / a.rows, i = r - head * a.rows;
+        row_of[t] = at < rows ? i : -1;
+        own[t] = a.masks ? a.masks[((int64_t)b * a.rows + i) * a.words + (i >> 6)] : ~(uint64_t)0;
+        const bf16_t* q = reinterpret_cast<const bf16_t*>(a.Q) + at_row(a.lq, b, h * a.group + head, i);
 #pragma unroll
-      for (int x = 0; x < 2 * G::JF; ++x) qf[x][t] = *reinterpret_cast<const bf16x8*>(q + 64 * (x >> 1) + 16 * ln.g + 8 * (x & 1));
-      if constexpr (G::REST) {
-        qf[2 * G::JF][t] = *reinterpret_cast<const bf16x8*>(q + (ln.has_rest ? 64 * G::JF + 8 * ln.g : 0));
-        if (G::REST < 4 && !ln.has_rest) qf[2 * G::JF][t] = zero8();
+        for (int x = 0; x < 2 * G::JF; ++x) qf[x][t] = *reinterpret_cast<const bf16x8*>(q + 64 * (x >> 1) + 16 * ln.g + 8 * (x & 1));
+        if constexpr (G::REST) {
+          qf[2 * G::JF][t] = *reinterpret_cast<const bf16x8*>(q + (ln.has_rest ? 64 * G::JF + 8 * ln.g : 0));
+          if (G::REST < 4 && !ln.has_rest) qf[2 * G::JF][t] = zero8();
+        }
       }
     }
     st.clear();
-    const int tokens = cached_tokens(a, b), cached = (tokens + STEP - 1) / STEP;
-    const int last = min(s1, cached);
-    if (s0 + wave < last) cache_steps(b, h, s0 + wave, last, tokens);
+    if (first < last) cache_steps(b, h, first, last, tokens);
     if (a.K) {
       // (those in front of the first drafted step are behind the wavefront's last cached one)
-      int s = s0 + wave;
+      int s = first;
       if (s < cached) s += (cached - s + WAVES - 1) / WAVES * WAVES;
       for (; s < s1; s += WAVES) draft_step(b, h, s - cached);
     }
   }
+  // does the lane's row of tile t exist, and is it a token (its own bit is set)?
+  __device__ __forceinline__ bool live(int t) const { return row_of[t] >= 0 && (own[t] >> (row_of[t] & 63) & 1); }
+
+  // the units of tile lane & 1 of the wavefront's step lane >> 1 of 32 from s on
+  __device__ __forceinline__ void look_up(int b, int h, int s, int tokens) {
+    const int tile = 2 * (s + WAVES * (lane >> 1)) + (lane & 1);
+    units = tile * 16 < tokens ? unit_of(a.c, b, h, tile) : NO_UNIT;
+  }
 
   __device__ __forceinline__ void cache_steps(int b, int h, int first, int last, int tokens) {
     Codes<H, FMT> c[2];
-    unsigned units = 0;                              // of tile lane & 1 of the wavefront's step lane >> 1, of 32
-    const auto look_up = [&](int s) {
-      const int tile = 2 * (s + WAVES * (lane >> 1)) + (lane & 1);
-      units = tile * 16 < tokens ? unit_of(a.c, b, h, tile) : NO_UNIT;
-    };
     unsigned vis = 0;
     const auto load = [&](int n, int s) {            // the wavefront's n-th step, s
       vis = 0;
@@ -360,7 +360,6 @@ struct Walk {
         load_unit<H, FMT>(c[k], a.c, u == NO_UNIT ? 0 : u, ln);
       }
     };
-    look_up(first);
     load(0, first);
     for (int s = first, n = 0; s < last; s += WAVES, ++n) {
       f32x4 sc[2][RT];
@@ -375,7 +374,7 @@ struct Walk {
       __builtin_amdgcn_sched_barrier(0);
       // the next step's codes, while this one is worked on (behind the last: the last again)
       const bool more = s + WAVES < last;
-      if (A2D_SELDOM((n & 31) == 31 && more)) look_up(s + WAVES);
+      if (A2D_SELDOM((n & 31) == 31 && more)) look_up(b, h, s + WAVES, tokens);
       load(more ? n + 1 : n, more ? s + WAVES : s);
       if (A2D_SELDOM(now != ~0u)) {
         const unsigned mine = now >> (4 * ln.g);
@@ -398,7 +397,7 @@ struct Walk {
     unsigned seen[RT], all = 0;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      seen[t] = live[t] ? seen_rows(a, b, row_of[t], step) : 0;
+      seen[t] = live(t) ? seen_rows(a, b, row_of[t], step) : 0;
       all |= seen[t];
     }
 #pragma unroll
@@ -466,7 +465,7 @@ struct Walk {
 };
 
 template <int H, int FMT, int RT>
-__global__ __launch_bounds__(64 * WAVES, RT == 1 ? 3 : RT == 2 ? 2 : 1) void cached_kernel(CachedArgs a) {
+__global__ __launch_bounds__(64 * WAVES, RT == 1 && FMT != A2D_CACHE_BF16 ? 3 : 2) void cached_kernel(CachedArgs a) {
   using G = Head<H>;
   constexpr int ROWS = 16 * RT, QUADS = H / 4;
   __shared__ __align__(1024) char area[WAVES][G::AREA];
@@ -479,49 +478,57 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 ? 3 : RT == 2 ? 2 : 1) void cac
   rd.init(lane, mine);
   Walk<H, FMT, RT> w{a, ln, rd, mine, lane, wave};
 
-  // the workgroup's run of the line of steps
+  // the workgroup's run of the line
   const int per_sequence = a.c.kv_heads * a.blocks;
-  int b, unit, s0;
-  unsigned left;
+  Batch batch;
+  int b, unit;
+  unsigned at, left;                                 // within the walk; of the run
   int worker = -1;
   if (a.workers == 0) {
     b = blockIdx.x / per_sequence;
     unit = blockIdx.x - b * per_sequence;
-    s0 = 0;
-    left = walk_steps(a, b);
+    batch.look(a, b, lane);
+    at = 0;
+    left = START + steps_of(a, batch.tokens_at(b));
   } else {
-    const Cut cut = make_cut(a, lane);
+    Cut cut;
+    unsigned places = 0;
+    for (int first = (a.sequences - 1) & ~63; first >= 0; first -= 64) {
+      batch.look(a, first, lane);                    // (ends with the first 64)
+      places += batch.all();
+    }
+    cut.make(a, places);
     // neighbours on the line, which share keys where a head has several blocks, to one XCD
     const unsigned per = (cut.workers + 7) / 8, n = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= per || n >= cut.workers) return;
     worker = (int)n;
-    unsigned at = cut.begin(n);
+    at = cut.begin(n);
     left = cut.begin(n + 1) - at;
-    unsigned before = 0;                             // of the sequences in front of the chunk
-    int first = 0;
-    unsigned sum;
-    for (;; first += 64) {
-      sum = sequence_sum(a, first, lane);
-      const unsigned all = __builtin_amdgcn_readlane((int)sum, 63);
-      if (at < before + all || first + 64 >= a.sequences) break;
-      before += all;
+    while (at >= batch.all() && batch.first + 64 < a.sequences) {
+      at -= batch.all();
+      batch.look(a, batch.first + 64, lane);
     }
-    const int in = __popcll(__ballot(before + sum <= at));       // sequences of the chunk that end in front of it
-    b = first + in;
-    if (in > 0) before += __builtin_amdgcn_readlane((int)sum, in - 1);
-    const int steps = walk_steps(a, b);
-    at -= before;
-    unit = at / steps;
-    s0 = at - unit * steps;
+    b = batch.first + __popcll(__ballot(batch.sum <= at));
+    at -= batch.before(b);
+    const unsigned walk = START + steps_of(a, batch.tokens_at(b));
+    unit = at / walk;
+    at -= unit * walk;
   }
-  b = __builtin_amdgcn_readfirstlane(b);
-  unit = __builtin_amdgcn_readfirstlane(unit);
-  s0 = __builtin_amdgcn_readfirstlane(s0);
 
   while (left > 0) {
-    const int steps = walk_steps(a, b), s1 = (int)min((unsigned)steps, s0 + left);
-    const int h = unit / a.blocks, block = unit - h * a.blocks;
-    w.run(b, h, block, s0, s1);
+    if (b >= batch.first + 64) batch.look(a, b, lane);
+    const int tokens = batch.tokens_at(b), steps = steps_of(a, tokens);
+    const unsigned walk = START + steps, to = min(walk, at + left);
+    const int s0 = at > START ? at - START : 0, s1 = to > START ? to - START : 0;
+    left -= to - at;
+    at = 0;
+    const int h = unit / a.blocks, block = unit - h * a.blocks, now = b;
+    if (++unit == per_sequence) {
+      unit = 0;
+      ++b;
+    }
+    if (s1 == 0) break;                              // (the run ends in front of its first step)
+    w.run(now, h, block, s0, s1, tokens);
 
     // the four wavefronts' results become one, 16 rows at a time
     const int lane = lane_again(), thread = 64 * wave + lane;
@@ -529,7 +536,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 ? 3 : RT == 2 ? 2 : 1) void cac
     for (int t = 0; t < RT; ++t) {
       const float l = row_reduce(w.st.l[t], [](float x, float y) { return x + y; });
       const float m = row_max(w.st.m[t]) * a.c2;
-      if (lane < 16) stat[wave][16 * t + lane] = f32x4{m, w.st.ref[t], w.live[t] ? l : 0.f, w.live[t] ? 1.f : 0.f};
+      if (lane < 16) stat[wave][16 * t + lane] = f32x4{m, w.st.ref[t], w.live(t) ? l : 0.f, w.live(t) ? 1.f : 0.f};
     }
     __syncthreads();
     const bool whole = s0 == 0 && s1 == steps;
@@ -575,7 +582,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 ? 3 : RT == 2 ? 2 : 1) void cac
         }
         if (whole) {
           const int g = index / a.rows, i = index - g * a.rows;
-          finish(a, b, h * a.group + g, i, H, quad, o, top, l);
+          finish(a, now, h * a.group + g, i, H, quad, o, top, l);
         } else {
           *reinterpret_cast<f32x4*>(part + 2 * ROWS + (size_t)r * H + 4 * quad) = o;
           if (quad == 0) {
@@ -586,12 +593,6 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 ? 3 : RT == 2 ? 2 : 1) void cac
       }
       __syncthreads();
     }
-    left -= s1 - s0;
-    s0 = 0;
-    if (++unit == per_sequence) {
-      unit = 0;
-      ++b;
-    }
   }
 }
 
@@ -600,8 +601,7 @@ hipError_t go_tiles(Phase ph, const CachedArgs& a, hipStream_t s) {
   if (ph == PREPARE) return hipSuccess;              // (no dynamic LDS)
   const dim3 grid(a.workers ? (unsigned)((a.workers + 7) / 8 * 8) : (unsigned)(a.sequences * a.c.kv_heads * a.blocks));
   if (a.tiles == 1) A2D_LAUNCH((cached_kernel<H, FMT, 1>), grid, dim3(64 * WAVES), 0, s, a);
-  else if (a.tiles == 2) A2D_LAUNCH((cached_kernel<H, FMT, 2>), grid, dim3(64 * WAVES), 0, s, a);
-  else A2D_LAUNCH((cached_kernel<H, FMT, 4>), grid, dim3(64 * WAVES), 0, s, a);
+  else A2D_LAUNCH((cached_kernel<H, FMT, 2>), grid, dim3(64 * WAVES), 0, s, a);
   return hipGetLastError();
 }
 template <int FMT>
