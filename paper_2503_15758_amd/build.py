@@ -61,7 +61,7 @@ def build(force=False, verbose=True):
                os.path.join(CSRC, "a2d_bwd_pairs.hpp"), os.path.join(CSRC, "a2d_bwd_wide.hpp"),
                os.path.join(CSRC, "a2d_grid.hpp"), os.path.join(CSRC, "a2d_scored.hpp"), os.path.join(CSRC, "a2d_fwd.hpp"), os.path.join(CSRC, "a2d_scored_rows.hpp"),
                os.path.join(CSRC, "a2d_f32.hpp"), os.path.join(CSRC, "a2d_cache.hpp"), os.path.join(CSRC, "a2d_cached_cut.hpp"),
-               os.path.join(CSRC, "a2d_cached_fwd.hpp"), os.path.join(ROOT, "include", "a2d.h")]
+               os.path.join(CSRC, "a2d_cached_fwd.hpp"), os.path.join(CSRC, "a2d_cached_wide.hpp"), os.path.join(ROOT, "include", "a2d.h")]
     jobs, objs = [], []
     for src in SOURCES:
         s = os.path.join(CSRC, src)

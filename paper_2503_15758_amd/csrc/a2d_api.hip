@@ -1091,6 +1091,7 @@ a2d_status cached_args(const a2d_cache* cache, const a2d_cached_desc* d, bool dr
   A2D_TRY(batch_layout(&d->lo, "O", cache->sequences, d->heads, d->rows, cache->hdim, 2, true, who, &a->lo));
   const a2d::CachedPlan p = a2d::plan_cached(cache->format, cache->hdim, *a, 1, false);
   a->tiles = p.tiles;
+  a->shift = p.shift;
   a->blocks = p.blocks;
   // (steps are numbered through in 32 bits, workgroups in 31)
   const double walks = (double)cache->sequences * cache->kv_heads * p.blocks;

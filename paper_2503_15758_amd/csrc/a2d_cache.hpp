@@ -82,12 +82,12 @@ struct CachedArgs {
   float *out1, *out2;
   // how the call goes out (plan_cached)
   int blocks;                          // row blocks of a key/value head, `tiles` tiles of 16 rows each
-  int tiles;
+  int tiles, shift;                    // a step has 2^shift keys
   int workers;                         // workgroups that share all steps; 0: one for each block
   float* parts;                        // two results of a block for each worker
 };
 struct CachedPlan {
-  int tiles, blocks, workers;
+  int tiles, shift, blocks, workers;
   size_t bytes;                        // of a.parts
 };
 // workspace: whether there may be one

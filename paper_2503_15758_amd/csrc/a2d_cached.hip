@@ -21,7 +21,7 @@ __global__ __launch_bounds__(256) void cached_merge_kernel(CachedArgs a, int per
     batch.look(a, first, lane);
     if (b >= first && b < first + 64) {
       const unsigned steps = steps_of(a, batch.tokens_at(b));
-      begin = places + batch.before(b) + unit * (START + steps) + START;
+      begin = places + batch.before(b) + unit * (start_of(a) + steps) + start_of(a);
       last = begin + steps - 1;
     }
     places += batch.all();
@@ -165,11 +165,14 @@ void go_merge(const CachedArgs& a, hipStream_t s) {
 CachedPlan plan_cached(int format, int hdim, const CachedArgs& a, int cus, bool workspace) {
   CachedPlan p{};
   const int64_t rows = (int64_t)a.group * a.rows;
-  p.tiles = rows <= 16 ? 1 : 2;
+  const auto padded = [&](int n) { return (rows + n - 1) / n * n; };
+  // up to 64 rows: blocks of 16 or 32, a wavefront has them all; else workgroups of 128 or 256, whichever leaves fewer rows empty
+  p.tiles = rows <= 16 ? 1 : rows <= 64 ? 2 : padded(256) <= padded(128) ? 16 : 8;
+  p.shift = p.tiles > 2 ? 6 : 5;
   p.blocks = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
-  const int64_t steps = ((int64_t)a.max_tokens + STEP - 1) / STEP + (a.K ? (a.rows + STEP - 1) / STEP : 0);
-  if (!workspace || steps <= 16) return p;
-  p.workers = 2 * cus;
+  const int64_t keys = (int64_t)a.max_tokens + (a.K ? a.rows : 0);
+  if (!workspace || keys <= 512) return p;
+  p.workers = (p.tiles == 16 ? 1 : 2) * cus;
   p.bytes = 2 * (size_t)p.workers * part_floats(16 * p.tiles, hdim) * sizeof(float);
   return p;
 }

@@ -5,17 +5,18 @@
 
 namespace a2d {
 
-// The walk of a block of rows: steps of 32 keys, those of the cached tokens first, then those of the drafted rows.  Sequence b has
+// The walk of a block of rows: steps of 32 keys (`shift`: 5), those of the cached tokens first, then those of the drafted rows.  Sequence b has
 // kv_heads * blocks such walks of the same length; all walks, one after another, are a line, cut into equal runs, one for each worker,
 // whatever the lengths are (which the host does not know).  On the line a walk is START places longer than its steps: what it costs
 // besides (Q, the table, the first codes, the join of the wavefronts: 8 sequences, one of them of a token alone, without 61 us, with 41).
-constexpr int STEP = 32;
-constexpr unsigned START = 8;
+// (The form of many rows has steps of 64 keys, and its START is half as many.)
 constexpr unsigned LEAST = 16;         // places of a worker
-__device__ __forceinline__ int draft_steps(const CachedArgs& a) { return a.K ? (a.rows + STEP - 1) / STEP : 0; }
+__device__ __forceinline__ unsigned start_of(const CachedArgs& a) { return a.shift == 6 ? 4 : 8; }
+__device__ __forceinline__ int steps_for(const CachedArgs& a, int keys) { return (keys + (1 << a.shift) - 1) >> a.shift; }
+__device__ __forceinline__ int draft_steps(const CachedArgs& a) { return a.K ? steps_for(a, a.rows) : 0; }
 __device__ __forceinline__ int tokens_of(const CachedArgs& a, int length) { return min(max(length, 0), a.max_tokens); }
 // (a walk of nothing is one step all the same: its results have to be written)
-__device__ __forceinline__ int steps_of(const CachedArgs& a, int tokens) { return max(1, (tokens + STEP - 1) / STEP + draft_steps(a)); }
+__device__ __forceinline__ int steps_of(const CachedArgs& a, int tokens) { return max(1, steps_for(a, tokens) + draft_steps(a)); }
 
 // sum over the lanes up to this one
 __device__ __forceinline__ unsigned lanes_sum(unsigned x) {
@@ -41,7 +42,7 @@ struct Batch {
     first = from;
     const int b = from + lane;
     tokens = b < a.sequences ? tokens_of(a, a.lens[b]) : 0;
-    sum = lanes_sum(b < a.sequences ? (steps_of(a, tokens) + START) * (unsigned)(a.c.kv_heads * a.blocks) : 0);
+    sum = lanes_sum(b < a.sequences ? (steps_of(a, tokens) + start_of(a)) * (unsigned)(a.c.kv_heads * a.blocks) : 0);
   }
   __device__ __forceinline__ int tokens_at(int b) const { return __builtin_amdgcn_readlane(tokens, b - first); }
   __device__ __forceinline__ unsigned before(int b) const { return b > first ? (unsigned)__builtin_amdgcn_readlane((int)sum, b - first - 1) : 0; }
@@ -63,6 +64,76 @@ struct Cut {
     return place < far ? place / (each + 1) : more + (place - far) / each;
   }
 };
+
+// What a worker does next: steps s0 .. s1 - 1 of the walk of block `block` of head h of sequence b
+struct Run {
+  int b, h, block, s0, s1, steps, tokens;
+};
+// A workgroup's run of the line
+struct Runs {
+  Batch batch;
+  int b, unit, worker;
+  unsigned at, left;                                 // within the walk; of the run
+  // false: there is none
+  __device__ __forceinline__ bool begin(const CachedArgs& a, int lane) {
+    const int per_sequence = a.c.kv_heads * a.blocks;
+    worker = -1;
+    if (a.workers == 0) {
+      b = blockIdx.x / per_sequence;
+      unit = blockIdx.x - b * per_sequence;
+      batch.look(a, b, lane);
+      at = 0;
+      left = start_of(a) + steps_of(a, batch.tokens_at(b));
+      return true;
+    }
+    Cut cut;
+    unsigned places = 0;
+    for (int first = (a.sequences - 1) & ~63; first >= 0; first -= 64) {
+      batch.look(a, first, lane);                    // (ends with the first 64)
+      places += batch.all();
+    }
+    cut.make(a, places);
+    // neighbours on the line, which share keys where a head has several blocks, to one XCD
+    const unsigned per = (cut.workers + 7) / 8, n = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= per || n >= cut.workers) return false;
+    worker = (int)n;
+    at = cut.begin(n);
+    left = cut.begin(n + 1) - at;
+    while (at >= batch.all() && batch.first + 64 < a.sequences) {
+      at -= batch.all();
+      batch.look(a, batch.first + 64, lane);
+    }
+    b = batch.first + __popcll(__ballot(batch.sum <= at));
+    at -= batch.before(b);
+    const unsigned walk = start_of(a) + steps_of(a, batch.tokens_at(b));
+    unit = at / walk;
+    at -= unit * walk;
+    return true;
+  }
+  __device__ __forceinline__ bool next(const CachedArgs& a, int lane, Run& r) {
+    if (left == 0) return false;
+    if (b >= batch.first + 64) batch.look(a, b, lane);
+    const unsigned start = start_of(a);
+    r.b = b;
+    r.tokens = batch.tokens_at(b);
+    r.steps = steps_of(a, r.tokens);
+    r.h = unit / a.blocks;
+    r.block = unit - r.h * a.blocks;
+    const unsigned to = min(start + r.steps, at + left);
+    r.s0 = at > start ? at - start : 0;
+    r.s1 = to > start ? to - start : 0;
+    left -= to - at;
+    at = 0;
+    if (++unit == a.c.kv_heads * a.blocks) {
+      unit = 0;
+      ++b;
+    }
+    return r.s1 > 0;                                 // (else the run ends in front of the walk's first step)
+  }
+};
+inline unsigned cached_grid(const CachedArgs& a) {
+  return a.workers ? (unsigned)((a.workers + 7) / 8 * 8) : (unsigned)(a.sequences * a.c.kv_heads * a.blocks);
+}
 
 // Results that are parts of a block's: m (log2 units), l, N of `rows` = 16 * tiles rows; a worker leaves at most one of a walk that
 // began before it (slot 2 w) and one of a walk that goes on behind it (slot 2 w + 1).

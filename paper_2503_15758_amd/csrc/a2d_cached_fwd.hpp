@@ -20,7 +20,7 @@ namespace cached {
 
 using namespace mfma;
 
-constexpr int WAVES = 4;
+constexpr int WAVES = 4, STEP = 32;
 constexpr float LOW = -3.0e38f;                      // a reference below every score
 
 template <int N>
@@ -478,57 +478,12 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && FMT != A2D_CACHE_BF16 ? 3 : 
   rd.init(lane, mine);
   Walk<H, FMT, RT> w{a, ln, rd, mine, lane, wave};
 
-  // the workgroup's run of the line
-  const int per_sequence = a.c.kv_heads * a.blocks;
-  Batch batch;
-  int b, unit;
-  unsigned at, left;                                 // within the walk; of the run
-  int worker = -1;
-  if (a.workers == 0) {
-    b = blockIdx.x / per_sequence;
-    unit = blockIdx.x - b * per_sequence;
-    batch.look(a, b, lane);
-    at = 0;
-    left = START + steps_of(a, batch.tokens_at(b));
-  } else {
-    Cut cut;
-    unsigned places = 0;
-    for (int first = (a.sequences - 1) & ~63; first >= 0; first -= 64) {
-      batch.look(a, first, lane);                    // (ends with the first 64)
-      places += batch.all();
-    }
-    cut.make(a, places);
-    // neighbours on the line, which share keys where a head has several blocks, to one XCD
-    const unsigned per = (cut.workers + 7) / 8, n = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((blockIdx.x >> 3) >= per || n >= cut.workers) return;
-    worker = (int)n;
-    at = cut.begin(n);
-    left = cut.begin(n + 1) - at;
-    while (at >= batch.all() && batch.first + 64 < a.sequences) {
-      at -= batch.all();
-      batch.look(a, batch.first + 64, lane);
-    }
-    b = batch.first + __popcll(__ballot(batch.sum <= at));
-    at -= batch.before(b);
-    const unsigned walk = START + steps_of(a, batch.tokens_at(b));
-    unit = at / walk;
-    at -= unit * walk;
-  }
-
-  while (left > 0) {
-    if (b >= batch.first + 64) batch.look(a, b, lane);
-    const int tokens = batch.tokens_at(b), steps = steps_of(a, tokens);
-    const unsigned walk = START + steps, to = min(walk, at + left);
-    const int s0 = at > START ? at - START : 0, s1 = to > START ? to - START : 0;
-    left -= to - at;
-    at = 0;
-    const int h = unit / a.blocks, block = unit - h * a.blocks, now = b;
-    if (++unit == per_sequence) {
-      unit = 0;
-      ++b;
-    }
-    if (s1 == 0) break;                              // (the run ends in front of its first step)
-    w.run(now, h, block, s0, s1, tokens);
+  Runs runs;
+  if (!runs.begin(a, lane)) return;
+  Run run;
+  while (runs.next(a, lane, run)) {
+    const int block = run.block;
+    w.run(run.b, run.h, block, run.s0, run.s1, run.tokens);
 
     // the four wavefronts' results become one, 16 rows at a time
     const int lane = lane_again(), thread = 64 * wave + lane;
@@ -539,8 +494,8 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && FMT != A2D_CACHE_BF16 ? 3 : 
       if (lane < 16) stat[wave][16 * t + lane] = f32x4{m, w.st.ref[t], w.live(t) ? l : 0.f, w.live(t) ? 1.f : 0.f};
     }
     __syncthreads();
-    const bool whole = s0 == 0 && s1 == steps;
-    float* part = whole ? nullptr : a.parts + (size_t)(2 * worker + (s0 == 0)) * part_floats(ROWS, H);
+    const bool whole = run.s0 == 0 && run.s1 == run.steps;
+    float* part = whole ? nullptr : a.parts + (size_t)(2 * runs.worker + (run.s0 == 0)) * part_floats(ROWS, H);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       {
@@ -582,7 +537,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && FMT != A2D_CACHE_BF16 ? 3 : 
         }
         if (whole) {
           const int g = index / a.rows, i = index - g * a.rows;
-          finish(a, now, h * a.group + g, i, H, quad, o, top, l);
+          finish(a, run.b, run.h * a.group + g, i, H, quad, o, top, l);
         } else {
           *reinterpret_cast<f32x4*>(part + 2 * ROWS + (size_t)r * H + 4 * quad) = o;
           if (quad == 0) {
@@ -599,7 +554,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && FMT != A2D_CACHE_BF16 ? 3 : 
 template <int H, int FMT>
 hipError_t go_tiles(Phase ph, const CachedArgs& a, hipStream_t s) {
   if (ph == PREPARE) return hipSuccess;              // (no dynamic LDS)
-  const dim3 grid(a.workers ? (unsigned)((a.workers + 7) / 8 * 8) : (unsigned)(a.sequences * a.c.kv_heads * a.blocks));
+  const dim3 grid(cached_grid(a));
   if (a.tiles == 1) A2D_LAUNCH((cached_kernel<H, FMT, 1>), grid, dim3(64 * WAVES), 0, s, a);
   else A2D_LAUNCH((cached_kernel<H, FMT, 2>), grid, dim3(64 * WAVES), 0, s, a);
   return hipGetLastError();

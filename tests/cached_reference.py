@@ -131,17 +131,17 @@ def attention(Q, values, table, lens, K=None, V=None, masks=None, scale=1.0):
     return N, m, l, A, size
 
 
-def bounds(N, m, l, A, size, H, keys):
+def bounds(N, m, l, A, size, H, keys, coarse=False):
     """How far (N, l relative to the kernel's own m), m and lse may be, and O in bf16.  fp32: H products of a score and their sum, then its
     product with scale log2(e) and the reference taken off (4 more), each 2^-24 of sum |q k| or less: ds.  An exponential: that, and an ulp of
     2^x.  P as two bf16 numbers: 2^-16.  Sums of `keys` terms in any order, four partial ones: (keys + 8) 2^-24; merges rescale a few
-    times: 2^-20 covers them."""
+    times: 2^-20 covers them.  coarse: P of O as one bf16 number, each at most half a step off, 2^-8: of the sum of the |p v| that is as much."""
     ds = (H + 8) * 2.0 ** -24 * size
     rel = 2 * ds + 2.0 ** -16 + (keys + 8) * 2.0 ** -24 + 2.0 ** -20
     some = l > 0
     l1 = torch.where(some, l, torch.ones_like(l))
     O, a = N / l1.unsqueeze(-1), A / l1.unsqueeze(-1)
-    return {"O": (2.0 ** -8) * O.abs() + rel.unsqueeze(-1) * 2 * a, "N": rel.unsqueeze(-1) * A, "l": rel * l,
+    return {"O": (2.0 ** -8) * O.abs() + (rel.unsqueeze(-1) * 2 + (2.0 ** -8 if coarse else 0)) * a, "N": rel.unsqueeze(-1) * A, "l": rel * l,
             "m": ds + 2.0 ** -22 * m.abs().nan_to_num(0, 0, 0), "lse": rel + ds + 2.0 ** -21 * m.abs().nan_to_num(0, 0, 0) + 2.0 ** -22}
 
 

@@ -47,7 +47,8 @@ def _expect(x):
     values = [ref.cache_values(x["cache"], i) for i in range(2)]
     got = ref.attention(x["Q"], values, x["table"], x["lens"], x["K"], x["V"], x["masks"], x["scale"])
     keys = max(0, int(x["lens"].max())) + x["Q"].shape[2]
-    return got, ref.bounds(*got, x["Q"].shape[3], keys)
+    n, heads, rows, H = x["Q"].shape
+    return got, ref.bounds(*got, H, keys, coarse=heads // x["cache"][0].shape[1] * rows > 64)
 
 
 def _check(x, want=None, **more):
@@ -81,3 +82,11 @@ def test_against_64_bits(kernels, fmt, H, kv_heads, group, rows):
 def test_long_and_short_together(fmt, H, rows):
     """Walks that many workgroups share beside ones of a step."""
     _check(_problem(11, fmt, H, 2, 2, rows, [5000, 1, 0, 31, 2049, 333], 16, masked=rows > 1), max_tokens=5000)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3", "e2m1"])
+@pytest.mark.parametrize("H", [64, 80, 96, 128])
+@pytest.mark.parametrize("group, rows, masked", [(1, 65, True), (2, 100, True), (8, 33, True), (3, 130, False), (1, 256, True)])
+def test_many_rows(fmt, H, group, rows, masked):
+    """Workgroups of 128 and 256 rows, several blocks, trees of more than a word, chains."""
+    _check(_problem(5, fmt, H, 1, group, rows, [0, 65, 700], 48, masked=masked))
