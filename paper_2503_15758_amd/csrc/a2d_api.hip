@@ -999,7 +999,8 @@ a2d_status check_cache(const a2d_cache* c, const char* who) {
 
 a2d::CacheView view_of(const a2d_cache& c) {
   return a2d::CacheView{static_cast<char*>(c.K), static_cast<char*>(c.V), reinterpret_cast<char*>(c.K_scales),
-                        reinterpret_cast<char*>(c.V_scales), c.table, c.kv_heads, c.page_rows / 16, c.pages, c.max_pages};
+                        reinterpret_cast<char*>(c.V_scales), c.table, c.kv_heads, c.page_rows / 16, c.pages, c.max_pages,
+                        0xFFFFFFFFu / (unsigned)(c.page_rows / 16)};
 }
 
 // A layout with {0, 0, 0} filled in.  output: its rows must not overlap - the dimensions, by their strides, reach past all smaller ones

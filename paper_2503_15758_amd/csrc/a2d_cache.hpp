@@ -37,15 +37,34 @@ struct CacheView {
   char *Ks, *Vs;               // 4 bytes a row
   const int32_t* table;
   int kv_heads, page_units, pages, max_pages;
+  unsigned inverse;            // floor((2^32 - 1) / page_units)
 };
 constexpr unsigned NO_UNIT = 0xFFFFFFFFu;
-// of the 16 tokens of tile `tile` of sequence b, head h; NO_UNIT where the table names no page of the cache
+// The place of tile `tile` (16 tokens) of sequence b in the table and in its page; the page's number is then asked for, and unit() takes it.
+// (Two steps without a branch, so that other requests can go out in between.)
+struct Place {
+  int page, rest;              // the table's entry; -1: there is none
+  __device__ __forceinline__ void ask(const CacheView& c, int b, int tile, bool wanted = true) {
+    int at = (int)__umulhi((unsigned)tile, c.inverse);             // (one too few at the most)
+    rest = tile - at * c.page_units;
+    if (rest >= c.page_units) {
+      ++at;
+      rest -= c.page_units;
+    }
+    const bool there = wanted && (unsigned)at < (unsigned)c.max_pages && tile >= 0;
+    const int entry = c.table[(int64_t)b * c.max_pages + (there ? at : 0)];
+    rest = there ? rest : -1;
+    page = entry;
+  }
+  // of head h; NO_UNIT where the table names no page of the cache
+  __device__ __forceinline__ unsigned unit(const CacheView& c, int h) const {
+    return rest >= 0 && (unsigned)page < (unsigned)c.pages ? ((unsigned)page * c.kv_heads + h) * c.page_units + rest : NO_UNIT;
+  }
+};
 __device__ __forceinline__ unsigned unit_of(const CacheView& c, int b, int h, int tile) {
-  const int at = tile / c.page_units;
-  if (tile < 0 || at >= c.max_pages) return NO_UNIT;
-  const int page = c.table[(int64_t)b * c.max_pages + at];
-  if ((unsigned)page >= (unsigned)c.pages) return NO_UNIT;
-  return ((unsigned)page * c.kv_heads + h) * c.page_units + (tile - at * c.page_units);
+  Place p;
+  p.ask(c, b, tile);
+  return p.unit(c, h);
 }
 
 struct BatchLayout {           // elements between sequences, heads, rows

@@ -4,15 +4,17 @@
 namespace a2d {
 namespace {
 
-// Joins the parts of the blocks whose walk was cut: M = max m, N = sum 2^(m_k - M) N_k, l likewise, in the order of the keys.  A workgroup has
-// `per` rows of a block, one after another; eight groups of lanes take every eighth part and are joined in order.
-template <int H>
-__global__ __launch_bounds__(256) void cached_merge_kernel(CachedArgs a, int per, int groups) {
+// Joins the parts of the blocks whose walk was cut: M = max m, N = sum 2^(m_k - M) N_k, l likewise.  SHARED: a workgroup has one row, whose
+// parts its eight groups of 32 lanes take in turn (they are joined in order); else each group has a row of its own.
+// Bound: HBM and the last-level cache, each part read once; short calls: the launch.
+template <int H, bool SHARED>
+__global__ __launch_bounds__(256) void cached_merge_kernel(CachedArgs a, int groups) {
   constexpr int QUADS = H / 4;
   __shared__ f32x4 sums[8][QUADS];
   __shared__ float ms[8], ls[8];
+  warm_cached();
   const int lane = threadIdx.x & 63, group = threadIdx.x >> 5, quad = threadIdx.x & 31;
-  const int u = blockIdx.x / groups, from = (blockIdx.x - u * groups) * per, per_sequence = a.c.kv_heads * a.blocks;
+  const int u = blockIdx.x / groups, at = blockIdx.x - u * groups, per_sequence = a.c.kv_heads * a.blocks;
   const int b = u / per_sequence, unit = u - b * per_sequence;
   Batch batch;
   Cut cut;
@@ -30,12 +32,14 @@ __global__ __launch_bounds__(256) void cached_merge_kernel(CachedArgs a, int per
   const unsigned w0 = cut.worker_of(begin), parts = cut.worker_of(last) - w0 + 1;
   if (parts == 1) return;
   const int rows = 16 * a.tiles, h = unit / a.blocks, block = unit - h * a.blocks;
-  for (int r = from; r < from + per; ++r) {
-    const int index = block * rows + r;
-    if (r >= rows || index >= a.group * a.rows) return;
-    float m = -INFINITY, l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (unsigned k = group; k < parts; k += 8) {
+  const int r = SHARED ? at : 8 * at + group, index = block * rows + r;
+  const bool there = r < rows && index < a.group * a.rows;
+  if (SHARED && !there) return;
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  if (there) {
+#pragma unroll 4
+    for (unsigned k = SHARED ? group : 0; k < parts; k += SHARED ? 8 : 1) {
       const float* part = a.parts + (size_t)(2 * (w0 + k) + (k == 0)) * part_floats(rows, H);
       const float pm = part[r], pl = part[rows + r];
       f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -47,31 +51,32 @@ __global__ __launch_bounds__(256) void cached_merge_kernel(CachedArgs a, int per
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = o[e] * f + x[e] * g;
     }
-    __syncthreads();
+  }
+  if constexpr (SHARED) {
     if (quad < QUADS) sums[group][quad] = o;
     if (quad == 0) {
       ms[group] = m;
       ls[group] = l;
     }
     __syncthreads();
-    if (threadIdx.x < QUADS) {
-      float top = -INFINITY;
+    if (threadIdx.x >= QUADS) return;
+    m = -INFINITY;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) top = fmaxf(top, ms[k]);
-      l = 0.f;
-      o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < 8; ++k) m = fmaxf(m, ms[k]);
+    l = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float f = top == -INFINITY ? 0.f : fast_exp2(ms[k] - top);
-        const f32x4 x = sums[k][quad];
-        l += ls[k] * f;
+    for (int k = 0; k < 8; ++k) {
+      const float f = m == -INFINITY ? 0.f : fast_exp2(ms[k] - m);
+      const f32x4 x = sums[k][quad];
+      l += ls[k] * f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += x[e] * f;
-      }
-      const int g = index / a.rows;
-      finish(a, b, h * a.group + g, index - g * a.rows, H, quad, o, top, l);
+      for (int e = 0; e < 4; ++e) o[e] += x[e] * f;
     }
   }
+  if (!there || quad >= QUADS) return;
+  const int g = index / a.rows;
+  finish(a, b, h * a.group + g, index - g * a.rows, H, quad, o, m, l);
 }
 
 // The plain form, on the vector ALU: a wavefront for each row of each query head; a lane has one of 64 keys for the scores, and two columns of O.
@@ -155,9 +160,9 @@ template <int H>
 void go_merge(const CachedArgs& a, hipStream_t s) {
   const int rows = a.group * a.rows < 16 * a.tiles ? a.group * a.rows : 16 * a.tiles;
   const int64_t units = (int64_t)a.sequences * a.c.kv_heads * a.blocks;
-  // one row for a workgroup where that gives the chip work, else eight
-  const int per = units * rows > 4096 ? 8 : 1, groups = (rows + per - 1) / per;
-  A2D_LAUNCH((cached_merge_kernel<H>), dim3((unsigned)(units * groups)), dim3(256), 0, s, a, per, groups);
+  // (a workgroup finds out its walk's parts in 1.3 us: more of them than the chip holds cost more than long walks' rows side by side save)
+  if (units * rows <= 4096) A2D_LAUNCH((cached_merge_kernel<H, true>), dim3((unsigned)(units * rows)), dim3(256), 0, s, a, rows);
+  else A2D_LAUNCH((cached_merge_kernel<H, false>), dim3((unsigned)(units * ((rows + 7) / 8))), dim3(256), 0, s, a, (rows + 7) / 8);
 }
 
 }  // namespace

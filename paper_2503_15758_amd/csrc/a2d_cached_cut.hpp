@@ -5,12 +5,26 @@
 
 namespace a2d {
 
-// The walk of a block of rows: steps of 32 keys (`shift`: 5), those of the cached tokens first, then those of the drafted rows.  Sequence b has
+// Brings the kernel's arguments into the scalar cache in one go: read line after line as the prologue comes to them, a cold one is half a
+// microsecond each time.
+__device__ __forceinline__ void warm_cached() {
+  constexpr int last = ((int)sizeof(CachedArgs) - 1) / 64;
+  static_assert(last <= 5, "lines to touch");
+  int v[6];
+  asm volatile(
+      "s_load_dword %0, %6, 0x0\n\ts_load_dword %1, %6, 0x40\n\ts_load_dword %2, %6, 0x80\n\ts_load_dword %3, %6, 0xc0\n\t"
+      "s_load_dword %4, %6, %7\n\ts_load_dword %5, %6, %8\n\ts_waitcnt lgkmcnt(0)"
+      : "=&s"(v[0]), "=&s"(v[1]), "=&s"(v[2]), "=&s"(v[3]), "=&s"(v[4]), "=&s"(v[5])
+      : "s"(__builtin_amdgcn_kernarg_segment_ptr()), "i"(64 * (last < 4 ? last : 4)), "i"(64 * last));
+}
+
+// The walk of a block of rows: steps of 32 keys (`shift`: 5), those of the drafted rows first
+// (they need no table, whose entries are on their way meanwhile), then those of the cached tokens.  Sequence b has
 // kv_heads * blocks such walks of the same length; all walks, one after another, are a line, cut into equal runs, one for each worker,
 // whatever the lengths are (which the host does not know).  On the line a walk is START places longer than its steps: what it costs
 // besides (Q, the table, the first codes, the join of the wavefronts: 8 sequences, one of them of a token alone, without 61 us, with 41).
 // (The form of many rows has steps of 64 keys, and its START is half as many.)
-constexpr unsigned LEAST = 16;         // places of a worker
+__device__ __forceinline__ unsigned least_of(const CachedArgs& a) { return a.shift == 6 ? 6 : 12; }       // places of a worker
 __device__ __forceinline__ unsigned start_of(const CachedArgs& a) { return a.shift == 6 ? 4 : 8; }
 __device__ __forceinline__ int steps_for(const CachedArgs& a, int keys) { return (keys + (1 << a.shift) - 1) >> a.shift; }
 __device__ __forceinline__ int draft_steps(const CachedArgs& a) { return a.K ? steps_for(a, a.rows) : 0; }
@@ -54,7 +68,7 @@ struct Cut {
   unsigned workers;
   __device__ __forceinline__ void make(const CachedArgs& a, unsigned places) {
     total = places;
-    workers = min((unsigned)a.workers, max(1u, total / LEAST));
+    workers = min((unsigned)a.workers, max(1u, total / least_of(a)));
     each = total / workers;
     more = total - each * workers;
   }
@@ -149,7 +163,7 @@ __device__ __forceinline__ void finish(const CachedArgs& a, int b, int head, int
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = (bf16_t)(o[e] * inverse);
     *reinterpret_cast<bf16x4*>(static_cast<bf16_t*>(a.out0) + at_row(a.lo, b, head, i) + 4 * quad) = y;
-    if (quad == 0) a.out1[row] = l == 0.f ? -INFINITY : fmaf(top, kLn2, logf(l));
+    if (quad == 0) a.out1[row] = l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;      // (log2)
   } else {
     *reinterpret_cast<f32x4*>(static_cast<float*>(a.out0) + row * hdim + 4 * quad) = o;
     if (quad == 0) {

@@ -272,13 +272,12 @@ __device__ __forceinline__ void scores(f32x4 (&s)[RT], const bf16x8 (&kf)[Head<H
   }
 }
 
-// Is any of the eight numbers a NaN or an infinity?
-__device__ __forceinline__ bool not_finite(bf16x8 x) {
-  const u32x4 w = __builtin_bit_cast(u32x4, x);
-  bool bad = false;
+// Is any of the 16 numbers a NaN or an infinity?  (Their products with 0, two at a time, are 0 or NaN.)
+__device__ __forceinline__ bool not_finite(const Words<8>& w) {
+  float x = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) bad |= (w[i] & 0x7F80u) == 0x7F80u || (w[i] & 0x7F800000u) == 0x7F800000u;
-  return bad;
+  for (int i = 0; i < 8; ++i) x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w.w[i]), bf16x2{(bf16_t)0.f, (bf16_t)0.f}, x, false);
+  return !(x == 0.f);
 }
 
 // bits of 32 drafted rows from 32 * step on that row i of sequence b sees
@@ -308,9 +307,18 @@ struct Walk {
 
   // steps s0 .. s1 - 1 of block `block` of head h of sequence b, which has `tokens` cached ones
   __device__ __forceinline__ void run(int b, int h, int block, int s0, int s1, int tokens) {
-    const int rows = a.group * a.rows;
-    const int cached = (tokens + STEP - 1) / STEP, last = min(s1, cached), first = s0 + wave;
-    if (first < last) look_up(b, h, first, tokens);
+    const int rows = a.group * a.rows, drafts = draft_steps(a);
+    int s = s0 + wave;                               // the wavefront's steps: s, s + WAVES, ..
+    const int first = s < drafts ? s + (drafts - s + WAVES - 1) / WAVES * WAVES : s;       // the first one of cached tokens
+    // requests go out before any is waited for: pages, drafted rows, masks, Q
+    Place place;
+    look_up(place, b, first - drafts, tokens, first < s1);
+    Codes<H, A2D_CACHE_BF16> drafted;
+    if (s < min(s1, drafts)) {
+      Lane<H> ln;
+      ln.init(lane_again());
+      load_drafts<H>(drafted, a, b, h, STEP * s, ln);
+    }
     {
       Lane<H> ln;
       ln.init(lane_again());
@@ -330,21 +338,17 @@ struct Walk {
       }
     }
     st.clear();
-    if (first < last) cache_steps(b, h, first, last, tokens);
-    if (a.K) {
-      // (those in front of the first drafted step are behind the wavefront's last cached one)
-      int s = first;
-      if (s < cached) s += (cached - s + WAVES - 1) / WAVES * WAVES;
-      for (; s < s1; s += WAVES) draft_step(b, h, s - cached);
-    }
+    units = place.unit(a.c, h);
+    for (bool again = false; s < min(s1, drafts); s += WAVES, again = true) draft_step(b, h, s, drafted, again);
+    if (first < s1) cache_steps(b, h, first - drafts, min(s1 - drafts, (tokens + STEP - 1) / STEP), tokens);
   }
   // does the lane's row of tile t exist, and is it a token (its own bit is set)?
   __device__ __forceinline__ bool live(int t) const { return row_of[t] >= 0 && (own[t] >> (row_of[t] & 63) & 1); }
 
   // the units of tile lane & 1 of the wavefront's step lane >> 1 of 32 from s on
-  __device__ __forceinline__ void look_up(int b, int h, int s, int tokens) {
+  __device__ __forceinline__ void look_up(Place& p, int b, int s, int tokens, bool wanted = true) const {
     const int tile = 2 * (s + WAVES * (lane >> 1)) + (lane & 1);
-    units = tile * 16 < tokens ? unit_of(a.c, b, h, tile) : NO_UNIT;
+    p.ask(a.c, b, tile, wanted && tile < (tokens + 15) / 16);
   }
 
   __device__ __forceinline__ void cache_steps(int b, int h, int first, int last, int tokens) {
@@ -360,6 +364,7 @@ struct Walk {
         load_unit<H, FMT>(c[k], a.c, u == NO_UNIT ? 0 : u, ln);
       }
     };
+    if (first >= last) return;                       // (a walk of nothing)
     load(0, first);
     for (int s = first, n = 0; s < last; s += WAVES, ++n) {
       f32x4 sc[2][RT];
@@ -374,7 +379,11 @@ struct Walk {
       __builtin_amdgcn_sched_barrier(0);
       // the next step's codes, while this one is worked on (behind the last: the last again)
       const bool more = s + WAVES < last;
-      if (A2D_SELDOM((n & 31) == 31 && more)) look_up(b, h, s + WAVES, tokens);
+      if (A2D_SELDOM((n & 31) == 31 && more)) {
+        Place p;
+        look_up(p, b, s + WAVES, tokens);
+        units = p.unit(a.c, h);
+      }
       load(more ? n + 1 : n, more ? s + WAVES : s);
       if (A2D_SELDOM(now != ~0u)) {
         const unsigned mine = now >> (4 * ln.g);
@@ -391,10 +400,12 @@ struct Walk {
   }
 
   // (the lane's places are computed anew: kept beside the walk over the cache, they would take its registers)
-  __device__ __forceinline__ void draft_step(int b, int h, int step) {
+  // (c: the codes of its first tile, asked for already where it is not a further step)
+  __device__ __forceinline__ void draft_step(int b, int h, int step, Codes<H, A2D_CACHE_BF16>& c, bool further) {
     Lane<H> ln;
     ln.init(lane_again());
     unsigned seen[RT], all = 0;
+    if (further) load_drafts<H>(c, a, b, h, STEP * step, ln);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       seen[t] = live(t) ? seen_rows(a, b, row_of[t], step) : 0;
@@ -408,14 +419,21 @@ struct Walk {
     unsigned bad = 0;                                // drafted rows of the step whose V is not finite
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      Codes<H, A2D_CACHE_BF16> c;
-      load_drafts<H>(c, a, b, h, STEP * step + 16 * k, ln);
+      if (k == 1 && all >> 16 == 0) {                // (no second tile: zeros, since P = 0 meets them)
 #pragma unroll
-      for (int n = 0; n < G::NV; ++n) {
-        const bool odd = ln.vlive[n] && (all >> (16 * k + ln.vrow[n]) & 1) &&
-                         (not_finite(decode_half<A2D_CACHE_BF16>(c.v[n], 0, 1.f)) || not_finite(decode_half<A2D_CACHE_BF16>(c.v[n], 1, 1.f)));
-        bad |= odd ? 1u << (16 * k + ln.vrow[n]) : 0;
+        for (int n = 0; n < G::NV; ++n)
+          if (64 * n + 64 <= 16 * G::PIECES || ln.vlive[n]) {
+            lds_store(area + G::KS * BLOCK + ln.lds[n], zero8());
+            lds_store(area + G::KS * BLOCK + (ln.lds[n] ^ 16), zero8());
+          }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) sc[1][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        break;
       }
+      if (k) load_drafts<H>(c, a, b, h, STEP * step + 16, ln);
+#pragma unroll
+      for (int n = 0; n < G::NV; ++n)
+        if (ln.vlive[n] && (all >> (16 * k + ln.vrow[n]) & 1) && not_finite(c.v[n])) bad |= 1u << (16 * k + ln.vrow[n]);
       // (rows that none of the block's rows see are zeros: they may hold anything)
       decode_values<H, A2D_CACHE_BF16>(c, ln, area + k * G::KS * BLOCK, all >> (16 * k) & 0xFFFF);
       bf16x8 kf[G::KS];
@@ -465,11 +483,12 @@ struct Walk {
 };
 
 template <int H, int FMT, int RT>
-__global__ __launch_bounds__(64 * WAVES, RT == 1 && FMT != A2D_CACHE_BF16 ? 3 : 2) void cached_kernel(CachedArgs a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void cached_kernel(CachedArgs a) {
   using G = Head<H>;
   constexpr int ROWS = 16 * RT, QUADS = H / 4;
   __shared__ __align__(1024) char area[WAVES][G::AREA];
   __shared__ f32x4 stat[WAVES][ROWS];                // m (log2 units), ref, l of a wavefront's row
+  warm_cached();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Lane<H> ln;
   ln.init(lane);

@@ -54,9 +54,9 @@ struct WideWalk {
   __device__ __forceinline__ int tile_of(int n) const { return (wave + W * n) / G::NV & 3; }
   __device__ __forceinline__ bool is_value(int n) const { return wave + W * n >= LOADS / 2; }
 
-  __device__ __forceinline__ void look_up(int b, int h, int s, int tokens) {
+  __device__ __forceinline__ void look_up(Place& p, int b, int s, int tokens, bool wanted = true) const {
     const int tile = 4 * s + lane;
-    units = (int64_t)tile * 16 < tokens ? unit_of(a.c, b, h, tile) : NO_UNIT;
+    p.ask(a.c, b, tile, wanted && tile < (tokens + 15) / 16);
   }
   // asks for the codes of step s, the n-th of the walk; the keys of it that are there
   __device__ __forceinline__ uint64_t load(int n, int s, int tokens) {
@@ -153,9 +153,10 @@ struct WideWalk {
   }
 
   __device__ __forceinline__ void run(int b, int h, int block, int s0, int s1, int tokens) {
-    const int rows = a.group * a.rows, cached = (tokens + 63) / 64, last = min(s1, cached);
-    const bool some = (block * W + wave) * 32 < rows;                     // of the wavefront's rows
-    if (s0 < last) look_up(b, h, s0, tokens);
+    const int drafts = draft_steps(a), first = max(s0 - drafts, 0), last = min(s1 - drafts, (tokens + 63) / 64);
+    const bool some = (block * W + wave) * 32 < a.group * a.rows;         // of the wavefront's rows
+    Place place;
+    look_up(place, b, first, tokens, first < last);
     const int ln = lane_again();
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -173,16 +174,22 @@ struct WideWalk {
 #pragma unroll
       for (int x = 0; x < HT; ++x) o[x][q] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    if (s0 < last) {
-      uint64_t now = load(0, s0, tokens), next = 0;
+    units = place.unit(a.c, h);
+    for (int s = s0; s < min(s1, drafts); ++s) draft_step(b, h, block, s);
+    if (first < last) {
+      uint64_t now = load(0, first, tokens), next = 0;
       decode(0, now);
-      if (s0 + 1 < last) next = load(1, s0 + 1, tokens);
+      if (first + 1 < last) next = load(1, first + 1, tokens);
       __syncthreads();
-      for (int s = s0, n = 0; s < last; ++s, ++n) {
+      for (int s = first, n = 0; s < last; ++s, ++n) {
         uint64_t after = 0;
         if (s + 1 < last) {
           decode((n + 1) & 1, next);
-          if (A2D_SELDOM((n & 15) == 14)) look_up(b, h, s + 2, tokens);
+          if (A2D_SELDOM((n & 15) == 14)) {
+            Place p;
+            look_up(p, b, s + 2, tokens);
+            units = p.unit(a.c, h);
+          }
           // (behind the last step: the last again)
           after = load(s + 2 < last ? n + 2 : n + 1, s + 2 < last ? s + 2 : s + 1, tokens);
         }
@@ -210,8 +217,6 @@ struct WideWalk {
         next = after;
       }
     }
-    if (a.K)
-      for (int s = max(s0, cached); s < s1; ++s) draft_step(b, h, block, s - cached, some);
   }
   // the lane's row of tile q (the block's last one in place of those behind it); made again where it is needed, not kept on the walk
   struct Row {
@@ -230,7 +235,7 @@ struct WideWalk {
   }
 
   // 64 drafted rows, in the first buffer
-  __device__ __forceinline__ void draft_step(int b, int h, int block, int step, bool some) {
+  __device__ __forceinline__ void draft_step(int b, int h, int block, int step) {
     if (!a.masks) {
       // (a chain's rows see none behind themselves: the last row of a block that has rows of one head alone)
       const int from = block * W * 32, to = min(from + W * 32, a.group * a.rows) - 1;
@@ -249,12 +254,12 @@ struct WideWalk {
         const unsigned at = area + (value ? K_BYTES : 0) + t * KS * BLOCK + plds;
         lds_store(at, x);
         lds_store(at ^ 16, y);
-        if (value && (not_finite(x) || not_finite(y))) atomicOr(&bad[key >> 5], 1u << (key & 31));
+        if (value && not_finite(w)) atomicOr(&bad[key >> 5], 1u << (key & 31));
       }
     }
     __syncthreads();
-    const uint64_t odd = (uint64_t)__builtin_amdgcn_readfirstlane((int)bad[0]) & 0xFFFFFFFFu |
-                         (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)bad[1]) << 32;
+    const unsigned odd0 = (unsigned)__builtin_amdgcn_readfirstlane((int)bad[0]), odd1 = (unsigned)__builtin_amdgcn_readfirstlane((int)bad[1]);
+    const uint64_t odd = (uint64_t)odd1 << 32 | odd0;
     Scores sc;
     Ring ring;
     fwd_first_keys<H>(ring, rd, 0);
@@ -317,6 +322,7 @@ template <int H, int FMT, int W, bool FINE>
 __global__ __launch_bounds__(64 * W, 2) void cached_wide_kernel(CachedArgs a) {
   extern __shared__ __align__(1024) char lds[];
   constexpr int ROWS = 32 * W;
+  warm_cached();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned area = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   Blocks16 rd;
