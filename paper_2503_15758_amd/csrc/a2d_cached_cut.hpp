@@ -22,10 +22,10 @@ __device__ __forceinline__ void warm_cached() {
 // (they need no table, whose entries are on their way meanwhile), then those of the cached tokens.  Sequence b has
 // kv_heads * blocks such walks of the same length; all walks, one after another, are a line, cut into equal runs, one for each worker,
 // whatever the lengths are (which the host does not know).  On the line a walk is START places longer than its steps: what it costs
-// besides (Q, the table, the first codes, the join of the wavefronts: 8 sequences, one of them of a token alone, without 61 us, with 41).
+// besides (Q, the table, the first codes, the join of the wavefronts: 8 sequences, one of them of a token alone, without 61 us, with 8 41; 16, for 8, 32 sequences 27.1 -> 26.2).
 // (The form of many rows has steps of 64 keys, and its START is half as many.)
 __device__ __forceinline__ unsigned least_of(const CachedArgs& a) { return a.shift == 6 ? 6 : 12; }       // places of a worker
-__device__ __forceinline__ unsigned start_of(const CachedArgs& a) { return a.shift == 6 ? 4 : 8; }
+__device__ __forceinline__ unsigned start_of(const CachedArgs& a) { return a.shift == 6 ? 4 : 16; }
 __device__ __forceinline__ int steps_for(const CachedArgs& a, int keys) { return (keys + (1 << a.shift) - 1) >> a.shift; }
 __device__ __forceinline__ int draft_steps(const CachedArgs& a) { return a.K ? steps_for(a, a.rows) : 0; }
 __device__ __forceinline__ int tokens_of(const CachedArgs& a, int length) { return min(max(length, 0), a.max_tokens); }
@@ -131,8 +131,9 @@ struct Runs {
     r.b = b;
     r.tokens = batch.tokens_at(b);
     r.steps = steps_of(a, r.tokens);
-    r.h = unit / a.blocks;
-    r.block = unit - r.h * a.blocks;
+    const mfma::Split sp = mfma::split_by(unit, a.blocks);
+    r.h = sp.q;
+    r.block = sp.r;
     const unsigned to = min(start + r.steps, at + left);
     r.s0 = at > start ? at - start : 0;
     r.s1 = to > start ? to - start : 0;

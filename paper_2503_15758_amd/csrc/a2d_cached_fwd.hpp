@@ -215,7 +215,7 @@ __device__ __forceinline__ void soften(State<H, RT>& st, f32x4 (&s)[2][RT], floa
   if (A2D_SELDOM(__any(far))) {                      // a reference is only moved by more than 2^8
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      const float ref = fmaxf(st.ref[t], row_max(top[t]) * c2);
+      const float x = row_max(top[t]) * c2, ref = x > st.ref[t] + 8.f ? x : st.ref[t];      // (each row by its own scores alone)
       const float f = ref == st.ref[t] ? 1.f : fast_exp2(st.ref[t] - ref);
       st.ref[t] = ref;
       st.l[t] *= f;
@@ -280,10 +280,27 @@ __device__ __forceinline__ bool not_finite(const Words<8>& w) {
   return !(x == 0.f);
 }
 
-// bits of 32 drafted rows from 32 * step on that row i of sequence b sees
-__device__ __forceinline__ unsigned seen_rows(const CachedArgs& a, int b, int i, int step) {
+// with zeros in place of NaN and infinities
+__device__ __forceinline__ bf16x8 finite_part(bf16x8 x) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (float)x[i] - (float)x[i] == 0.f ? x[i] : (bf16_t)0.f;
+  return x;
+}
+
+// of the 16 lanes 0 .. 15 (which 16 .. 31 and so on repeat)
+__device__ __forceinline__ unsigned or16(unsigned x) {
+  const auto with = [&](auto C) { x |= __builtin_bit_cast(unsigned, lane_swap<decltype(C)::value>(__builtin_bit_cast(float, x))); };
+  with(std::integral_constant<int, 0xB1>{});         // lanes 1, 2 off, then those of the other half of 8, of 16
+  with(std::integral_constant<int, 0x4E>{});
+  with(std::integral_constant<int, 0x141>{});
+  with(std::integral_constant<int, 0x140>{});
+  return (unsigned)__builtin_amdgcn_readfirstlane((int)x);
+}
+
+// bits of 32 drafted rows from 32 * step on that row i of sequence b sees (own: the word of its mask with its own bit)
+__device__ __forceinline__ unsigned seen_rows(const CachedArgs& a, int b, int i, int step, uint64_t own) {
   if (a.masks) {
-    const uint64_t w = a.masks[((int64_t)b * a.rows + i) * a.words + (step >> 1)];
+    const uint64_t w = a.words == 1 ? own : a.masks[((int64_t)b * a.rows + i) * a.words + (step >> 1)];
     const unsigned x = (unsigned)(w >> (32 * (step & 1)));
     const int left = a.rows - STEP * step;            // (bits of no row)
     return left < 32 ? x & ((1u << left) - 1) : x;
@@ -408,12 +425,10 @@ struct Walk {
     if (further) load_drafts<H>(c, a, b, h, STEP * step, ln);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      seen[t] = live(t) ? seen_rows(a, b, row_of[t], step) : 0;
+      seen[t] = live(t) ? seen_rows(a, b, row_of[t], step, own[t]) : 0;
       all |= seen[t];
     }
-#pragma unroll
-    for (int d = 1; d < 16; d *= 2) all |= (unsigned)__shfl_xor((int)all, d);
-    all = __builtin_amdgcn_readfirstlane((int)all);
+    all = or16(all);
     if (all == 0) return;
     f32x4 sc[2][RT];
     unsigned bad = 0;                                // drafted rows of the step whose V is not finite
@@ -452,8 +467,8 @@ struct Walk {
     products<H, RT>(st, sc, rd);
   }
 
-  // A drafted row's V with a NaN or an infinity may be added to those rows only that see it, and a product with P = 0 is not 0 then: such
-  // keys are added one at a time and become zeros in LDS.
+  // A NaN or an infinity in a drafted row's V may be added to those rows only that see it, and its product with P = 0 is not 0: such numbers
+  // are added one at a time and become zeros in LDS.
   __device__ __forceinline__ void apart(const f32x4 (&sc)[2][RT], const unsigned (&seen)[RT], unsigned bad) {
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) bad |= (unsigned)__shfl_xor((int)bad, d);
@@ -475,9 +490,12 @@ struct Walk {
 #pragma unroll
         for (int h = 0; h < G::HT; ++h)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) st.o[h][t][i] = fmaf(p, lds_number(column(16 * h + 4 * (lane >> 4) + i)), st.o[h][t][i]);
+          for (int i = 0; i < 4; ++i) {
+            const float v = lds_number(column(16 * h + 4 * (lane >> 4) + i));
+            st.o[h][t][i] = v - v == 0.f ? st.o[h][t][i] : fmaf(p, v, st.o[h][t][i]);
+          }
       }
-      if (lane < H / 8) lds_store(column(8 * lane), zero8());
+      if (lane < H / 8) lds_store(column(8 * lane), finite_part(lds_load_b128(column(8 * lane))));
     }
   }
 };

@@ -116,7 +116,8 @@ struct WideWalk {
     if (A2D_SELDOM(__any(far))) {
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const float to = fmaxf(ref[q], row_max(top[q]) * a.c2), f = to == ref[q] ? 1.f : fast_exp2(ref[q] - to);
+        const float x = row_max(top[q]) * a.c2, to = x > ref[q] + 8.f ? x : ref[q];         // (each row by its own scores alone)
+        const float f = to == ref[q] ? 1.f : fast_exp2(ref[q] - to);
         ref[q] = to;
         l[q] *= f;
 #pragma unroll
@@ -222,6 +223,7 @@ struct WideWalk {
   struct Row {
     int head, i;
     bool there, token;                               // token: and its own bit is set
+    uint64_t own;                                    // the word with it
   };
   __device__ __forceinline__ Row row(int b, int h, int block, int q) const {
     const int at = ((block * W + wave) * 2 + q) * 16 + (lane_again() & 15), rows = a.group * a.rows, r = min(at, rows - 1);
@@ -230,7 +232,8 @@ struct WideWalk {
     x.i = r - x.head * a.rows;
     x.head += h * a.group;
     x.there = at < rows;
-    x.token = x.there && (!a.masks || (a.masks[((int64_t)b * a.rows + x.i) * a.words + (x.i >> 6)] >> (x.i & 63) & 1));
+    x.own = a.masks ? a.masks[((int64_t)b * a.rows + x.i) * a.words + (x.i >> 6)] : ~(uint64_t)0;
+    x.token = x.there && (x.own >> (x.i & 63) & 1);
     return x;
   }
 
@@ -269,7 +272,8 @@ struct WideWalk {
     for (int q = 0; q < 2; ++q) {
       seen[q] = 0;
       const Row r = row(b, h, block, q);
-      if (r.token) seen[q] = seen_rows(a, b, r.i, 2 * step) | (uint64_t)(64 * step + 32 < a.rows ? seen_rows(a, b, r.i, 2 * step + 1) : 0) << 32;
+      if (r.token)
+        seen[q] = seen_rows(a, b, r.i, 2 * step, r.own) | (uint64_t)(64 * step + 32 < a.rows ? seen_rows(a, b, r.i, 2 * step + 1, r.own) : 0) << 32;
       const uint64_t mine = seen[q] >> (4 * (lane >> 4));
 #pragma unroll
       for (int k = 0; k < 4; ++k)
@@ -283,7 +287,7 @@ struct WideWalk {
     __syncthreads();
   }
 
-  // as in the form of few rows: V that is not finite goes to the rows that see it, one key at a time, and becomes zeros
+  // as in the form of few rows: numbers of V that are not finite go to the rows that see them, one at a time, and become zeros
   __device__ __forceinline__ void apart(const Scores& sc, const uint64_t (&seen)[2], uint64_t odd) {
     const int ln = lane_again();
     for (uint64_t left = odd; left; left &= left - 1) {
@@ -301,7 +305,8 @@ struct WideWalk {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int c = 16 * x + 4 * (ln >> 4) + i;
-            o[x][q][i] = fmaf(p, lds_number(row + (c >> 5) * BLOCK + 16 * ((c >> 3 & 3) ^ block_swap(r >> 2)) + 2 * (c & 7)), o[x][q][i]);
+            const float v = lds_number(row + (c >> 5) * BLOCK + 16 * ((c >> 3 & 3) ^ block_swap(r >> 2)) + 2 * (c & 7));
+            o[x][q][i] = v - v == 0.f ? o[x][q][i] : fmaf(p, v, o[x][q][i]);
           }
       }
     }
@@ -309,7 +314,8 @@ struct WideWalk {
     for (uint64_t left = odd; left; left &= left - 1) {
       const int key = __builtin_ctzll(left), r = key & 15;
       const unsigned row = area + K_BYTES + (key >> 4) * KS * BLOCK + r * 64;
-      if (ln < H / 8) lds_store(row + (ln >> 2) * BLOCK + 16 * ((ln & 3) ^ block_swap(r >> 2)), zero8());
+      const unsigned at = row + (ln >> 2) * BLOCK + 16 * ((ln & 3) ^ block_swap(r >> 2));
+      if (wave == 0 && ln < H / 8) lds_store(at, finite_part(lds_load_b128(at)));
     }
     __syncthreads();
   }
