@@ -51,7 +51,7 @@ __device__ __forceinline__ Words<N> load_words(gptr_t base, unsigned off) {
 template <int H>
 struct Head {
   static constexpr int HD = padded_head(H), KS = HD / 32, HT = H / 16, JF = H / 64, REST = (H % 64) / 8;
-  static constexpr int PIECES = H / 16, NV = (16 * PIECES + 63) / 64;      // of a row of V; loads of a tile
+  static constexpr int PIECES = H / 16, NV = (PIECES + 3) / 4;             // of a row of V; loads of a tile
   static constexpr int AREA = 2 * KS * BLOCK;                              // of a wavefront in LDS
 };
 
@@ -62,30 +62,26 @@ struct Codes {
   static constexpr int W = code_bytes<FMT>(16) / 4;
   Words<W> k[G::JF], v[G::NV];
   Words<(W + 1) / 2> rest;
-  unsigned ks, vs[G::NV];
+  unsigned ks, vs;
 };
 
-// where a lane's pieces lie in a tile of 16 rows
+// Where a lane's pieces lie in a tile of 16 rows: of row lane & 15, of K as above, of V the pieces 4 n + g.  (16 lanes that write into LDS together
+// then meet every bank once; with a row's pieces side by side they met a quarter of them, four times: trees of 64 on 8 sequences 144 us.)
 template <int H>
 struct Lane {
   using G = Head<H>;
-  int row, g, vrow[G::NV];
-  unsigned lds[G::NV];
-  bool has_rest, vlive[G::NV];
-  unsigned vpiece[G::NV];
+  int row, g;
+  unsigned lds;                // of its first piece in the blocks of a tile of V
+  bool has_rest;
   __device__ __forceinline__ void init(int lane) {
     row = lane & 15;
     g = lane >> 4;
     has_rest = g < G::REST;
-#pragma unroll
-    for (int n = 0; n < G::NV; ++n) {
-      const int at = min(64 * n + lane, 16 * G::PIECES - 1);
-      vlive[n] = 64 * n + lane < 16 * G::PIECES;
-      vrow[n] = at / G::PIECES;
-      vpiece[n] = at % G::PIECES;
-      lds[n] = (vpiece[n] >> 1) * BLOCK + vrow[n] * 64 + 16 * ((2 * (vpiece[n] & 1)) ^ block_swap(vrow[n] >> 2));
-    }
+    lds = (g >> 1) * BLOCK + row * 64 + 16 * ((2 * (g & 1)) ^ block_swap(row >> 2));
   }
+  __device__ __forceinline__ bool live(int n) const { return 4 * n + 4 <= G::PIECES || 4 * n + g < G::PIECES; }
+  // (pieces that there are none of: the row's first)
+  __device__ __forceinline__ int piece(int n) const { return live(n) ? 4 * n + g : 0; }
 };
 
 // The codes of one unit of the cache
@@ -99,12 +95,11 @@ __device__ __forceinline__ void load_unit(Codes<H, FMT>& c, const CacheView& vie
   if constexpr (G::REST)       // (lanes without columns there take the row's first)
     c.rest = load_words<(W + 1) / 2>(k, l.row * ROW + (l.has_rest ? code_bytes<FMT>(64) * G::JF + l.g * code_bytes<FMT>(8) : 0));
 #pragma unroll
-  for (int n = 0; n < G::NV; ++n) c.v[n] = load_words<W>(v, l.vrow[n] * ROW + l.vpiece[n] * code_bytes<FMT>(16));
+  for (int n = 0; n < G::NV; ++n) c.v[n] = load_words<W>(v, l.row * ROW + l.piece(n) * code_bytes<FMT>(16));
   if constexpr (FMT != A2D_CACHE_BF16) {
     const gptr_t ks = uniform_gptr(view.Ks + (uint64_t)unit * 64), vs = uniform_gptr(view.Vs + (uint64_t)unit * 64);
     c.ks = load_words<1>(ks, l.row * 4).w[0];
-#pragma unroll
-    for (int n = 0; n < G::NV; ++n) c.vs[n] = load_words<1>(vs, l.vrow[n] * 4).w[0];
+    c.vs = load_words<1>(vs, l.row * 4).w[0];
   }
 }
 
@@ -119,7 +114,7 @@ __device__ __forceinline__ void load_drafts(Codes<H, A2D_CACHE_BF16>& c, const C
   if constexpr (G::REST) c.rest = load_words<4>(k, kr + (l.has_rest ? 128 * G::JF + l.g * 16 : 0));
 #pragma unroll
   for (int n = 0; n < G::NV; ++n)
-    c.v[n] = load_words<8>(v, (unsigned)min(first + l.vrow[n], a.rows - 1) * (unsigned)(2 * a.lv.row) + l.vpiece[n] * 32);
+    c.v[n] = load_words<8>(v, (unsigned)min(first + l.row, a.rows - 1) * (unsigned)(2 * a.lv.row) + l.piece(n) * 32);
 }
 
 template <int FMT, int N>
@@ -165,16 +160,16 @@ __device__ __forceinline__ void decode_values(const Codes<H, FMT>& c, const Lane
 #pragma unroll
   for (int n = 0; n < G::NV; ++n) {
     float scale = 1.f;
-    if constexpr (FMT != A2D_CACHE_BF16) scale = scale_number(c.vs[n] >> (8 * (l.vpiece[n] >> 1)) & 255);
+    if constexpr (FMT != A2D_CACHE_BF16) scale = scale_number(c.vs >> (8 * (2 * n + (l.g >> 1))) & 255);
     bf16x8 x = decode_half<FMT>(c.v[n], 0, scale), y = decode_half<FMT>(c.v[n], 1, scale);
     if (A2D_SELDOM(vis != 0xFFFFu)) {
-      const bool keep = vis >> l.vrow[n] & 1;
+      const bool keep = vis >> l.row & 1;
       x = keep ? x : zero8();
       y = keep ? y : zero8();
     }
-    if (64 * n + 64 <= 16 * G::PIECES || l.vlive[n]) {
-      lds_store(at + l.lds[n], x);
-      lds_store(at + (l.lds[n] ^ 16), y);
+    if (l.live(n)) {
+      lds_store(at + l.lds + 2 * n * BLOCK, x);
+      lds_store(at + (l.lds ^ 16) + 2 * n * BLOCK, y);
     }
   }
 }
@@ -321,6 +316,7 @@ struct Walk {
   int row_of[RT];                                    // the lane's row of a tile within its sequence; -1: there is none
   uint64_t own[RT];                                  // the word of its mask with its own bit
   unsigned units;
+  uint64_t some, good;                               // bits of the lanes whose tile is there; is there, all of it
 
   // steps s0 .. s1 - 1 of block `block` of head h of sequence b, which has `tokens` cached ones
   __device__ __forceinline__ void run(int b, int h, int block, int s0, int s1, int tokens) {
@@ -355,7 +351,7 @@ struct Walk {
       }
     }
     st.clear();
-    units = place.unit(a.c, h);
+    take(place, h, first - drafts, tokens);
     for (bool again = false; s < min(s1, drafts); s += WAVES, again = true) draft_step(b, h, s, drafted, again);
     if (first < s1) cache_steps(b, h, first - drafts, min(s1 - drafts, (tokens + STEP - 1) / STEP), tokens);
   }
@@ -368,18 +364,30 @@ struct Walk {
     p.ask(a.c, b, tile, wanted && tile < (tokens + 15) / 16);
   }
 
+  __device__ __forceinline__ void take(const Place& p, int h, int s, int tokens) {
+    units = p.unit(a.c, h);
+    some = __ballot(units != NO_UNIT);
+    good = some & __ballot(16 * (2 * (s + WAVES * (lane >> 1)) + (lane & 1)) + 16 <= tokens);
+    if (units == NO_UNIT) units = 0;                 // (some tile, whose keys are not seen)
+  }
+  // keys of step s, the wavefront's n-th, that are there
+  __device__ __forceinline__ unsigned there(int n, int s, int tokens) const {
+    const int at = 2 * (n & 31);
+    if (A2D_OFTEN(((unsigned)(good >> at) & 3) == 3)) return ~0u;
+    unsigned vis = 0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (some >> (at + k) & 1) vis |= ((1u << min(max(tokens - STEP * s - 16 * k, 0), 16)) - 1) << (16 * k);
+    return vis;
+  }
+
   __device__ __forceinline__ void cache_steps(int b, int h, int first, int last, int tokens) {
     Codes<H, FMT> c[2];
     unsigned vis = 0;
     const auto load = [&](int n, int s) {            // the wavefront's n-th step, s
-      vis = 0;
+      vis = there(n, s, tokens);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const unsigned u = __builtin_amdgcn_readlane((int)units, 2 * (n & 31) + k);
-        const int there = min(max(tokens - STEP * s - 16 * k, 0), 16);
-        if (u != NO_UNIT) vis |= ((1u << there) - 1) << (16 * k);
-        load_unit<H, FMT>(c[k], a.c, u == NO_UNIT ? 0 : u, ln);
-      }
+      for (int k = 0; k < 2; ++k) load_unit<H, FMT>(c[k], a.c, __builtin_amdgcn_readlane((int)units, 2 * (n & 31) + k), ln);
     };
     if (first >= last) return;                       // (a walk of nothing)
     load(0, first);
@@ -399,7 +407,7 @@ struct Walk {
       if (A2D_SELDOM((n & 31) == 31 && more)) {
         Place p;
         look_up(p, b, s + WAVES, tokens);
-        units = p.unit(a.c, h);
+        take(p, h, s + WAVES, tokens);
       }
       load(more ? n + 1 : n, more ? s + WAVES : s);
       if (A2D_SELDOM(now != ~0u)) {
@@ -437,9 +445,9 @@ struct Walk {
       if (k == 1 && all >> 16 == 0) {                // (no second tile: zeros, since P = 0 meets them)
 #pragma unroll
         for (int n = 0; n < G::NV; ++n)
-          if (64 * n + 64 <= 16 * G::PIECES || ln.vlive[n]) {
-            lds_store(area + G::KS * BLOCK + ln.lds[n], zero8());
-            lds_store(area + G::KS * BLOCK + (ln.lds[n] ^ 16), zero8());
+          if (ln.live(n)) {
+            lds_store(area + (G::KS + 2 * n) * BLOCK + ln.lds, zero8());
+            lds_store(area + (G::KS + 2 * n) * BLOCK + (ln.lds ^ 16), zero8());
           }
 #pragma unroll
         for (int t = 0; t < RT; ++t) sc[1][t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -448,7 +456,7 @@ struct Walk {
       if (k) load_drafts<H>(c, a, b, h, STEP * step + 16, ln);
 #pragma unroll
       for (int n = 0; n < G::NV; ++n)
-        if (ln.vlive[n] && (all >> (16 * k + ln.vrow[n]) & 1) && not_finite(c.v[n])) bad |= 1u << (16 * k + ln.vrow[n]);
+        if ((all >> (16 * k + ln.row) & 1) && not_finite(c.v[n])) bad |= 1u << (16 * k + ln.row);
       // (rows that none of the block's rows see are zeros: they may hold anything)
       decode_values<H, A2D_CACHE_BF16>(c, ln, area + k * G::KS * BLOCK, all >> (16 * k) & 0xFFFF);
       bf16x8 kf[G::KS];

@@ -25,7 +25,7 @@ struct WideWalk {
   unsigned* bad;                                     // LDS: drafted rows of a step whose V is not finite
   int lane, wave;
   // the lane's place in the tiles that its wavefront loads
-  int prow, ppiece;
+  int prow, ppiece;            // (pieces that there are none of: the row's first)
   bool plive;
   unsigned plds;
   // rows
@@ -33,15 +33,18 @@ struct WideWalk {
   float m[2], ref[2], l[2];
   bf16x8 qf[KS][2];
   unsigned units;                                    // of tile lane & 3 of step lane >> 2 of 16
+  uint64_t some, good;                               // bits of the lanes whose tile is there; is there, all of it
   Words<WORDS> code[PER];
   unsigned scale[PER];
 
   __device__ __forceinline__ void init() {
-    const int at = 64 * (wave % G::NV) + lane, in = min(at, 16 * G::PIECES - 1);
-    plive = at < 16 * G::PIECES;
-    prow = in / G::PIECES;
-    ppiece = in % G::PIECES;
-    plds = (ppiece >> 1) * BLOCK + prow * 64 + 16 * ((2 * (ppiece & 1)) ^ block_swap(prow >> 2));
+    const int n = wave % G::NV;
+    Lane<H> ln;
+    ln.init(lane);
+    plive = ln.live(n);
+    prow = ln.row;
+    ppiece = ln.piece(n);
+    plds = ln.lds + 2 * n * BLOCK;
     if constexpr (H % 32 != 0) {                     // K's columns behind the last: they meet zeros of Q, and must be numbers
       static_assert(H % 32 == 16, "two chunks of a row");
       for (int x = 64 * wave + lane; x < 2 * 4 * 16 * 2; x += 64 * W) {
@@ -58,27 +61,34 @@ struct WideWalk {
     const int tile = 4 * s + lane;
     p.ask(a.c, b, tile, wanted && tile < (tokens + 15) / 16);
   }
-  // asks for the codes of step s, the n-th of the walk; the keys of it that are there
-  __device__ __forceinline__ uint64_t load(int n, int s, int tokens) {
-    constexpr int ROW = code_bytes<FMT>(H);
+  __device__ __forceinline__ void take(const Place& p, int h, int s, int tokens) {
+    units = p.unit(a.c, h);
+    some = __ballot(units != NO_UNIT);
+    good = some & __ballot(16 * (4 * s + lane) + 16 <= tokens);
+    if (units == NO_UNIT) units = 0;                 // (some tile, whose keys are not seen)
+  }
+  // keys of step s, the n-th of the walk, that are there
+  __device__ __forceinline__ uint64_t there(int n, int s, int tokens) const {
+    const int at = 4 * (n & 15);
+    if (A2D_OFTEN(((unsigned)(good >> at) & 15) == 15)) return ~(uint64_t)0;
     uint64_t vis = 0;
-    unsigned u[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      u[t] = __builtin_amdgcn_readlane((int)units, 4 * (n & 15) + t);
-      const int there = min(max(tokens - 64 * s - 16 * t, 0), 16);
-      if (u[t] != NO_UNIT) vis |= (uint64_t)((1u << there) - 1) << (16 * t);
-    }
+    for (int t = 0; t < 4; ++t)
+      if (some >> (at + t) & 1) vis |= (uint64_t)((1u << min(max(tokens - 64 * s - 16 * t, 0), 16)) - 1) << (16 * t);
+    return vis;
+  }
+  // asks for the codes of the walk's n-th step
+  __device__ __forceinline__ void load(int n) {
+    constexpr int ROW = code_bytes<FMT>(H);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int t = tile_of(i);
-      const unsigned at = __builtin_amdgcn_readlane((int)units, 4 * (n & 15) + t), unit = at == NO_UNIT ? 0 : at;
+      const unsigned unit = __builtin_amdgcn_readlane((int)units, 4 * (n & 15) + t);
       const gptr_t p = uniform_gptr((is_value(i) ? a.c.V : a.c.K) + (uint64_t)unit * (16 * ROW));
       code[i] = load_words<WORDS>(p, prow * ROW + ppiece * code_bytes<FMT>(16));
       if constexpr (FMT != A2D_CACHE_BF16)
         scale[i] = load_words<1>(uniform_gptr((is_value(i) ? a.c.Vs : a.c.Ks) + (uint64_t)unit * 64), prow * 4).w[0];
     }
-    return vis;
   }
   // the codes that have come become bf16 in a buffer; V of keys that are not there: zeros
   __device__ __forceinline__ void decode(int buf, uint64_t vis) {
@@ -94,7 +104,7 @@ struct WideWalk {
         y = keep ? y : zero8();
       }
       const unsigned at = area + buf * BUF + (is_value(i) ? K_BYTES : 0) + t * KS * BLOCK + plds;
-      if (64 * G::NV <= 16 * G::PIECES || plive) {
+      if (4 * G::NV == G::PIECES || plive) {
         lds_store(at, x);
         lds_store(at ^ 16, y);
       }
@@ -155,7 +165,7 @@ struct WideWalk {
 
   __device__ __forceinline__ void run(int b, int h, int block, int s0, int s1, int tokens) {
     const int drafts = draft_steps(a), first = max(s0 - drafts, 0), last = min(s1 - drafts, (tokens + 63) / 64);
-    const bool some = (block * W + wave) * 32 < a.group * a.rows;         // of the wavefront's rows
+    const bool any_row = (block * W + wave) * 32 < a.group * a.rows;      // of the wavefront's
     Place place;
     look_up(place, b, first, tokens, first < last);
     const int ln = lane_again();
@@ -175,12 +185,16 @@ struct WideWalk {
 #pragma unroll
       for (int x = 0; x < HT; ++x) o[x][q] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    units = place.unit(a.c, h);
+    take(place, h, first, tokens);
     for (int s = s0; s < min(s1, drafts); ++s) draft_step(b, h, block, s);
     if (first < last) {
-      uint64_t now = load(0, first, tokens), next = 0;
+      uint64_t now = there(0, first, tokens), next = 0;
+      load(0);
       decode(0, now);
-      if (first + 1 < last) next = load(1, first + 1, tokens);
+      if (first + 1 < last) {
+        next = there(1, first + 1, tokens);
+        load(1);
+      }
       __syncthreads();
       for (int s = first, n = 0; s < last; ++s, ++n) {
         uint64_t after = 0;
@@ -189,12 +203,12 @@ struct WideWalk {
           if (A2D_SELDOM((n & 15) == 14)) {
             Place p;
             look_up(p, b, s + 2, tokens);
-            units = p.unit(a.c, h);
+            take(p, h, s + 2, tokens);
           }
-          // (behind the last step: the last again)
-          after = load(s + 2 < last ? n + 2 : n + 1, s + 2 < last ? s + 2 : s + 1, tokens);
+          if (s + 2 < last) after = there(n + 2, s + 2, tokens);
+          load(n + 2);                               // (behind the last step: nothing that is used)
         }
-        if (some) {
+        if (any_row) {
           const unsigned at = (n & 1) * BUF;
           Scores sc;
           Ring ring;
@@ -253,7 +267,7 @@ struct WideWalk {
       const bool value = is_value(i);
       const Words<8> w = load_words<8>(value ? base[1] : base[0], (unsigned)r * (unsigned)(2 * (value ? a.lv.row : a.lk.row)) + ppiece * 32);
       const bf16x8 x = decode_half<A2D_CACHE_BF16>(w, 0, 1.f), y = decode_half<A2D_CACHE_BF16>(w, 1, 1.f);
-      if (64 * G::NV <= 16 * G::PIECES || plive) {
+      if (4 * G::NV == G::PIECES || plive) {
         const unsigned at = area + (value ? K_BYTES : 0) + t * KS * BLOCK + plds;
         lds_store(at, x);
         lds_store(at ^ 16, y);
