@@ -383,6 +383,7 @@ struct Walk {
 
   __device__ __forceinline__ void cache_steps(int b, int h, int first, int last, int tokens) {
     Codes<H, FMT> c[2];
+    Place place;                                     // (asked for a step before it is taken)
     unsigned vis = 0;
     const auto load = [&](int n, int s) {            // the wavefront's n-th step, s
       vis = there(n, s, tokens);
@@ -404,11 +405,8 @@ struct Walk {
       __builtin_amdgcn_sched_barrier(0);
       // the next step's codes, while this one is worked on (behind the last: the last again)
       const bool more = s + WAVES < last;
-      if (A2D_SELDOM((n & 31) == 31 && more)) {
-        Place p;
-        look_up(p, b, s + WAVES, tokens);
-        take(p, h, s + WAVES, tokens);
-      }
+      if (A2D_SELDOM((n & 31) == 30)) look_up(place, b, s + 2 * WAVES, tokens);
+      if (A2D_SELDOM((n & 31) == 31)) take(place, h, s + WAVES, tokens);
       load(more ? n + 1 : n, more ? s + WAVES : s);
       if (A2D_SELDOM(now != ~0u)) {
         const unsigned mine = now >> (4 * ln.g);
