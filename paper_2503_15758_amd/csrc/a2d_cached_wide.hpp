@@ -18,7 +18,6 @@ struct WideWalk {
   static constexpr int BUF = buf_bytes(HD), K_BYTES = BUF / 2;
   static constexpr int LOADS = 8 * G::NV, PER = (LOADS + W - 1) / W;       // of K and V of a step: of a wavefront
   static constexpr int WORDS = code_bytes<FMT>(16) / 4;
-  static constexpr int SLOTS = W == 8 ? 2 : 1, AHEAD = SLOTS + 1;          // steps that are on their way beside the two in LDS
   static_assert(LOADS % W == 0 && W % G::NV == 0, "a wavefront's loads are of one half of their tiles");
   const CachedArgs& a;
   const Blocks16& rd;
@@ -35,8 +34,8 @@ struct WideWalk {
   bf16x8 qf[KS][2];
   unsigned units;                                    // of tile lane & 3 of step lane >> 2 of 16
   uint64_t some, good;                               // bits of the lanes whose tile is there; is there, all of it
-  Words<WORDS> code[SLOTS][PER];                     // of the steps that are on their way
-  unsigned scale[SLOTS][PER];
+  Words<WORDS> code[PER];
+  unsigned scale[PER];
 
   __device__ __forceinline__ void init() {
     const int n = wave % G::NV;
@@ -79,7 +78,6 @@ struct WideWalk {
     return vis;
   }
   // asks for the codes of the walk's n-th step
-  template <int SLOT>
   __device__ __forceinline__ void load(int n) {
     constexpr int ROW = code_bytes<FMT>(H);
 #pragma unroll
@@ -87,19 +85,18 @@ struct WideWalk {
       const int t = tile_of(i);
       const unsigned unit = __builtin_amdgcn_readlane((int)units, 4 * (n & 15) + t);
       const gptr_t p = uniform_gptr((is_value(i) ? a.c.V : a.c.K) + (uint64_t)unit * (16 * ROW));
-      code[SLOT][i] = load_words<WORDS>(p, prow * ROW + ppiece * code_bytes<FMT>(16));
+      code[i] = load_words<WORDS>(p, prow * ROW + ppiece * code_bytes<FMT>(16));
       if constexpr (FMT != A2D_CACHE_BF16)
-        scale[SLOT][i] = load_words<1>(uniform_gptr((is_value(i) ? a.c.Vs : a.c.Ks) + (uint64_t)unit * 64), prow * 4).w[0];
+        scale[i] = load_words<1>(uniform_gptr((is_value(i) ? a.c.Vs : a.c.Ks) + (uint64_t)unit * 64), prow * 4).w[0];
     }
   }
   // the codes that have come become bf16 in a buffer; V of keys that are not there: zeros
-  template <int SLOT>
   __device__ __forceinline__ void decode(int buf, uint64_t vis) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       float f = 1.f;
-      if constexpr (FMT != A2D_CACHE_BF16) f = scale_number(scale[SLOT][i] >> (8 * (ppiece >> 1)) & 255);
-      bf16x8 x = decode_half<FMT>(code[SLOT][i], 0, f), y = decode_half<FMT>(code[SLOT][i], 1, f);
+      if constexpr (FMT != A2D_CACHE_BF16) f = scale_number(scale[i] >> (8 * (ppiece >> 1)) & 255);
+      bf16x8 x = decode_half<FMT>(code[i], 0, f), y = decode_half<FMT>(code[i], 1, f);
       const int t = tile_of(i);
       if (A2D_SELDOM(vis != ~(uint64_t)0)) {
         const bool keep = !is_value(i) || (vis >> (16 * t + prow) & 1);
@@ -190,58 +187,50 @@ struct WideWalk {
     }
     take(place, h, first, tokens);
     for (int s = s0; s < min(s1, drafts); ++s) draft_step(b, h, block, s);
-    const int count = last - first;
-    if (count > 0) cached_steps(b, h, first, count, tokens, any_row);
-  }
-  // steps first .. of the cached tokens.  Of a compute unit's one workgroup codes are on their way for two steps (for one, 16 KiB, they came too
-  // late: trees of 64 on 8 sequences 137 us), of each of two for one; page numbers for one more.
-  __device__ __forceinline__ void cached_steps(int b, int h, int first, int count, int tokens, bool any_row) {
-    Place place;
-    uint64_t now = there(0, first, tokens), next = 0, after = 0;
-    load<0>(0);
-    if (count > 1) next = there(1, first + 1, tokens);
-    if constexpr (SLOTS == 2) load<1>(1);
-    decode<0>(0, now);
-    if (SLOTS == 2 && count > 2) after = there(2, first + 2, tokens);
-    load<0>(AHEAD - 1);
-    __syncthreads();
-    const auto step = [&](int n, auto P) {           // in buffer P; behind the last step: codes of some tile, which nothing uses
-      constexpr int p = decltype(P)::value, slot = SLOTS == 2 ? 1 - p : 0;
-      uint64_t later = 0;
-      if (n + 1 < count) {
-        decode<slot>(1 - p, next);
-        if (A2D_SELDOM((n & 15) == 15 - AHEAD)) look_up(place, b, first + n + AHEAD + 1, tokens);
-        if (A2D_SELDOM((n & 15) == 16 - AHEAD)) take(place, h, first + n + AHEAD, tokens);
-        if (n + AHEAD < count) later = there(n + AHEAD, first + n + AHEAD, tokens);
-        load<slot>(n + AHEAD);
-      }
-      if (any_row) {
-        constexpr unsigned at = p * BUF;
-        Scores sc;
-        Ring ring;
-        fwd_first_keys<H>(ring, rd, at);
-        fwd_scores<H>(sc, ring, qf, rd, at);
-        if (A2D_SELDOM(now != ~(uint64_t)0)) {
-          const uint64_t mine = now >> (4 * (lane >> 4));
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) sc[k][q][i] = mine >> (16 * k + i) & 1 ? sc[k][q][i] : -INFINITY;
-        }
-        fwd_first_values<H>(ring, rd, at);
-        soften(sc);
-        products(sc, ring, at);
+    if (first < last) {
+      uint64_t now = there(0, first, tokens), next = 0;
+      load(0);
+      decode(0, now);
+      if (first + 1 < last) {
+        next = there(1, first + 1, tokens);
+        load(1);
       }
       __syncthreads();
-      now = next;
-      next = SLOTS == 2 ? after : later;
-      after = later;
-    };
-    for (int n = 0; n < count; n += 2) {
-      step(n, std::integral_constant<int, 0>{});
-      if (n + 1 < count) step(n + 1, std::integral_constant<int, 1>{});
+      for (int s = first, n = 0; s < last; ++s, ++n) {
+        uint64_t after = 0;
+        if (s + 1 < last) {
+          decode((n + 1) & 1, next);
+          if (A2D_SELDOM((n & 15) == 14)) {
+            Place p;
+            look_up(p, b, s + 2, tokens);
+            take(p, h, s + 2, tokens);
+          }
+          if (s + 2 < last) after = there(n + 2, s + 2, tokens);
+          load(n + 2);                               // (behind the last step: nothing that is used)
+        }
+        if (any_row) {
+          const unsigned at = (n & 1) * BUF;
+          Scores sc;
+          Ring ring;
+          fwd_first_keys<H>(ring, rd, at);
+          fwd_scores<H>(sc, ring, qf, rd, at);
+          if (A2D_SELDOM(now != ~(uint64_t)0)) {
+            const uint64_t mine = now >> (4 * (lane >> 4));
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+              for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sc[k][q][i] = mine >> (16 * k + i) & 1 ? sc[k][q][i] : -INFINITY;
+          }
+          fwd_first_values<H>(ring, rd, at);
+          soften(sc);
+          products(sc, ring, at);
+        }
+        __syncthreads();
+        now = next;
+        next = after;
+      }
     }
   }
   // the lane's row of tile q (the block's last one in place of those behind it); made again where it is needed, not kept on the walk
