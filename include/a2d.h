@@ -518,7 +518,8 @@ a2d_status a2d_tree_masks(int32_t sequences, int32_t rows, const int32_t* parent
  *   out: flags 0: out0 = N [sequences][heads][rows][H] fp32 (plain), out1 = m, out2 = l [sequences][heads][rows] fp32: the partial triple of
  *   a2d_partial_fwd, to be merged by a2d_fix with those of other shares of the text;
  *   A2D_TILE_NORMALISED: out0 = O in bf16 (layout lo), out1 = lse fp32, out2 is ignored.
- * Codes enter the products exactly; P is taken as two bf16 numbers (2^-17 off), all else is fp32.
+ * Codes enter the products exactly.  P is taken as two bf16 numbers (2^-17 off) for the partial triple, and for O where a key/value head has up to
+ * 32 rows (heads / kv_heads * rows); for more it is rounded to one, as in the tile calls.  All else is fp32.
  * What no row sees - tokens behind lens[b], rows whose bit no mask of the sequence has, Q, K and V of rows that are no tokens - may hold anything.
  * workspace: NULL, or at least a2d_cached_workspace_bytes(cache, desc) bytes, through which workgroups share long walks; calls that share one
  * must be ordered on one stream.  The same sizes, lengths and workspace (or none) give the same bits.
