@@ -352,8 +352,17 @@ struct Walk {
     }
     st.clear();
     take(place, h, first - drafts, tokens);
+    // (of one row tile the first codes are asked for before the drafted rows are worked on; two leave no registers for that)
+    constexpr bool EARLY = RT == 1;
+    const int from = first - drafts, last = min(s1 - drafts, (tokens + STEP - 1) / STEP);
+    Codes<H, FMT> c[2];
+    unsigned vis = 0;
+    if (EARLY && from < last) vis = load(c, 0, from, tokens);
     for (bool again = false; s < min(s1, drafts); s += WAVES, again = true) draft_step(b, h, s, drafted, again);
-    if (first < s1) cache_steps(b, h, first - drafts, min(s1 - drafts, (tokens + STEP - 1) / STEP), tokens);
+    if (from < last) {
+      if (!EARLY) vis = load(c, 0, from, tokens);
+      cache_steps(c, vis, b, h, from, last, tokens);
+    }
   }
   // does the lane's row of tile t exist, and is it a token (its own bit is set)?
   __device__ __forceinline__ bool live(int t) const { return row_of[t] >= 0 && (own[t] >> (row_of[t] & 63) & 1); }
@@ -381,17 +390,14 @@ struct Walk {
     return vis;
   }
 
-  __device__ __forceinline__ void cache_steps(int b, int h, int first, int last, int tokens) {
-    Codes<H, FMT> c[2];
-    Place place;                                     // (asked for a step before it is taken)
-    unsigned vis = 0;
-    const auto load = [&](int n, int s) {            // the wavefront's n-th step, s
-      vis = there(n, s, tokens);
+  // asks for the codes of the wavefront's n-th step, s; returns the keys of it that are there
+  __device__ __forceinline__ unsigned load(Codes<H, FMT> (&c)[2], int n, int s, int tokens) const {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) load_unit<H, FMT>(c[k], a.c, __builtin_amdgcn_readlane((int)units, 2 * (n & 31) + k), ln);
-    };
-    if (first >= last) return;                       // (a walk of nothing)
-    load(0, first);
+    for (int k = 0; k < 2; ++k) load_unit<H, FMT>(c[k], a.c, __builtin_amdgcn_readlane((int)units, 2 * (n & 31) + k), ln);
+    return there(n, s, tokens);
+  }
+  __device__ __forceinline__ void cache_steps(Codes<H, FMT> (&c)[2], unsigned vis, int b, int h, int first, int last, int tokens) {
+    Place place;                                     // (asked for a step before it is taken)
     for (int s = first, n = 0; s < last; s += WAVES, ++n) {
       f32x4 sc[2][RT];
       const unsigned now = vis;
@@ -407,7 +413,7 @@ struct Walk {
       const bool more = s + WAVES < last;
       if (A2D_SELDOM((n & 31) == 30)) look_up(place, b, s + 2 * WAVES, tokens);
       if (A2D_SELDOM((n & 31) == 31)) take(place, h, s + WAVES, tokens);
-      load(more ? n + 1 : n, more ? s + WAVES : s);
+      vis = load(c, more ? n + 1 : n, more ? s + WAVES : s, tokens);
       if (A2D_SELDOM(now != ~0u)) {
         const unsigned mine = now >> (4 * ln.g);
 #pragma unroll
@@ -511,7 +517,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_kernel(CachedArgs a) {
   using G = Head<H>;
   constexpr int ROWS = 16 * RT, QUADS = H / 4;
   __shared__ __align__(1024) char area[WAVES][G::AREA];
-  __shared__ f32x4 stat[WAVES][ROWS];                // m (log2 units), ref, l of a wavefront's row
+  __shared__ f32x4 stat[WAVES][ROWS];                // m (log2 units), ref, l of a wavefront's row; whether it is a token's
+  __shared__ f32x2 joined[ROWS];                     // m, l of all four
   warm_cached();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Lane<H> ln;
@@ -543,10 +550,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_kernel(CachedArgs a) {
     for (int t = 0; t < RT; ++t) {
       {
         const int r = 16 * t + (lane & 15);
-        float top = -INFINITY;
+        f32x4 of[WAVES];
+        float top = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int v = 0; v < WAVES; ++v) top = fmaxf(top, stat[v][r][0]);
-        const float f = top == -INFINITY ? 0.f : fast_exp2(w.st.ref[t] - top);
+        for (int v = 0; v < WAVES; ++v) {
+          of[v] = stat[v][r];
+          top = fmaxf(top, of[v][0]);
+        }
+        const bool any = top != -INFINITY;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) l += any ? of[v][2] * fast_exp2(of[v][1] - top) : 0.f;
+        if (wave == 0 && lane < 16) {
+          const bool empty = of[0][3] == 0.f || l == 0.f;
+          joined[r] = f32x2{empty ? -INFINITY : top, empty ? 0.f : l};
+        }
+        const float f = any ? fast_exp2(w.st.ref[t] - top) : 0.f;
 #pragma unroll
         for (int x = 0; x < G::HT; ++x) {
           f32x4 o = w.st.o[x][t];
@@ -560,32 +578,23 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_kernel(CachedArgs a) {
         const int row = at / QUADS, quad = at - row * QUADS, r = 16 * t + row;
         const int index = (block * RT + t) * 16 + row;
         if (index >= a.group * a.rows) continue;
-        float top = -INFINITY, l = 0.f;
-#pragma unroll
-        for (int v = 0; v < WAVES; ++v) top = fmaxf(top, stat[v][r][0]);
+        const f32x2 of = joined[r];
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int v = 0; v < WAVES; ++v) {
-          const f32x4 s = stat[v][r];
-          l += s[2] * (top == -INFINITY ? 0.f : fast_exp2(s[1] - top));
           const f32x4 x = *reinterpret_cast<const f32x4*>(area[v] + 4 * H * row + 16 * (quad ^ (row & 3)));
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[i] += x[i];
         }
-        const bool empty = stat[0][r][3] == 0.f || l == 0.f;
-        if (empty) {
-          top = -INFINITY;
-          l = 0.f;
-          o = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
+        if (of[1] == 0.f) o = f32x4{0.f, 0.f, 0.f, 0.f};
         if (whole) {
-          const int g = index / a.rows, i = index - g * a.rows;
-          finish(a, run.b, run.h * a.group + g, i, H, quad, o, top, l);
+          const Split sp = split_by(index, a.rows);
+          finish(a, run.b, run.h * a.group + (a.rows == 1 ? index : sp.q), a.rows == 1 ? 0 : sp.r, H, quad, o, of[0], of[1]);
         } else {
           *reinterpret_cast<f32x4*>(part + 2 * ROWS + (size_t)r * H + 4 * quad) = o;
           if (quad == 0) {
-            part[r] = top;
-            part[ROWS + r] = l;
+            part[r] = of[0];
+            part[ROWS + r] = of[1];
           }
         }
       }
