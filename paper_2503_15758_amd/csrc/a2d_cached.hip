@@ -18,16 +18,17 @@ __global__ __launch_bounds__(256) void cached_merge_kernel(CachedArgs a, int gro
   const int b = u / per_sequence, unit = u - b * per_sequence;
   Batch batch;
   Cut cut;
-  unsigned places = 0, begin = 0, last = 0;            // of the walk's first step and its last
-  for (int first = 0; first < a.sequences; first += 64) {
-    batch.look(a, first, lane);
-    if (b >= first && b < first + 64) {
-      const unsigned steps = steps_of(a, batch.tokens_at(b));
-      begin = places + batch.before(b) + unit * (start_of(a) + steps) + start_of(a);
-      last = begin + steps - 1;
+  unsigned places = 0, before = 0, begin = 0, steps = 0;     // before: of the 64s of sequences in front of that of b; begin: of the walk's first step
+  all_batches(a, lane, batch, [&] {                    // (the last ones first)
+    if (b >= batch.first && b < batch.first + 64) {
+      steps = steps_of(a, batch.tokens_at(b));
+      begin = batch.before(b) + unit * (start_of(a) + steps) + start_of(a);
     }
+    if (b >= batch.first + 64) before += batch.all();
     places += batch.all();
-  }
+  });
+  begin += before;
+  const unsigned last = begin + steps - 1;
   cut.make(a, places);
   const unsigned w0 = cut.worker_of(begin), parts = cut.worker_of(last) - w0 + 1;
   if (parts == 1) return;

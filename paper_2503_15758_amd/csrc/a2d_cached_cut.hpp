@@ -52,16 +52,35 @@ struct Batch {
   int first;
   int tokens;
   unsigned sum;
-  __device__ __forceinline__ void look(const CachedArgs& a, int from, int lane) {
+  __device__ __forceinline__ void set(const CachedArgs& a, int from, int lane, int length) {
     first = from;
     const int b = from + lane;
-    tokens = b < a.sequences ? tokens_of(a, a.lens[b]) : 0;
+    tokens = b < a.sequences ? tokens_of(a, length) : 0;
     sum = lanes_sum(b < a.sequences ? (steps_of(a, tokens) + start_of(a)) * (unsigned)(a.c.kv_heads * a.blocks) : 0);
+  }
+  __device__ __forceinline__ void look(const CachedArgs& a, int from, int lane) {
+    set(a, from, lane, a.lens[min(from + lane, a.sequences - 1)]);
   }
   __device__ __forceinline__ int tokens_at(int b) const { return __builtin_amdgcn_readlane(tokens, b - first); }
   __device__ __forceinline__ unsigned before(int b) const { return b > first ? (unsigned)__builtin_amdgcn_readlane((int)sum, b - first - 1) : 0; }
   __device__ __forceinline__ unsigned all() const { return (unsigned)__builtin_amdgcn_readlane((int)sum, 63); }
 };
+
+// All sequences, 64 at a time, the last ones first; f(batch) for each.  (256 lengths are asked for at once.)
+template <class F>
+__device__ __forceinline__ void all_batches(const CachedArgs& a, int lane, Batch& batch, F&& f) {
+  for (int from = (a.sequences - 1) & ~255; from >= 0; from -= 256) {
+    int length[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) length[i] = a.lens[min(from + 64 * i + lane, a.sequences - 1)];
+#pragma unroll
+    for (int i = 3; i >= 0; --i) {
+      if (from + 64 * i >= a.sequences) continue;
+      batch.set(a, from + 64 * i, lane, length[i]);
+      f();
+    }
+  }
+}
 
 struct Cut {
   unsigned total, each, more;          // places; of a worker; the first `more` workers have one more
@@ -102,10 +121,7 @@ struct Runs {
     }
     Cut cut;
     unsigned places = 0;
-    for (int first = (a.sequences - 1) & ~63; first >= 0; first -= 64) {
-      batch.look(a, first, lane);                    // (ends with the first 64)
-      places += batch.all();
-    }
+    all_batches(a, lane, batch, [&] { places += batch.all(); });     // (ends with the first 64)
     cut.make(a, places);
     // neighbours on the line, which share keys where a head has several blocks, to one XCD
     const unsigned per = (cut.workers + 7) / 8, n = (blockIdx.x & 7) * per + (blockIdx.x >> 3);

@@ -301,6 +301,13 @@ def test_many_sequences():
     _check(_problem(14, "bf16", 64, 1, 1, 1, lens, 16, masked=False, drafts=False), _without_drafts(14, lens), max_tokens=1500)
 
 
+def test_hundreds_of_sequences():
+    """More than the 256 whose lengths are asked for at once."""
+    lens = [(13 * i) % 40 if i % 3 else 0 for i in range(600)]
+    lens[3], lens[255], lens[256], lens[599] = 700, 100, 650, 300
+    _check(_problem(21, "e4m3", 64, 1, 1, 2, lens, 16), max_tokens=700)
+
+
 def _without_drafts(seed, lens):
     x = _problem(seed, "bf16", 64, 1, 1, 1, lens, 16, masked=False, drafts=False)
     values = [ref.cache_values(x["cache"], i) for i in range(2)]
