@@ -175,10 +175,13 @@ CachedPlan plan_cached(int format, int hdim, const CachedArgs& a, int cus, bool 
   // Up to 32 rows: blocks of 16 or 32, a wavefront has them all.  More: workgroups of 128 or 256, whichever leaves fewer rows empty.
   // us of blocks of 32 / 128 / 256, 8 sequences of 8192 tokens, 8 heads of 128, e4m3: 40 rows 60.9 / 53.8 / 61.2, 100 rows 87 / 58 / 62, 160 rows
   // 116 / 92 / 78, 256 rows 142 / 98 / 91; 4 sequences, 300 rows of 4 heads of 64, bf16 50 / 35 / 39.
-  p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : padded(256) <= padded(128) ? 16 : 8;
+  // Calls of short walks that leave most of the chip idle take blocks of 16 up to 32 rows: 28 rows of 2 heads of 64, 307 keys 8.7 -> 7.6 us, of 16 heads
+  // 9.5 -> 9.1 (elsewhere two blocks that read the same keys: 8 sequences of 8192 tokens, 28 rows of 8 heads 39.6, not 49.9).
+  const int64_t keys = (int64_t)a.max_tokens + (a.K ? a.rows : 0), walks = (int64_t)a.sequences * a.c.kv_heads;
+  const bool idle = keys <= 512 && 2 * walks <= mfma::kXcds * mfma::kXcdCus;
+  p.tiles = rows <= 16 || (rows <= 32 && idle) ? 1 : rows <= 32 ? 2 : padded(256) <= padded(128) ? 16 : 8;
   p.shift = p.tiles > 2 ? 6 : 5;
   p.blocks = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
-  const int64_t keys = (int64_t)a.max_tokens + (a.K ? a.rows : 0);
   if (!workspace || keys <= 512) return p;
   p.workers = (p.tiles == 16 ? 1 : 2) * cus;
   p.bytes = 2 * (size_t)p.workers * part_floats(16 * p.tiles, hdim) * sizeof(float);

@@ -78,7 +78,7 @@ def test_against_64_bits(kernels, fmt, H, kv_heads, group, rows):
 
 
 @pytest.mark.parametrize("fmt, H", [("bf16", 64), ("e4m3", 128), ("e2m1", 80), ("e4m3", 96)])
-@pytest.mark.parametrize("rows", [1, 5, 40])
+@pytest.mark.parametrize("rows", [1, 5, 12, 40])
 def test_long_and_short_together(fmt, H, rows):
     """Walks that many workgroups share beside ones of a step."""
     _check(_problem(11, fmt, H, 2, 2, rows, [5000, 1, 0, 31, 2049, 333], 16, masked=rows > 1), max_tokens=5000)

@@ -108,10 +108,10 @@ def test_what_may_hold_anything(fmt, H, group, rows):
 
 
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-@pytest.mark.parametrize("group, rows", [(1, 5), (4, 9), (2, 40)])
+@pytest.mark.parametrize("group, rows", [(1, 5), (4, 9), (3, 10), (2, 40)])
 def test_values_that_are_not_finite(bad, group, rows):
     """A drafted row's V with a NaN or an infinity reaches the rows that see it, and no others; a key's NaN likewise."""
-    x = _problem(6, "e4m3", 80, 2, group, rows, [50, 0], 16)
+    x = _problem(6, "e4m3", 80, 2, group, rows, [50 if rows != 10 else 600, 0], 16)
     clean = [y.float() for y in _call(x, normalised=True)]
     seen = [ref.ancestors(p) for p in x["parents"]]
     hit = torch.tensor([[s is not None and 2 in s for s in b] for b in seen]).view(2, 1, rows, 1).cuda()
