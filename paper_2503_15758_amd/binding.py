@@ -8,13 +8,13 @@ not been built (python -m paper_2503_15758_amd.build) every call raises.
 
 Memory: a tile call whose row blocks are too few for the chip shares their walks
 among several workgroups and takes up to 32 MiB for each result it shares (forward;
-dQ; dK and dV; 128 MiB for each in partial_bwd_scored) from torch's allocator while it runs, also where `out` and `workspace`
+dQ; dK and dV; 128 MiB for each in partial_bwd_scored; 65 MiB in partial_fwd_cached) from torch's allocator while it runs, also where `out` and `workspace`
 are given.  Under torch.cuda.graph that is the graph's own pool.  On a stream that the
 program captures by other means, no memory is taken and no walk is shared: the same
 results up to the order of fp32 sums (in bf16 probabilities are rounded relative to
 the maximum of a shared walk's part, so each anew).  The same where there is no memory,
-with a RuntimeWarning.  Slopes, ranges, starts, prefix and positions that begin at no
-multiple of 16 bytes (views) are copied first; in such a capture they are refused.
+with a RuntimeWarning.  Slopes, ranges, starts, prefix, positions, and the tables,
+lengths, indexes, parents and masks of the paged cache that begin at no multiple of 16 bytes (views) are copied first; in such a capture they are refused.
 """
 import ctypes
 import math
@@ -456,7 +456,7 @@ def partial_fwd_cached(Q, cache, table, lens, K=None, V=None, masks=None, scale=
     first lens[b] tokens of its cache and against K, V [sequences][kv_heads][rows][H], the rows' own, which are not in the cache yet: row i
     sees row j if its mask (tree_masks) has bit j, without masks if j <= i.  Rows that are no tokens get the empty partial.  max_tokens: the
     host's bound on lens (longer ones count as this), by which the call is planned.  Returns the partial (N, m, l) fp32, or with
-    normalised=True (O in bf16, lse).  Takes up to 35 MiB from torch's allocator while it runs, as the tile calls do."""
+    normalised=True (O in bf16, lse).  Takes up to 65 MiB from torch's allocator while it runs, as the tile calls do."""
     return (_native or _ext()).partial_fwd_cached(Q, cache, table, lens, K, V, masks, scale, max_tokens, out, normalised)
 
 

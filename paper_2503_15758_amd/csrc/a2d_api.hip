@@ -1081,7 +1081,6 @@ a2d_status cached_args(const a2d_cache* cache, const a2d_cached_desc* d, bool dr
   const int32_t room = cache->max_pages * cache->page_rows;
   a->max_tokens = d->max_tokens == 0 || d->max_tokens > room ? room : d->max_tokens;
   a->words = (d->rows + 63) / 64;
-  a->scale = d->scale;
   a->c2 = d->scale * a2d::kLog2e;
   a->lens = d->lens;
   a->masks = d->masks;

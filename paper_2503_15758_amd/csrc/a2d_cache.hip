@@ -214,7 +214,8 @@ hipError_t go_format(bool write, int format, int hdim, const CacheRows& a, hipSt
 }
 
 // Ancestors: round k lets every row take what the row 2^k steps up has, so a chain of 256 rows takes eight rounds.  up: a row before it,
-// -1: the text, -2: no token (padding, and what follows padding), which is handed down.
+// -1: the text, -2: no token (padding, and what follows padding), which is handed down.  Bound: the launch: one sequence of 7 rows 1.8 us, 64 of 250
+// 3.9.
 constexpr int TREE_ROWS = A2D_TREE_MAX_ROWS, TREE_WORDS = TREE_ROWS / 64;
 __global__ __launch_bounds__(TREE_ROWS) void tree_masks_kernel(int rows, int words, const int32_t* parents, const int32_t* lens, uint64_t* masks,
                                                                int32_t* positions) {

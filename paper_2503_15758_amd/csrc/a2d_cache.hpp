@@ -92,7 +92,7 @@ struct CachedArgs {
   CacheView c;
   int sequences, heads, group, rows;   // group: query heads of a key/value head
   int max_tokens, words, norm;         // words: of a row's mask
-  float scale, c2;                     // c2 = scale log2(e)
+  float c2;                            // scale log2(e)
   const int32_t* lens;
   const uint64_t* masks;
   const char *Q, *K, *V;               // K, V: drafted rows, or NULL

@@ -18,12 +18,11 @@ __device__ __forceinline__ void warm_cached() {
       : "s"(__builtin_amdgcn_kernarg_segment_ptr()), "i"(64 * (last < 4 ? last : 4)), "i"(64 * last));
 }
 
-// The walk of a block of rows: steps of 32 keys (`shift`: 5), those of the drafted rows first
-// (they need no table, whose entries are on their way meanwhile), then those of the cached tokens.  Sequence b has
-// kv_heads * blocks such walks of the same length; all walks, one after another, are a line, cut into equal runs, one for each worker,
-// whatever the lengths are (which the host does not know).  On the line a walk is START places longer than its steps: what it costs
-// besides (Q, the table, the first codes, the join of the wavefronts: 8 sequences, one of them of a token alone, without 61 us, with 8 41; 16, for 8, 32 sequences 27.1 -> 26.2).
-// (The form of many rows has steps of 64 keys, and its START is half as many.)
+// The walk of a block of rows: steps of 32 keys (`shift` 5; in the form of many rows 64), those of the drafted rows first, which need no table, then
+// those of the cached tokens.  Sequence b has kv_heads * blocks such walks of the same length.  All walks, one after another, are a line that is
+// cut into equal runs, one for each worker, whatever the lengths are (which the host does not know).  On the line a walk takes start_of() places
+// more than its steps: what it costs besides (Q, the table, the first codes, the join of the wavefronts).  With 0 / 8 places a call on 8 sequences,
+// one of them of a single token, took 61 / 41 us; with 8 / 16 one on 32 sequences 27.1 / 26.2.
 __device__ __forceinline__ unsigned least_of(const CachedArgs& a) { return a.shift == 6 ? 6 : 12; }       // places of a worker
 __device__ __forceinline__ unsigned start_of(const CachedArgs& a) { return a.shift == 6 ? 4 : 16; }
 __device__ __forceinline__ int steps_for(const CachedArgs& a, int keys) { return (keys + (1 << a.shift) - 1) >> a.shift; }
