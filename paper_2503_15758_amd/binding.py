@@ -456,7 +456,7 @@ def partial_fwd_cached(Q, cache, table, lens, K=None, V=None, masks=None, scale=
     first lens[b] tokens of its cache and against K, V [sequences][kv_heads][rows][H], the rows' own, which are not in the cache yet: row i
     sees row j if its mask (tree_masks) has bit j, without masks if j <= i.  Rows that are no tokens get the empty partial.  max_tokens: the
     host's bound on lens (longer ones count as this), by which the call is planned.  Returns the partial (N, m, l) fp32, or with
-    normalised=True (O in bf16, lse).  Takes up to 65 MiB from torch's allocator while it runs, as the tile calls do."""
+    normalised=True (O in bf16, lse).  Takes up to 65 MiB and 8 bytes for each walk from torch's allocator while it runs, as the tile calls do."""
     return (_native or _ext()).partial_fwd_cached(Q, cache, table, lens, K, V, masks, scale, max_tokens, out, normalised)
 
 

@@ -1198,6 +1198,7 @@ a2d_status a2d_partial_fwd_cached(const a2d_cache* cache, const a2d_cached_desc*
     if (!aligned16(workspace)) return fail(A2D_ERR_MISALIGNED, "%s: workspace is not 16-byte aligned", who);
     a.workers = p.workers;
     a.parts = static_cast<float*>(workspace);
+    a.cuts = reinterpret_cast<int2*>(static_cast<char*>(workspace) + p.part_bytes);
   }
   A2D_TRY(hip_result(a2d::launch_cached(a2d::PREPARE, cache->format, cache->hdim, a, s), who));
   a2d::trace_mark(s);

@@ -104,10 +104,11 @@ struct CachedArgs {
   int tiles, shift;                    // a step has 2^shift keys
   int workers;                         // workgroups that share all steps; 0: one for each block
   float* parts;                        // two results of a block for each worker
+  int2* cuts;                          // of each walk: the first worker that has steps of it, and how many have
 };
 struct CachedPlan {
   int tiles, shift, blocks, workers;
-  size_t bytes;                        // of a.parts
+  size_t part_bytes, bytes;            // of a.parts; with a.cuts behind them
 };
 // workspace: whether there may be one
 CachedPlan plan_cached(int format, int hdim, const CachedArgs& a, int cus, bool workspace);

@@ -13,24 +13,11 @@ __global__ __launch_bounds__(256) void cached_merge_kernel(CachedArgs a, int gro
   __shared__ f32x4 sums[8][QUADS];
   __shared__ float ms[8], ls[8];
   warm_cached();
-  const int lane = threadIdx.x & 63, group = threadIdx.x >> 5, quad = threadIdx.x & 31;
+  const int group = threadIdx.x >> 5, quad = threadIdx.x & 31;
   const int u = blockIdx.x / groups, at = blockIdx.x - u * groups, per_sequence = a.c.kv_heads * a.blocks;
   const int b = u / per_sequence, unit = u - b * per_sequence;
-  Batch batch;
-  Cut cut;
-  unsigned places = 0, before = 0, begin = 0, steps = 0;     // before: of the 64s of sequences in front of that of b; begin: of the walk's first step
-  all_batches(a, lane, batch, [&] {                    // (the last ones first)
-    if (b >= batch.first && b < batch.first + 64) {
-      steps = steps_of(a, batch.tokens_at(b));
-      begin = batch.before(b) + unit * (start_of(a) + steps) + start_of(a);
-    }
-    if (b >= batch.first + 64) before += batch.all();
-    places += batch.all();
-  });
-  begin += before;
-  const unsigned last = begin + steps - 1;
-  cut.make(a, places);
-  const unsigned w0 = cut.worker_of(begin), parts = cut.worker_of(last) - w0 + 1;
+  const int2 cut = a.cuts[u];                          // (as the workers found it)
+  const unsigned w0 = cut.x, parts = cut.y;
   if (parts == 1) return;
   const int rows = 16 * a.tiles, h = unit / a.blocks, block = unit - h * a.blocks;
   const int r = SHARED ? at : 8 * at + group, index = block * rows + r;
@@ -184,7 +171,8 @@ CachedPlan plan_cached(int format, int hdim, const CachedArgs& a, int cus, bool 
   p.blocks = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
   if (!workspace || keys <= 512) return p;
   p.workers = (p.tiles == 16 ? 1 : 2) * cus;
-  p.bytes = 2 * (size_t)p.workers * part_floats(16 * p.tiles, hdim) * sizeof(float);
+  p.part_bytes = 2 * (size_t)p.workers * part_floats(16 * p.tiles, hdim) * sizeof(float);
+  p.bytes = p.part_bytes + (size_t)(walks * p.blocks) * sizeof(int2);
   return p;
 }
 

@@ -1,5 +1,4 @@
-// How the steps of a batch's walks are dealt to the workgroups of a cached call (a2d_cached_fwd.hpp), found alike by the workgroups
-// that walk and by those that merge.
+// How the steps of a batch's walks are dealt to the workgroups of a cached call (a2d_cached_fwd.hpp).
 #pragma once
 #include "a2d_cache.hpp"
 
@@ -104,8 +103,10 @@ struct Run {
 // A workgroup's run of the line
 struct Runs {
   Batch batch;
+  Cut cut;
   int b, unit, worker;
   unsigned at, left;                                 // within the walk; of the run
+  unsigned walk0;                                    // the walk's first place on the line
   // false: there is none
   __device__ __forceinline__ bool begin(const CachedArgs& a, int lane) {
     const int per_sequence = a.c.kv_heads * a.blocks;
@@ -118,7 +119,6 @@ struct Runs {
       left = start_of(a) + steps_of(a, batch.tokens_at(b));
       return true;
     }
-    Cut cut;
     unsigned places = 0;
     all_batches(a, lane, batch, [&] { places += batch.all(); });     // (ends with the first 64)
     cut.make(a, places);
@@ -126,7 +126,7 @@ struct Runs {
     const unsigned per = (cut.workers + 7) / 8, n = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= per || n >= cut.workers) return false;
     worker = (int)n;
-    at = cut.begin(n);
+    at = walk0 = cut.begin(n);
     left = cut.begin(n + 1) - at;
     while (at >= batch.all() && batch.first + 64 < a.sequences) {
       at -= batch.all();
@@ -137,6 +137,7 @@ struct Runs {
     const unsigned walk = start_of(a) + steps_of(a, batch.tokens_at(b));
     unit = at / walk;
     at -= unit * walk;
+    walk0 -= at;
     return true;
   }
   __device__ __forceinline__ bool next(const CachedArgs& a, int lane, Run& r) {
@@ -152,8 +153,11 @@ struct Runs {
     const unsigned to = min(start + r.steps, at + left);
     r.s0 = at > start ? at - start : 0;
     r.s1 = to > start ? to - start : 0;
+    if (worker >= 0 && r.s0 == 0 && r.s1 > 0 && threadIdx.x == 0)      // (every walk has one worker with its first step)
+      a.cuts[b * (a.c.kv_heads * a.blocks) + unit] = int2{worker, r.s1 == r.steps ? 1 : (int)cut.worker_of(walk0 + start + r.steps - 1) - worker + 1};
     left -= to - at;
     at = 0;
+    walk0 += start + r.steps;
     if (++unit == a.c.kv_heads * a.blocks) {
       unit = 0;
       ++b;
