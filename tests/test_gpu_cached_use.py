@@ -273,6 +273,45 @@ def test_a_step_as_a_graph(rows):
             assert all(torch.equal(a, b) for a, b in zip(out, want)), turn
 
 
+def test_a_foreign_capture_takes_no_memory():
+    """A stream captured by the program itself: the call shares no walks there, and numbers that it would have to copy are refused."""
+    x = _problem(31, "e4m3", 128, 2, 2, 5, [3000, 400], 64)
+    table, lens, masks = x["table"].cuda(), x["lens"].cuda(), x["masks"].cuda()
+    out = [torch.empty_like(t) for t in _call(x)]
+    call = lambda lens: a2d.partial_fwd_cached(x["Q"], x["cache"], table, lens, x["K"], x["V"], masks, scale=x["scale"], out=out)
+    hip = ctypes.CDLL(a2d._loaded_hip_runtime())
+    side, graph, run = torch.cuda.Stream(), ctypes.c_void_p(), ctypes.c_void_p()
+    stream, odd = ctypes.c_void_p(side.cuda_stream), _offset(lens)
+    with torch.cuda.stream(side):
+        call(lens)                                          # (kernels loaded)
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_stats()["allocation.all.allocated"]
+        assert hip.hipStreamBeginCapture(stream, ctypes.c_int(1)) == 0       # hipStreamCaptureModeThreadLocal
+        try:
+            call(lens)
+            with pytest.raises(a2d.A2DError):
+                call(odd)
+        finally:
+            ended = hip.hipStreamEndCapture(stream, ctypes.byref(graph))
+        assert ended == 0 and torch.cuda.memory_stats()["allocation.all.allocated"] == before
+    assert hip.hipGraphInstantiate(ctypes.byref(run), graph, None, None, ctypes.c_size_t(0)) == 0
+    (N, m, l, A, size), most = _expect(x)
+    first = None
+    for _ in range(3):
+        for t in out:
+            t.fill_(math.nan)
+        torch.cuda.synchronize()
+        assert hip.hipGraphLaunch(run, stream) == 0
+        torch.cuda.synchronize()
+        some = l > 0
+        f = torch.where(some, torch.exp(out[1].double().cpu() - m), torch.ones_like(m)).unsqueeze(-1)
+        assert bool(((out[0].double().cpu() * f - N).abs() <= most["N"] + most["m"].unsqueeze(-1) * A)[some].all())
+        assert torch.equal((out[2] == 0).cpu(), ~some)
+        first = first or [t.clone() for t in out]
+        assert _same(first, out)
+    assert hip.hipGraphExecDestroy(run) == 0 and hip.hipGraphDestroy(graph) == 0
+
+
 def test_a_cache_of_more_than_4_gib():
     """Offsets in codes that pass 32 bits (5.4 GiB of K, pages at its ends)."""
     kv_heads, page_rows, H, pages = 8, 64, 128, 88000
