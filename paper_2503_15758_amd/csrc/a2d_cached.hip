@@ -119,7 +119,7 @@ __global__ __launch_bounds__(64) void cached_generic_kernel(CachedArgs a, int hd
     for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
     top = fmaxf(top, m);
     const float f = m == top ? 1.f : fast_exp2(m - top);
-    const float w = see && !(top == -INFINITY) ? fast_exp2(z - top) : 0.f;
+    const float w = z == -INFINITY ? 0.f : fast_exp2(z - top);         // (NaN: NaN, whatever the others are)
     p[lane] = w;
     m = top;
     l = l * f + w;

@@ -173,7 +173,8 @@ inline unsigned cached_grid(const CachedArgs& a) {
 // began before it (slot 2 w) and one of a walk that goes on behind it (slot 2 w + 1).
 __host__ __device__ inline size_t part_floats(int rows, int hdim) { return (size_t)rows * (hdim + 2); }
 
-// Columns 4 quad .. + 3 of row i of query head `head` of sequence b, from N, l relative to m = top (log2 units; l = 0: an empty row)
+// Columns 4 quad .. + 3 of row i of query head `head` of sequence b, from N, l relative to m = top (log2 units; l = 0: an empty row).
+// A NaN among the row's scores is in l and N, but in no maximum: m is NaN with l, since merges leave out what has m = -inf.
 __device__ __forceinline__ void finish(const CachedArgs& a, int b, int head, int i, int hdim, int quad, f32x4 o, float top, float l) {
   constexpr float kLn2 = 0.69314718055994531f;
   const int64_t row = ((int64_t)b * a.heads + head) * a.rows + i;
@@ -187,7 +188,7 @@ __device__ __forceinline__ void finish(const CachedArgs& a, int b, int head, int
   } else {
     *reinterpret_cast<f32x4*>(static_cast<float*>(a.out0) + row * hdim + 4 * quad) = o;
     if (quad == 0) {
-      a.out1[row] = top * kLn2;
+      a.out1[row] = l != l ? l : top * kLn2;
       a.out2[row] = l;
     }
   }

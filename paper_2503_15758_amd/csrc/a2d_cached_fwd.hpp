@@ -562,7 +562,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cached_kernel(CachedArgs a) {
         }
         const bool any = top != -INFINITY;
 #pragma unroll
-        for (int v = 0; v < WAVES; ++v) l += any ? of[v][2] * fast_exp2(of[v][1] - top) : 0.f;
+        for (int v = 0; v < WAVES; ++v) l += of[v][2] * (any ? fast_exp2(of[v][1] - top) : 0.f);      // (any or not: NaN stays NaN)
         if (wave == 0 && lane < 16) {
           const bool empty = of[0][3] == 0.f || l == 0.f;
           joined[r] = f32x2{empty ? -INFINITY : top, empty ? 0.f : l};
