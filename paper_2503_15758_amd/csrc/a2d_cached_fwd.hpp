@@ -24,7 +24,22 @@ namespace cached {
 using namespace mfma;
 
 constexpr int WAVES = 4, STEP = 32;
-constexpr float LOW = -3.0e38f;                      // a reference below every score
+constexpr float LOW = -0x1.fffffep127f;              // a reference that no score is below
+// References (log2 units) from which on a score's product with the scale is rounded before the reference is taken off, as the reference is: a row's
+// largest exponent is then 0.  Taken from the unrounded product it is the reference's rounding, up to half a step, which is 1/2 below 2^24 (and all of
+// a row's probabilities have that factor), but passes the range of the exponential from 2^31 on.  Below, the unrounded product is the
+// more exact one: keys next to each other differ by their scores alone.
+constexpr float ROUNDED = 0x1p24f;
+// (keeps a branch one whose scores stay where they are: as selects of all of them it takes a register more for each)
+__device__ __forceinline__ float in_place(float x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+// what a wavefront's part of a row is to be multiplied with to be relative to the row's largest score, top = m * c2
+__device__ __forceinline__ float part_factor(float ref, float top) {
+#pragma clang fp contract(off)                       // (not from the unrounded product, which the reference may be)
+  return fast_exp2(ref - top);
+}
 
 template <int N>
 struct Words { unsigned w[N]; };
@@ -184,7 +199,9 @@ struct State {
   float m[RT];          // largest score the lane has seen, as it comes from the matrix unit
   float ref[RT];        // log2 units: what the exponentials are relative to, the same in the four lanes of a row
   float l[RT];
+  bool far;             // some reference is ROUNDED or more, up or down
   __device__ __forceinline__ void clear() {
+    far = false;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       m[t] = -INFINITY;
@@ -210,17 +227,36 @@ __device__ __forceinline__ void soften(State<H, RT>& st, f32x4 (&s)[2][RT], floa
     st.m[t] = fmaxf(st.m[t], x);
     far |= x * c2 > st.ref[t] + 8.f;
   }
-  if (A2D_SELDOM(__any(far))) {                      // a reference is only moved by more than 2^8
+  float by[RT];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const float x = row_max(top[t]) * c2, ref = x > st.ref[t] + 8.f ? x : st.ref[t];      // (each row by its own scores alone)
-      const float f = ref == st.ref[t] ? 1.f : fast_exp2(st.ref[t] - ref);
-      st.ref[t] = ref;
-      st.l[t] *= f;
+  for (int t = 0; t < RT; ++t) by[t] = c2;
+  if (A2D_SELDOM(__any(far || st.far))) {
+    if (__any(far)) {                                // a reference is only moved by more than 2^8
+      far = false;
 #pragma unroll
-      for (int h = 0; h < Head<H>::HT; ++h)
+      for (int t = 0; t < RT; ++t) {
+        const float x = row_max(top[t]) * c2, ref = x > st.ref[t] + 8.f ? x : st.ref[t];    // (each row by its own scores alone)
+        const float f = ref == st.ref[t] ? 1.f : fast_exp2(st.ref[t] - ref);
+        far |= ref != LOW && fabsf(ref) >= ROUNDED;
+        st.ref[t] = ref;
+        st.l[t] *= f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) st.o[h][t][i] *= f;
+        for (int h = 0; h < Head<H>::HT; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st.o[h][t][i] *= f;
+      }
+      st.far |= __any(far) != 0;
+    }
+    if (A2D_SELDOM(st.far)) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        const bool rounded = fabsf(st.ref[t]) >= ROUNDED;
+        by[t] = rounded ? 1.f : c2;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[k][t][i] = in_place(s[k][t][i] * (rounded ? c2 : 1.f));
+      }
     }
   }
 #pragma unroll
@@ -229,7 +265,7 @@ __device__ __forceinline__ void soften(State<H, RT>& st, f32x4 (&s)[2][RT], floa
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[k][t][i] = fast_exp2(fmaf(s[k][t][i], c2, -st.ref[t]));
+        s[k][t][i] = fast_exp2(fmaf(s[k][t][i], by[t], -st.ref[t]));
         st.l[t] += s[k][t][i];
       }
 }

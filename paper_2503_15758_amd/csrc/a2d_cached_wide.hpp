@@ -33,6 +33,7 @@ struct WideWalk {
   // rows
   f32x4 o[HT][2];
   float m[2], ref[2], l[2];
+  bool far;                                          // some reference is ROUNDED or more, up or down
   bf16x8 qf[KS][2];
   unsigned units;                                    // of tile lane & 3 of step lane >> 2 of 16
   uint64_t some, good;                               // bits of the lanes whose tile is there; is there, all of it
@@ -125,24 +126,39 @@ struct WideWalk {
       m[q] = fmaxf(m[q], x);
       far |= x * a.c2 > ref[q] + 8.f;
     }
-    if (A2D_SELDOM(__any(far))) {
+    float by[2] = {a.c2, a.c2};
+    if (A2D_SELDOM(__any(far || this->far))) {
+      if (__any(far)) {
+        far = false;
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const float x = row_max(top[q]) * a.c2, to = x > ref[q] + 8.f ? x : ref[q];         // (each row by its own scores alone)
-        const float f = to == ref[q] ? 1.f : fast_exp2(ref[q] - to);
-        ref[q] = to;
-        l[q] *= f;
+        for (int q = 0; q < 2; ++q) {
+          const float x = row_max(top[q]) * a.c2, to = x > ref[q] + 8.f ? x : ref[q];       // (each row by its own scores alone)
+          const float f = to == ref[q] ? 1.f : fast_exp2(ref[q] - to);
+          ref[q] = to;
+          far |= to != LOW && fabsf(to) >= ROUNDED;
+          l[q] *= f;
 #pragma unroll
-        for (int h = 0; h < HT; ++h)
+          for (int h = 0; h < HT; ++h)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[h][q][i] *= f;
+            for (int i = 0; i < 4; ++i) o[h][q][i] *= f;
+        }
+        this->far |= __any(far) != 0;
+      }
+      if (A2D_SELDOM(this->far)) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const bool rounded = fabsf(ref[q]) >= ROUNDED;
+          by[q] = rounded ? 1.f : a.c2;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[e >> 2][q][e & 3] = in_place(s[e >> 2][q][e & 3] * (rounded ? a.c2 : 1.f));
+        }
       }
     }
 #pragma unroll
     for (int q = 0; q < 2; ++q)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        s[e >> 2][q][e & 3] = fast_exp2(fmaf(s[e >> 2][q][e & 3], a.c2, -ref[q]));
+        s[e >> 2][q][e & 3] = fast_exp2(fmaf(s[e >> 2][q][e & 3], by[q], -ref[q]));
         l[q] += s[e >> 2][q][e & 3];
       }
   }
@@ -171,6 +187,7 @@ struct WideWalk {
     Place place;
     look_up(place, b, first, tokens, first < last);
     const int ln = lane_again();
+    far = false;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       const Row r = row(b, h, block, q);
@@ -362,7 +379,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_wide_kernel(CachedArgs a) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       float l = row_sum(w.l[q]), top = row_max(w.m[q]) * a.c2;
-      float f = top == -INFINITY ? 0.f : fast_exp2(w.ref[q] - top);
+      float f = top == -INFINITY ? 0.f : part_factor(w.ref[q], top);
       l *= f;
       const auto row = w.row(run.b, run.h, run.block, q);
       const bool empty = !row.token || l == 0.f;
