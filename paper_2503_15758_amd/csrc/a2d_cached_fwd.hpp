@@ -148,8 +148,12 @@ __device__ __forceinline__ bf16x8 decode_half(const Words<N>& w, int half, float
 __device__ __forceinline__ void lds_store(unsigned at, bf16x8 x) {
   *reinterpret_cast<__attribute__((address_space(3))) bf16x8*>((uintptr_t)at) = x;
 }
-__device__ __forceinline__ float lds_number(unsigned at) {
-  return (float)*reinterpret_cast<const __attribute__((address_space(3))) bf16_t*>((uintptr_t)at);
+// Columns 16 h + 4 g .. + 3 of row r of a tile, which begins at `row` in the tile's first block
+__device__ __forceinline__ unsigned quad_at(unsigned row, int r, int h, int g) {
+  return row + (h >> 1) * BLOCK + 16 * ((2 * (h & 1) + (g >> 1)) ^ block_swap(r >> 2)) + 8 * (g & 1);
+}
+__device__ __forceinline__ bf16x4 lds_quad(unsigned at) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) bf16x4*>((uintptr_t)at);
 }
 __device__ __forceinline__ bf16x8 zero8() { return __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0}); }
 
@@ -314,11 +318,25 @@ __device__ __forceinline__ bool not_finite(const Words<8>& w) {
   return !(x == 0.f);
 }
 
+// May a value of a cached V be infinite?  (of 8 and 4 bits, by its scale: 448 2^119 is not)
+constexpr float LARGE_SCALE = 0x1p120f;
+template <int FMT, int N>
+__device__ __forceinline__ bool maybe_infinite(const Words<N>& w, float scale) {
+  if constexpr (FMT == A2D_CACHE_BF16) return not_finite(w);
+  else return scale >= LARGE_SCALE;
+}
+
 // with zeros in place of NaN and infinities
 __device__ __forceinline__ bf16x8 finite_part(bf16x8 x) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = (float)x[i] - (float)x[i] == 0.f ? x[i] : (bf16_t)0.f;
   return x;
+}
+
+// rows of a tile some lane of which is set
+__device__ __forceinline__ unsigned rows_of(uint64_t lanes) {
+  const unsigned x = (unsigned)lanes | (unsigned)(lanes >> 32);
+  return (x | x >> 16) & 0xFFFF;
 }
 
 // of the 16 lanes 0 .. 15 (which 16 .. 31 and so on repeat)
@@ -440,9 +458,14 @@ struct Walk {
     for (int s = first, n = 0; s < last; s += WAVES, ++n) {
       f32x4 sc[2][RT];
       const unsigned now = vis;
+      uint64_t large[2];                             // lanes that have a value of V that may be infinite
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         bf16x8 kf[G::KS];
+        bool some_large = false;
+#pragma unroll
+        for (int x = 0; x < G::NV; ++x) some_large |= maybe_infinite<FMT>(c[k].v[x], scale_number(c[k].vs >> (8 * (2 * x + (ln.g >> 1))) & 255));
+        large[k] = __ballot(some_large);
         decode_values<H, FMT>(c[k], ln, area + k * G::KS * BLOCK, k ? now >> 16 : now & 0xFFFF);
         decode_keys<H, FMT>(kf, c[k], ln);
         scores<H, RT>(sc[k], kf, qf);
@@ -463,6 +486,12 @@ struct Walk {
             for (int i = 0; i < 4; ++i) sc[k][t][i] = mine >> (16 * k + i) & 1 ? sc[k][t][i] : -INFINITY;
       }
       soften<H, RT>(st, sc, a.c2);
+      if (A2D_SELDOM((large[0] | large[1]) != 0)) {  // (P's second number, 0 or below, would make NaN of infinities)
+        unsigned all[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) all[t] = ~0u;
+        apart(sc, all, rows_of(large[0]) | rows_of(large[1]) << 16);
+      }
       products<H, RT>(st, sc, rd);
     }
   }
@@ -514,23 +543,22 @@ struct Walk {
 #pragma unroll
         for (int i = 0; i < 4; ++i) sc[k][t][i] = seen[t] >> (16 * k + 4 * ln.g + i) & 1 ? sc[k][t][i] : -INFINITY;
     soften<H, RT>(st, sc, a.c2);
-    if (A2D_SELDOM(__any(bad != 0))) apart(sc, seen, bad);
+    if (A2D_SELDOM(__any(bad != 0))) {
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) bad |= (unsigned)__shfl_xor((int)bad, d);
+      apart(sc, seen, __builtin_amdgcn_readfirstlane((int)bad));
+    }
     products<H, RT>(st, sc, rd);
   }
 
-  // A NaN or an infinity in a drafted row's V may be added to those rows only that see it, and its product with P = 0 is not 0: such numbers
-  // are added one at a time and become zeros in LDS.
+  // A NaN or an infinity in a drafted row's V may be added to those rows only that see it, and its product with P = 0, or with P's second
+  // number, is not 0: such numbers, also those of a cached V, are added one at a time and become zeros in LDS.  bad: keys of the step that may have any.
   __device__ __forceinline__ void apart(const f32x4 (&sc)[2][RT], const unsigned (&seen)[RT], unsigned bad) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) bad |= (unsigned)__shfl_xor((int)bad, d);
-    bad = __builtin_amdgcn_readfirstlane((int)bad);
     const int lane = lane_again();
     while (bad) {
       const int key = __builtin_ctz(bad), k = key >> 4, r = key & 15;
       bad &= bad - 1;
-      // column c of the key: block c / 32, chunk c / 8 % 4 of its row
       const unsigned row = area + k * G::KS * BLOCK + r * 64;
-      const auto column = [&](int c) { return row + (c >> 5) * BLOCK + 16 * ((c >> 3 & 3) ^ block_swap(r >> 2)) + 2 * (c & 7); };
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         float p = 0.f;
@@ -539,14 +567,17 @@ struct Walk {
         p = __shfl(p, 16 * (r >> 2) + (lane & 15));
         if (!(seen[t] >> key & 1)) continue;
 #pragma unroll
-        for (int h = 0; h < G::HT; ++h)
+        for (int h = 0; h < G::HT; ++h) {
+          const bf16x4 v4 = lds_quad(quad_at(row, r, h, lane >> 4));
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float v = lds_number(column(16 * h + 4 * (lane >> 4) + i));
-            st.o[h][t][i] = v - v == 0.f ? st.o[h][t][i] : fmaf(p, v, st.o[h][t][i]);
+            const float v = (float)v4[i];
+            st.o[h][t][i] = in_place(v - v == 0.f ? st.o[h][t][i] : fmaf(p, v, st.o[h][t][i]));
           }
+        }
       }
-      if (lane < H / 8) lds_store(column(8 * lane), finite_part(lds_load_b128(column(8 * lane))));
+      const unsigned at = row + (lane >> 2) * BLOCK + 16 * ((lane & 3) ^ block_swap(r >> 2));
+      if (lane < H / 8) lds_store(at, finite_part(lds_load_b128(at)));
     }
   }
 };

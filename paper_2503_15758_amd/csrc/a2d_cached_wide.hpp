@@ -24,7 +24,10 @@ struct WideWalk {
   const CachedArgs& a;
   const Blocks16& rd;
   unsigned area;                                     // LDS: two buffers
-  unsigned* bad;                                     // LDS: drafted rows of a step whose V is not finite
+  unsigned* bad;                                     // LDS: drafted rows of a step whose V is not finite (64 bits); of each buffer, LARGE where a
+                                                     // cached V in it may be infinite (FINE; never cleared beforehand, which would take a barrier:
+                                                     // the same number found there by chance changes no result)
+  static constexpr unsigned LARGE = 0x1A26E1A2;
   int lane, wave;
   // the lane's place in the tiles that its wavefront loads
   int prow, ppiece;            // (pieces that there are none of: the row's first)
@@ -58,7 +61,10 @@ struct WideWalk {
   }
   // the wavefront's n-th load of a step: K or V, of which tile
   __device__ __forceinline__ int tile_of(int n) const { return (wave + W * n) / G::NV & 3; }
-  __device__ __forceinline__ bool is_value(int n) const { return wave + W * n >= LOADS / 2; }
+  // (known beforehand where the wavefronts' loads of K end together, but for one form whose registers spill then; a partial of 25 rows in
+  // e4m3 takes 31.9 us so, 33.0 otherwise)
+  static constexpr bool APART = LOADS / 2 % W == 0 && !(FINE && FMT == A2D_CACHE_BF16 && H == 128 && W == 4);
+  __device__ __forceinline__ bool is_value(int n) const { return (APART ? 0 : wave) + W * n >= LOADS / 2; }
 
   __device__ __forceinline__ void look_up(Place& p, int b, int s, int tokens, bool wanted = true) const {
     const int tile = 4 * s + lane;
@@ -95,11 +101,14 @@ struct WideWalk {
   }
   // the codes that have come become bf16 in a buffer; V of keys that are not there: zeros
   __device__ __forceinline__ void decode(int buf, uint64_t vis) {
+    bool large = false;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       float f = 1.f;
       if constexpr (FMT != A2D_CACHE_BF16) f = scale_number(scale[i] >> (8 * (ppiece >> 1)) & 255);
       bf16x8 x = decode_half<FMT>(code[i], 0, f), y = decode_half<FMT>(code[i], 1, f);
+      if constexpr (FINE)
+        if (is_value(i)) large |= maybe_infinite<FMT>(code[i], f);
       const int t = tile_of(i);
       if (A2D_SELDOM(vis != ~(uint64_t)0)) {
         const bool keep = !is_value(i) || (vis >> (16 * t + prow) & 1);
@@ -112,6 +121,22 @@ struct WideWalk {
         lds_store(at ^ 16, y);
       }
     }
+    if (FINE && A2D_SELDOM(__any(large)) && lane == 0) bad[2 + buf] = LARGE;
+  }
+  // a buffer's V with zeros in place of infinities (which P's second number, 0 or below, would make NaN of), the flag taken back; for all
+  // wavefronts between the products of P's first number and those of its second
+  __device__ __forceinline__ void finite_values(int buf) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const unsigned at = area + buf * BUF + K_BYTES + tile_of(i) * KS * BLOCK + plds;
+      if (is_value(i) && (4 * G::NV == G::PIECES || plive)) {
+        lds_store(at, finite_part(lds_load_b128(at)));
+        lds_store(at ^ 16, finite_part(lds_load_b128(at ^ 16)));
+      }
+    }
+    if (wave == 0 && lane == 0) bad[2 + buf] = 0;
+    __syncthreads();
   }
 
   __device__ __forceinline__ void soften(Scores& s) {
@@ -162,22 +187,26 @@ struct WideWalk {
         l[q] += s[e >> 2][q][e & 3];
       }
   }
-  __device__ __forceinline__ void products(const Scores& s, Ring& vr, unsigned at) {
-    bf16x8 p[2][2], rest[2][2];
+  // P as one bf16 number, or two
+  struct Weights {
+    bf16x8 p[2][2], rest[FINE ? 2 : 1][2];
+    __device__ __forceinline__ void set(const Scores& s) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int q = 0; q < 2; ++q)
+        for (int q = 0; q < 2; ++q)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x = s[2 * k + (e >> 2)][q][e & 3];
-          p[k][q][e] = (bf16_t)x;
-          if constexpr (FINE) rest[k][q][e] = (bf16_t)(x - (float)p[k][q][e]);
-        }
-    fwd_products<H>(o, p, vr, rd, at);
+          for (int e = 0; e < 8; ++e) {
+            const float x = s[2 * k + (e >> 2)][q][e & 3];
+            p[k][q][e] = (bf16_t)x;
+            if constexpr (FINE) rest[k][q][e] = (bf16_t)(x - (float)p[k][q][e]);
+          }
+    }
+  };
+  __device__ __forceinline__ void rest_products(const Weights& w, Ring& vr, unsigned at) {
     if constexpr (FINE) {
       fwd_first_values<H>(vr, rd, at);
-      fwd_products<H>(o, rest, vr, rd, at);
+      fwd_products<H>(o, w.rest, vr, rd, at);
     }
   }
 
@@ -227,10 +256,12 @@ struct WideWalk {
           if (s + 2 < last) after = there(n + 2, s + 2, tokens);
           load(n + 2);                               // (behind the last step: nothing that is used)
         }
+        const unsigned at = (n & 1) * BUF;
+        const unsigned large = FINE ? bad[2 + (n & 1)] : 0;      // (asked for here, looked at behind the products)
+        Weights w;
+        Ring ring;
         if (any_row) {
-          const unsigned at = (n & 1) * BUF;
           Scores sc;
-          Ring ring;
           fwd_first_keys<H>(ring, rd, at);
           fwd_scores<H>(sc, ring, qf, rd, at);
           if (A2D_SELDOM(now != ~(uint64_t)0)) {
@@ -244,7 +275,12 @@ struct WideWalk {
           }
           fwd_first_values<H>(ring, rd, at);
           soften(sc);
-          products(sc, ring, at);
+          w.set(sc);
+          fwd_products<H>(o, w.p, ring, rd, at);
+        }
+        if constexpr (FINE) {
+          if (A2D_SELDOM(__builtin_amdgcn_readfirstlane((int)large) == LARGE)) finite_values(n & 1);
+          if (any_row) rest_products(w, ring, at);
         }
         __syncthreads();
         now = next;
@@ -316,7 +352,10 @@ struct WideWalk {
     soften(sc);
     if (A2D_SELDOM(odd != 0)) apart(sc, seen, odd);
     fwd_first_values<H>(ring, rd, 0);
-    products(sc, ring, 0);
+    Weights w;
+    w.set(sc);
+    fwd_products<H>(o, w.p, ring, rd, 0);
+    rest_products(w, ring, 0);
     __syncthreads();
   }
 
@@ -334,13 +373,14 @@ struct WideWalk {
         p = __shfl(p, 16 * (r >> 2) + (ln & 15));
         if (!(seen[q] >> key & 1)) continue;
 #pragma unroll
-        for (int x = 0; x < HT; ++x)
+        for (int x = 0; x < HT; ++x) {
+          const bf16x4 v4 = lds_quad(quad_at(row, r, x, ln >> 4));
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int c = 16 * x + 4 * (ln >> 4) + i;
-            const float v = lds_number(row + (c >> 5) * BLOCK + 16 * ((c >> 3 & 3) ^ block_swap(r >> 2)) + 2 * (c & 7));
+            const float v = (float)v4[i];
             o[x][q][i] = v - v == 0.f ? o[x][q][i] : fmaf(p, v, o[x][q][i]);
           }
+        }
       }
     }
     __syncthreads();
