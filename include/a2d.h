@@ -528,7 +528,8 @@ a2d_status a2d_tree_masks(int32_t sequences, int32_t rows, const int32_t* parent
  */
 typedef struct {
   int32_t heads;         /* query heads of a sequence, a multiple of kv_heads; 1 .. 65535                        */
-  int32_t rows;          /* 1 .. 2^20; with masks 1 .. A2D_TREE_MAX_ROWS; heads / kv_heads * rows <= 2^22        */
+  int32_t rows;          /* 1 .. 2^20; with masks 1 .. A2D_TREE_MAX_ROWS; heads / kv_heads * rows <= 2^22; fewer than 2^24 blocks of up
+                            to 128 rows of a key/value head, 2^23 of 256, in a call                              */
   int32_t max_tokens;    /* the host's bound on the lengths: a longer lens[b] counts as this.  0: what the table holds */
   float scale;           /* > 0, at most 1e30 */
   a2d_batch_layout lq, lk, lv, lo;

@@ -1093,10 +1093,13 @@ a2d_status cached_args(const a2d_cache* cache, const a2d_cached_desc* d, bool dr
   a->tiles = p.tiles;
   a->shift = p.shift;
   a->blocks = p.blocks;
-  // (steps are numbered through in 32 bits, workgroups in 31)
+  // (steps are numbered through in 32 bits, rows in 31)
   const double walks = (double)cache->sequences * cache->kv_heads * p.blocks;
   if (walks * ((a->max_tokens + 31) / 32 + (d->rows + 31) / 32) >= 0x1p31 || (double)cache->sequences * d->heads * d->rows >= 0x1p31)
     return fail(A2D_ERR_UNSUPPORTED, "%s: more than 2^31 steps of 32 keys, or rows of all heads, in one call", who);
+  if (walks * a2d::cached_threads(p.tiles) >= (double)a2d::MAX_THREADS)
+    return fail(A2D_ERR_UNSUPPORTED, "%s: %.0f blocks of rows, each of %d threads: a launch has fewer than 2^32", who, walks,
+                a2d::cached_threads(p.tiles));
   return A2D_OK;
 }
 
@@ -1184,6 +1187,9 @@ a2d_status a2d_partial_fwd_cached(const a2d_cache* cache, const a2d_cached_desc*
   a.out2 = out2;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (a2d::force_generic()) {
+    const int64_t all = (int64_t)a.sequences * a.heads * a.rows;
+    if (all * 64 >= a2d::MAX_THREADS)
+      return fail(A2D_ERR_UNSUPPORTED, "%s: %lld rows, each of 64 threads: a launch has fewer than 2^32", who, (long long)all);
     a2d::trace_mark(s);
     return hip_result(a2d::launch_cached_generic(cache->format, cache->hdim, a, s), who);
   }

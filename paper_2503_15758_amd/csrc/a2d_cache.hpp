@@ -110,6 +110,8 @@ struct CachedPlan {
   int tiles, shift, blocks, workers;
   size_t part_bytes, bytes;            // of a.parts; with a.cuts behind them
 };
+constexpr int64_t MAX_THREADS = (int64_t)1 << 32;      // a launch has fewer
+inline int cached_threads(int tiles) { return 64 * (tiles == 16 ? 8 : 4); }       // of a workgroup
 // workspace: whether there may be one
 CachedPlan plan_cached(int format, int hdim, const CachedArgs& a, int cus, bool workspace);
 hipError_t launch_cached(Phase ph, int format, int hdim, const CachedArgs& a, hipStream_t s);

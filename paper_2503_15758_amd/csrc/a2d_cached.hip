@@ -1,4 +1,6 @@
 // Attention over the paged cache: how a call goes out, the merge of walks that several workgroups share, and the plain kernel.
+#include <algorithm>
+
 #include "a2d_cached_cut.hpp"
 
 namespace a2d {
@@ -144,13 +146,24 @@ __global__ __launch_bounds__(64) void cached_generic_kernel(CachedArgs a, int hd
   if (lane < hdim / 4) finish(a, b, head, i, hdim, lane, *reinterpret_cast<const f32x4*>(q + 4 * lane), l == 0.f ? -INFINITY : m, l);
 }
 
+// How the rows of `walks` blocks are merged: `groups` workgroups for each
+struct Merge {
+  bool shared;
+  int groups;
+  Merge(int64_t walks, int64_t rows_of_head, int tiles) {
+    const int rows = (int)std::min<int64_t>(rows_of_head, 16 * tiles);
+    // (a workgroup finds out its walk's parts in 1.3 us: more of them than the chip holds cost more than long walks' rows side by side save)
+    shared = walks * rows <= 4096;
+    groups = shared ? rows : (rows + 7) / 8;
+  }
+};
 template <int H>
 void go_merge(const CachedArgs& a, hipStream_t s) {
-  const int rows = a.group * a.rows < 16 * a.tiles ? a.group * a.rows : 16 * a.tiles;
-  const int64_t units = (int64_t)a.sequences * a.c.kv_heads * a.blocks;
-  // (a workgroup finds out its walk's parts in 1.3 us: more of them than the chip holds cost more than long walks' rows side by side save)
-  if (units * rows <= 4096) A2D_LAUNCH((cached_merge_kernel<H, true>), dim3((unsigned)(units * rows)), dim3(256), 0, s, a, rows);
-  else A2D_LAUNCH((cached_merge_kernel<H, false>), dim3((unsigned)(units * ((rows + 7) / 8))), dim3(256), 0, s, a, (rows + 7) / 8);
+  const int64_t walks = (int64_t)a.sequences * a.c.kv_heads * a.blocks;
+  const Merge m(walks, (int64_t)a.group * a.rows, a.tiles);
+  const dim3 grid((unsigned)(walks * m.groups));
+  if (m.shared) A2D_LAUNCH((cached_merge_kernel<H, true>), grid, dim3(256), 0, s, a, m.groups);
+  else A2D_LAUNCH((cached_merge_kernel<H, false>), grid, dim3(256), 0, s, a, m.groups);
 }
 
 }  // namespace
@@ -169,7 +182,8 @@ CachedPlan plan_cached(int format, int hdim, const CachedArgs& a, int cus, bool 
   p.tiles = rows <= 16 || (rows <= 32 && idle) ? 1 : rows <= 32 ? 2 : padded(256) <= padded(128) ? 16 : 8;
   p.shift = p.tiles > 2 ? 6 : 5;
   p.blocks = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
-  if (!workspace || keys <= 512) return p;
+  // (walks whose merge one launch could not hold are many times what fills the chip)
+  if (!workspace || keys <= 512 || walks * p.blocks * Merge(walks * p.blocks, rows, p.tiles).groups * 256 >= MAX_THREADS) return p;
   p.workers = (p.tiles == 16 ? 1 : 2) * cus;
   p.part_bytes = 2 * (size_t)p.workers * part_floats(16 * p.tiles, hdim) * sizeof(float);
   p.bytes = p.part_bytes + (size_t)(walks * p.blocks) * sizeof(int2);
