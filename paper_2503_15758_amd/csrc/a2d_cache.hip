@@ -68,8 +68,8 @@ __device__ __forceinline__ void store_codes(char* p, const float (&v)[8], float 
 __host__ __device__ constexpr int row_lanes(int h) { return (h + CACHE_BLOCK - 1) / CACHE_BLOCK * 4; }
 
 // A thread has eight values of K and the same eight of V; blockIdx: rows, head, sequence.
-// Bound: HBM, each value read once and its code written once: 8 heads of 128, 16384 tokens from a packed projection 21.6 us, 4.7 TB/s; a token of
-// 64 sequences 3.5 us, its call 6.
+// Bound: HBM, each value read once and its code written once: 8 heads of 128, 16384 tokens from a packed projection 23.8 us, 4.3 TB/s, where a copy of
+// as many bytes takes 19.5 (three inputs in turn, of which the last-level cache holds a part, 21.3 us); a token of 64 sequences 3.5 us, its call 6.
 template <int H, int FMT, typename T>
 __global__ __launch_bounds__(256) void cache_write_kernel(CacheRows a) {
   constexpr int LANES = row_lanes(H), ROW = code_bytes<FMT>(H);
@@ -118,9 +118,10 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheRows a) {
 }
 
 // Values of a token that a thread reads: as many as make a store of 16 bytes, so that neighbours' stores are one run, which may leave
-// non-temporal.  Bound: HBM, mostly writes.  8 heads of 128, 16384 tokens to bf16: 17.2 us (through the L2s 18.0), 5.9 TB/s of reads and
-// writes; 5 sequences, 12 heads of 80, 4135 tokens to fp32, behind the write of 40 rows: 30.2 us, 5.5 TB/s (through the L2s 38.5, two stores
-// of every second 16 bytes 40.4).
+// non-temporal.  Bound: HBM, mostly writes; codes that the last-level cache still holds come from there.  8 heads of 128, 16384 tokens to bf16:
+// 23.6 us, 4.3 TB/s of reads and writes, where a copy of as many bytes takes 19.5; caches of 34 MB, three in turn, 17.1 us, 5.9 TB/s (through the L2s
+// 18.0).  5 sequences, 12 heads of 80, 4135 tokens to fp32, behind the write of 40 rows: 36.0 us, 4.6 TB/s, up to 16 caches in turn 30.6 (through
+// the L2s 38.5, two stores of every second 16 bytes 40.4).
 template <typename T>
 struct Piece;
 template <>

@@ -13,7 +13,7 @@
 //    numbers (2^-17): these calls wait for memory.
 //  - Pages: 64 page numbers at a time are in the lanes of a register, and a step's two are read from there as scalars.
 // Bound: HBM for long texts.  A token of 8 sequences, 32 / 8 heads of 128, 73622 tokens in e4m3: 28 us, 5.5 TB/s (with the merge and the second launch
-// 38).  Short ones: what a walk costs besides its steps, some 5 us of dependent requests and of instructions that are fetched for the first time
+// 37).  Short ones: what a walk costs besides its steps, some 5 us of dependent requests and of instructions that are fetched for the first time
 // (7 rows over 300 tokens, 8 / 2 heads of 64: 6.9 us a call).
 #pragma once
 #include "a2d_cached_cut.hpp"

@@ -3,9 +3,9 @@
 //
 // A workgroup has 32 rows for each of its wavefronts, which share the keys: 64 a step, decoded once into LDS as bf16 by all wavefronts together
 // (a piece of 16 values a lane), two buffers, one barrier a step.  A step's codes are asked for a step before they are decoded and are decoded a step
-// before they are used.  The contractions are those of the bf16 forward (a2d_fwd.hpp).  Bound: power.  64 rows of 8
-// sequences, 32 / 8 heads of 128, 9001 to 16384 tokens in e4m3: 128 us, 950 TFLOP/s at 1.87 GHz, MFMA busy 39 %, vector ALU 47 % of the cycles; with the
-// merge of the parts 138.
+// before they are used.  The contractions are those of the bf16 forward (a2d_fwd.hpp).  Bound: power, and the vector ALU beside
+// the matrix units.  64 rows of 8 sequences, 32 / 8 heads of 128, 9001 to 16384 tokens in e4m3: calls that follow one another 141 us, 860 TFLOP/s with the
+// merge of the parts; this kernel by itself under the profiler 158 us, 765 TFLOP/s, at 1.93 GHz, MFMA busy 38 %, vector ALU 46 % of the cycles.
 #pragma once
 #include "a2d_cached_fwd.hpp"
 #include "a2d_fwd.hpp"
