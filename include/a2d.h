@@ -521,7 +521,7 @@ a2d_status a2d_tree_masks(int32_t sequences, int32_t rows, const int32_t* parent
  * Codes enter the products exactly.  P is taken as two bf16 numbers (2^-17 off) for the partial triple, and for O where a key/value head has up to
  * 32 rows (heads / kv_heads * rows); for more it is rounded to one, as in the tile calls.  All else is fp32.
  * Scores are numbers of fp32, in units of log 2: scale <q, k> log2(e) beyond its range is infinite.  A row one of whose scores is NaN, or
- * infinite upwards, is NaN: O and lse; N, l and m (which a2d_fix hands on).  A score of -inf has weight 0.
+ * infinite upwards, is NaN: O and lse; N, l and m (which a2d_fix hands on to O).  A score of -inf has weight 0.
  * What no row sees - tokens behind lens[b], rows whose bit no mask of the sequence has, Q, K and V of rows that are no tokens - may hold anything.
  * workspace: NULL, or at least a2d_cached_workspace_bytes(cache, desc) bytes, through which workgroups share long walks; calls that share one
  * must be ordered on one stream.  The same sizes, lengths and workspace (or none) give the same bits.
